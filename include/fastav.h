@@ -12,6 +12,9 @@
  *     fastav_compact  the survivor layout: gather hidden states, position ids, K and V rows
  *     fastav_prune    all three in one enqueue
  *
+ * and beside it what its survivors are kept and used with: an 8-bit cache and the attention over it (fastav_cache_write,
+ * fastav_cache_read, fastav_attend).
+ *
  * Conventions shared by every call
  *   - Plain C.  No CUDA types: `stream` is a cudaStream_t passed as void*.
  *   - Every data pointer is a DEVICE pointer unless its comment says "host".  The params struct
@@ -346,6 +349,123 @@ int32_t fastav_rollout_read(int32_t n, int32_t layers_applied, const void* state
                             float* rollout_out_opt, void* stream);
 int32_t fastav_rollout_threshold(int32_t n, const float* importance, float threshold, const uint8_t* protect_opt,
                                  uint8_t* keep_mask_out, int32_t* cut_out, void* stream);
+
+/*
+ * ---- The survivors' K/V cache in 8 bits, and attention over it ----------------------------------------------
+ *
+ * What is left after a layer's prune step is what its attention reads from then on, while answers are written: the survivors'
+ * K and V (Section 2.2: later layers and all later tokens see the survivors only).  These calls keep them in 8 bits, in pages,
+ * and answer from there:
+ *
+ *     fastav_cache_write   K and V rows (a layer's survivors by their keep list, or every row, or one decoded token per
+ *                          sequence) quantised into the pages
+ *     fastav_cache_read    rows of the cache as bf16 again (for a later prune call, or a prefill kernel)
+ *     fastav_attend        attention of a few or many query rows per sequence over [a prefix that several sequences share] ++
+ *                          [the sequence's own tokens]
+ *
+ * Layout.  A cache is a pool of num_pages pages of page_tokens tokens, page-major, then KV head:
+ *
+ *     k, v              [num_pages, num_kv_heads, page_tokens, head_dim]  one byte per value
+ *     k_scale, v_scale  [num_pages, num_kv_heads, page_tokens] fp32       one scale per token and KV head
+ *
+ * Value = code * scale.  A row x of a token and head is laid down with
+ *
+ *     a = max_i |x_i|,   scale = a / L,   code_i = round(x_i L / a)  (to nearest, ties to even; 0 where a = 0)
+ *
+ * with L = 127 and whole-number codes (FASTAV_CACHE_INT8) or L = 448 and e4m3 codes (FASTAV_CACHE_FP8).  A row that holds an
+ * infinity or a NaN reads back as NaN throughout.  Values that no call has written are never used, whatever they are.
+ *
+ * Page tables.  Row b of `page_table` (int32, `table_stride` entries from one row to the next) lists sequence b's pages:
+ * its token t lies in page page_table[b * table_stride + t / page_tokens] at place t % page_tokens.  Entries of pages that a
+ * call does not touch may hold anything.  An entry it touches that names no page of the pool sets FASTAV_DEV_BAD_INDEX; writes and
+ * reads of such rows are left out, fastav_attend's results for the sequences that use it are not valid.
+ */
+#define FASTAV_CACHE_INT8 0
+#define FASTAV_CACHE_FP8 1 /* e4m3 */
+
+typedef struct fastav_cache { /* host memory; read at call time */
+  int32_t format;             /* FASTAV_CACHE_INT8 or FASTAV_CACHE_FP8 */
+  int32_t page_tokens;        /* 16, 32, 64, 128 or 256 */
+  int32_t num_pages;          /* >= 1 */
+  int32_t num_kv_heads, head_dim; /* as in fastav_params; head_dim 64 or 128 */
+  void *k, *v;                /* device, 128-byte aligned */
+  float *k_scale, *v_scale;   /* device, 16-byte aligned */
+} fastav_cache;
+
+/*
+ * Rows into the cache.  Sequence b's rows are its tokens cu_seqlens[b] ... of k and v -- all of them, or with keep_idx_opt (then
+ * cu_keep_opt, too; both as fastav_select writes them, FASTAV_KEEP_IDX_GLOBAL included) the survivors only -- and become tokens
+ * start_opt[b], start_opt[b] + 1, ... of the cached sequence (start_opt NULL: 0, 1, ...).
+ *
+ * Of params: batch, total_tokens, max_seqlen, total_keep and max_keep (with a keep list), num_kv_heads, head_dim, the strides of k and v,
+ * FASTAV_KEEP_IDX_GLOBAL, FASTAV_CHAIN_CALLS (here: cu_seqlens, cu_keep_opt and keep_idx_opt too were complete before the preceding work).
+ *
+ *   k, v        [N, Hkv, head_dim] bf16
+ *   page_table  [B, table_stride] int32
+ *   start_opt   [B] int32 or NULL
+ *
+ * No two rows of a call may go to the same place.  A row whose place lies before token 0 or behind the table's last entry is left out
+ * (FASTAV_DEV_SHAPE_MISMATCH), as is one of a survivor outside its sequence (FASTAV_DEV_BAD_INDEX).
+ */
+int32_t fastav_cache_write(const fastav_params* params, const fastav_cache* cache, const void* k, const void* v,
+                           const int32_t* cu_seqlens, const int32_t* keep_idx_opt, const int32_t* cu_keep_opt,
+                           const int32_t* page_table, int32_t table_stride, const int32_t* start_opt, int32_t* device_status,
+                           void* stream);
+
+/*
+ * Rows of the cache in bf16: output row cu_seqlens[b] + i is token start_opt[b] + i (NULL: i) of sequence b, rounded once.
+ * Of params: batch, total_tokens, max_seqlen, num_kv_heads, head_dim, the ko_ and vo_ strides (of k_out and v_out), FASTAV_CHAIN_CALLS.
+ * A row whose token lies outside the table, or in no page of the pool, is left out as above.
+ */
+int32_t fastav_cache_read(const fastav_params* params, const fastav_cache* cache, const int32_t* page_table, int32_t table_stride,
+                          const int32_t* start_opt, const int32_t* cu_seqlens, void* k_out, void* v_out, int32_t* device_status,
+                          void* stream);
+
+/* Shapes of one fastav_attend call (host memory). */
+typedef struct fastav_attend_params {
+  int32_t batch;               /* B >= 1; batch + num_prefixes <= FASTAV_ATTEND_MAX_BATCH */
+  int32_t total_q, max_qlen;   /* sum_b R_b = cu_qlens[B]; max_b R_b (upper bounds are fine) */
+  int32_t num_q_heads;         /* a multiple of the cache's num_kv_heads */
+  int32_t max_kv_len;          /* max_b n_b (an upper bound is fine) */
+  int32_t table_stride;        /* entries per row of page_table */
+  int32_t num_prefixes;        /* 0: no prefix */
+  int32_t max_prefix_len, prefix_table_stride;
+  int32_t max_prefix_q;        /* most scored rows that share one prefix (an upper bound is fine) */
+  int64_t q_stride_tok, q_stride_head, o_stride_tok, o_stride_head;
+  float softmax_scale;         /* <= 0 selects 1/sqrt(head_dim) */
+  uint32_t flags;              /* FASTAV_CAUSAL, FASTAV_CHAIN_CALLS (here: cu_qlens, kv_lens, cu_prefix, prefix_lens and the page tables
+                                  were complete before the preceding work) */
+} fastav_attend_params;
+#define FASTAV_ATTEND_MAX_BATCH 4096
+
+/*
+ * Attention over the cache.  Sequence b has n_b = kv_lens[b] own tokens in the cache (the query rows' own among them, if they were
+ * written) and R_b query rows; prefix p is shared by the sequences cu_prefix[p] <= b < cu_prefix[p + 1].  For query row r of sequence b
+ * and query head h (KV head h / G):
+ *
+ *   V(r)     = all tokens of the prefix that b shares, and its own tokens, or {j <= n_b - R_b + r} of them under FASTAV_CAUSAL
+ *              (the query rows are the sequence's last tokens)
+ *   lse      = log sum_{j in V(r)} exp(scale <q[r,h,:], k_j>)
+ *   out      = sum_{j in V(r)} exp(scale <q[r,h,:], k_j> - lse) v_j
+ *
+ * A row that sees no key gets out = 0 and lse = -inf.
+ *
+ *   q            [total_q, Hq, head_dim] bf16
+ *   cu_qlens     [B+1] int32
+ *   page_table   [B, table_stride] int32        kv_lens      [B] int32
+ *   cu_prefix    [P+1] int32, prefix_table [P, prefix_table_stride] int32, prefix_lens [P] int32; all NULL if num_prefixes = 0
+ *   out          [total_q, Hq, head_dim] bf16 (strides from params)
+ *   lse_out_opt  [total_q, Hq] fp32 or NULL; natural logarithm, what fastav_score takes as lse_opt
+ *   workspace    fastav_attend_workspace_bytes() bytes, 256-byte aligned
+ *
+ * One query row is decoding, several are drafted tokens or a question at once.  A prefix's keys are read once for all rows that
+ * share it.  Sums run in a fixed order: equal calls give equal bits.
+ */
+int32_t fastav_attend_workspace_bytes(const fastav_attend_params* params, const fastav_cache* cache, size_t* out_bytes);
+int32_t fastav_attend(const fastav_attend_params* params, const fastav_cache* cache, const void* q, const int32_t* cu_qlens,
+                      const int32_t* page_table, const int32_t* kv_lens, const int32_t* cu_prefix, const int32_t* prefix_table,
+                      const int32_t* prefix_lens, void* out, float* lse_out_opt, void* workspace, size_t workspace_bytes,
+                      int32_t* device_status, void* stream);
 
 /*
  * Number of kernels this library has launched in this process so far (a diagnostic counter).

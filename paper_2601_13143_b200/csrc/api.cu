@@ -16,11 +16,6 @@ namespace {
 thread_local char g_cuda_error[256] = "";
 std::atomic<long long> g_launches{0};
 
-int32_t cuda_failed(cudaError_t e) {
-  std::snprintf(g_cuda_error, sizeof g_cuda_error, "%s: %s", cudaGetErrorName(e), cudaGetErrorString(e));
-  return FASTAV_ERR_CUDA;
-}
-
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Shape checks shared by all entry points.
@@ -32,18 +27,6 @@ int32_t check_params(const fastav_params* p) {
   if (p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_q_heads % p->num_kv_heads != 0) return FASTAV_ERR_INVALID_ARG;
   if (p->head_dim != 64 && p->head_dim != 128) return FASTAV_ERR_UNSUPPORTED;
   if (p->hidden < 0 || p->hidden % 8 != 0) return FASTAV_ERR_UNSUPPORTED;
-  return FASTAV_OK;
-}
-
-// A [tokens, heads, dim] view: the head stride must hold a row, the token stride must hold all heads,
-// and both must keep rows 16-byte aligned.
-// Two layouts pass: heads inside a token (st >= heads * sh, e.g. a view into a packed projection output) and
-// tokens inside a head (sh > st, a head-major cache; its extent is the caller's business).  What is rejected is
-// the one case that is certainly wrong: heads inside a token whose rows overlap the next token's.
-int32_t check_strides(int64_t st, int64_t sh, int heads, int dim) {
-  if (sh < dim || st < dim) return FASTAV_ERR_INVALID_ARG;
-  if (st % 8 != 0 || sh % 8 != 0) return FASTAV_ERR_UNSUPPORTED;
-  if (heads > 1 && st >= sh && st < (int64_t)(heads - 1) * sh + dim) return FASTAV_ERR_INVALID_ARG;
   return FASTAV_OK;
 }
 
@@ -116,6 +99,23 @@ int32_t check_compact_args(const fastav_params* p, const int32_t* keep_idx, cons
 }
 
 }  // namespace
+
+int32_t cuda_failed(cudaError_t e) {
+  std::snprintf(g_cuda_error, sizeof g_cuda_error, "%s: %s", cudaGetErrorName(e), cudaGetErrorString(e));
+  return FASTAV_ERR_CUDA;
+}
+
+// A [tokens, heads, dim] view: the head stride must hold a row, the token stride must hold all heads,
+// and both must keep rows 16-byte aligned.
+// Two layouts pass: heads inside a token (st >= heads * sh, e.g. a view into a packed projection output) and
+// tokens inside a head (sh > st, a head-major cache; its extent is the caller's business).  What is rejected is
+// the one case that is certainly wrong: heads inside a token whose rows overlap the next token's.
+int32_t check_strides(int64_t st, int64_t sh, int heads, int dim) {
+  if (sh < dim || st < dim) return FASTAV_ERR_INVALID_ARG;
+  if (st % 8 != 0 || sh % 8 != 0) return FASTAV_ERR_UNSUPPORTED;
+  if (heads > 1 && st >= sh && st < (int64_t)(heads - 1) * sh + dim) return FASTAV_ERR_INVALID_ARG;
+  return FASTAV_OK;
+}
 
 Shapes make_shapes(const fastav_params& p) {
   Shapes s{};

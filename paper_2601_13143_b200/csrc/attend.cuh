@@ -1,0 +1,185 @@
+// Attention over the 8-bit cache (fastav_attend): what its kernels share.
+//
+// The work of a call is a list of jobs.  An ENTRY is a set of query rows that see the same keys of the same page-table row: the rows of a
+// sequence with the sequence's own tokens, or the rows of all sequences that share a prefix with the prefix.  Its query rows times the
+// G query heads of a KV head are stacked (row i of the stack: query row i / G, head i % G) and cut into tiles; a JOB is one (entry, KV head,
+// tile), its keys cut into granules, the UNITS.  All units of a launch form one list, keys innermost, and every worker takes an equal run
+// of it, whatever the lengths.  A run that begins or ends inside a job leaves a part (running maximum, sum and weighted values); the
+// parts of a job lie with consecutive blocks, and the kernel that joins them works out which from the list alone.
+#pragma once
+
+#include "cache.cuh"
+
+namespace fastav {
+
+struct AttendCall {
+  CacheView cache;
+  int batch, total_q, max_qlen, hq, group;
+  int max_len, table_stride;
+  int prefixes, max_prefix_len, prefix_stride, max_prefix_q;
+  long long q_st, q_sh, o_st, o_sh;
+  float scale_log2;  // softmax scale * log2(e): logits are kept in base-2 units
+  bool causal;
+  const int32_t *cu_qlens, *table, *lens, *cu_prefix, *prefix_table, *prefix_lens;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse_out;
+  int32_t* device_status;
+  // results of jobs that one block finished, where another level's are still to be joined: [2][total_q, Hq]
+  float* whole_out;
+  float2* whole_ml;
+  int head_wait;
+};
+inline void mark_head(AttendCall& c, bool head) { c.head_wait = head ? 1 : 0; }
+
+// One launch's list: the prefixes' entries (from_prefix of them), then the sequences' own (from_own).
+struct AttendList {
+  int from_prefix, from_own;
+  int tile_rows, unit_keys;  // of a tile; of a granule
+  int grid;                  // blocks that share the list
+  int32_t* ahead;            // [entries + 1] units before an entry, left for the kernel that joins
+  float* part_out;           // [grid][2][tile_rows][dim]
+  float2* part_ml;           // [grid][2][tile_rows]: running maximum (base 2), sum
+  __host__ __device__ int entries() const { return from_prefix + from_own; }
+};
+
+// Few rows per KV head: mma.sync, a granule per warp (attend_few.cu).
+constexpr int kFewTile = 16, kFewKeys = 32;
+cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream);
+
+// The pools as [rows of the pool, dim] bytes, boxes of box_rows rows, swizzled by the row's bytes.  `map`: a CUtensorMap.
+bool encode_pool_map(const CacheView& c, const void* pool, int box_rows, void* map);
+
+#ifdef __CUDACC__
+struct Entry {
+  int row0, rows;  // query rows
+  int len;         // keys
+  const int32_t* table;
+  bool own;
+};
+__device__ __forceinline__ Entry entry_of(const AttendCall& c, const AttendList& list, int e, bool& bad) {
+  Entry x;
+  x.own = e >= list.from_prefix;
+  if (x.own) {
+    const int b = e - list.from_prefix;
+    const Span rows = checked_span<true>(c.cu_qlens, b, c.total_q, c.max_qlen);
+    x.row0 = rows.first;
+    x.rows = rows.count;
+    x.len = chain_load_cached(c.lens + b);
+    x.table = c.table + (long long)b * c.table_stride;
+    bad |= rows.bad;
+  } else {
+    const int from = chain_load_cached(c.cu_prefix + e), to = chain_load_cached(c.cu_prefix + e + 1);
+    const bool fits = from >= 0 && from <= to && to <= c.batch;
+    const Span rows = fits ? checked_words(chain_load_cached(c.cu_qlens + from), chain_load_cached(c.cu_qlens + to), c.total_q, c.max_prefix_q)
+                           : Span{0, 0, true};
+    x.row0 = rows.first;
+    x.rows = rows.count;
+    x.len = chain_load_cached(c.prefix_lens + e);
+    x.table = c.prefix_table + (long long)e * c.prefix_stride;
+    bad |= rows.bad;
+  }
+  const long long room = (long long)(x.own ? c.table_stride : c.prefix_stride) << c.cache.page_shift;
+  const int most = (int)min((long long)(x.own ? c.max_len : c.max_prefix_len), room);
+  if (x.len < 0 || x.len > most) {
+    bad = true;
+    x.len = max(0, min(x.len, most));
+  }
+  return x;
+}
+__device__ __forceinline__ int tiles_of(const AttendCall& c, const AttendList& list, const Entry& x) {
+  return (x.rows * c.group + list.tile_rows - 1) / list.tile_rows;
+}
+__device__ __forceinline__ int granules_of(const AttendList& list, const Entry& x) { return (x.len + list.unit_keys - 1) / list.unit_keys; }
+__device__ __forceinline__ int units_of(const AttendCall& c, const AttendList& list, const Entry& x) {
+  return c.cache.hkv * tiles_of(c, list, x) * granules_of(list, x);
+}
+
+// Blocks that have units: all, or the first of them, one unit each.
+__device__ __forceinline__ int workers_of(const AttendList& list, int total) { return max(1, min(list.grid, total)); }
+// Worker w of `workers` takes the units [run_start(w), run_start(w + 1)) of `total`; worker_of is the one that has unit u.
+__device__ __forceinline__ int run_start(int w, int workers, int total) { return (int)((long long)total * w / workers); }
+__device__ __forceinline__ int worker_of(int u, int workers, int total) { return (int)(((long long)(u + 1) * workers - 1) / total); }
+
+// The list, all threads of the block: ahead[e] in shared memory, [entries + 1]; the total.  Block 0 leaves a copy.
+template <int THREADS>
+__device__ int open_list(const AttendCall& c, const AttendList& list, int* ahead, int* warp_sum) {
+  const int entries = list.entries(), each = (entries + THREADS - 1) / THREADS;
+  const int e0 = min(entries, (int)threadIdx.x * each), e1 = min(entries, e0 + each);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int sum = 0;
+  bool bad = false;
+#pragma unroll 1
+  for (int e = e0; e < e1; ++e) {
+    ahead[e] = sum;
+    sum += units_of(c, list, entry_of(c, list, e, bad));
+  }
+  int upto = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int t = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+    if (lane >= d) upto += t;
+  }
+  if (lane == 31) warp_sum[warp] = upto;
+  __syncthreads();
+  int before = upto - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < warp) before += warp_sum[w];
+    total += warp_sum[w];
+  }
+#pragma unroll 1
+  for (int e = e0; e < e1; ++e) {
+    ahead[e] += before;
+    if (blockIdx.x == 0) list.ahead[e] = ahead[e];
+  }
+  if (threadIdx.x == 0) {
+    ahead[entries] = total;
+    if (blockIdx.x == 0) list.ahead[entries] = total;
+  }
+  if (blockIdx.x == 0 && bad && c.device_status) atomicOr(c.device_status, FASTAV_DEV_SHAPE_MISMATCH);
+  __syncthreads();
+  return total;
+}
+
+// A walk along the list: the unit it stands at.
+struct Walk {
+  Entry x;
+  int e, head, tile, granule;
+  int tiles, granules;
+  int job_start;  // first unit of the job
+  __device__ __forceinline__ void load(const AttendCall& c, const AttendList& list) {
+    bool bad = false;  // (reported by open_list)
+    x = entry_of(c, list, e, bad);
+    tiles = tiles_of(c, list, x);
+    granules = granules_of(list, x);
+  }
+  __device__ void seek(const AttendCall& c, const AttendList& list, const int* ahead, int u) {  // u < the total
+    int lo = 0, hi = list.entries();  // the last entry that begins at or before u: one with units
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (ahead[mid] <= u) lo = mid; else hi = mid;
+    }
+    e = lo;
+    load(c, list);
+    const int r = u - ahead[e], job = r / granules;
+    granule = r - job * granules;
+    head = job / tiles;
+    tile = job - head * tiles;
+    job_start = u - granule;
+  }
+  __device__ __forceinline__ void step(const AttendCall& c, const AttendList& list, const int* ahead) {  // the next unit exists
+    if (++granule < granules) return;
+    granule = 0;
+    job_start += granules;
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++head < c.cache.hkv) return;
+    head = 0;
+    do ++e; while (ahead[e + 1] <= job_start);
+    load(c, list);
+  }
+};
+#endif
+
+}  // namespace fastav

@@ -1,0 +1,44 @@
+// 8-bit codes as operands of mma.sync in f16.  int8 codes and e4m3 values are exact in f16.
+#pragma once
+
+#include <stdint.h>
+
+namespace fastav {
+
+// Four codes -> two pairs of f16 (bytes 0 and 1; bytes 2 and 3).  int8: the code plus 128 as the low bits of an f16 in [1024, 2048), less 1152.
+template <bool FP8>
+__device__ __forceinline__ void four_codes(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (FP8) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+  } else {
+    w ^= 0x80808080u;
+    const uint32_t magic = 0x64646464u, less = 0xE480E480u;  // -1152, twice
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(__byte_perm(w, magic, 0x4140)), "r"(less));
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(__byte_perm(w, magic, 0x4342)), "r"(less));
+  }
+}
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t two_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// The power of two that brings a magnitude with these float bits into [1, 2) (into f32's range where it is tiny or huge; 1 where it is not finite).
+__device__ __forceinline__ float to_one(float magnitude) {
+  const int e = (int)(__float_as_uint(magnitude) >> 23 & 255u);
+  return e == 255 ? 1.f : __uint_as_float((unsigned)min(max(254 - e, 1), 240) << 23);  // (room for a further factor)
+}
+
+}  // namespace fastav

@@ -164,6 +164,11 @@ cudaError_t enqueue_selection(const fastav_params& params, const void* q, const 
                               const RowStreams* rows, float* scores_out, int32_t* keep_idx_out, int32_t* cu_keep_out, unsigned char* ws,
                               int32_t* device_status, cudaStream_t st, bool* gathered);
 
+// Argument checks that the entry points share.
+int32_t check_strides(int64_t st, int64_t sh, int heads, int dim);
+// Keeps the runtime's text for fastav_last_cuda_error; FASTAV_ERR_CUDA.
+int32_t cuda_failed(cudaError_t e);
+
 // Diagnostic launch counter (fastav_kernel_launches).
 void count_launches(int n);
 

@@ -101,6 +101,12 @@ __device__ __forceinline__ uint4 ld_shared4(uint32_t at) {  // 16-byte aligned
   return v;
 }
 
+__device__ __forceinline__ uint2 ld_shared2(uint32_t at) {  // 8-byte aligned
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+
 // ---- proxies and fences ------------------------------------------------------------------------
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }

@@ -31,6 +31,9 @@ FASTAV_DEV_BAD_INDEX = 8
 FASTAV_DEV_SHAPE_MISMATCH = 16
 FASTAV_DEV_SLOW_PATH = 32
 
+FASTAV_CACHE_INT8 = 0
+FASTAV_CACHE_FP8 = 1
+
 FASTAV_OK = 0
 FASTAV_ERR_INVALID_ARG = -1
 FASTAV_ERR_UNSUPPORTED = -2
@@ -42,7 +45,8 @@ EXPORTS = ("fastav_version", "fastav_status_string", "fastav_last_cuda_error", "
            "fastav_score", "fastav_lse", "fastav_select", "fastav_compact", "fastav_prune", "fastav_host_arena_bytes",
            "fastav_prune_host", "fastav_kernel_launches", "fastav_select_noalloc", "fastav_select_mask", "fastav_selftest_bounded_wait",
            "fastav_rollout_state_bytes", "fastav_rollout_workspace_bytes", "fastav_rollout_begin", "fastav_rollout_layer",
-           "fastav_rollout_read", "fastav_rollout_threshold")
+           "fastav_rollout_read", "fastav_rollout_threshold", "fastav_cache_write", "fastav_cache_read", "fastav_attend_workspace_bytes",
+           "fastav_attend")
 
 
 class fastav_params(ctypes.Structure):
@@ -58,6 +62,29 @@ class fastav_params(ctypes.Structure):
         ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
         ("ko_stride_tok", ctypes.c_int64), ("ko_stride_head", ctypes.c_int64),
         ("vo_stride_tok", ctypes.c_int64), ("vo_stride_head", ctypes.c_int64),
+        ("softmax_scale", ctypes.c_float),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class fastav_cache(ctypes.Structure):
+    _fields_ = [
+        ("format", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class fastav_attend_params(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("total_q", ctypes.c_int32), ("max_qlen", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32),
+        ("max_kv_len", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+        ("num_prefixes", ctypes.c_int32), ("max_prefix_len", ctypes.c_int32), ("prefix_table_stride", ctypes.c_int32),
+        ("max_prefix_q", ctypes.c_int32),
+        ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+        ("o_stride_tok", ctypes.c_int64), ("o_stride_head", ctypes.c_int64),
         ("softmax_scale", ctypes.c_float),
         ("flags", ctypes.c_uint32),
     ]
@@ -144,6 +171,15 @@ def library() -> ctypes.CDLL:
         lib.fastav_rollout_read.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, ctypes.c_size_t, vp, vp, vp]
         lib.fastav_rollout_threshold.restype = ctypes.c_int32
         lib.fastav_rollout_threshold.argtypes = [ctypes.c_int32, vp, ctypes.c_float, vp, vp, i32p, vp]
+        cp, ap = ctypes.POINTER(fastav_cache), ctypes.POINTER(fastav_attend_params)
+        lib.fastav_cache_write.restype = ctypes.c_int32
+        lib.fastav_cache_write.argtypes = [pp, cp, vp, vp, i32p, i32p, i32p, i32p, ctypes.c_int32, i32p, i32p, vp]
+        lib.fastav_cache_read.restype = ctypes.c_int32
+        lib.fastav_cache_read.argtypes = [pp, cp, i32p, ctypes.c_int32, i32p, i32p, vp, vp, i32p, vp]
+        lib.fastav_attend_workspace_bytes.restype = ctypes.c_int32
+        lib.fastav_attend_workspace_bytes.argtypes = [ap, cp, szp]
+        lib.fastav_attend.restype = ctypes.c_int32
+        lib.fastav_attend.argtypes = [ap, cp, vp, i32p, i32p, i32p, i32p, i32p, i32p, vp, vp, vp, ctypes.c_size_t, i32p, vp]
         _lib = lib
     return _lib
 
@@ -330,6 +366,88 @@ def fastav_prune(params, q, q_idx, cu_qlens, k, v, cu_seqlens, keep_counts, prot
                              hidden_in, pos_in, scores_out, keep_idx_out, cu_keep_out, hidden_out, pos_out, k_out, v_out, workspace,
                              device_status, _stream(stream))
     _check(status, "fastav_prune")
+
+
+# ---- the survivors' K/V cache in 8 bits, and attention over it: argument marshalling only ---------------------
+
+class KvCache:
+    """The handle of an 8-bit K/V cache over its pools: codes [pages, KV heads, page tokens, head_dim] (``torch.int8``, or
+    ``torch.float8_e4m3fn``) and scales [pages, KV heads, page tokens] (fp32), all contiguous."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        formats = {torch.int8: FASTAV_CACHE_INT8, torch.float8_e4m3fn: FASTAV_CACHE_FP8}
+        if k.dtype not in formats or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("expected k and v of one shape [pages, KV heads, page tokens, head_dim], int8 or float8_e4m3fn")
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
+            raise ValueError("expected fp32 scales [pages, KV heads, page tokens]")
+        if not all(t.is_contiguous() for t in (k, v, k_scale, v_scale)):
+            raise ValueError("the pools of a cache are contiguous")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct = fastav_cache(formats[k.dtype], k.shape[2], k.shape[0], k.shape[1], k.shape[3], k.data_ptr(), v.data_ptr(),
+                                   k_scale.data_ptr(), v_scale.data_ptr())
+
+
+def make_cache(num_pages: int, num_kv_heads: int, head_dim: int, page_tokens: int = 64, format: int = FASTAV_CACHE_INT8,
+               device="cuda") -> KvCache:
+    """Allocate the pools of a cache (uninitialised: a place is written before it is read)."""
+    code = {FASTAV_CACHE_INT8: torch.int8, FASTAV_CACHE_FP8: torch.float8_e4m3fn}[format]
+    shape = (num_pages, num_kv_heads, page_tokens)
+    codes = [torch.empty(*shape, head_dim, dtype=torch.int8, device=device).view(code) for _ in range(2)]
+    scales = [torch.empty(shape, dtype=torch.float32, device=device) for _ in range(2)]
+    return KvCache(*codes, *scales)
+
+
+def _table(t: torch.Tensor | None) -> int:
+    """Entries from one row of a page table to the next."""
+    if t is None:
+        return 0
+    if t.dim() != 2 or t.dtype != torch.int32 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("expected an int32 page table [sequences, pages] with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def fastav_cache_write(params, cache: KvCache, k, v, cu_seqlens, keep_idx_opt, cu_keep_opt, page_table, start_opt=None, device_status=None,
+                       stream=None) -> None:
+    """Quantise K and V rows (the survivors of a keep list, or all of them) into the cache's pages."""
+    _check(library().fastav_cache_write(ctypes.byref(params), ctypes.byref(cache.struct), _p(k), _p(v), _p(cu_seqlens), _p(keep_idx_opt),
+                                        _p(cu_keep_opt), _p(page_table), _table(page_table), _p(start_opt), _p(device_status),
+                                        _stream(stream)), "fastav_cache_write")
+
+
+def fastav_cache_read(params, cache: KvCache, page_table, start_opt, cu_seqlens, k_out, v_out, device_status=None, stream=None) -> None:
+    """Rows of the cache as bf16."""
+    _check(library().fastav_cache_read(ctypes.byref(params), ctypes.byref(cache.struct), _p(page_table), _table(page_table), _p(start_opt),
+                                       _p(cu_seqlens), _p(k_out), _p(v_out), _p(device_status), _stream(stream)), "fastav_cache_read")
+
+
+def make_attend_params(*, batch, total_q, max_qlen, num_q_heads, max_kv_len, q, out, page_table, prefix_table=None, max_prefix_len=0,
+                       max_prefix_q=0, softmax_scale=0.0, flags=0) -> fastav_attend_params:
+    """Fill a ``fastav_attend_params`` from host scalars and the tensors whose strides it records."""
+    p = fastav_attend_params()
+    p.batch, p.total_q, p.max_qlen, p.num_q_heads = batch, total_q, max_qlen, num_q_heads
+    p.max_kv_len, p.table_stride = max_kv_len, _table(page_table)
+    p.num_prefixes = 0 if prefix_table is None else prefix_table.shape[0]
+    p.max_prefix_len, p.prefix_table_stride, p.max_prefix_q = max_prefix_len, _table(prefix_table), max_prefix_q
+    p.q_stride_tok, p.q_stride_head = _strides3(q, num_q_heads, q.shape[2])
+    p.o_stride_tok, p.o_stride_head = _strides3(out, num_q_heads, out.shape[2])
+    p.softmax_scale, p.flags = float(softmax_scale), int(flags)
+    return p
+
+
+def fastav_attend_workspace_bytes(params: fastav_attend_params, cache: KvCache) -> int:
+    out = ctypes.c_size_t(0)
+    _check(library().fastav_attend_workspace_bytes(ctypes.byref(params), ctypes.byref(cache.struct), ctypes.byref(out)),
+           "fastav_attend_workspace_bytes")
+    return int(out.value)
+
+
+def fastav_attend(params, cache: KvCache, q, cu_qlens, page_table, kv_lens, out, workspace, cu_prefix=None, prefix_table=None,
+                  prefix_lens=None, lse_out_opt=None, device_status=None, stream=None) -> None:
+    """Attention of q's rows over the cache: a prefix that several sequences share (optional), then each sequence's own tokens."""
+    ws, ws_bytes = _ws(workspace)
+    _check(library().fastav_attend(ctypes.byref(params), ctypes.byref(cache.struct), _p(q), _p(cu_qlens), _p(page_table), _p(kv_lens),
+                                   _p(cu_prefix), _p(prefix_table), _p(prefix_lens), _p(out), _p(lse_out_opt), ws, ws_bytes,
+                                   _p(device_status), _stream(stream)), "fastav_attend")
 
 
 def fastav_kernel_launches() -> int:
