@@ -36,7 +36,7 @@ __device__ Parts find_parts(const AttendCall& c, const AttendList& list, int e, 
   const int r = row - x.row0, granules = granules_of(list, x);
   if (r < 0 || r >= x.rows || granules == 0) return p;
   const int kv = head / c.group, i = r * c.group + head - kv * c.group, tile = i / list.tile_rows;
-  const int start = chain_load_cached(list.ahead + e) + (kv * tiles_of(c, list, x) + tile) * granules;
+  const int start = chain_load_cached(list.ahead + e) + (kv * tiles_of(c, list, x) + tile) * (list.job_cost + granules) + list.job_cost;
   const int total = chain_load_cached(list.ahead + list.entries());
   if (start < 0 || start + granules > total) return p;  // (the arrays changed meanwhile)
   p.row = i - tile * list.tile_rows;
@@ -115,38 +115,49 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(AttendCall c,
   if (c.lse_out && lane == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
+// The levels' entries go to the kernel that suits their rows: few (mma.sync) up to kMostFew stacked rows, else many (tcgen05).
+constexpr int kMostFew = 48;
+
 struct Plan {
-  AttendList own{}, shared{};
-  size_t ahead_own = 0, ahead_shared = 0, out_own = 0, out_shared = 0, ml_own = 0, ml_shared = 0, whole_out = 0, whole_ml = 0, total = 0;
+  AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
+  bool own_many, shared_many;
+  size_t ahead[2], out[2], ml[2], whole_out, whole_ml, total = 0;  // offsets into the workspace: few, many
   bool fits = true;
 };
 
 // Most units of `entries` entries of at most `rows` query rows and `len` keys.
-long long most_units(const fastav_attend_params& p, const fastav_cache& cache, long long entries, long long rows, long long len, int tile_rows, int unit_keys) {
+long long most_units(const fastav_attend_params& p, const fastav_cache& cache, const AttendList& list, long long entries, long long rows, long long len) {
   const long long group = p.num_q_heads / cache.num_kv_heads;
-  return entries * cache.num_kv_heads * ((rows * group + tile_rows - 1) / tile_rows) * ((len + unit_keys - 1) / unit_keys);
+  return entries * cache.num_kv_heads * ((rows * group + list.tile_rows - 1) / list.tile_rows) * (list.job_cost + (len + list.unit_keys - 1) / list.unit_keys);
 }
 
 Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   Plan w;
   size_t off = 0;
   auto carve = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
-  const long long units = most_units(p, cache, p.batch, p.max_qlen, p.max_kv_len, kFewTile, kFewKeys) +
-                          most_units(p, cache, p.num_prefixes, p.max_prefix_q, p.max_prefix_len, kFewTile, kFewKeys);
-  w.fits = units < INT_MAX;
-  AttendList& own = w.own;
-  own.from_prefix = p.num_prefixes;
-  own.from_own = p.batch;
-  own.tile_rows = kFewTile;
-  own.unit_keys = kFewKeys;
-  own.grid = (int)(units < 1 ? 1 : units < kNumSMs ? units : kNumSMs);
-  w.ahead_own = carve((size_t)(own.entries() + 1) * sizeof(int32_t));
-  w.out_own = carve((size_t)own.grid * 2 * own.tile_rows * cache.head_dim * sizeof(float));
-  w.ml_own = carve((size_t)own.grid * 2 * own.tile_rows * sizeof(float2));
-  w.shared = own;
-  w.ahead_shared = w.ahead_own;
-  w.out_shared = w.out_own;
-  w.ml_shared = w.ml_own;
+  const long long group = p.num_q_heads / cache.num_kv_heads;
+  w.own_many = p.max_qlen * group > kMostFew;
+  w.shared_many = p.num_prefixes > 0 && p.max_prefix_q * group > kMostFew;
+  w.few.tile_rows = kFewTile;
+  w.few.unit_keys = kFewKeys;
+  w.many.tile_rows = kManyTile;
+  w.many.unit_keys = kManyKeys;
+  w.few.job_cost = kFewJobCost;
+  w.many.job_cost = kManyJobCost;
+  (w.own_many ? w.many : w.few).from_own = p.batch;
+  (w.shared_many ? w.many : w.few).from_prefix = p.num_prefixes;
+  AttendList* const lists[2] = {&w.few, &w.many};
+  for (int i = 0; i < 2; ++i) {
+    AttendList& list = *lists[i];
+    const long long units = most_units(p, cache, list, list.from_own, p.max_qlen, p.max_kv_len) +
+                            most_units(p, cache, list, list.from_prefix, p.max_prefix_q, p.max_prefix_len);
+    w.fits &= units < INT_MAX;
+    list.grid = (int)(units < 1 ? 1 : units < kNumSMs ? units : kNumSMs);
+    const size_t parts = list.entries() > 0 ? (size_t)list.grid * 2 * list.tile_rows : 0;
+    w.ahead[i] = carve((size_t)(list.entries() + 1) * sizeof(int32_t));
+    w.out[i] = carve(parts * cache.head_dim * sizeof(float));
+    w.ml[i] = carve(parts * sizeof(float2));
+  }
   const size_t rows = p.num_prefixes > 0 ? (size_t)2 * p.total_q * p.num_q_heads : 0;
   w.whole_out = carve(rows * cache.head_dim * sizeof(float));
   w.whole_ml = carve(rows * sizeof(float2));
@@ -228,15 +239,17 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
   c.whole_out = reinterpret_cast<float*>(ws + w.whole_out);
   c.whole_ml = reinterpret_cast<float2*>(ws + w.whole_ml);
-  AttendList own = w.own, shared = w.shared;
-  own.ahead = reinterpret_cast<int32_t*>(ws + w.ahead_own);
-  own.part_out = reinterpret_cast<float*>(ws + w.out_own);
-  own.part_ml = reinterpret_cast<float2*>(ws + w.ml_own);
-  shared.ahead = reinterpret_cast<int32_t*>(ws + w.ahead_shared);
-  shared.part_out = reinterpret_cast<float*>(ws + w.out_shared);
-  shared.part_ml = reinterpret_cast<float2*>(ws + w.ml_shared);
+  AttendList lists[2] = {w.few, w.many};
+  for (int i = 0; i < 2; ++i) {
+    lists[i].ahead = reinterpret_cast<int32_t*>(ws + w.ahead[i]);
+    lists[i].part_out = reinterpret_cast<float*>(ws + w.out[i]);
+    lists[i].part_ml = reinterpret_cast<float2*>(ws + w.ml[i]);
+  }
+  const AttendList &own = lists[w.own_many], &shared = lists[w.shared_many];
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_attend_few(c, own, st);
+  cudaError_t e = cudaSuccess;
+  if (lists[1].entries() > 0) e = launch_attend_many(c, lists[1], st);
+  if (e == cudaSuccess && lists[0].entries() > 0) e = launch_attend_few(c, lists[0], st);
   if (e != cudaSuccess) return cuda_failed(e);
   const int warps = kJoinThreads / 32;
   const dim3 grid((unsigned)(((long long)c.total_q * c.hq + warps - 1) / warps));

@@ -5,7 +5,9 @@
 // G query heads of a KV head are stacked (row i of the stack: query row i / G, head i % G) and cut into tiles; a JOB is one (entry, KV head,
 // tile), its keys cut into granules, the UNITS.  All units of a launch form one list, keys innermost, and every worker takes an equal run
 // of it, whatever the lengths.  A run that begins or ends inside a job leaves a part (running maximum, sum and weighted values); the
-// parts of a job lie with consecutive blocks, and the kernel that joins them works out which from the list alone.
+// parts of a job lie with consecutive blocks, and the kernel that joins them works out which from the list alone.  A job begins with
+// `job_cost` units that hold nothing: what its queries, its output and its first logits cost, in granules; short jobs would else
+// all fall to a few workers.
 #pragma once
 
 #include "cache.cuh"
@@ -36,6 +38,7 @@ inline void mark_head(AttendCall& c, bool head) { c.head_wait = head ? 1 : 0; }
 struct AttendList {
   int from_prefix, from_own;
   int tile_rows, unit_keys;  // of a tile; of a granule
+  int job_cost;              // units ahead of a job's granules
   int grid;                  // blocks that share the list
   int32_t* ahead;            // [entries + 1] units before an entry, left for the kernel that joins
   float* part_out;           // [grid][2][tile_rows][dim]
@@ -44,8 +47,12 @@ struct AttendList {
 };
 
 // Few rows per KV head: mma.sync, a granule per warp (attend_few.cu).
-constexpr int kFewTile = 16, kFewKeys = 32;
+constexpr int kFewTile = 16, kFewKeys = 32, kFewJobCost = 0;
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream);
+
+// Many: tcgen05, a granule per step of a block (attend_many.cu).
+constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4;
+cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 // The pools as [rows of the pool, dim] bytes, boxes of box_rows rows, swizzled by the row's bytes.  `map`: a CUtensorMap.
 bool encode_pool_map(const CacheView& c, const void* pool, int box_rows, void* map);
@@ -92,7 +99,8 @@ __device__ __forceinline__ int tiles_of(const AttendCall& c, const AttendList& l
 }
 __device__ __forceinline__ int granules_of(const AttendList& list, const Entry& x) { return (x.len + list.unit_keys - 1) / list.unit_keys; }
 __device__ __forceinline__ int units_of(const AttendCall& c, const AttendList& list, const Entry& x) {
-  return c.cache.hkv * tiles_of(c, list, x) * granules_of(list, x);
+  const int granules = granules_of(list, x);
+  return granules ? c.cache.hkv * tiles_of(c, list, x) * (list.job_cost + granules) : 0;
 }
 
 // Blocks that have units: all, or the first of them, one unit each.
@@ -142,19 +150,22 @@ __device__ int open_list(const AttendCall& c, const AttendList& list, int* ahead
   return total;
 }
 
-// A walk along the list: the unit it stands at.
+// A walk along the list: the granule it stands at.
 struct Walk {
   Entry x;
   int e, head, tile, granule;
   int tiles, granules;
-  int job_start;  // first unit of the job
+  int unit;  // of the granule
+  __device__ __forceinline__ int job_first() const { return unit - granule; }             // the unit of the job's first granule
+  __device__ __forceinline__ int job_end() const { return unit - granule + granules; }
   __device__ __forceinline__ void load(const AttendCall& c, const AttendList& list) {
     bool bad = false;  // (reported by open_list)
     x = entry_of(c, list, e, bad);
     tiles = tiles_of(c, list, x);
     granules = granules_of(list, x);
   }
-  __device__ void seek(const AttendCall& c, const AttendList& list, const int* ahead, int u) {  // u < the total
+  // To the first granule at or behind unit u, which is less than the total.
+  __device__ void seek(const AttendCall& c, const AttendList& list, const int* ahead, int u) {
     int lo = 0, hi = list.entries();  // the last entry that begins at or before u: one with units
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -162,22 +173,26 @@ struct Walk {
     }
     e = lo;
     load(c, list);
-    const int r = u - ahead[e], job = r / granules;
-    granule = r - job * granules;
+    const int r = u - ahead[e], each = list.job_cost + granules, job = r / each;
+    granule = max(0, r - job * each - list.job_cost);
     head = job / tiles;
     tile = job - head * tiles;
-    job_start = u - granule;
+    unit = ahead[e] + job * each + list.job_cost + granule;
   }
-  __device__ __forceinline__ void step(const AttendCall& c, const AttendList& list, const int* ahead) {  // the next unit exists
-    if (++granule < granules) return;
+  // To the next granule, whose unit is less than `end`, the end of a run; false if there is none.
+  __device__ __forceinline__ bool step(const AttendCall& c, const AttendList& list, const int* ahead, int end) {
+    ++unit;
+    if (++granule < granules) return unit < end;
+    unit += list.job_cost;
+    if (unit >= end) return false;
     granule = 0;
-    job_start += granules;
-    if (++tile < tiles) return;
+    if (++tile < tiles) return true;
     tile = 0;
-    if (++head < c.cache.hkv) return;
+    if (++head < c.cache.hkv) return true;
     head = 0;
-    do ++e; while (ahead[e + 1] <= job_start);
+    do ++e; while (ahead[e + 1] < unit);  // (its first granule stands job_cost units behind its beginning)
     load(c, list);
+    return true;
   }
 };
 #endif

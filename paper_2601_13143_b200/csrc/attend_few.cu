@@ -39,7 +39,7 @@ struct Few {
 
 // A part of a job that a warp leaves for the other warps of its block.
 struct Left {
-  int job_start, job_end, row0, rows, tile, head, own;
+  int job_first, job_end, row0, rows, tile, head, own;
 };
 
 template <int DIM>
@@ -90,7 +90,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     for (int i = 0; i < F::kStages; ++i) ptx::mbar_init(ptx::smem_u32(&full[warp][i]), 1);
     ptx::fence_barrier_init();
   }
-  if (lane < 2) left[warp][lane].job_start = -1;
+  if (lane < 2) left[warp][lane].job_first = -1;
   chain_enter_late(c);
   pdl_wait();  // everything may be what earlier work wrote
   const int total = open_list<kThreads>(c, list, ahead, warp_sum);
@@ -101,11 +101,12 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   const uint32_t ring = ptx::smem_u32(smem.ring(warp));
   const float* const scales = smem.scales(warp);
   bool ok = true;
-  int issued = u0;  // units asked for
-  if (u0 < u1) {
-    Walk next, at;
-    next.seek(c, list, ahead, u0);
-    at = next;
+  int issued = 0;  // granules asked for
+  Walk next;
+  if (u0 < u1) next.seek(c, list, ahead, u0);
+  if (u0 < u1 && next.unit < u1) {
+    Walk at = next;
+    bool more = true;                                        // `next` stands at a granule of the run
     const int box = min(1 << c.cache.page_shift, kFewKeys);  // keys of a copy; lane i has copy i
     int page = 0;                                            // of this lane's copy of the next unit
     auto boxes = [&](const Walk& x) { return (min(kFewKeys, x.x.len - x.granule * kFewKeys) + box - 1) / box; };
@@ -119,7 +120,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
       }
     };
     auto issue = [&] {  // the unit that `next` stands at; then the one after it is looked up
-      const int stage = (issued - u0) % F::kStages, count = boxes(next);
+      const int stage = issued % F::kStages, count = boxes(next);
       const uint32_t bar = ptx::smem_u32(&full[warp][stage]);
       __syncwarp();  // what the stage held has been read
       if (lane == 0) ptx::mbar_arrive_expect_tx(bar, count * box * 2 * (DIM + 4));
@@ -132,21 +133,20 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         bulk_load(to_scale, c.cache.k_scale + row, box * 4, bar);
         bulk_load(to_scale + kFewKeys * 4, c.cache.v_scale + row, box * 4, bar);
       }
-      if (++issued < u1) {
-        next.step(c, list, ahead);
-        look_up();
-      }
+      ++issued;
+      more = next.step(c, list, ahead, u1);
+      if (more) look_up();
     };
     look_up();
-    while (issued < u1 && issued < u0 + F::kStages) issue();
+    while (more && issued < F::kStages) issue();
 
     uint32_t qf[kSteps][4];
     float o[kTiles][4], m[2], l[2], power[2], row_scale[2];
     int sees[2], all_see = 0;
 #pragma unroll 1
-    for (int u = u0; u < u1; ++u) {
+    for (int n = 0;; ++n) {
       const int key0 = at.granule * kFewKeys;
-      if (u == u0 || at.granule == 0) {  // another job: its query rows
+      if (n == 0 || at.granule == 0) {  // another job: its query rows
         all_see = INT_MAX;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -186,8 +186,8 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
       }
-      const int stage = (u - u0) % F::kStages;
-      ok = ptx::mbar_wait_warp(ptx::smem_u32(&full[warp][stage]), ((u - u0) / F::kStages) & 1, &abort_flag);
+      const int stage = n % F::kStages;
+      ok = ptx::mbar_wait_warp(ptx::smem_u32(&full[warp][stage]), (n / F::kStages) & 1, &abort_flag);
       if (!ok) break;
       const uint32_t kt = ring + stage * F::kStage, vt = kt + F::kHalf;
       const float* const ks = scales + stage * F::kScales;
@@ -307,12 +307,12 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             mma_f16(o[4 * j + 2 * half + 1], weight[2 * s][0], weight[2 * s][1], weight[2 * s + 1][0], weight[2 * s + 1][1], b01, b11);
           }
       }
-      if (issued < u1) issue();
+      if (more) issue();
 
-      const int job_end = at.job_start + at.granules;
-      if (u + 1 == u1 || u + 1 == job_end) {  // the end of the job, or of the run
-        const bool whole = at.job_start >= u0 && job_end <= u1;
-        const int slot = at.job_start < u0 ? 0 : 1;
+      const int job_first = at.job_first(), job_end = at.job_end();
+      if (at.unit + 1 == u1 || at.unit + 1 == job_end) {  // the end of the job, or of the run
+        const bool whole = job_first >= u0 && job_end <= u1;
+        const int slot = job_first < u0 ? 0 : 1;
         // (a run's last part may lie where its ring was: nothing is in flight any more)
         float* const part = slot == 0 ? smem.first_part(warp, part_rows) : reinterpret_cast<float*>(smem.ring(warp));
         if (!whole) __syncwarp();  // (the ring has been read)
@@ -355,16 +355,16 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             }
           }
         }
-        if (!whole && lane == 0) left[warp][slot] = Left{at.job_start, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own};
+        if (!whole && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own};
       }
-      if (u + 1 < u1) at.step(c, list, ahead);
+      if (!at.step(c, list, ahead, u1)) break;
     }
     if (!ok) {
       if (lane == 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_WAIT_EXPIRED);
       // The copies in flight write into this block's shared memory: they are waited for before it may exit, also where another warp gave up.
       int never = 0;
-      for (int u = max(u0, issued - F::kStages); u < issued; ++u)
-        ptx::mbar_wait_bounded(ptx::smem_u32(&full[warp][(u - u0) % F::kStages]), ((u - u0) / F::kStages) & 1, &never);
+      for (int n = max(0, issued - F::kStages); n < issued; ++n)
+        ptx::mbar_wait_bounded(ptx::smem_u32(&full[warp][n % F::kStages]), (n / F::kStages) & 1, &never);
     }
   }
   pdl_trigger();
@@ -374,29 +374,29 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   // The parts of one job that several warps left, joined in their order: to the output if the block has the whole job, else to the block's place.
   for (int i = 0; i < 2 * kWarps;) {
     const Left job = left[i / 2][i % 2];
-    if (job.job_start < 0) {
+    if (job.job_first < 0) {
       ++i;
       continue;
     }
     int end = i + 1;  // (unused slots lie between)
     for (int j = i + 1; j < 2 * kWarps; ++j) {
-      const int start = left[j / 2][j % 2].job_start;
-      if (start >= 0 && start != job.job_start) break;
+      const int start = left[j / 2][j % 2].job_first;
+      if (start >= 0 && start != job.job_first) break;
       end = j + 1;
     }
-    const bool whole = job.job_start >= block_u0 && job.job_end <= block_u1;
-    const int slot = job.job_start < block_u0 ? 0 : 1;
+    const bool whole = job.job_first >= block_u0 && job.job_end <= block_u1;
+    const int slot = job.job_first < block_u0 ? 0 : 1;
     const int rows = min(kFewTile, job.rows * c.group - job.tile * kFewTile);
     for (int item = threadIdx.x; item < rows * (DIM / 4); item += kThreads) {
       const int row = item / (DIM / 4), piece = item % (DIM / 4);
       float top = -INFINITY;
       for (int j = i; j < end; ++j)
-        if (left[j / 2][j % 2].job_start >= 0) top = fmaxf(top, left_ml[j / 2][j % 2][row].x);
+        if (left[j / 2][j % 2].job_first >= 0) top = fmaxf(top, left_ml[j / 2][j % 2][row].x);
       const float base = top == -INFINITY ? 0.f : top;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       float sum = 0.f;
       for (int j = i; j < end; ++j) {
-        if (left[j / 2][j % 2].job_start < 0) continue;
+        if (left[j / 2][j % 2].job_first < 0) continue;
         const float2 ml = left_ml[j / 2][j % 2][row];
         const float f = ptx::ex2_approx(ml.x - base);
         const float* const part = j % 2 == 0 ? smem.first_part(j / 2, part_rows) : reinterpret_cast<const float*>(smem.ring(j / 2));
