@@ -3,21 +3,21 @@
 // Dense contractions, so they run on the fifth-generation tensor cores: S = Q K^T and O += P V (tcgen05.mma, f16 operands, fp32 sums in
 // tensor memory).  A unit is 128 keys of one KV head for up to 256 stacked query rows.  Per block, one per SM:
 //
-//   warps 0-7    softmax, a thread per row: warps 0-3 and 4-7 are two STREAMS with an S and an O of their own, so that the matrix pipe
-//                works on one while the exponentials of the other are taken.  With more than 128 rows the streams are the two halves of
-//                the rows and share every tile of keys; with fewer they take the tiles in turn and their sums are joined at the end.
-//   warps 8-15   codes -> f16, 16 keys of every tile each: straight from global memory (one tile ahead in registers) to the operand
+//   warps 0-15   softmax, two threads per row with half of a visit's columns each.  Warps 0-7 and 8-15 are two STREAMS with an S and an O
+//                of their own, so that the matrix pipe works on one while the exponentials of the other are taken.  With more than 128
+//                rows the streams are the two halves of the rows and share every tile of keys; with fewer they take the tiles in turn
+//                and their sums are joined at the end.
+//   warps 16-23  codes -> f16, 16 keys of every tile each: straight from global memory (one tile ahead in registers) to the operand
 //                tiles in shared memory
-//   warp 16      issues the MMAs: QK of a visit goes out before PV of the visit before it (warps 17-19 fill its warpgroup)
+//   warp 24      issues the MMAs: QK of a visit goes out before PV of the visit before it (warps 25-27 fill its warpgroup)
 //
-// Registers move from the warps that need few to the softmax's, which hold a visit's weights.
+// Registers move from the warps that need few to the softmax's, which hold a visit's logits.
 //
 // A value's scale is folded into its f16 operand relative to the power of two E of the largest scale of 16 keys, and E joins the exponent:
 // w = 2^(z + E - m + kOffset) is rounded to f16 for the matrix pipe, l = sum w 2^(-E - kOffset) stays in fp32.  So no weight is
 // multiplied by a scale, and values of very different size keep their bits.  The keys' scales multiply the logits in fp32.
 //
-// The weights of a visit are taken with the maximum of the visits before; only where one comes out above 2^15 (or a row meets its first keys)
-// the visit's own maximum is taken first, and O rescaled.
+// O is rescaled only when a row's maximum has grown by 2^kSlack: until then its weights are larger than 2^kOffset, which f16 has room for.
 #include <limits.h>
 
 #include <cuda.h>
@@ -30,15 +30,15 @@ namespace fastav {
 namespace {
 
 constexpr int kSub = 128;  // rows of a stream
-constexpr int kSoftWarps = 8, kConvWarps = 8, kIssueWarp = kSoftWarps + kConvWarps, kWarps = kIssueWarp + 4;
+constexpr int kSoftWarps = 16, kConvWarps = 8, kIssueWarp = kSoftWarps + kConvWarps, kWarps = kIssueWarp + 4;
 constexpr int kSoftThreads = 32 * kSoftWarps, kThreads = 32 * kWarps;
 // Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
-constexpr int kSoftRegs = 152, kConvRegs = 72, kIssueRegs = 24;
+constexpr int kSoftRegs = 88, kConvRegs = 64, kIssueRegs = 24;
 constexpr int kRegsNeeded = 32 * (kSoftWarps * kSoftRegs + kConvWarps * kConvRegs + 4 * kIssueRegs);
 constexpr int kGroups = kManyKeys / 16;          // of 16 keys: a converting warp's
 constexpr int kScaleRing = 4;
 constexpr int kOffset = 11;                      // the largest weight of a row's first visit is 2^kOffset ...
-constexpr unsigned kMostWeight = 0x7800;          // ... and of any visit at most this: 2^15 as f16 bits (f16 ends at 65,504)
+constexpr float kSlack = 4.f;                     // ... and the maximum is moved when a logit is this much above it (f16 ends at 2^16)
 constexpr int kValuePower = 7;                   // a value operand is code * (scale / 2^E) * 2^kValuePower, below 2^15
 constexpr int kTmemCols = 512;
 static_assert(kConvWarps == kGroups);
@@ -58,10 +58,13 @@ struct Control {
   int warp_sum[kWarps];
   alignas(16) float k_scale[kScaleRing][kManyKeys];
   float exponent[kScaleRing][kGroups], unscale[kScaleRing][kGroups];  // E; 2^(-E - kOffset)
-  float2 row_ml[2][kSub];                                             // the streams' statistics, to be joined
+  float row_scale[2][kSub];                                           // of a stream's query rows
+  float row_top[2][2][2][kSub];                                       // [visit & 1][stream][half of the columns]
+  float row_m[2][kSub], row_l[2][2][kSub];                            // of a stream; of a half of its columns
 };
 
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory"); }
+__device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 64;" ::"r"(2 + pair) : "memory"); }  // the two warps of 32 rows
 
 // What a block does of its run in one job: `tiles` tiles of keys from `first` on.
 struct Segment {
@@ -80,17 +83,28 @@ __device__ __forceinline__ bool skip(const AttendCall& c, const AttendList& list
 }
 
 // ---- codes to f16 ----------------------------------------------------------------------------------------------------
-// One warp's 16 keys of a tile: lane's 16-byte pieces of K or V.  DIM 128: rows 4 j + lane / 8, piece lane % 8; DIM 64: rows 8 j + lane / 4, piece lane % 4.
+// One warp's 16 keys of a tile, 16 codes per lane and load.  DIM 128: a load is 4 keys of 8 pieces; lane bits 0, 1 and 3 name the piece, 2 and 4 the
+// key, so that the eight lanes of a phase store to eight different banks' quarters.  DIM 64: 8 keys of 4 pieces.
 template <int DIM>
 struct Piece {
-  static constexpr int kLoads = DIM / 32, kRowLanes = DIM / 16;
-  static __device__ __forceinline__ int row(int j, int lane) { return j * (32 / kRowLanes) + lane / kRowLanes; }
+  static constexpr int kLoads = DIM / 32, kRows = 16 / kLoads;  // loads; keys of one
+  int piece, row;
+  uint32_t to[2];  // where the first half of the piece goes in an operand tile, from the tile's start: keys of even and of odd loads
+  __device__ __forceinline__ Piece(int warp, int lane) {
+    piece = DIM == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+    row = DIM == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+      const int r = 16 * warp + row + odd * kRows;
+      to[odd] = (piece >> 2) * Many<DIM>::kHalfBytes + (16 * warp + row) * 128 + (((2 * (piece & 3)) ^ (r & 7)) << 4);
+    }
+  }
+  __device__ __forceinline__ int key(int j) const { return j * kRows + row; }
 };
 
 // 16 codes -> 32 bytes of a swizzled operand row.  `times`: f16x2 factor (values only).
-template <int DIM, bool FP8, bool VALUES>
-__device__ __forceinline__ void convert_piece(const uint4& x, uint32_t tile, int row, int lane, uint32_t times) {
-  const int piece = lane & (Piece<DIM>::kRowLanes - 1);
+template <bool FP8, bool VALUES>
+__device__ __forceinline__ void convert_piece(const uint4& x, uint32_t at, uint32_t times) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t h[8];
 #pragma unroll
@@ -101,22 +115,15 @@ __device__ __forceinline__ void convert_piece(const uint4& x, uint32_t tile, int
       asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h[2 * i + 1]) : "r"(times));
     }
   }
-  const uint32_t at = tile + (piece >> 2) * Many<DIM>::kHalfBytes + row * 128;
-  const int chunk = 2 * (piece & 3), turn = DIM == 128 ? piece >> 2 : 0;  // (lanes of the second half the other way round: no two on one bank)
-  const uint32_t first = at + ((chunk ^ turn ^ (row & 7)) << 4), second = at + ((chunk ^ turn ^ 1 ^ (row & 7)) << 4);
-  if (turn) {
-    ptx::st_shared4(first, h[4], h[5], h[6], h[7]);
-    ptx::st_shared4(second, h[0], h[1], h[2], h[3]);
-  } else {
-    ptx::st_shared4(first, h[0], h[1], h[2], h[3]);
-    ptx::st_shared4(second, h[4], h[5], h[6], h[7]);
-  }
+  ptx::st_shared4(at, h[0], h[1], h[2], h[3]);
+  ptx::st_shared4(at ^ 16, h[4], h[5], h[6], h[7]);
 }
 
 template <int DIM, bool FP8>
 __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t k_tiles, uint32_t v_tiles, int u0,
                                              int u1, int warp, int lane) {
   using P = Piece<DIM>;
+  const P mine(warp, lane);
   Walk at;
   at.seek(c, list, ahead, u0);
   if (at.unit >= u1) return;
@@ -138,11 +145,11 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     }
     pool = (int)pool_row(c.cache, page, at.head, key0);
   };
-  const int piece = lane & (P::kRowLanes - 1);
+  // (What lies behind a sequence's end in its last page may be anything: the logits of such keys are hidden, and values are zeroed below.)
   auto ask = [&](const uint8_t* codes, uint4 (&to)[P::kLoads]) {
+    const uint8_t* const from = codes + (long long)pool * DIM + mine.row * DIM + mine.piece * 16;
 #pragma unroll
-    for (int j = 0; j < P::kLoads; ++j)
-      to[j] = P::row(j, lane) < have ? chain_load(reinterpret_cast<const uint4*>(codes + ((long long)pool + P::row(j, lane)) * DIM + piece * 16)) : make_uint4(0, 0, 0, 0);
+    for (int j = 0; j < P::kLoads; ++j) to[j] = chain_load(reinterpret_cast<const uint4*>(from + j * P::kRows * DIM));
   };
   auto ask_scales = [&] {
     ks = lane < have ? chain_load(c.cache.k_scale + pool + lane) : 0.f;
@@ -165,7 +172,9 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     for (int d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     const int e = top > 0.f ? min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 118) : 0;  // top <= 2^e (lanes 0 to 15)
     const float times = good ? vs * __uint_as_float((unsigned)(127 + kValuePower - e) << 23) : 0.f;
+    const uint32_t factor = two_f16(times, times);
     const float key_scale = good ? ks : __uint_as_float(0x7FC00000u);
+    const int exist = have;
 
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), free_parity, &ctl.abort);  // (a wait that gives up only marks the results as invalid)
     if (lane < 16) ctl.k_scale[ring][16 * warp + lane] = key_scale;
@@ -175,7 +184,7 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     }
 #pragma unroll
     for (int j = 0; j < P::kLoads; ++j)
-      convert_piece<DIM, FP8, false>(k[j], k_tiles + slot * Many<DIM>::kTileBytes, 16 * warp + P::row(j, lane), lane, 0);
+      convert_piece<FP8, false>(k[j], k_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, 0);
     ptx::fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
@@ -188,11 +197,13 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
       ask_scales();
     }
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.v_empty[slot]), free_parity, &ctl.abort);
+    if (exist < 16)
 #pragma unroll
-    for (int j = 0; j < P::kLoads; ++j) {
-      const float f = __shfl_sync(0xFFFFFFFFu, times, P::row(j, lane));
-      convert_piece<DIM, FP8, true>(v[j], v_tiles + slot * Many<DIM>::kTileBytes, 16 * warp + P::row(j, lane), lane, two_f16(f, f));
-    }
+      for (int j = 0; j < P::kLoads; ++j)
+        if (mine.key(j) >= exist) v[j] = make_uint4(0, 0, 0, 0);  // (e4m3 has NaN, which a factor of 0 does not take away)
+#pragma unroll
+    for (int j = 0; j < P::kLoads; ++j)
+      convert_piece<FP8, true>(v[j], v_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, __shfl_sync(0xFFFFFFFFu, factor, mine.key(j)));
     ptx::fence_proxy_async_smem();
     ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.v_full[slot]), lane);
     if (!more) break;
@@ -262,82 +273,71 @@ struct Visit {
   const float *exponent, *unscale;
 };
 
-// One visit's weights with the maximum `m` (base 2): f16 pairs, and their fp32 sum.  `limit`: columns from there on are hidden.
-template <bool MASKED>
-__device__ __forceinline__ float visit_weights(const Visit& x, float row_scale, float m, int limit, uint32_t (&p)[kManyKeys / 2]) {
-  float l = 0.f;
-  const float2 rs = make_float2(row_scale, row_scale);
-  uint32_t v[2][32];
-  ptx::tmem_ld32(x.s, v[0]);
+constexpr int kCols = kManyKeys / 2;  // of a thread
+
+// A visit's logits times the scales of their keys (and not yet of the row), and the largest z + E of them; `limit`: columns from there on are hidden.
+__device__ __forceinline__ float visit_logits(const Visit& x, float row_scale, bool masked, int limit, float2 (&t)[kCols / 2]) {
+  uint32_t (&v)[kCols / 32][32] = reinterpret_cast<uint32_t(&)[kCols / 32][32]>(t);
 #pragma unroll
-  for (int b = 0; b < kManyKeys / 32; ++b) {
-    uint32_t(&z)[32] = v[b & 1];
-    ptx::tmem_ld_wait_for(z);
-    if (b + 1 < kManyKeys / 32) ptx::tmem_ld32(x.s + (b + 1) * 32, v[(b + 1) & 1]);
+  for (int b = 0; b < kCols / 32; ++b) ptx::tmem_ld32(x.s + b * 32, v[b]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int g = 2 * b + h;
-      const float add = x.exponent[g] - m + kOffset;
-      const float2 plus = make_float2(add, add);
-      float2 sum = make_float2(0.f, 0.f);
+  for (int b = 0; b < kCols / 32; ++b) ptx::tmem_ld_wait_for(v[b]);
 #pragma unroll
-      for (int j = 0; j < 16; j += 4) {
-        const float4 ks = *reinterpret_cast<const float4*>(x.ks + g * 16 + j);
-        const uint32_t* const t = z + h * 16 + j;
-        float2 t0 = __fmul2_rn(make_float2(__uint_as_float(t[0]), __uint_as_float(t[1])), make_float2(ks.x, ks.y));
-        float2 t1 = __fmul2_rn(make_float2(__uint_as_float(t[2]), __uint_as_float(t[3])), make_float2(ks.z, ks.w));
-        t0 = __ffma2_rn(t0, rs, plus);
-        t1 = __ffma2_rn(t1, rs, plus);
-        float2 w0 = make_float2(ptx::ex2_approx(t0.x), ptx::ex2_approx(t0.y)), w1 = make_float2(ptx::ex2_approx(t1.x), ptx::ex2_approx(t1.y));
-        if (MASKED) {
-          const int k = g * 16 + j;
-          w0.x = k < limit ? w0.x : 0.f;
-          w0.y = k + 1 < limit ? w0.y : 0.f;
-          w1.x = k + 2 < limit ? w1.x : 0.f;
-          w1.y = k + 3 < limit ? w1.y : 0.f;
-        }
-        sum = __fadd2_rn(sum, __fadd2_rn(w0, w1));
-        p[(g * 16 + j) / 2] = two_f16(w0.x, w0.y);
-        p[(g * 16 + j) / 2 + 1] = two_f16(w1.x, w1.y);
-      }
-      l = fmaf(sum.x + sum.y, x.unscale[g], l);
+  for (int j = 0; j < kCols / 2; j += 2) {
+    const float4 ks = *reinterpret_cast<const float4*>(x.ks + 2 * j);
+    t[j] = __fmul2_rn(t[j], make_float2(ks.x, ks.y));
+    t[j + 1] = __fmul2_rn(t[j + 1], make_float2(ks.z, ks.w));
+  }
+  if (masked) {
+#pragma unroll
+    for (int j = 0; j < kCols / 2; ++j) {
+      if (2 * j >= limit) t[j].x = -INFINITY;
+      if (2 * j + 1 >= limit) t[j].y = -INFINITY;
     }
   }
-  return l;
-}
-
-// The largest z + E of the visit's visible keys (-inf: none).
-__device__ __forceinline__ float visit_top(const Visit& x, float row_scale, int limit) {
   float top = -INFINITY;
-#pragma unroll 1
-  for (int b = 0; b < kManyKeys / 32; ++b) {
-    uint32_t z[32];
-    ptx::tmem_ld32(x.s + b * 32, z);
-    ptx::tmem_ld_wait_for(z);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float most = -INFINITY;
+  for (int g = 0; g < kCols / 16; ++g) {
+    float most = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float t = __uint_as_float(z[h * 16 + j]) * x.ks[b * 32 + h * 16 + j];
-        most = fmaxf(most, b * 32 + h * 16 + j < limit ? t : -INFINITY);
-      }
-      top = fmaxf(top, fmaf(most, row_scale, x.exponent[2 * b + h]));
-    }
+    for (int j = g * 8; j < g * 8 + 8; ++j) most = ptx::max3(most, t[j].x, t[j].y);
+    top = fmaxf(top, fmaf(most, row_scale, x.exponent[g]));
   }
   return top;
 }
+// Their weights with the maximum `m` (base 2) as f16 pairs to tensor memory; the fp32 sum.
+__device__ __forceinline__ float visit_weights(const Visit& x, uint32_t to, float row_scale, float m, float2 (&t)[kCols / 2]) {
+  float l = 0.f;
+  const float2 rs = make_float2(row_scale, row_scale);
+  uint32_t p[kCols / 2];
+#pragma unroll
+  for (int g = 0; g < kCols / 16; ++g) {
+    const float add = x.exponent[g] - m + kOffset;
+    const float2 plus = make_float2(add, add);
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = g * 8; j < g * 8 + 8; ++j) {
+      const float2 z = __ffma2_rn(t[j], rs, plus), w = make_float2(ptx::ex2_approx(z.x), ptx::ex2_approx(z.y));
+      sum = __fadd2_rn(sum, w);
+      p[j] = two_f16(w.x, w.y);
+    }
+    l = fmaf(sum.x + sum.y, x.unscale[g], l);
+  }
+  ptx::tmem_st32(to, p);
+  return l;
+}
 
 template <int DIM>
-__device__ __forceinline__ void rescale_output(uint32_t o, float factor) {
+__device__ __forceinline__ void rescale_output(uint32_t o, float factor) {  // (few registers: the visit's logits are held meanwhile)
 #pragma unroll 1
-  for (int i = 0; i < DIM; i += 32) {
-    uint32_t v[32];
-    ptx::tmem_ld32(o + i, v);
+  for (int i = 0; i < DIM / 2; i += 8) {
+    uint32_t v[8];
+    ptx::tmem_ld8(o + i, v);
     ptx::tmem_ld_wait_for(v);
+    float f[8];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * factor);
-    ptx::tmem_st32(o + i, v);
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[j]) * factor;
+    ptx::tmem_st8(o + i, f);
   }
   ptx::tmem_st_wait();
 }
@@ -352,59 +352,54 @@ __device__ __forceinline__ Place place_of(const AttendCall& c, const Walk& at, i
   return Place{(long long)at.x.row0 + r, at.head * c.group + i - r * c.group, r};
 }
 
-// 32 query rows of a warp into their operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16;
-// for the lane's own row what takes that back, times the softmax scale.
+// 16 query rows into their operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to
+// `scale` what takes that back, times the softmax scale.
 template <int DIM>
-__device__ __forceinline__ float load_queries(const AttendCall& c, const Walk& at, int first_row, uint32_t tile, int row_in_tile, int lane) {
-  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kAtOnce = 8;  // rows of a load; loads in flight
+__device__ __forceinline__ void load_queries(const AttendCall& c, const Walk& at, int first_row, uint32_t tile, int row_in_tile, float* scale, int lane) {
+  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kLoads = 16 / kRows;  // rows of a load; loads, all in flight
   const int sub = lane / kLanes, piece = lane % kLanes;
-  float mine = 0.f;
+  uint4 x[kLoads];
 #pragma unroll
-  for (int j0 = 0; j0 < 32 / kRows; j0 += kAtOnce) {
-    uint4 x[kAtOnce];
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      const int tile_row = first_row + (j0 + j) * kRows + sub;
-      const Place q = place_of(c, at, tile_row);
-      x[j] = q.r < at.x.rows ? chain_load_cached(reinterpret_cast<const uint4*>(c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8)) : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      const unsigned m = 0x7FFF7FFFu;
-      unsigned top = __vmaxu2(__vmaxu2(x[j].x & m, x[j].y & m), __vmaxu2(x[j].z & m, x[j].w & m));  // what is not a number is larger than the rest
-      top = max(top >> 16, top & 0xFFFFu);
-#pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-      const float to = to_one(__uint_as_float(top << 16));
-      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-      uint32_t h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xFFFF0000u) * to);
-      const int row = row_in_tile + (j0 + j) * kRows + sub;
-      ptx::st_shared4(tile + (piece >> 3) * Many<DIM>::kHalfBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4), h[0], h[1], h[2], h[3]);
-      const float of_row = __shfl_sync(0xFFFFFFFFu, to, lane % kRows * kLanes);
-      if (lane / kRows == j0 + j) mine = c.scale_log2 / of_row;
-    }
+  for (int j = 0; j < kLoads; ++j) {
+    const Place q = place_of(c, at, first_row + j * kRows + sub);
+    x[j] = q.r < at.x.rows ? chain_load_cached(reinterpret_cast<const uint4*>(c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8)) : make_uint4(0, 0, 0, 0);
   }
-  return mine;
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const unsigned m = 0x7FFF7FFFu;
+    unsigned top = __vmaxu2(__vmaxu2(x[j].x & m, x[j].y & m), __vmaxu2(x[j].z & m, x[j].w & m));  // what is not a number is larger than the rest
+    top = max(top >> 16, top & 0xFFFFu);
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const float to = to_one(__uint_as_float(top << 16));
+    const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xFFFF0000u) * to);
+    const int row = row_in_tile + j * kRows + sub;
+    ptx::st_shared4(tile + (piece >> 3) * Many<DIM>::kHalfBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4), h[0], h[1], h[2], h[3]);
+    if (piece == 0) scale[row] = c.scale_log2 / to;
+  }
 }
 
 template <int DIM>
 __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t q_tiles, int u0, int u1, int warp, int lane) {
   using M = Many<DIM>;
-  const int stream = warp >> 2, row = (warp & 3) * 32 + lane;
-  const uint32_t lanes = ctl.tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-  const uint32_t s = lanes + stream * kManyKeys, o = lanes + 2 * kManyKeys + stream * 128;
+  const int stream = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, row = quarter * 32 + lane, pair = stream * 4 + quarter;
+  const uint32_t lanes = ctl.tmem_base + ((uint32_t)(quarter * 32) << 16), outputs = lanes + 2 * kManyKeys;
+  const uint32_t s = lanes + stream * kManyKeys;
   Walk at;
   at.seek(c, list, ahead, u0);
   int visits = 0, done = 0;  // of this stream; tiles before the segment
   for (bool more = at.unit < u1; more;) {
     const Segment seg = segment_of(c, at, u1);
     // With two streams of rows a thread's row is of its stream's half; else threads of both streams have the same one.
-    const int warp_row = (seg.two ? stream * kSub : 0) + (warp & 3) * 32;
-    const float row_scale = load_queries<DIM>(c, at, warp_row, q_tiles + stream * M::kTileBytes, (warp & 3) * 32, lane);
+    const int warp_row = (seg.two ? stream * kSub : 0) + quarter * 32;
+    load_queries<DIM>(c, at, warp_row + half * 16, q_tiles + stream * M::kTileBytes, quarter * 32 + half * 16, ctl.row_scale[stream], lane);
     ptx::fence_proxy_async_smem();
     ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.q_full), lane);
+    pair_sync(pair);
+    const float row_scale = ctl.row_scale[stream][row];
     int sees, all_see;
     bool there;
     {
@@ -419,42 +414,28 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
 #pragma unroll 1
     for (int tile = seg.two ? 0 : stream; tile < seg.tiles; tile += seg.two ? 1 : 2) {
       const int n = done + tile, ring = n & (kScaleRing - 1);
-      const Visit x{s, ctl.k_scale[ring], ctl.exponent[ring], ctl.unscale[ring]};
+      const Visit x{s + half * kCols, ctl.k_scale[ring] + half * kCols, ctl.exponent[ring] + half * (kGroups / 2), ctl.unscale[ring] + half * (kGroups / 2)};
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.scale_full[ring]), (n / kScaleRing) & 1, &ctl.abort);
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[stream]), visits & 1, &ctl.abort);
       ptx::tc_fence_after_sync();
       const int key0 = (seg.first + tile) * kManyKeys;
-      const int limit = sees - key0;  // columns of this row that are visible
-      uint32_t p[kManyKeys / 2];
-      float sum = 0.f;
-      bool redo = first, masked = key0 + kManyKeys > all_see;
-      if (!first && !masked) {
-        sum = visit_weights<false>(x, row_scale, m == -INFINITY ? 0.f : m, limit, p);
-        uint32_t most[2] = {p[0], p[1]};
-#pragma unroll
-        for (int j = 2; j < kManyKeys / 2; ++j) asm("max.f16x2 %0, %0, %1;" : "+r"(most[j & 1]) : "r"(p[j]));
-        asm("max.f16x2 %0, %0, %1;" : "+r"(most[0]) : "r"(most[1]));
-        const unsigned top = max(most[0] >> 16, most[0] & 0xFFFFu);  // (not negative: bits compare as values)
-        redo = __any_sync(0xFFFFFFFFu, there && (top > kMostWeight || m == -INFINITY));
+      float2 t[kCols / 2];
+      float top = visit_logits(x, row_scale, key0 + kManyKeys > all_see, sees - key0 - half * kCols, t);
+      float(&tops)[2][kSub] = ctl.row_top[visits & 1][stream];
+      tops[half][row] = top;
+      pair_sync(pair);  // ... and both have read their logits: the weights may take their place
+      top = fmaxf(top, tops[half ^ 1][row]);
+      if (first) {
+        m = top;
+      } else if (__any_sync(0xFFFFFFFFu, there && (top > m + kSlack || (m == -INFINITY && top > m)))) {  // the sums so far
+        const float to = fmaxf(top, m), factor = m == -INFINITY ? 0.f : ptx::ex2_approx(m - to);
+        l *= factor;
+        m = to;
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.pv_done[stream]), (visits - 1) & 1, &ctl.abort);
+        ptx::tc_fence_after_sync();
+        rescale_output<DIM>(outputs + stream * 128 + half * (DIM / 2), factor);
       }
-      if (redo || masked) {  // the visit's own maximum first
-        const float top = visit_top(x, row_scale, limit);
-        if (first) {
-          m = top;
-        } else if (__any_sync(0xFFFFFFFFu, top > m)) {  // the sums so far
-          const float to = fmaxf(top, m), factor = m == -INFINITY ? 0.f : ptx::ex2_approx(m - to);
-          l *= factor;
-          m = to;
-          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.pv_done[stream]), (visits - 1) & 1, &ctl.abort);
-          ptx::tc_fence_after_sync();
-          rescale_output<DIM>(o, factor);
-        }
-        sum = visit_weights<true>(x, row_scale, m == -INFINITY ? 0.f : m, limit, p);
-      }
-      l += sum;
-      __syncwarp();
-      ptx::tmem_st32(s, p);
-      ptx::tmem_st32(s + 32, p + 32);
+      l += visit_weights(x, s + half * (kCols / 2), row_scale, m == -INFINITY ? 0.f : m, t);
       ptx::tmem_st_wait();
       ptx::tc_fence_before_sync();
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.p_full[stream]), lane);
@@ -463,22 +444,26 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     }
     if (!first) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.pv_done[stream]), (visits - 1) & 1, &ctl.abort);
 
-    // The end of the segment.  O is sum 2^(z - m) v times 2^(kOffset + kValuePower).
-    const bool both = !seg.two && seg.tiles > 1;  // the other stream has a part of the row, too
+    // The end of the segment: the halves' sums, and those of the streams where both have a part of the row.  O is sum 2^(z - m) v times
+    // 2^(kOffset + kValuePower).
+    if (half == 0) ctl.row_m[stream][row] = m;
+    ctl.row_l[stream][half][row] = l;
+    ptx::tc_fence_before_sync();
+    soft_sync();
+    ptx::tc_fence_after_sync();
+    const int mine = seg.two ? stream : 0;
+    const bool both = !seg.two && seg.tiles > 1;
+    m = ctl.row_m[mine][row];
+    l = ctl.row_l[mine][0][row] + ctl.row_l[mine][1][row];
     float other = 0.f, back = __uint_as_float((unsigned)(127 - kOffset - kValuePower) << 23);
     if (both) {
-      ctl.row_ml[stream][row] = make_float2(m, l);
-      ptx::tc_fence_before_sync();
-      soft_sync();
-      const float2 ml = ctl.row_ml[stream ^ 1][row];
-      const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
-      const float mine = ptx::ex2_approx(m - base), theirs = ptx::ex2_approx(ml.x - base);
-      l = l * mine + ml.y * theirs;
-      other = back * theirs;
-      back *= mine;
-      m = top;
+      const float m1 = ctl.row_m[1][row], to = fmaxf(m, m1), base = to == -INFINITY ? 0.f : to;
+      const float f0 = ptx::ex2_approx(m - base), f1 = ptx::ex2_approx(m1 - base);
+      l = l * f0 + (ctl.row_l[1][0][row] + ctl.row_l[1][1][row]) * f1;
+      other = back * f1;
+      back *= f0;
+      m = to;
     }
-    ptx::tc_fence_after_sync();
     const bool whole = at.job_first() >= u0 && at.job_end() <= u1, final = whole && c.prefixes == 0;
     const long long level = at.x.own ? 0ll : (long long)c.total_q * c.hq;
     const long long part = ((long long)blockIdx.x * 2 + (at.job_first() < u0 ? 0 : 1)) * kManyTile;  // the block's place for what it did not finish
@@ -487,36 +472,36 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
       back *= inv;
       other *= inv;
     }
-    // A stream writes its rows; where both have the same rows, half of the columns each.  By 64 columns through this warp's part of the
-    // stream's query tile, which nobody needs any more, so that rows are written in whole lines.
-    const int from = both ? stream * (DIM / 2) : 0, to = seg.two ? DIM : both ? from + DIM / 2 : stream == 0 ? DIM : 0;
-    constexpr int kWide = DIM == 128 ? 64 : 32, kLanes = kWide / 4, kRows = 32 / kLanes;
-    const uint32_t stage = q_tiles + stream * M::kTileBytes + (warp & 3) * (32 * kWide * 4);
+    // The warps of 32 rows share the columns.  By kWide of them through shared memory (the query tiles, which nobody needs any more), so that
+    // rows are written in whole lines.
+    constexpr int kWide = DIM / 4, kLanes = kWide / 4, kRows = 32 / kLanes;
+    const int from = seg.two ? half * (DIM / 2) : (stream * 2 + half) * kWide, to = from + (seg.two ? DIM / 2 : kWide);
+    const uint32_t stage = q_tiles + warp * (32 * kWide * 4);
 #pragma unroll 1
     for (int d = from; d < to; d += kWide) {
 #pragma unroll
-      for (int h = 0; h < kWide; h += 32) {
-        uint32_t v[32], y[32];
-        ptx::tmem_ld32(o + d + h, v);
-        if (both) ptx::tmem_ld32(lanes + 2 * kManyKeys + (stream ^ 1) * 128 + d + h, y);
+      for (int h = 0; h < kWide; h += 8) {
+        uint32_t v[8], y[8];
+        ptx::tmem_ld8(outputs + mine * 128 + d + h, v);
+        if (both) ptx::tmem_ld8(outputs + 128 + d + h, y);
         ptx::tmem_ld_wait_for(v);
         if (both) ptx::tmem_ld_wait_for(y);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
+        for (int j = 0; j < 8; ++j) {
           float f = __uint_as_float(v[j]) * back;
           if (both) f = fmaf(__uint_as_float(y[j]), other, f);
           v[j] = __float_as_uint(f);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          ptx::st_shared4(stage + lane * (kWide * 4) + (((h / 4 + j) ^ (lane & 7)) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        for (int j = 0; j < 2; ++j)
+          ptx::st_shared4(stage + lane * (kWide * 4) + (((h / 4 + j) ^ (lane & (kLanes - 1))) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
       }
       __syncwarp();
       const int piece = lane % kLanes;
-#pragma unroll 4
+#pragma unroll
       for (int j = 0; j < 32 / kRows; ++j) {
         const int r = j * kRows + lane / kLanes;
-        const uint4 x = ptx::ld_shared4(stage + r * (kWide * 4) + ((piece ^ (r & 7)) << 4));
+        const uint4 x = ptx::ld_shared4(stage + r * (kWide * 4) + ((piece ^ (r & (kLanes - 1))) << 4));
         const Place q = place_of(c, at, warp_row + r);
         if (q.r >= at.x.rows) continue;
         if (final) {
@@ -529,7 +514,7 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
       }
       __syncwarp();
     }
-    if (there && (seg.two || stream == 0)) {
+    if (there && half == 0 && (seg.two || stream == 0)) {
       const Place q = place_of(c, at, warp_row + lane);
       if (final) {
         if (c.lse_out) c.lse_out[q.q_row * c.hq + q.head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -538,7 +523,7 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
       }
     }
     ptx::tc_fence_before_sync();
-    soft_sync();  // the other stream has read this one's O, and Q is free
+    soft_sync();  // O has been read, and the query tiles are free
     done += seg.tiles;
     more = skip(c, list, ahead, at, seg, u1);
   }

@@ -347,6 +347,12 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
+// The largest; of what is a number.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 // The product, 0 where it is below 2^-126.
 __device__ __forceinline__ float mul_ftz(float a, float b) {
   float y;
