@@ -3,15 +3,17 @@
 // Dense contractions, so they run on the fifth-generation tensor cores: S = Q K^T and O += P V (tcgen05.mma, f16 operands, fp32 sums in
 // tensor memory).  A unit is 128 keys of one KV head for up to 256 stacked query rows.  Per block, one per SM:
 //
-//   warps 0-15   softmax, two threads per row with half of a visit's columns each.  Warps 0-7 and 8-15 are two STREAMS with an S and an O
-//                of their own, so that the matrix pipe works on one while the exponentials of the other are taken.  With more than 128
-//                rows the streams are the two halves of the rows and share every tile of keys; with fewer they take the tiles in turn
-//                and their sums are joined at the end.
-//   warps 16-23  codes -> f16, 16 keys of every tile each: straight from global memory (one tile ahead in registers) to the operand
+//   warps 0-7    softmax, a thread per row.  Warps 0-3 and 4-7 are two STREAMS with an S, an O and two P of their own.  With more than 128
+//                rows the streams are the two halves of the rows and share every key; with fewer they take 64 keys of every tile each and
+//                their sums are joined at the end.  A VISIT is 64 keys of a stream.
+//   warps 8-15   codes -> f16, 16 keys of every tile each: straight from global memory (one tile ahead in registers) to the operand
 //                tiles in shared memory
-//   warp 24      issues the MMAs: QK of a visit goes out before PV of the visit before it (warps 25-27 fill its warpgroup)
+//   warp 16      issues the MMAs: the S of a stream's next visit as soon as the logits of this one are in registers, PV when its weights are
+//                there (warps 17-19 fill its warpgroup)
 //
-// Registers move from the warps that need few to the softmax's, which hold a visit's logits.
+// Tensor memory is used up: 2 x 64 columns of S, 4 x 32 of P, 2 x 128 of O.  (128 keys at a time with P in the place of S: the next S had to
+// wait for PV, and a stream stood still for the way to the issuing warp, PV, QK and back; 16 questions on 16,384 keys, Mistral-7B shapes,
+// FIGURE_OLD us.)  Registers move from the warps that need few to the softmax's, which hold a visit's logits.
 //
 // A value's scale is folded into its f16 operand relative to the power of two E of the largest scale of 16 keys, and E joins the exponent:
 // w = 2^(z + E - m + kOffset) is rounded to f16 for the matrix pipe, l = sum w 2^(-E - kOffset) stays in fp32.  So no weight is
@@ -30,18 +32,19 @@ namespace fastav {
 namespace {
 
 constexpr int kSub = 128;  // rows of a stream
-constexpr int kSoftWarps = 16, kConvWarps = 8, kIssueWarp = kSoftWarps + kConvWarps, kWarps = kIssueWarp + 4;
+constexpr int kVisit = 64;  // keys of a visit
+constexpr int kSoftWarps = 8, kConvWarps = 8, kIssueWarp = kSoftWarps + kConvWarps, kWarps = kIssueWarp + 4;
 constexpr int kSoftThreads = 32 * kSoftWarps, kThreads = 32 * kWarps;
 // Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
-constexpr int kSoftRegs = 88, kConvRegs = 64, kIssueRegs = 24;
+constexpr int kSoftRegs = 144, kConvRegs = 72, kIssueRegs = 48;
 constexpr int kRegsNeeded = 32 * (kSoftWarps * kSoftRegs + kConvWarps * kConvRegs + 4 * kIssueRegs);
 constexpr int kGroups = kManyKeys / 16;          // of 16 keys: a converting warp's
 constexpr int kScaleRing = 4;
 constexpr int kOffset = 11;                      // the largest weight of a row's first visit is 2^kOffset ...
-constexpr float kSlack = 4.f;                     // ... and the maximum is moved when a logit is this much above it (f16 ends at 2^16)
-constexpr int kValuePower = 7;                   // a value operand is code * (scale / 2^E) * 2^kValuePower, below 2^15
-constexpr int kTmemCols = 512;
-static_assert(kConvWarps == kGroups);
+constexpr float kSlack = 4.f;                    // ... and the maximum is moved when a logit is this much above it (f16 ends at 2^16)
+constexpr int kValuePower = 7;                   // a value operand is code * (scale / 2^E) * 2^kValuePower, below 2^16
+constexpr int kTmemCols = 512, kWeightsAt = 2 * kVisit, kOutputAt = kWeightsAt + 4 * (kVisit / 2);  // columns: S, P, O
+static_assert(kConvWarps == kGroups && kOutputAt + 2 * 128 <= kTmemCols);
 
 template <int DIM>
 struct Many {
@@ -52,19 +55,18 @@ struct Many {
 };
 
 struct Control {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], pv_done[2], scale_full[kScaleRing], q_full, last;
+  // [stream], [slot of a tile] or [stream][buffer of the weights]
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_free[2], p_full[2][2], pv_done[2][2], scale_full[kScaleRing], q_full, last;
   uint32_t tmem_base;
   int abort;
   int warp_sum[kWarps];
   alignas(16) float k_scale[kScaleRing][kManyKeys];
   float exponent[kScaleRing][kGroups], unscale[kScaleRing][kGroups];  // E; 2^(-E - kOffset)
   float row_scale[2][kSub];                                           // of a stream's query rows
-  float row_top[2][2][2][kSub];                                       // [visit & 1][stream][half of the columns]
-  float row_m[2][kSub], row_l[2][2][kSub];                            // of a stream; of a half of its columns
+  float2 row_ml[2][kSub];                                             // the streams' statistics, to be joined
 };
 
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory"); }
-__device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 64;" ::"r"(2 + pair) : "memory"); }  // the two warps of 32 rows
 
 // What a block does of its run in one job: `tiles` tiles of keys from `first` on.
 struct Segment {
@@ -218,45 +220,51 @@ template <int DIM>
 __device__ __forceinline__ void issue_mmas(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles, int u0,
                            int u1, int lane) {
   using M = Many<DIM>;
-  constexpr uint32_t kScores = ptx::umma_idesc_f16(kSub, kManyKeys, false), kOutput = ptx::umma_idesc_f16(kSub, DIM, true);
+  constexpr uint32_t kScores = ptx::umma_idesc_f16(kSub, kVisit, false), kOutput = ptx::umma_idesc_f16(kSub, DIM, true);
+  constexpr uint64_t kHalfTile = kVisit * 128 >> 4, kTile = M::kTileBytes >> 4;  // in units of a descriptor's address
   const uint32_t tmem = ctl.tmem_base;
+  const uint64_t q_desc = ptx::umma_desc_sw128(q_tiles, 0), k_desc = ptx::umma_desc_sw128(k_tiles, 0), v_desc = ptx::umma_desc_sw128_mn(v_tiles, M::kHalfBytes);
   Walk at;
   at.seek(c, list, ahead, u0);
-  int visits[2] = {0, 0};  // weights consumed, per stream
-  int segments = 0, done = 0;  // tiles before the segment
+  int segments = 0, done = 0, before = 0;  // tiles, and visits of a stream, before the segment
   for (bool more = at.unit < u1; more;) {
     const Segment seg = segment_of(c, at, u1);
+    const int per = seg.two ? 2 : 1, total = 2 * per * seg.tiles;  // visits of a stream and tile; of the segment, the streams in turn
+    auto scores = [&](int v) {                                     // S = Q K^T
+      const int stream = v & 1, nth = v >> 1, tile = seg.two ? nth >> 1 : nth, half = seg.two ? nth & 1 : stream, i = done + tile, slot = i & 1;
+      if (half == 0 && stream == 0) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_full[slot]), (i >> 1) & 1, &ctl.abort);
+      ptx::tc_fence_after_sync();
+      ptx::umma_bf16_steps<DIM / 16, M::kHalfBytes, M::kHalfBytes>(tmem + stream * kVisit, q_desc + (seg.two ? stream : 0) * kTile, k_desc + slot * kTile + half * kHalfTile,
+                                                                   kScores, false);
+      ptx::umma_commit(ptx::smem_u32(&ctl.s_full[stream]));
+      if (half == 1 && stream == 1) ptx::umma_commit(ptx::smem_u32(&ctl.k_empty[slot]));
+    };
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full), segments & 1, &ctl.abort);
-    ptx::tc_fence_after_sync();
-    const int total = seg.two ? 2 * seg.tiles : seg.tiles;
+    scores(0);
+    scores(1);
+#pragma unroll 1
     for (int v = 0; v <= total; ++v) {
-      if (v < total) {  // S = Q K^T
-        const int tile = seg.two ? v >> 1 : v, i = done + tile, slot = i & 1, stream = v & 1;
-        if (!seg.two || stream == 0) {
-          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_full[slot]), (i >> 1) & 1, &ctl.abort);
-          ptx::tc_fence_after_sync();
-        }
-        const uint64_t a = ptx::umma_desc_sw128(q_tiles + (seg.two ? stream : 0) * M::kTileBytes, 0), b = ptx::umma_desc_sw128(k_tiles + slot * M::kTileBytes, 0);
-        ptx::umma_bf16_steps<DIM / 16, M::kHalfBytes, M::kHalfBytes>(tmem + stream * kManyKeys, a, b, kScores, false);
-        ptx::umma_commit(ptx::smem_u32(&ctl.s_full[stream]));
-        if (!seg.two || stream == 1) ptx::umma_commit(ptx::smem_u32(&ctl.k_empty[slot]));
+      if (v + 2 < total) {
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_free[v & 1]), (before + (v >> 1)) & 1, &ctl.abort);
+        scores(v + 2);
       }
       if (v > 0) {  // O += P V of the visit before
-        const int w = v - 1, tile = seg.two ? w >> 1 : w, i = done + tile, slot = i & 1, stream = w & 1;
-        if (!seg.two || stream == 0) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.v_full[slot]), (i >> 1) & 1, &ctl.abort);
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.p_full[stream]), visits[stream] & 1, &ctl.abort);
-        ++visits[stream];
+        const int w = v - 1, stream = w & 1, nth = w >> 1, tile = seg.two ? nth >> 1 : nth, half = seg.two ? nth & 1 : stream, i = done + tile, slot = i & 1;
+        const int buffer = (before + nth) & 1;
+        if (half == 0 && stream == 0) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.v_full[slot]), (i >> 1) & 1, &ctl.abort);
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.p_full[stream][buffer]), (before + nth) >> 1 & 1, &ctl.abort);
         ptx::tc_fence_after_sync();
-        const uint32_t values = v_tiles + slot * M::kTileBytes;
+        const uint32_t d = tmem + kOutputAt + stream * 128, a = tmem + kWeightsAt + (stream * 2 + buffer) * (kVisit / 2);
+        const uint64_t b = v_desc + slot * kTile + half * kHalfTile;
 #pragma unroll
-        for (int ks = 0; ks < kManyKeys / 16; ++ks)  // 16 keys: 16 rows of 128 bytes further on
-          ptx::umma_ts(tmem + 2 * kManyKeys + stream * 128, tmem + stream * kManyKeys + ks * 8, ptx::umma_desc_sw128_mn(values + ks * 2048, M::kHalfBytes), kOutput,
-                       w > 1 || ks > 0 ? 1u : 0u);  // (the first visit of either stream begins anew)
-        ptx::umma_commit(ptx::smem_u32(&ctl.pv_done[stream]));
-        if (!seg.two || stream == 1) ptx::umma_commit(ptx::smem_u32(&ctl.v_empty[slot]));
+        for (int ks = 0; ks < kVisit / 16; ++ks)  // 16 keys: 8 columns of weights, 16 rows of 128 bytes of values
+          ptx::umma_ts(d, a + ks * 8, b + ks * (16 * 128 >> 4), kOutput, nth > 0 || ks > 0 ? 1u : 0u);
+        ptx::umma_commit(ptx::smem_u32(&ctl.pv_done[stream][buffer]));
+        if (half == 1 && stream == 1) ptx::umma_commit(ptx::smem_u32(&ctl.v_empty[slot]));
       }
     }
     done += seg.tiles;
+    before += per * seg.tiles;
     ++segments;
     more = skip(c, list, ahead, at, seg, u1);
   }
@@ -273,31 +281,29 @@ struct Visit {
   const float *exponent, *unscale;
 };
 
-constexpr int kCols = kManyKeys / 2;  // of a thread
-
 // A visit's logits times the scales of their keys (and not yet of the row), and the largest z + E of them; `limit`: columns from there on are hidden.
-__device__ __forceinline__ float visit_logits(const Visit& x, float row_scale, bool masked, int limit, float2 (&t)[kCols / 2]) {
-  uint32_t (&v)[kCols / 32][32] = reinterpret_cast<uint32_t(&)[kCols / 32][32]>(t);
+__device__ __forceinline__ float visit_logits(const Visit& x, float row_scale, bool masked, int limit, float2 (&t)[kVisit / 2]) {
+  uint32_t (&v)[kVisit / 32][32] = reinterpret_cast<uint32_t(&)[kVisit / 32][32]>(t);
 #pragma unroll
-  for (int b = 0; b < kCols / 32; ++b) ptx::tmem_ld32(x.s + b * 32, v[b]);
+  for (int b = 0; b < kVisit / 32; ++b) ptx::tmem_ld32(x.s + b * 32, v[b]);
 #pragma unroll
-  for (int b = 0; b < kCols / 32; ++b) ptx::tmem_ld_wait_for(v[b]);
+  for (int b = 0; b < kVisit / 32; ++b) ptx::tmem_ld_wait_for(v[b]);
 #pragma unroll
-  for (int j = 0; j < kCols / 2; j += 2) {
+  for (int j = 0; j < kVisit / 2; j += 2) {
     const float4 ks = *reinterpret_cast<const float4*>(x.ks + 2 * j);
     t[j] = __fmul2_rn(t[j], make_float2(ks.x, ks.y));
     t[j + 1] = __fmul2_rn(t[j + 1], make_float2(ks.z, ks.w));
   }
   if (masked) {
 #pragma unroll
-    for (int j = 0; j < kCols / 2; ++j) {
+    for (int j = 0; j < kVisit / 2; ++j) {
       if (2 * j >= limit) t[j].x = -INFINITY;
       if (2 * j + 1 >= limit) t[j].y = -INFINITY;
     }
   }
   float top = -INFINITY;
 #pragma unroll
-  for (int g = 0; g < kCols / 16; ++g) {
+  for (int g = 0; g < kVisit / 16; ++g) {
     float most = -INFINITY;
 #pragma unroll
     for (int j = g * 8; j < g * 8 + 8; ++j) most = ptx::max3(most, t[j].x, t[j].y);
@@ -306,12 +312,12 @@ __device__ __forceinline__ float visit_logits(const Visit& x, float row_scale, b
   return top;
 }
 // Their weights with the maximum `m` (base 2) as f16 pairs to tensor memory; the fp32 sum.
-__device__ __forceinline__ float visit_weights(const Visit& x, uint32_t to, float row_scale, float m, float2 (&t)[kCols / 2]) {
+__device__ __forceinline__ float visit_weights(const Visit& x, uint32_t to, float row_scale, float m, float2 (&t)[kVisit / 2]) {
   float l = 0.f;
   const float2 rs = make_float2(row_scale, row_scale);
-  uint32_t p[kCols / 2];
+  uint32_t p[kVisit / 2];
 #pragma unroll
-  for (int g = 0; g < kCols / 16; ++g) {
+  for (int g = 0; g < kVisit / 16; ++g) {
     const float add = x.exponent[g] - m + kOffset;
     const float2 plus = make_float2(add, add);
     float2 sum = make_float2(0.f, 0.f);
@@ -330,7 +336,7 @@ __device__ __forceinline__ float visit_weights(const Visit& x, uint32_t to, floa
 template <int DIM>
 __device__ __forceinline__ void rescale_output(uint32_t o, float factor) {  // (few registers: the visit's logits are held meanwhile)
 #pragma unroll 1
-  for (int i = 0; i < DIM / 2; i += 8) {
+  for (int i = 0; i < DIM; i += 8) {
     uint32_t v[8];
     ptx::tmem_ld8(o + i, v);
     ptx::tmem_ld_wait_for(v);
@@ -352,42 +358,47 @@ __device__ __forceinline__ Place place_of(const AttendCall& c, const Walk& at, i
   return Place{(long long)at.x.row0 + r, at.head * c.group + i - r * c.group, r};
 }
 
-// 16 query rows into their operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to
+// A warp's 32 query rows into their operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to
 // `scale` what takes that back, times the softmax scale.
 template <int DIM>
 __device__ __forceinline__ void load_queries(const AttendCall& c, const Walk& at, int first_row, uint32_t tile, int row_in_tile, float* scale, int lane) {
-  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kLoads = 16 / kRows;  // rows of a load; loads, all in flight
+  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kLoads = 8;  // rows of a load; loads in flight
   const int sub = lane / kLanes, piece = lane % kLanes;
-  uint4 x[kLoads];
+#pragma unroll 1
+  for (int j0 = 0; j0 < 32; j0 += kLoads * kRows) {
+    uint4 x[kLoads];
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const Place q = place_of(c, at, first_row + j * kRows + sub);
-    x[j] = q.r < at.x.rows ? chain_load_cached(reinterpret_cast<const uint4*>(c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8)) : make_uint4(0, 0, 0, 0);
-  }
+    for (int j = 0; j < kLoads; ++j) {
+      const Place q = place_of(c, at, first_row + j0 + j * kRows + sub);
+      x[j] = q.r < at.x.rows ? chain_load_cached(reinterpret_cast<const uint4*>(c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8)) : make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const unsigned m = 0x7FFF7FFFu;
-    unsigned top = __vmaxu2(__vmaxu2(x[j].x & m, x[j].y & m), __vmaxu2(x[j].z & m, x[j].w & m));  // what is not a number is larger than the rest
-    top = max(top >> 16, top & 0xFFFFu);
+    for (int j = 0; j < kLoads; ++j) {
+      const unsigned m = 0x7FFF7FFFu;
+      unsigned top = __vmaxu2(__vmaxu2(x[j].x & m, x[j].y & m), __vmaxu2(x[j].z & m, x[j].w & m));  // what is not a number is larger than the rest
+      top = max(top >> 16, top & 0xFFFFu);
 #pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    const float to = to_one(__uint_as_float(top << 16));
-    const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-    uint32_t h[4];
+      for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      const float to = to_one(__uint_as_float(top << 16));
+      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+      uint32_t h[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xFFFF0000u) * to);
-    const int row = row_in_tile + j * kRows + sub;
-    ptx::st_shared4(tile + (piece >> 3) * Many<DIM>::kHalfBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4), h[0], h[1], h[2], h[3]);
-    if (piece == 0) scale[row] = c.scale_log2 / to;
+      for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xFFFF0000u) * to);
+      const int row = row_in_tile + j0 + j * kRows + sub;
+      ptx::st_shared4(tile + (piece >> 3) * Many<DIM>::kHalfBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4), h[0], h[1], h[2], h[3]);
+      if (piece == 0) scale[row] = c.scale_log2 / to;
+    }
   }
 }
 
 template <int DIM>
 __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t q_tiles, int u0, int u1, int warp, int lane) {
   using M = Many<DIM>;
-  const int stream = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, row = quarter * 32 + lane, pair = stream * 4 + quarter;
-  const uint32_t lanes = ctl.tmem_base + ((uint32_t)(quarter * 32) << 16), outputs = lanes + 2 * kManyKeys;
-  const uint32_t s = lanes + stream * kManyKeys;
+  const int stream = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+  const uint32_t lanes = ctl.tmem_base + ((uint32_t)(quarter * 32) << 16), outputs = lanes + kOutputAt;
+  const uint32_t s = lanes + stream * kVisit, weights = lanes + kWeightsAt + stream * kVisit;
+  const uint32_t s_full = ptx::smem_u32(&ctl.s_full[stream]), s_free = ptx::smem_u32(&ctl.s_free[stream]);
+  const uint32_t p_full = ptx::smem_u32(&ctl.p_full[stream][0]), pv_done = ptx::smem_u32(&ctl.pv_done[stream][0]);
   Walk at;
   at.seek(c, list, ahead, u0);
   int visits = 0, done = 0;  // of this stream; tiles before the segment
@@ -395,10 +406,9 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     const Segment seg = segment_of(c, at, u1);
     // With two streams of rows a thread's row is of its stream's half; else threads of both streams have the same one.
     const int warp_row = (seg.two ? stream * kSub : 0) + quarter * 32;
-    load_queries<DIM>(c, at, warp_row + half * 16, q_tiles + stream * M::kTileBytes, quarter * 32 + half * 16, ctl.row_scale[stream], lane);
+    load_queries<DIM>(c, at, warp_row, q_tiles + stream * M::kTileBytes, quarter * 32, ctl.row_scale[stream], lane);
     ptx::fence_proxy_async_smem();
     ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.q_full), lane);
-    pair_sync(pair);
     const float row_scale = ctl.row_scale[stream][row];
     int sees, all_see;
     bool there;
@@ -410,59 +420,54 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     }
 
     float m = -INFINITY, l = 0.f;
-    bool first = true;
+    const int count = seg.two ? 2 * seg.tiles : seg.tiles;
 #pragma unroll 1
-    for (int tile = seg.two ? 0 : stream; tile < seg.tiles; tile += seg.two ? 1 : 2) {
-      const int n = done + tile, ring = n & (kScaleRing - 1);
-      const Visit x{s + half * kCols, ctl.k_scale[ring] + half * kCols, ctl.exponent[ring] + half * (kGroups / 2), ctl.unscale[ring] + half * (kGroups / 2)};
+    for (int v = 0; v < count; ++v, ++visits) {
+      const int tile = seg.two ? v >> 1 : v, half = seg.two ? v & 1 : stream, n = done + tile, ring = n & (kScaleRing - 1);
+      const Visit x{s, ctl.k_scale[ring] + half * kVisit, ctl.exponent[ring] + half * (kGroups / 2), ctl.unscale[ring] + half * (kGroups / 2)};
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.scale_full[ring]), (n / kScaleRing) & 1, &ctl.abort);
-      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[stream]), visits & 1, &ctl.abort);
+      ptx::mbar_wait_warp(s_full, visits & 1, &ctl.abort);
       ptx::tc_fence_after_sync();
-      const int key0 = (seg.first + tile) * kManyKeys;
-      float2 t[kCols / 2];
-      float top = visit_logits(x, row_scale, key0 + kManyKeys > all_see, sees - key0 - half * kCols, t);
-      float(&tops)[2][kSub] = ctl.row_top[visits & 1][stream];
-      tops[half][row] = top;
-      pair_sync(pair);  // ... and both have read their logits: the weights may take their place
-      top = fmaxf(top, tops[half ^ 1][row]);
-      if (first) {
+      const int key0 = (seg.first + tile) * kManyKeys + half * kVisit;
+      float2 t[kVisit / 2];
+      const float top = visit_logits(x, row_scale, key0 + kVisit > all_see, sees - key0, t);
+      ptx::tc_fence_before_sync();
+      ptx::mbar_arrive_warp(s_free, lane);
+      if (v == 0) {
         m = top;
       } else if (__any_sync(0xFFFFFFFFu, there && (top > m + kSlack || (m == -INFINITY && top > m)))) {  // the sums so far
         const float to = fmaxf(top, m), factor = m == -INFINITY ? 0.f : ptx::ex2_approx(m - to);
         l *= factor;
         m = to;
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.pv_done[stream]), (visits - 1) & 1, &ctl.abort);
+        ptx::mbar_wait_warp(pv_done + ((visits - 1) & 1) * 8, (visits - 1) >> 1 & 1, &ctl.abort);
         ptx::tc_fence_after_sync();
-        rescale_output<DIM>(outputs + stream * 128 + half * (DIM / 2), factor);
+        rescale_output<DIM>(outputs + stream * 128, factor);
       }
-      l += visit_weights(x, s + half * (kCols / 2), row_scale, m == -INFINITY ? 0.f : m, t);
+      const int buffer = visits & 1;
+      if (visits >= 2) {  // the weights that lay there have been used
+        ptx::mbar_wait_warp(pv_done + buffer * 8, ((visits >> 1) - 1) & 1, &ctl.abort);
+        ptx::tc_fence_after_sync();
+      }
+      l += visit_weights(x, weights + buffer * (kVisit / 2), row_scale, m == -INFINITY ? 0.f : m, t);
       ptx::tmem_st_wait();
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.p_full[stream]), lane);
-      first = false;
-      ++visits;
+      ptx::mbar_arrive_warp(p_full + buffer * 8, lane);
     }
-    if (!first) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.pv_done[stream]), (visits - 1) & 1, &ctl.abort);
+    ptx::mbar_wait_warp(pv_done + ((visits - 1) & 1) * 8, (visits - 1) >> 1 & 1, &ctl.abort);
 
-    // The end of the segment: the halves' sums, and those of the streams where both have a part of the row.  O is sum 2^(z - m) v times
-    // 2^(kOffset + kValuePower).
-    if (half == 0) ctl.row_m[stream][row] = m;
-    ctl.row_l[stream][half][row] = l;
+    // The end of the segment; the streams' sums are joined where both have a part of the row.  O is sum 2^(z - m) v times 2^(kOffset + kValuePower).
+    ctl.row_ml[stream][row] = make_float2(m, l);
     ptx::tc_fence_before_sync();
     soft_sync();
     ptx::tc_fence_after_sync();
-    const int mine = seg.two ? stream : 0;
-    const bool both = !seg.two && seg.tiles > 1;
-    m = ctl.row_m[mine][row];
-    l = ctl.row_l[mine][0][row] + ctl.row_l[mine][1][row];
     float other = 0.f, back = __uint_as_float((unsigned)(127 - kOffset - kValuePower) << 23);
-    if (both) {
-      const float m1 = ctl.row_m[1][row], to = fmaxf(m, m1), base = to == -INFINITY ? 0.f : to;
-      const float f0 = ptx::ex2_approx(m - base), f1 = ptx::ex2_approx(m1 - base);
-      l = l * f0 + (ctl.row_l[1][0][row] + ctl.row_l[1][1][row]) * f1;
+    if (!seg.two) {
+      const float2 a = ctl.row_ml[0][row], b = ctl.row_ml[1][row];
+      m = fmaxf(a.x, b.x);
+      const float base = m == -INFINITY ? 0.f : m, f0 = ptx::ex2_approx(a.x - base), f1 = ptx::ex2_approx(b.x - base);
+      l = a.y * f0 + b.y * f1;
       other = back * f1;
       back *= f0;
-      m = to;
     }
     const bool whole = at.job_first() >= u0 && at.job_end() <= u1, final = whole && c.prefixes == 0;
     const long long level = at.x.own ? 0ll : (long long)c.total_q * c.hq;
@@ -472,36 +477,35 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
       back *= inv;
       other *= inv;
     }
-    // The warps of 32 rows share the columns.  By kWide of them through shared memory (the query tiles, which nobody needs any more), so that
-    // rows are written in whole lines.
-    constexpr int kWide = DIM / 4, kLanes = kWide / 4, kRows = 32 / kLanes;
-    const int from = seg.two ? half * (DIM / 2) : (stream * 2 + half) * kWide, to = from + (seg.two ? DIM / 2 : kWide);
-    const uint32_t stage = q_tiles + warp * (32 * kWide * 4);
+    // A stream writes its rows; where both have the same ones, half of the columns each.  By kWide columns through shared memory (the query
+    // tiles, which nobody needs any more), so that rows are written in whole lines.
+    constexpr int kWide = DIM / 2, kLanes = kWide / 4, kRows = 32 / kLanes;
+    const uint32_t stage = q_tiles + warp * (32 * kWide * 4), mine = outputs + (seg.two ? stream * 128 : 0);
 #pragma unroll 1
-    for (int d = from; d < to; d += kWide) {
+    for (int d = seg.two ? 0 : stream * kWide; d < (seg.two ? DIM : (stream + 1) * kWide); d += kWide) {
+#pragma unroll 1
+      for (int h = 0; h < kWide; h += 32) {
+        uint32_t x[32], y[32];
+        ptx::tmem_ld32(mine + d + h, x);
+        if (!seg.two) ptx::tmem_ld32(outputs + 128 + d + h, y);
+        ptx::tmem_ld_wait_for(x);
+        if (!seg.two) ptx::tmem_ld_wait_for(y);
 #pragma unroll
-      for (int h = 0; h < kWide; h += 8) {
-        uint32_t v[8], y[8];
-        ptx::tmem_ld8(outputs + mine * 128 + d + h, v);
-        if (both) ptx::tmem_ld8(outputs + 128 + d + h, y);
-        ptx::tmem_ld_wait_for(v);
-        if (both) ptx::tmem_ld_wait_for(y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float f = __uint_as_float(v[j]) * back;
-          if (both) f = fmaf(__uint_as_float(y[j]), other, f);
-          v[j] = __float_as_uint(f);
+        for (int j = 0; j < 32; ++j) {
+          float f = __uint_as_float(x[j]) * back;
+          if (!seg.two) f = fmaf(__uint_as_float(y[j]), other, f);
+          x[j] = __float_as_uint(f);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          ptx::st_shared4(stage + lane * (kWide * 4) + (((h / 4 + j) ^ (lane & (kLanes - 1))) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        for (int j = 0; j < 8; ++j)
+          ptx::st_shared4(stage + lane * (kWide * 4) + (((h / 4 + j) ^ (lane & 7)) << 4), x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
       }
       __syncwarp();
       const int piece = lane % kLanes;
-#pragma unroll
+#pragma unroll 4
       for (int j = 0; j < 32 / kRows; ++j) {
         const int r = j * kRows + lane / kLanes;
-        const uint4 x = ptx::ld_shared4(stage + r * (kWide * 4) + ((piece ^ (r & (kLanes - 1))) << 4));
+        const uint4 x = ptx::ld_shared4(stage + r * (kWide * 4) + ((piece ^ (r & 7)) << 4));
         const Place q = place_of(c, at, warp_row + r);
         if (q.r >= at.x.rows) continue;
         if (final) {
@@ -514,7 +518,7 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
       }
       __syncwarp();
     }
-    if (there && half == 0 && (seg.two || stream == 0)) {
+    if (there && (seg.two || stream == 0)) {
       const Place q = place_of(c, at, warp_row + lane);
       if (final) {
         if (c.lse_out) c.lse_out[q.q_row * c.hq + q.head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -545,8 +549,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
       ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.v_empty[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.s_full[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&ctl.p_full[i]), kSoftWarps / 2);
-      ptx::mbar_init(ptx::smem_u32(&ctl.pv_done[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.s_free[i]), kSoftWarps / 2);
+      for (int b = 0; b < 2; ++b) {
+        ptx::mbar_init(ptx::smem_u32(&ctl.p_full[i][b]), kSoftWarps / 2);
+        ptx::mbar_init(ptx::smem_u32(&ctl.pv_done[i][b]), 1);
+      }
     }
     for (int i = 0; i < kScaleRing; ++i) ptx::mbar_init(ptx::smem_u32(&ctl.scale_full[i]), kConvWarps);
     ptx::mbar_init(ptx::smem_u32(&ctl.q_full), kSoftWarps);
