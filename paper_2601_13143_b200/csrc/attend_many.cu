@@ -8,8 +8,8 @@
 //                their sums are joined at the end.  A VISIT is 64 keys of a stream.
 //   warps 8-15   codes -> f16, 16 keys of every tile each: straight from global memory (one tile ahead in registers) to the operand
 //                tiles in shared memory
-//   warp 16      issues the MMAs: the S of a stream's next visit as soon as the logits of this one are in registers, PV when its weights are
-//                there (warps 17-19 fill its warpgroup)
+//   warps 16-19  issue the MMAs: the S of a stream's next visit as soon as the logits of this one are in registers, PV when its weights are
+//                there
 //
 // Tensor memory is used up: 2 x 64 columns of S, 4 x 32 of P, 2 x 128 of O.  (128 keys at a time with P in the place of S: the next S had to
 // wait for PV, and a stream stood still for the way to the issuing warp, PV, QK and back; 16 questions on 16,384 keys, Mistral-7B shapes,
@@ -216,56 +216,53 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
 }
 
 // ---- the MMAs -----------------------------------------------------------------------------------------------------------
-template <int DIM>
+// Four warps issue, QK and PV of either stream each, on a scheduler of their own: what lies between two visits' MMAs (waits that are over
+// already, addresses, commits) is some hundred cycles of a warp among busy ones, and one warp for all of it left the matrix pipe idle half of the
+// time.  S and P being apart, the four need not know of each other; tiles of keys are given back by two arrivals.
+template <int DIM, bool SCORES>
 __device__ __forceinline__ void issue_mmas(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles, int u0,
-                           int u1, int lane) {
+                                           int u1, int stream) {
   using M = Many<DIM>;
   constexpr uint32_t kScores = ptx::umma_idesc_f16(kSub, kVisit, false), kOutput = ptx::umma_idesc_f16(kSub, DIM, true);
-  constexpr uint64_t kHalfTile = kVisit * 128 >> 4, kTile = M::kTileBytes >> 4;  // in units of a descriptor's address
+  constexpr uint32_t kHalfTile = kVisit * 128 >> 4, kTile = M::kTileBytes >> 4;  // in units of a descriptor's address
   const uint32_t tmem = ctl.tmem_base;
-  const uint64_t q_desc = ptx::umma_desc_sw128(q_tiles, 0), k_desc = ptx::umma_desc_sw128(k_tiles, 0), v_desc = ptx::umma_desc_sw128_mn(v_tiles, M::kHalfBytes);
+  const uint64_t q_desc = ptx::umma_desc_sw128(q_tiles, 0), tile_desc = SCORES ? ptx::umma_desc_sw128(k_tiles, 0) : ptx::umma_desc_sw128_mn(v_tiles, M::kHalfBytes);
+  const uint32_t full = ptx::smem_u32(SCORES ? &ctl.k_full[0] : &ctl.v_full[0]), empty = ptx::smem_u32(SCORES ? &ctl.k_empty[0] : &ctl.v_empty[0]);
+  const uint32_t s_full = ptx::smem_u32(&ctl.s_full[stream]), s_free = ptx::smem_u32(&ctl.s_free[stream]);
+  const uint32_t p_full = ptx::smem_u32(&ctl.p_full[stream][0]), pv_done = ptx::smem_u32(&ctl.pv_done[stream][0]);
   Walk at;
   at.seek(c, list, ahead, u0);
-  int segments = 0, done = 0, before = 0;  // tiles, and visits of a stream, before the segment
-  for (bool more = at.unit < u1; more;) {
+  int segments = 0, tile = 0, visit = 0;  // of the run
+  for (bool more = at.unit < u1; more; ++segments) {
     const Segment seg = segment_of(c, at, u1);
-    const int per = seg.two ? 2 : 1, total = 2 * per * seg.tiles;  // visits of a stream and tile; of the segment, the streams in turn
-    auto scores = [&](int v) {                                     // S = Q K^T
-      const int stream = v & 1, nth = v >> 1, tile = seg.two ? nth >> 1 : nth, half = seg.two ? nth & 1 : stream, i = done + tile, slot = i & 1;
-      if (half == 0 && stream == 0) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_full[slot]), (i >> 1) & 1, &ctl.abort);
-      ptx::tc_fence_after_sync();
-      ptx::umma_bf16_steps<DIM / 16, M::kHalfBytes, M::kHalfBytes>(tmem + stream * kVisit, q_desc + (seg.two ? stream : 0) * kTile, k_desc + slot * kTile + half * kHalfTile,
-                                                                   kScores, false);
-      ptx::umma_commit(ptx::smem_u32(&ctl.s_full[stream]));
-      if (half == 1 && stream == 1) ptx::umma_commit(ptx::smem_u32(&ctl.k_empty[slot]));
-    };
-    ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full), segments & 1, &ctl.abort);
-    scores(0);
-    scores(1);
+    const int halves = seg.two ? 2 : 1;
+    if (SCORES) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full), segments & 1, &ctl.abort);
+    const uint64_t a_desc = q_desc + (seg.two ? stream * kTile : 0);
 #pragma unroll 1
-    for (int v = 0; v <= total; ++v) {
-      if (v + 2 < total) {
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_free[v & 1]), (before + (v >> 1)) & 1, &ctl.abort);
-        scores(v + 2);
-      }
-      if (v > 0) {  // O += P V of the visit before
-        const int w = v - 1, stream = w & 1, nth = w >> 1, tile = seg.two ? nth >> 1 : nth, half = seg.two ? nth & 1 : stream, i = done + tile, slot = i & 1;
-        const int buffer = (before + nth) & 1;
-        if (half == 0 && stream == 0) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.v_full[slot]), (i >> 1) & 1, &ctl.abort);
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.p_full[stream][buffer]), (before + nth) >> 1 & 1, &ctl.abort);
-        ptx::tc_fence_after_sync();
-        const uint32_t d = tmem + kOutputAt + stream * 128, a = tmem + kWeightsAt + (stream * 2 + buffer) * (kVisit / 2);
-        const uint64_t b = v_desc + slot * kTile + half * kHalfTile;
+    for (int t = 0; t < seg.tiles; ++t, ++tile) {
+      const int slot = tile & 1;
+      ptx::mbar_wait_warp(full + slot * 8, (tile >> 1) & 1, &ctl.abort);
+#pragma unroll 1
+      for (int h = 0; h < halves; ++h, ++visit) {
+        const uint64_t b_desc = tile_desc + (slot * kTile + (seg.two ? h : stream) * kHalfTile);
+        if (SCORES) {  // S = Q K^T
+          if (t + h > 0) ptx::mbar_wait_warp(s_free, (visit - 1) & 1, &ctl.abort);
+          ptx::tc_fence_after_sync();
+          ptx::umma_bf16_steps<DIM / 16, M::kHalfBytes, M::kHalfBytes>(tmem + stream * kVisit, a_desc, b_desc, kScores, false);
+          ptx::umma_commit(s_full);
+        } else {  // O += P V
+          const int buffer = visit & 1;
+          ptx::mbar_wait_warp(p_full + buffer * 8, (visit >> 1) & 1, &ctl.abort);
+          ptx::tc_fence_after_sync();
+          const uint32_t d = tmem + kOutputAt + stream * 128, a = tmem + kWeightsAt + (stream * 2 + buffer) * (kVisit / 2);
 #pragma unroll
-        for (int ks = 0; ks < kVisit / 16; ++ks)  // 16 keys: 8 columns of weights, 16 rows of 128 bytes of values
-          ptx::umma_ts(d, a + ks * 8, b + ks * (16 * 128 >> 4), kOutput, nth > 0 || ks > 0 ? 1u : 0u);
-        ptx::umma_commit(ptx::smem_u32(&ctl.pv_done[stream][buffer]));
-        if (half == 1 && stream == 1) ptx::umma_commit(ptx::smem_u32(&ctl.v_empty[slot]));
+          for (int ks = 0; ks < kVisit / 16; ++ks)  // 16 keys: 8 columns of weights, 16 rows of 128 bytes of values
+            ptx::umma_ts(d, a + ks * 8, b_desc + ks * (16 * 128 >> 4), kOutput, t + h + ks > 0 ? 1u : 0u);
+          ptx::umma_commit(pv_done + buffer * 8);
+        }
       }
+      ptx::umma_commit(empty + slot * 8);
     }
-    done += seg.tiles;
-    before += per * seg.tiles;
-    ++segments;
     more = skip(c, list, ahead, at, seg, u1);
   }
   ptx::umma_commit(ptx::smem_u32(&ctl.last));
@@ -546,8 +543,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.k_full[i]), kConvWarps);
       ptx::mbar_init(ptx::smem_u32(&ctl.v_full[i]), kConvWarps);
-      ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&ctl.v_empty[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 2);
+      ptx::mbar_init(ptx::smem_u32(&ctl.v_empty[i]), 2);
       ptx::mbar_init(ptx::smem_u32(&ctl.s_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.s_free[i]), kSoftWarps / 2);
       for (int b = 0; b < 2; ++b) {
@@ -557,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     }
     for (int i = 0; i < kScaleRing; ++i) ptx::mbar_init(ptx::smem_u32(&ctl.scale_full[i]), kConvWarps);
     ptx::mbar_init(ptx::smem_u32(&ctl.q_full), kSoftWarps);
-    ptx::mbar_init(ptx::smem_u32(&ctl.last), 1);
+    ptx::mbar_init(ptx::smem_u32(&ctl.last), 4);
     ctl.abort = 0;
     ptx::fence_barrier_init();
   }
@@ -579,7 +576,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     if (u0 < u1) convert_keys<DIM, FP8>(c, list, ahead, ctl, k_tiles, v_tiles, u0, u1, warp - kSoftWarps, lane);
   } else {
     ptx::fewer_registers<kIssueRegs>();
-    if (u0 < u1 && warp == kIssueWarp) issue_mmas<DIM>(c, list, ahead, ctl, q_tiles, k_tiles, v_tiles, u0, u1, lane);
+    if (u0 < u1 && warp < kIssueWarp + 2) issue_mmas<DIM, true>(c, list, ahead, ctl, q_tiles, k_tiles, v_tiles, u0, u1, warp & 1);
+    else if (u0 < u1) issue_mmas<DIM, false>(c, list, ahead, ctl, q_tiles, k_tiles, v_tiles, u0, u1, warp & 1);
   }
   pdl_trigger();
   ptx::tc_fence_before_sync();
