@@ -10,109 +10,200 @@
 namespace fastav {
 namespace {
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinWarps = 8;
 
 // The parts of one row and head at one level: which job, which blocks.
 struct Parts {
-  const float* out = nullptr;
-  const float2* ml = nullptr;
   int first = 0, count = 0;  // blocks
   int row = 0;               // of the tile
   bool whole = false;
 };
-
-template <int DIM>
-__device__ __forceinline__ const float* part_row(const AttendList& list, const Parts& p, int i) {  // part i: a job's first block has it second
-  return list.part_out + ((long long)((p.first + i) * 2 + (i == 0 ? 1 : 0)) * list.tile_rows + p.row) * DIM;
-}
-__device__ __forceinline__ float2 part_stat(const AttendList& list, const Parts& p, int i) {
-  return chain_load(list.part_ml + ((long long)((p.first + i) * 2 + (i == 0 ? 1 : 0)) * list.tile_rows + p.row));
+// Part i of a row: a job's first block has it in its second place.
+__device__ __forceinline__ int part_of(const AttendList& list, const Parts& p, int i) {
+  return ((p.first + i) * 2 + (i == 0 ? 1 : 0)) * list.tile_rows + p.row;
 }
 
-__device__ Parts find_parts(const AttendCall& c, const AttendList& list, int e, int row, int head) {
-  Parts p;
+// What the rows of an entry have in common.
+struct Found {
+  Entry x;
+  int granules = 0, ahead, total;
+};
+__device__ __forceinline__ Found find_entry(const AttendCall& c, const AttendList& list, int e) {
+  Found f;
+  f.ahead = chain_load_cached(list.ahead + e);  // (asked for together)
+  f.total = chain_load_cached(list.ahead + list.entries());
   bool bad = false;
-  const Entry x = entry_of(c, list, e, bad);
-  const int r = row - x.row0, granules = granules_of(list, x);
-  if (r < 0 || r >= x.rows || granules == 0) return p;
+  f.x = entry_of(c, list, e, bad);
+  f.granules = granules_of(list, f.x);
+  return f;
+}
+__device__ __forceinline__ Parts find_parts(const AttendCall& c, const AttendList& list, const Found& f, int row, int head) {
+  Parts p;
+  const int r = row - f.x.row0;
+  if (r < 0 || r >= f.x.rows || f.granules == 0) return p;
   const int kv = head / c.group, i = r * c.group + head - kv * c.group, tile = i / list.tile_rows;
-  const int start = chain_load_cached(list.ahead + e) + (kv * tiles_of(c, list, x) + tile) * (list.job_cost + granules) + list.job_cost;
-  const int total = chain_load_cached(list.ahead + list.entries());
-  if (start < 0 || start + granules > total) return p;  // (the arrays changed meanwhile)
+  const int start = f.ahead + (kv * tiles_of(c, list, f.x) + tile) * (list.job_cost + f.granules) + list.job_cost;
+  if (start < 0 || start + f.granules > f.total) return p;  // (the arrays changed meanwhile)
+  const int workers = workers_of(list, f.total);
   p.row = i - tile * list.tile_rows;
-  const int workers = workers_of(list, total);
-  p.first = worker_of(start, workers, total);
-  p.count = worker_of(start + granules - 1, workers, total) - p.first + 1;
+  p.first = worker_of(start, workers, f.total);
+  p.count = worker_of(start + f.granules - 1, workers, f.total) - p.first + 1;
   p.whole = p.count == 1;
   return p;
 }
 
-// A warp per (query row, head): joins what the levels' blocks left.  With m the largest of the parts' maxima,
+// The last of n ascending numbers that is at most x (0 if none is); the whole warp, 32 looks at a time.
+__device__ __forceinline__ int last_upto(const int32_t* a, int n, int x, int lane) {
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const unsigned upto = __ballot_sync(0xFFFFFFFFu, lane * step < n && chain_load_cached(a + lo + min(lane * step, n - 1)) <= x);
+    const int k = upto ? 31 - __clz(upto) : 0;
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
+// Joins what the levels' blocks left.  With m the largest of the parts' maxima,
 //   out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i,  lse = ln 2 (m + log2 sum).
 // Rows of one level that one block finished are there already; a row that sees no key gets 0 and -inf.
-template <int DIM>
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(AttendCall c, AttendList own, AttendList shared) {
-  constexpr int kEach = DIM / 32;
+//
+// Bound by latency: a few trips to memory one after the other (the row's sequence; its bounds; the parts' statistics; the parts).  So a lane
+// asks for one part's statistics each, and where rows are few and parts many, WARPS warps share those of a (row, head), eight at a time
+// each (1 x 1,024 keys, 28 heads of up to 32 parts: 7.3 us instead of 24 with a warp that went through them four at a time).  Many rows: a
+// warp takes HEADS heads of a row and finds their jobs in as many lanes (41,000 (row, head): FIGURE_JOIN us instead of 51).
+template <int DIM, int WARPS, int HEADS>
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall c, AttendList own, AttendList shared) {
+  static_assert(WARPS == 1 || HEADS == 1);
+  constexpr int kEach = DIM / 32, kHeads = kJoinWarps / WARPS * HEADS, kAtOnce = WARPS > 1 ? 8 : 2;
+  __shared__ float part_acc[WARPS > 1 ? kJoinWarps : 1][DIM];
+  __shared__ float2 part_ml[kJoinWarps];
   chain_enter(c);
   pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const int at = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5), row = at / c.hq, head = at - row * c.hq;
-  if (row >= c.total_q) return;
-  int lo = 0, hi = c.batch;  // the row's sequence: the last one that begins at or before it
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (chain_load_cached(c.cu_qlens + mid) <= row) lo = mid; else hi = mid;
-  }
-  if (row < chain_load_cached(c.cu_qlens + lo) || row >= chain_load_cached(c.cu_qlens + lo + 1)) return;  // nobody's row
-  Parts level[2];
-  level[0] = find_parts(c, own, own.from_prefix + lo, row, head);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % WARPS;
+  const int head_blocks = (c.hq + kHeads - 1) / kHeads, row = blockIdx.x / head_blocks, head0 = (blockIdx.x - row * head_blocks) * kHeads + warp / WARPS * HEADS;
+  const int b = last_upto(c.cu_qlens, c.batch, row, lane);
+  if (row < chain_load_cached(c.cu_qlens + b) || row >= chain_load_cached(c.cu_qlens + b + 1)) return;  // nobody's row (the whole block's answer)
+  Parts found[2];  // of head head0 + lane
+  const int lane_head = head0 + lane;
+  const bool lane_there = lane < HEADS && lane_head < c.hq;
+  const Found f = find_entry(c, own, own.from_prefix + b);
+  if (lane_there) found[0] = find_parts(c, own, f, row, lane_head);
   if (c.prefixes > 0) {
-    int a = 0, z = c.prefixes;  // the last prefix that begins at or before the sequence
-    while (z - a > 1) {
-      const int mid = (a + z) >> 1;
-      if (chain_load_cached(c.cu_prefix + mid) <= lo) a = mid; else z = mid;
+    const int a = last_upto(c.cu_prefix, c.prefixes, b, lane);
+    if (b >= chain_load_cached(c.cu_prefix + a) && b < chain_load_cached(c.cu_prefix + a + 1)) {
+      const Found g = find_entry(c, shared, a);
+      if (lane_there) found[1] = find_parts(c, shared, g, row, lane_head);
     }
-    if (lo >= chain_load_cached(c.cu_prefix + a) && lo < chain_load_cached(c.cu_prefix + a + 1)) level[1] = find_parts(c, shared, a, row, head);
-  } else if (level[0].whole) {
-    return;
   }
-  float top = -INFINITY;
-  const long long flat = (long long)row * c.hq + head;
-  auto stat = [&](int l, int i) {
-    return level[l].whole ? chain_load(c.whole_ml + (long long)l * c.total_q * c.hq + flat) : part_stat(l ? shared : own, level[l], i);
-  };
+#pragma unroll 1
+  for (int h = 0; h < HEADS; ++h) {
+    const int head = head0 + h;
+    const bool there = head < c.hq, done = c.prefixes == 0 && __shfl_sync(0xFFFFFFFFu, found[0].whole, h);
+    const long long flat = (long long)row * c.hq + head, flats = (long long)c.total_q * c.hq;
+    float top = -INFINITY, acc[kEach] = {}, sum = 0.f;
 #pragma unroll
-  for (int l = 0; l < 2; ++l)
-    for (int i = lane; i < level[l].count; i += 32) top = fmaxf(top, stat(l, i).x);
+    for (int l = 0; l < 2; ++l) {
+      const AttendList& list = l ? shared : own;
+      Parts p;
+      p.first = __shfl_sync(0xFFFFFFFFu, found[l].first, h);
+      p.count = __shfl_sync(0xFFFFFFFFu, found[l].count, h);
+      p.row = __shfl_sync(0xFFFFFFFFu, found[l].row, h);
+      p.whole = p.count == 1;
+      const float2* const stats = p.whole ? c.whole_ml + l * flats + flat : list.part_ml;
+      const float* const outs = (p.whole ? c.whole_out + (l * flats + flat) * DIM : list.part_out) + lane * kEach;
+      for (int i0 = 0; !done && i0 < p.count; i0 += 32 * WARPS) {  // a lane's part: WARPS lane + sub
+        const int mine = i0 + lane * WARPS + sub;
+        const int at = p.whole ? 0 : part_of(list, p, mine);
+        const float2 ml = mine < p.count ? chain_load(stats + at) : make_float2(-INFINITY, 0.f);
+        float to = ml.x;
 #pragma unroll
-  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-  const float base = top == -INFINITY ? 0.f : top;
-  float acc[kEach] = {}, sum = 0.f;
+        for (int d = 16; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, d));
+        to = fmaxf(to, top);
+        const float base = to == -INFINITY ? 0.f : to, before = exp2f(top - base), weight = exp2f(ml.x - base);
+        top = to;
+        sum = sum * before + weight * ml.y;  // (a lane's own; added up below)
 #pragma unroll
-  for (int l = 0; l < 2; ++l) {
-#pragma unroll 4
-    for (int i = 0; i < level[l].count; ++i) {
-      const float2 ml = stat(l, i);
-      const float weight = exp2f(ml.x - base);
-      const float* const o = (level[l].whole ? c.whole_out + ((long long)l * c.total_q * c.hq + flat) * DIM : part_row<DIM>(l ? shared : own, level[l], i)) + lane * kEach;
-      sum += weight * ml.y;
-      if (kEach == 4) {
-        const float4 v = chain_load(reinterpret_cast<const float4*>(o));
-        acc[0] += weight * v.x; acc[1] += weight * v.y; acc[2 % kEach] += weight * v.z; acc[3 % kEach] += weight * v.w;
-      } else {
-        const float2 v = chain_load(reinterpret_cast<const float2*>(o));
-        acc[0] += weight * v.x; acc[1] += weight * v.y;
+        for (int e = 0; e < kEach; ++e) acc[e] *= before;
+        const int parts = min(32, (p.count - i0 - sub + WARPS - 1) / WARPS);  // of this warp
+        for (int j0 = 0; j0 < parts; j0 += kAtOnce) {
+          float v[kAtOnce][kEach];
+#pragma unroll
+          for (int j = 0; j < kAtOnce; ++j) {
+            const int from = __shfl_sync(0xFFFFFFFFu, at, (j0 + j) & 31);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) v[j][e] = 0.f;
+            if (j0 + j < parts) {
+              if (kEach == 4) {
+                const float4 x = chain_load(reinterpret_cast<const float4*>(outs + (long long)from * DIM));
+                v[j][0] = x.x; v[j][1] = x.y; v[j][2 % kEach] = x.z; v[j][3 % kEach] = x.w;
+              } else {
+                const float2 x = chain_load(reinterpret_cast<const float2*>(outs + (long long)from * DIM));
+                v[j][0] = x.x; v[j][1] = x.y;
+              }
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kAtOnce; ++j) {
+            const float w = __shfl_sync(0xFFFFFFFFu, weight, (j0 + j) & 31);
+            if (j0 + j < parts)
+#pragma unroll
+              for (int e = 0; e < kEach; ++e) acc[e] = fmaf(w, v[j][e], acc[e]);
+          }
+        }
       }
     }
-  }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint32_t packed[kEach / 2];
 #pragma unroll
-  for (int i = 0; i < kEach / 2; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed[i]) : "f"(acc[2 * i + 1] * inv), "f"(acc[2 * i] * inv));
-  uint16_t* const to = c.out + (long long)row * c.o_st + (long long)head * c.o_sh + lane * kEach;
-  if (kEach == 4) *reinterpret_cast<uint2*>(to) = make_uint2(packed[0], packed[kEach / 2 - 1]);
-  else *reinterpret_cast<uint32_t*>(to) = packed[0];
-  if (c.lse_out && lane == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    if (WARPS > 1) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) part_acc[warp][lane * kEach + e] = acc[e];
+      if (lane == 0) part_ml[warp] = make_float2(top, sum);
+      __syncthreads();
+      if (sub != 0) return;
+      float to = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) to = fmaxf(to, part_ml[warp + w].x);
+      const float base = to == -INFINITY ? 0.f : to;
+      top = to;
+      sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float weight = exp2f(part_ml[warp + w].x - base);
+        sum += weight * part_ml[warp + w].y;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) acc[e] = fmaf(weight, part_acc[warp + w][lane * kEach + e], acc[e]);
+      }
+    }
+    if (!there || done) continue;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint32_t packed[kEach / 2];
+#pragma unroll
+    for (int i = 0; i < kEach / 2; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed[i]) : "f"(acc[2 * i + 1] * inv), "f"(acc[2 * i] * inv));
+    uint16_t* const to = c.out + (long long)row * c.o_st + (long long)head * c.o_sh + lane * kEach;
+    if (kEach == 4) *reinterpret_cast<uint2*>(to) = make_uint2(packed[0], packed[kEach / 2 - 1]);
+    else *reinterpret_cast<uint32_t*>(to) = packed[0];
+    if (c.lse_out && lane == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  }
+}
+
+template <int DIM, int WARPS, int HEADS>
+cudaError_t launch_join(const AttendCall& c, const AttendList& own, const AttendList& shared, cudaStream_t stream) {
+  constexpr int kHeads = kJoinWarps / WARPS * HEADS;
+  const long long blocks = (long long)c.total_q * ((c.hq + kHeads - 1) / kHeads);
+  count_launches(1);
+  return launch_chained(attend_join_kernel<DIM, WARPS, HEADS>, dim3((unsigned)blocks), dim3(32 * kJoinWarps), 0, stream, c, own, shared);
+}
+template <int DIM>
+cudaError_t launch_join(const AttendCall& c, const AttendList& own, const AttendList& shared, cudaStream_t stream) {
+  // As many warps per row and head as are resident at once (two blocks an SM); many rows: several heads per warp.
+  const long long flats = (long long)c.total_q * c.hq, room = kNumSMs * 2 * kJoinWarps;
+  if (flats * 8 <= room) return launch_join<DIM, 8, 1>(c, own, shared, stream);
+  if (flats * 2 <= room) return launch_join<DIM, 2, 1>(c, own, shared, stream);
+  return flats <= 4 * room ? launch_join<DIM, 1, 1>(c, own, shared, stream) : launch_join<DIM, 1, 4>(c, own, shared, stream);
 }
 
 // The levels' entries go to the kernel that suits their rows: few (mma.sync) up to kMostFew stacked rows, else many (tcgen05).
@@ -251,10 +342,6 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
   if (lists[1].entries() > 0) e = launch_attend_many(c, lists[1], st);
   if (e == cudaSuccess && lists[0].entries() > 0) e = launch_attend_few(c, lists[0], st);
   if (e != cudaSuccess) return cuda_failed(e);
-  const int warps = kJoinThreads / 32;
-  const dim3 grid((unsigned)(((long long)c.total_q * c.hq + warps - 1) / warps));
-  count_launches(1);
-  e = c.cache.dim == 128 ? launch_chained(attend_join_kernel<128>, grid, dim3(kJoinThreads), 0, st, c, own, shared)
-                         : launch_chained(attend_join_kernel<64>, grid, dim3(kJoinThreads), 0, st, c, own, shared);
+  e = c.cache.dim == 128 ? launch_join<128>(c, own, shared, st) : launch_join<64>(c, own, shared, st);
   return e == cudaSuccess ? FASTAV_OK : cuda_failed(e);
 }

@@ -10,6 +10,8 @@
 // all fall to a few workers.
 #pragma once
 
+#include <limits.h>
+
 #include "cache.cuh"
 
 namespace fastav {
@@ -106,8 +108,14 @@ __device__ __forceinline__ int units_of(const AttendCall& c, const AttendList& l
 // Blocks that have units: all, or the first of them, one unit each.
 __device__ __forceinline__ int workers_of(const AttendList& list, int total) { return max(1, min(list.grid, total)); }
 // Worker w of `workers` takes the units [run_start(w), run_start(w + 1)) of `total`; worker_of is the one that has unit u.
-__device__ __forceinline__ int run_start(int w, int workers, int total) { return (int)((long long)total * w / workers); }
-__device__ __forceinline__ int worker_of(int u, int workers, int total) { return (int)(((long long)(u + 1) * workers - 1) / total); }
+// (32 bits wherever they do: a 64-bit division is a hundred instructions.)
+__device__ __forceinline__ int scaled(int x, int times, int by) {
+  return x <= INT_MAX / kNumSMs ? (int)((unsigned)x * (unsigned)times / (unsigned)by) : (int)((long long)x * times / by);
+}
+__device__ __forceinline__ int run_start(int w, int workers, int total) { return scaled(total, w, workers); }
+__device__ __forceinline__ int worker_of(int u, int workers, int total) {
+  return u < INT_MAX / kNumSMs ? (int)(((unsigned)(u + 1) * (unsigned)workers - 1u) / (unsigned)total) : (int)(((long long)(u + 1) * workers - 1) / total);
+}
 
 // The list, all threads of the block: ahead[e] in shared memory, [entries + 1]; the total.  Block 0 leaves a copy.
 template <int THREADS>
