@@ -212,7 +212,7 @@ constexpr int kMostFew = 48;
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
   bool own_many, shared_many;
-  size_t ahead[2], out[2], ml[2], whole_out, whole_ml, total = 0;  // offsets into the workspace: few, many
+  size_t ahead[2], out[2], ml[2], scratch, whole_out, whole_ml, total = 0;  // offsets into the workspace: few, many
   bool fits = true;
 };
 
@@ -229,7 +229,8 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   const long long group = p.num_q_heads / cache.num_kv_heads;
   w.own_many = p.max_qlen * group > kMostFew;
   w.shared_many = p.num_prefixes > 0 && p.max_prefix_q * group > kMostFew;
-  w.few.tile_rows = kFewTile;
+  const long long few_rows = (w.own_many ? 0 : p.max_qlen * group) > (w.shared_many ? 0 : p.max_prefix_q * group) ? p.max_qlen * group : p.max_prefix_q * group;
+  w.few.tile_rows = few_rows <= 8 ? 8 : 16;
   w.few.unit_keys = kFewKeys;
   w.many.tile_rows = kManyTile;
   w.many.unit_keys = kManyKeys;
@@ -249,6 +250,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
     w.out[i] = carve(parts * cache.head_dim * sizeof(float));
     w.ml[i] = carve(parts * sizeof(float2));
   }
+  w.scratch = carve(w.few.entries() > 0 ? few_scratch_floats(w.few, cache.head_dim) * sizeof(float) : 0);
   const size_t rows = p.num_prefixes > 0 ? (size_t)2 * p.total_q * p.num_q_heads : 0;
   w.whole_out = carve(rows * cache.head_dim * sizeof(float));
   w.whole_ml = carve(rows * sizeof(float2));
@@ -336,6 +338,7 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
     lists[i].part_out = reinterpret_cast<float*>(ws + w.out[i]);
     lists[i].part_ml = reinterpret_cast<float2*>(ws + w.ml[i]);
   }
+  lists[0].scratch = reinterpret_cast<float*>(ws + w.scratch);
   const AttendList &own = lists[w.own_many], &shared = lists[w.shared_many];
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;

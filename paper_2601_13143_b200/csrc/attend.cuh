@@ -45,11 +45,13 @@ struct AttendList {
   int32_t* ahead;            // [entries + 1] units before an entry, left for the kernel that joins
   float* part_out;           // [grid][2][tile_rows][dim]
   float2* part_ml;           // [grid][2][tile_rows]: running maximum (base 2), sum
+  float* scratch;            // few: parts that warps of one block exchange
   __host__ __device__ int entries() const { return from_prefix + from_own; }
 };
 
-// Few rows per KV head: mma.sync, a granule per warp (attend_few.cu).
-constexpr int kFewTile = 16, kFewKeys = 32, kFewJobCost = 0;
+// Few rows per KV head: mma.sync, a granule per warp, tiles of 8 or 16 rows (attend_few.cu).
+constexpr int kFewKeys = 32, kFewJobCost = 0;
+size_t few_scratch_floats(const AttendList& list, int dim);
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 // Many: tcgen05, a granule per step of a block (attend_many.cu).

@@ -1,16 +1,19 @@
 // Attention over the 8-bit cache for few query rows per KV head: decoding, drafted tokens, and short questions.
 //
 // Bound by reading the cache once from HBM.  A unit is 32 keys of one KV head; every warp takes an equal run of the call's units, and has a
-// ring of its own that it fills itself with TMA (no barrier between warps until the end).  Up to 16 stacked query rows are the A operand
-// of mma.sync (f16, fp32 sums): S = Q K^T over 8 keys at a time, softmax in registers, O += P V.  Codes become f16 exactly on
-// their way from shared memory; a query row is scaled by a power of two first, so that bf16 values are exact in f16 too; the keys'
-// scales multiply the logits, the values' scales the weights.  The weights 2^(z - m) vs are rounded to f16 (11 bits; the output has 8) after
-// another power of two per row.  Running maxima move only when a logit is 2^8 above them, so
-// that the sums are hardly ever rescaled.
+// ring of its own that it fills itself with TMA (no barrier between warps until the end).  mma.sync (f16, fp32 sums) with the keys as
+// the rows: S^T = K Q^T, softmax in registers, O^T += V^T P^T, so that up to eight stacked query rows fill an instruction (sixteen: two, on the
+// same operands from the cache).  Codes become f16 exactly on their way from shared memory; a query row is scaled by a power of two first,
+// so that bf16 values are exact in f16 too; the keys' scales multiply the logits, the values' scales the weights.  The weights
+// 2^(z - m) vs are rounded to f16 (11 bits; the output has 8) after another power of two per row.  Running maxima move only when a logit
+// is 2^8 above them, so that the sums are hardly ever rescaled.
 //
-// Any order of the contractions will do as long as both operands have it.  Lane 4 n + t holds, of Q and of key n of a group of eight, the
-// elements DIM/4 t ..; of V the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9 and the elements DIM/8 n ..: 16-byte reads (8 for head_dim 64), free of bank
-// conflicts for head_dim 128 in the swizzle that the copies write.
+// Any order of the contractions will do as long as both operands have it.  Lane 4 n + t holds, of query row n and of keys n and n + 8 of
+// sixteen, the elements DIM/4 t ..; of V the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9 and the elements DIM/8 n ..: 16-byte reads (8 for head_dim 64),
+// free of bank conflicts for head_dim 128 in the swizzle that the copies write.
+//
+// The query rows as the rows of the instructions (half of each empty with 8 rows, 243 registers, 8 warps): 4 x 16,384 keys FIGURE_OLD us
+// instead of FIGURE_NEW.
 #include <limits.h>
 
 #include <cuda.h>
@@ -23,7 +26,7 @@
 namespace fastav {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kWarps = 12, kThreads = 32 * kWarps;
 constexpr float kSlack = 8.f;        // log2 of what a weight may reach before the maximum is moved
 // A row's weights 2^(z - m) vs times a power of two that brings the largest to 2,048 .. 4,096, and moved when one is above 32,768 (f16 ends at
 // 65,504): what lies under f16's normal numbers is less than 2^-25 of the largest.
@@ -35,6 +38,7 @@ struct Few {
   static constexpr int kHalf = kFewKeys * DIM, kStage = 2 * kHalf;  // bytes: K or V; both
   static constexpr int kScales = 2 * kFewKeys;                      // floats of a stage
   static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr size_t smem(int entries) { return 1024 + kRing + (size_t)kWarps * kStages * kScales * 4 + (size_t)(entries + 1) * 4; }
 };
 
 // A part of a job that a warp leaves for the other warps of its block.
@@ -42,45 +46,36 @@ struct Left {
   int job_first, job_end, row0, rows, tile, head, own;
 };
 
+// Where four values of a part lie in shared memory: row-major, the pieces of a row turned by the row (no two lanes on one bank).
 template <int DIM>
-struct FewSmem {
-  using F = Few<DIM>;
-  unsigned char* base;
-  __device__ unsigned char* ring(int warp) const { return base + warp * F::kStages * F::kStage; }
-  __device__ float* scales(int warp) const { return reinterpret_cast<float*>(base + F::kRing) + warp * F::kStages * F::kScales; }
-  __device__ float* first_part(int warp, int rows) const {
-    return reinterpret_cast<float*>(base + F::kRing) + kWarps * F::kStages * F::kScales + warp * rows * DIM;
-  }
-  __device__ int* ahead(int rows) const { return reinterpret_cast<int*>(first_part(kWarps, rows)); }
-};
-template <int DIM>
-size_t few_smem(int rows, int entries) {
-  using F = Few<DIM>;
-  return 1024 + F::kRing + (size_t)kWarps * F::kStages * F::kScales * 4 + (size_t)kWarps * rows * DIM * 4 + (size_t)(entries + 1) * 4;
+__device__ __forceinline__ int part_at(int row, int piece) { return row * DIM + (piece ^ (row >> 1 & 3)) * 4; }
+
+// 8 x 8 f16 values, a row per four lanes -> a column per four lanes.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
-// Where four values of a part lie: row-major, the 16-byte pieces of a thread's run of DIM / 4 values turned by its lane.
-template <int DIM>
-__device__ __forceinline__ int part_at(int row, int piece) {  // piece: of four values, DIM / 4 of them
-  constexpr int kRun = DIM / 16;
-  const int t = piece / kRun, q = piece % kRun;
-  return row * DIM + (t * kRun + (q ^ ((row * 4 + t) & (kRun - 1)))) * 4;
-}
-
-template <int DIM, bool FP8>
+// NT: groups of eight stacked rows.
+template <int DIM, bool FP8, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
-attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, AttendCall c, AttendList list, int part_rows) {
+attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, AttendCall c, AttendList list) {
   using F = Few<DIM>;
-  constexpr int kSteps = DIM / 16;   // of the contraction over head_dim, and 8-column groups of a lane's two
-  constexpr int kTiles = DIM / 8;    // groups of eight output columns
+  constexpr int kTile = 8 * NT;      // stacked rows
+  constexpr int kSteps = DIM / 16;   // of the contraction over head_dim, and groups of sixteen output elements
+  constexpr int kRun = DIM / 8;      // output elements of a lane, per row
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t full[kWarps][F::kStages];
   __shared__ Left left[kWarps][2];
-  __shared__ float2 left_ml[kWarps][2][kFewTile];
+  __shared__ float2 left_ml[kWarps][2][kTile];
   __shared__ int warp_sum[kWarps], abort_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n8 = lane >> 2, t4 = lane & 3;
-  const FewSmem<DIM> smem{smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u)};
-  int* const ahead = smem.ahead(part_rows);
+  unsigned char* const smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  unsigned char* const my_ring = smem + warp * F::kStages * F::kStage;
+  const float* const scales = reinterpret_cast<float*>(smem + F::kRing) + warp * F::kStages * F::kScales;
+  int* const ahead = reinterpret_cast<int*>(smem + F::kRing) + kWarps * F::kStages * F::kScales;
+  float* const scratch = list.scratch + (long long)blockIdx.x * kWarps * kTile * DIM;  // a warp's first part
   if (threadIdx.x == 0) {
     abort_flag = 0;
     ptx::prefetch_tensormap(&k_map);
@@ -98,8 +93,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   const int block_u1 = run_start(min((int)blockIdx.x + 1, workers), workers, total);
   const int u0 = block_u0 + run_start(warp, kWarps, block_u1 - block_u0), u1 = block_u0 + run_start(warp + 1, kWarps, block_u1 - block_u0);
 
-  const uint32_t ring = ptx::smem_u32(smem.ring(warp));
-  const float* const scales = smem.scales(warp);
+  const uint32_t ring = ptx::smem_u32(my_ring);
   bool ok = true;
   int issued = 0;  // granules asked for
   Walk next;
@@ -140,20 +134,18 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     look_up();
     while (more && issued < F::kStages) issue();
 
-    uint32_t qf[kSteps][4];
-    float o[kTiles][4], m[2], l[2], power[2], row_scale[2];
-    int sees[2], all_see = 0;
+    uint32_t qf[NT][kSteps][2];
+    float o[NT][kSteps][4];                                        // elements kRun n8 + 2 i + (0, 1) of rows 2 t4 + (0, 1)
+    float m[NT][2], l[NT][2], power[NT][2], row_scale[NT][2];      // of those rows
+    int sees[NT][2], all_see = 0;
 #pragma unroll 1
     for (int n = 0;; ++n) {
       const int key0 = at.granule * kFewKeys;
       if (n == 0 || at.granule == 0) {  // another job: its query rows
-        all_see = INT_MAX;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int i = at.tile * kFewTile + n8 + 8 * e, r = i / c.group;
+        for (int g = 0; g < NT; ++g) {
+          const int i = at.tile * kTile + 8 * g + n8, r = i / c.group;
           const bool there = r < at.x.rows;
-          sees[e] = !there ? 0 : at.x.own && c.causal ? max(0, at.x.len - at.x.rows + r + 1) : at.x.len;
-          all_see = min(all_see, there ? sees[e] : INT_MAX);
           const uint4* const from = reinterpret_cast<const uint4*>(c.q + (long long)(at.x.row0 + r) * c.q_st + (long long)(at.head * c.group + i - r * c.group) * c.q_sh + t4 * (DIM / 4));
           uint32_t x[kSteps * 2];
 #pragma unroll
@@ -168,23 +160,28 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
           const float to = to_one(__uint_as_float(top << 16));
-          row_scale[e] = c.scale_log2 / to;
 #pragma unroll
           for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               const uint32_t v = x[2 * s + half];
-              qf[s][2 * half + e] = two_f16(__uint_as_float(v << 16) * to, __uint_as_float(v & 0xFFFF0000u) * to);
+              qf[g][s][half] = two_f16(__uint_as_float(v << 16) * to, __uint_as_float(v & 0xFFFF0000u) * to);
             }
-          m[e] = -INFINITY;
-          l[e] = power[e] = 0.f;
+          const int own_sees = !there ? 0 : at.x.own && c.causal ? max(0, at.x.len - at.x.rows + r + 1) : at.x.len;
+          const int least = __reduce_min_sync(0xFFFFFFFFu, there ? own_sees : INT_MAX);
+          all_see = g == 0 ? least : min(all_see, least);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {  // of row n8 -> of rows 2 t4 + e
+            row_scale[g][e] = c.scale_log2 / __shfl_sync(0xFFFFFFFFu, to, 4 * (2 * t4 + e));
+            sees[g][e] = __shfl_sync(0xFFFFFFFFu, own_sees, 4 * (2 * t4 + e));
+            m[g][e] = -INFINITY;
+            l[g][e] = power[g][e] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[g][j][e] = 0.f;
         }
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) all_see = min(all_see, __shfl_xor_sync(0xFFFFFFFFu, all_see, d));
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
       }
       const int stage = n % F::kStages;
       ok = ptx::mbar_wait_warp(ptx::smem_u32(&full[warp][stage]), (n / F::kStages) & 1, &abort_flag);
@@ -192,99 +189,99 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
       const uint32_t kt = ring + stage * F::kStage, vt = kt + F::kHalf;
       const float* const ks = scales + stage * F::kScales;
 
-      float z[4][4];  // key 8 j + 2 t4 + (0, 1): row n8, row n8 + 8
+      float z[NT][2][4];  // of 16 keys h: key n8, rows 2 t4 + (0, 1); key n8 + 8, the same
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[j][i] = 0.f;
-        const int key = 8 * j + n8;
+        for (int g = 0; g < NT; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[g][h][i] = 0.f;
 #pragma unroll
         for (int p = 0; p < kSteps / 4; ++p) {
-          const uint32_t piece = DIM == 128 ? ((2 * t4 + p) ^ (key & 7)) : (t4 ^ (key >> 1 & 3));
-          const uint4 v = ptx::ld_shared4(kt + key * DIM + piece * 16);
-          const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+          const int key = 16 * h + n8;
+          const uint32_t piece = DIM == 128 ? ((2 * t4 + p) ^ n8) : (t4 ^ (n8 >> 1 & 3)), from = kt + key * DIM + piece * 16;
+          const uint4 a = ptx::ld_shared4(from), b = ptx::ld_shared4(from + 8 * DIM);
+          const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint32_t lo, hi;
-            four_codes<FP8>(word[i], lo, hi);
-            const int s = 4 * p + i;
-            mma_f16(z[j], qf[s][0], qf[s][1], qf[s][2], qf[s][3], lo, hi);
+            uint32_t a0, a1, a2, a3;
+            four_codes<FP8>(wa[i], a0, a2);
+            four_codes<FP8>(wb[i], a1, a3);
+#pragma unroll
+            for (int g = 0; g < NT; ++g) mma_f16(z[g][h], a0, a1, a2, a3, qf[g][4 * p + i][0], qf[g][4 * p + i][1]);
           }
         }
       }
       const bool masked = key0 + kFewKeys > all_see;
-      float factor[2];
-      bool moved = false;
+      float k_scale[4], v_scale[4];  // of keys n8, n8 + 8, n8 + 16, n8 + 24
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 s = *reinterpret_cast<const float2*>(ks + 8 * j + 2 * t4);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float& x = z[j][2 * e + i];
-            x = x * ((i ? s.y : s.x) * row_scale[e]);
-            if (masked && key0 + 8 * j + 2 * t4 + i >= sees[e]) x = -INFINITY;
-            top = fmaxf(top, x);
-          }
-        }
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        factor[e] = 1.f;
-        if (top > m[e] + kSlack || (m[e] == -INFINITY && top > m[e])) {
-          factor[e] = ptx::ex2_approx(m[e] - top);
-          m[e] = top;
-          l[e] *= factor[e];
-          moved = true;
-        }
+      for (int i = 0; i < 4; ++i) {
+        k_scale[i] = ks[8 * i + n8];
+        v_scale[i] = ks[kFewKeys + 8 * i + n8];
       }
-      uint32_t weight[4][2];
+      float factor[NT][2];
+      bool moved = false;
+      uint32_t weight[NT][4];  // keys 8 i + 2 t4 + (0, 1) of row n8
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float base = m[e] == -INFINITY ? 0.f : m[e];
-        float top = 0.f;
+      for (int g = 0; g < NT; ++g) {
+        float w[4][2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 s = *reinterpret_cast<const float2*>(ks + kFewKeys + 8 * j + 2 * t4);
+        for (int e = 0; e < 2; ++e) {
+          float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float& x = z[j][2 * e + i];
-            const float p = ptx::ex2_approx(x - base);
-            l[e] += p;
-            // (a place that no key fills may hold any scale)
-            x = masked && key0 + 8 * j + 2 * t4 + i >= sees[e] ? 0.f : p * (i ? s.y : s.x);
+          for (int i = 0; i < 4; ++i) {
+            float& x = z[g][i / 2][i % 2 * 2 + e];
+            x = x * (k_scale[i] * row_scale[g][e]);
+            if (masked && key0 + 8 * i + n8 >= sees[g][e]) x = -INFINITY;
             top = fmaxf(top, x);
           }
-        }
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        if (top * power[e] > kMostWeight || (power[e] == 0.f && top > 0.f)) {
-          const float to = to_one(top) * kWeightPower;
-          factor[e] = power[e] == 0.f ? 0.f : factor[e] * (to / power[e]);
-          power[e] = to;
-          moved = true;
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+          factor[g][e] = 1.f;
+          if (top > m[g][e] + kSlack || (m[g][e] == -INFINITY && top > m[g][e])) {
+            factor[g][e] = ptx::ex2_approx(m[g][e] - top);
+            m[g][e] = top;
+            l[g][e] *= factor[g][e];
+            moved = true;
+          }
+          const float base = m[g][e] == -INFINITY ? 0.f : m[g][e];
+          float most = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = ptx::ex2_approx(z[g][i / 2][i % 2 * 2 + e] - base);
+            l[g][e] += p;
+            // (a place that no key fills may hold any scale)
+            w[i][e] = masked && key0 + 8 * i + n8 >= sees[g][e] ? 0.f : p * v_scale[i];
+            most = fmaxf(most, w[i][e]);
+          }
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+          if (most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f)) {
+            const float to = to_one(most) * kWeightPower;
+            factor[g][e] = power[g][e] == 0.f ? 0.f : factor[g][e] * (to / power[g][e]);
+            power[g][e] = to;
+            moved = true;
+          }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) weight[j][e] = two_f16(z[j][2 * e] * power[e], z[j][2 * e + 1] * power[e]);
+        for (int i = 0; i < 4; ++i) weight[g][i] = transposed(two_f16(w[i][0] * power[g][0], w[i][1] * power[g][1]));
       }
       if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          o[i][0] *= factor[0];
-          o[i][1] *= factor[0];
-          o[i][2] *= factor[1];
-          o[i][3] *= factor[1];
-        }
+        for (int g = 0; g < NT; ++g)
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[g][j][e] *= factor[g][e & 1];
       }
       // Keys behind the sequence's end: what their places hold is multiplied by a weight of 0, so it must not be NaN or infinite.  e4m3 has NaN.
       const int have = at.x.len - key0;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
+      for (int h = 0; h < 2; ++h) {
         uint32_t v[4][DIM / 32];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int key = 16 * s + 2 * t4 + (i & 1) + (i & 2) * 4;
+          const int key = 16 * h + 2 * t4 + (i & 1) + (i & 2) * 4;
           if (DIM == 128) {
             const uint4 x = ptx::ld_shared4(vt + key * DIM + ((n8 ^ (key & 7)) << 4));
             v[i][0] = x.x; v[i][1] = x.y; v[i][2 % (DIM / 32)] = x.z; v[i][3 % (DIM / 32)] = x.w;
@@ -299,62 +296,57 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
         for (int j = 0; j < DIM / 32; ++j)
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t b00, b01, b10, b11;  // (key pair, column)
-            four_codes<FP8>(__byte_perm(v[0][j], v[1][j], half ? 0x7362 : 0x5140), b00, b01);
-            four_codes<FP8>(__byte_perm(v[2][j], v[3][j], half ? 0x7362 : 0x5140), b10, b11);
-            mma_f16(o[4 * j + 2 * half], weight[2 * s][0], weight[2 * s][1], weight[2 * s + 1][0], weight[2 * s + 1][1], b00, b10);
-            mma_f16(o[4 * j + 2 * half + 1], weight[2 * s][0], weight[2 * s][1], weight[2 * s + 1][0], weight[2 * s + 1][1], b01, b11);
+          for (int half = 0; half < 2; ++half) {  // elements kRun n8 + 4 j + 2 half + (0, 1)
+            uint32_t a0, a1, a2, a3;
+            four_codes<FP8>(__byte_perm(v[0][j], v[1][j], half ? 0x7362 : 0x5140), a0, a1);
+            four_codes<FP8>(__byte_perm(v[2][j], v[3][j], half ? 0x7362 : 0x5140), a2, a3);
+#pragma unroll
+            for (int g = 0; g < NT; ++g) mma_f16(o[g][2 * j + half], a0, a1, a2, a3, weight[g][2 * h], weight[g][2 * h + 1]);
           }
       }
       if (more) issue();
 
       const int job_first = at.job_first(), job_end = at.job_end();
       if (at.unit + 1 == u1 || at.unit + 1 == job_end) {  // the end of the job, or of the run
-        const bool whole = job_first >= u0 && job_end <= u1;
+        const bool whole = job_first >= u0 && job_end <= u1, final = whole && c.prefixes == 0;
         const int slot = job_first < u0 ? 0 : 1;
         // (a run's last part may lie where its ring was: nothing is in flight any more)
-        float* const part = slot == 0 ? smem.first_part(warp, part_rows) : reinterpret_cast<float*>(smem.ring(warp));
+        float* const part = slot == 0 ? scratch + warp * kTile * DIM : reinterpret_cast<float*>(my_ring);
         if (!whole) __syncwarp();  // (the ring has been read)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 1);
-          l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 2);
-          const int row = n8 + 8 * e, i = at.tile * kFewTile + row, r = i / c.group;
-          if (r >= at.x.rows) continue;
-          const float back = power[e] == 0.f ? 0.f : 1.f / power[e];
-          const long long q_row = at.x.row0 + r;
-          const int head = at.head * c.group + i - r * c.group;
-          if (whole && c.prefixes == 0) {
-            const float inv = l[e] == 0.f ? 0.f : back / l[e];
-            uint16_t* const to = c.out + q_row * c.o_st + (long long)head * c.o_sh + t4 * (DIM / 4);
+        for (int g = 0; g < NT; ++g)
 #pragma unroll
-            for (int col = 0; col < 2; ++col)  // columns 2 t4 + col of every group of eight: elements DIM / 8 (2 t4 + col) ..
+          for (int e = 0; e < 2; ++e) {
 #pragma unroll
-              for (int j = 0; j < kTiles / 8; ++j) {
+            for (int d = 4; d < 32; d <<= 1) l[g][e] += __shfl_xor_sync(0xFFFFFFFFu, l[g][e], d);
+            const int row = 8 * g + 2 * t4 + e, i = at.tile * kTile + row, r = i / c.group;
+            if (r >= at.x.rows) continue;
+            const float back = power[g][e] == 0.f ? 0.f : 1.f / power[g][e];
+            const long long q_row = at.x.row0 + r;
+            const int head = at.head * c.group + i - r * c.group;
+            const long long flat = (at.x.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
+            if (final) {
+              const float inv = l[g][e] == 0.f ? 0.f : back / l[g][e];
+              uint16_t* const to = c.out + q_row * c.o_st + (long long)head * c.o_sh + n8 * kRun;
+#pragma unroll
+              for (int j = 0; j < kRun / 8; ++j) {
                 uint32_t x[4];
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) x[i4] = pair_bf16(o[8 * j + 2 * i4][2 * e + col] * inv, o[8 * j + 2 * i4 + 1][2 * e + col] * inv);
-                *reinterpret_cast<uint4*>(to + col * (DIM / 8) + 8 * j) = make_uint4(x[0], x[1], x[2], x[3]);
+                for (int i4 = 0; i4 < 4; ++i4) x[i4] = pair_bf16(o[g][4 * j + i4][e] * inv, o[g][4 * j + i4][2 + e] * inv);
+                *reinterpret_cast<uint4*>(to + 8 * j) = make_uint4(x[0], x[1], x[2], x[3]);
               }
-            if (c.lse_out && t4 == 0) c.lse_out[q_row * c.hq + head] = l[e] == 0.f ? -INFINITY : (m[e] + log2f(l[e])) * kLn2;
-          } else {
-            const long long flat = (at.x.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
-            float* const to = whole ? c.whole_out + flat * DIM : part;
+              if (c.lse_out && n8 == 0) c.lse_out[flat] = l[g][e] == 0.f ? -INFINITY : (m[g][e] + log2f(l[g][e])) * kLn2;
+            } else {
+              float* const to = whole ? c.whole_out + flat * DIM : part;
 #pragma unroll
-            for (int col = 0; col < 2; ++col)
-#pragma unroll
-              for (int j = 0; j < kTiles / 4; ++j) {
-                const int piece = t4 * (DIM / 16) + col * (DIM / 32) + j;
+              for (int j = 0; j < kRun / 4; ++j) {
+                const int piece = n8 * (kRun / 4) + j;
                 *reinterpret_cast<float4*>(to + (whole ? piece * 4 : part_at<DIM>(row, piece))) =
-                    make_float4(o[4 * j][2 * e + col] * back, o[4 * j + 1][2 * e + col] * back, o[4 * j + 2][2 * e + col] * back, o[4 * j + 3][2 * e + col] * back);
+                    make_float4(o[g][2 * j][e] * back, o[g][2 * j][2 + e] * back, o[g][2 * j + 1][e] * back, o[g][2 * j + 1][2 + e] * back);
               }
-            if (t4 == 0) {
-              if (whole) c.whole_ml[flat] = make_float2(m[e], l[e]);
-              else left_ml[warp][slot][row] = make_float2(m[e], l[e]);
+              if (n8 == 0) *(whole ? c.whole_ml + flat : &left_ml[warp][slot][row]) = make_float2(m[g][e], l[g][e]);
             }
           }
-        }
         if (!whole && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own};
       }
       if (!at.step(c, list, ahead, u1)) break;
@@ -386,7 +378,7 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
     const bool whole = job.job_first >= block_u0 && job.job_end <= block_u1;
     const int slot = job.job_first < block_u0 ? 0 : 1;
-    const int rows = min(kFewTile, job.rows * c.group - job.tile * kFewTile);
+    const int rows = min(kTile, job.rows * c.group - job.tile * kTile);
     for (int item = threadIdx.x; item < rows * (DIM / 4); item += kThreads) {
       const int row = item / (DIM / 4), piece = item % (DIM / 4);
       float top = -INFINITY;
@@ -399,19 +391,19 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (left[j / 2][j % 2].job_first < 0) continue;
         const float2 ml = left_ml[j / 2][j % 2][row];
         const float f = ptx::ex2_approx(ml.x - base);
-        const float* const part = j % 2 == 0 ? smem.first_part(j / 2, part_rows) : reinterpret_cast<const float*>(smem.ring(j / 2));
+        const float* const part = j % 2 == 0 ? scratch + j / 2 * kTile * DIM : reinterpret_cast<float*>(smem + j / 2 * F::kStages * F::kStage);
         const float4 v = *reinterpret_cast<const float4*>(part + part_at<DIM>(row, piece));
         sum += f * ml.y;
         acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
       }
-      const int stacked = job.tile * kFewTile + row, r = stacked / c.group, head = job.head * c.group + stacked - r * c.group;
+      const int stacked = job.tile * kTile + row, r = stacked / c.group, head = job.head * c.group + stacked - r * c.group;
       const long long q_row = job.row0 + r, flat = (job.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
       if (whole && c.prefixes == 0) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         *reinterpret_cast<uint2*>(c.out + q_row * c.o_st + (long long)head * c.o_sh + piece * 4) = make_uint2(pair_bf16(acc.x * inv, acc.y * inv), pair_bf16(acc.z * inv, acc.w * inv));
         if (c.lse_out && piece == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
       } else {
-        const long long place = ((long long)blockIdx.x * 2 + slot) * kFewTile + row;
+        const long long place = ((long long)blockIdx.x * 2 + slot) * kTile + row;
         *reinterpret_cast<float4*>((whole ? c.whole_out + flat * DIM : list.part_out + place * DIM) + piece * 4) = acc;
         if (piece == 0) *(whole ? c.whole_ml + flat : list.part_ml + place) = make_float2(top, sum);
       }
@@ -420,20 +412,23 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   }
 }
 
-template <int DIM, bool FP8>
+template <int DIM, bool FP8, int NT>
 cudaError_t run(const AttendCall& c, const AttendList& list, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t stream) {
-  const long long most_rows = (long long)(c.prefixes > 0 && c.max_prefix_q > c.max_qlen ? c.max_prefix_q : c.max_qlen) * c.group;
-  const int part_rows = most_rows < kFewTile ? (int)most_rows : kFewTile;
-  const size_t smem = few_smem<DIM>(part_rows, list.entries());
   const cudaError_t e = once_per_context([] {
-    return cudaFuncSetAttribute(attend_few_kernel<DIM, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem<DIM>(kFewTile, FASTAV_ATTEND_MAX_BATCH));
+    return cudaFuncSetAttribute(attend_few_kernel<DIM, FP8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few<DIM>::smem(FASTAV_ATTEND_MAX_BATCH));
   });
   if (e != cudaSuccess) return e;
   count_launches(1);
-  return launch_chained(attend_few_kernel<DIM, FP8>, dim3(list.grid), dim3(kThreads), smem, stream, k_map, v_map, c, list, part_rows);
+  return launch_chained(attend_few_kernel<DIM, FP8, NT>, dim3(list.grid), dim3(kThreads), Few<DIM>::smem(list.entries()), stream, k_map, v_map, c, list);
+}
+template <int DIM, bool FP8>
+cudaError_t run(const AttendCall& c, const AttendList& list, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t stream) {
+  return list.tile_rows == 8 ? run<DIM, FP8, 1>(c, list, k_map, v_map, stream) : run<DIM, FP8, 2>(c, list, k_map, v_map, stream);
 }
 
 }  // namespace
+
+size_t few_scratch_floats(const AttendList& list, int dim) { return (size_t)list.grid * kWarps * list.tile_rows * dim; }
 
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
   CUtensorMap k_map, v_map;
