@@ -26,7 +26,8 @@
 namespace fastav {
 namespace {
 
-constexpr int kWarps = 12, kThreads = 32 * kWarps;
+constexpr int kWarps = 12, kThreads = 32 * kWarps, kFewKeysShift = 5;
+static_assert(1 << kFewKeysShift == kFewKeys);
 constexpr float kSlack = 8.f;        // log2 of what a weight may reach before the maximum is moved
 // A row's weights 2^(z - m) vs times a power of two that brings the largest to 2,048 .. 4,096, and moved when one is above 32,768 (f16 ends at
 // 65,504): what lies under f16's normal numbers is less than 2^-25 of the largest.
@@ -101,9 +102,9 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   if (u0 < u1 && next.unit < u1) {
     Walk at = next;
     bool more = true;                                        // `next` stands at a granule of the run
-    const int box = min(1 << c.cache.page_shift, kFewKeys);  // keys of a copy; lane i has copy i
-    int page = 0;                                            // of this lane's copy of the next unit
-    auto boxes = [&](const Walk& x) { return (min(kFewKeys, x.x.len - x.granule * kFewKeys) + box - 1) / box; };
+    const int box_shift = min(c.cache.page_shift, kFewKeysShift), box = 1 << box_shift;  // keys of a copy; lane i has copy i
+    int page = 0;                                                                        // of this lane's copy of the next unit
+    auto boxes = [&](const Walk& x) { return (min(kFewKeys, x.x.len - x.granule * kFewKeys) + box - 1) >> box_shift; };
     auto look_up = [&] {
       if (lane < boxes(next)) {
         page = chain_load_cached(next.x.table + (next.granule * kFewKeys + lane * box >> c.cache.page_shift));
@@ -219,61 +220,87 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         k_scale[i] = ks[8 * i + n8];
         v_scale[i] = ks[kFewKeys + 8 * i + n8];
       }
-      float factor[NT][2];
-      bool moved = false;
-      uint32_t weight[NT][4];  // keys 8 i + 2 t4 + (0, 1) of row n8
+      // The maxima and the powers of two are moved only when a lane meets a value above what they allow; only then the lanes of a row compare theirs.
+      bool over = false;
 #pragma unroll
-      for (int g = 0; g < NT; ++g) {
-        float w[4][2];
+      for (int g = 0; g < NT; ++g)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float& x = z[g][i / 2][i % 2 * 2 + e];
-            x = x * (k_scale[i] * row_scale[g][e]);
+            x *= k_scale[i];
             if (masked && key0 + 8 * i + n8 >= sees[g][e]) x = -INFINITY;
             top = fmaxf(top, x);
           }
+          over |= top * row_scale[g][e] > m[g][e] + kSlack;  // (no key yet: -inf)
+        }
+      if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-          factor[g][e] = 1.f;
-          if (top > m[g][e] + kSlack || (m[g][e] == -INFINITY && top > m[g][e])) {
-            factor[g][e] = ptx::ex2_approx(m[g][e] - top);
+        for (int g = 0; g < NT; ++g) {
+          float factor[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = fmaxf(fmaxf(z[g][0][e], z[g][0][2 + e]), fmaxf(z[g][1][e], z[g][1][2 + e])) * row_scale[g][e];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            top = fmaxf(top, m[g][e]);
+            factor[e] = m[g][e] == -INFINITY ? 0.f : ptx::ex2_approx(m[g][e] - top);
             m[g][e] = top;
-            l[g][e] *= factor[g][e];
-            moved = true;
+            l[g][e] *= factor[e];
           }
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[g][j][e] *= factor[e & 1];
+        }
+      }
+      over = false;
+#pragma unroll
+      for (int g = 0; g < NT; ++g)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
           const float base = m[g][e] == -INFINITY ? 0.f : m[g][e];
           float most = 0.f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float p = ptx::ex2_approx(z[g][i / 2][i % 2 * 2 + e] - base);
+            float& x = z[g][i / 2][i % 2 * 2 + e];
+            const float p = ptx::ex2_approx(fmaf(x, row_scale[g][e], -base));
             l[g][e] += p;
-            // (a place that no key fills may hold any scale)
-            w[i][e] = masked && key0 + 8 * i + n8 >= sees[g][e] ? 0.f : p * v_scale[i];
-            most = fmaxf(most, w[i][e]);
+            x = p * v_scale[i];
+            if (masked && key0 + 8 * i + n8 >= sees[g][e]) x = 0.f;  // (a place that no key fills may hold any scale)
+            most = fmaxf(most, x);
           }
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-          if (most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f)) {
-            const float to = to_one(most) * kWeightPower;
-            factor[g][e] = power[g][e] == 0.f ? 0.f : factor[g][e] * (to / power[g][e]);
-            power[g][e] = to;
-            moved = true;
-          }
+          over |= most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f);
         }
+      if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) weight[g][i] = transposed(two_f16(w[i][0] * power[g][0], w[i][1] * power[g][1]));
-      }
-      if (__any_sync(0xFFFFFFFFu, moved)) {
+        for (int g = 0; g < NT; ++g) {
+          float factor[2];
 #pragma unroll
-        for (int g = 0; g < NT; ++g)
+          for (int e = 0; e < 2; ++e) {
+            float most = fmaxf(fmaxf(z[g][0][e], z[g][0][2 + e]), fmaxf(z[g][1][e], z[g][1][2 + e]));
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+            factor[e] = 1.f;
+            if (most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f)) {
+              const float to = to_one(most) * kWeightPower;
+              factor[e] = power[g][e] == 0.f ? 0.f : to / power[g][e];
+              power[g][e] = to;
+            }
+          }
 #pragma unroll
           for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[g][j][e] *= factor[g][e & 1];
+            for (int e = 0; e < 4; ++e) o[g][j][e] *= factor[e & 1];
+        }
       }
+      uint32_t weight[NT][4];  // keys 8 i + 2 t4 + (0, 1) of row n8
+#pragma unroll
+      for (int g = 0; g < NT; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weight[g][i] = transposed(two_f16(z[g][i / 2][i % 2 * 2] * power[g][0], z[g][i / 2][i % 2 * 2 + 1] * power[g][1]));
       // Keys behind the sequence's end: what their places hold is multiplied by a weight of 0, so it must not be NaN or infinite.  e4m3 has NaN.
       const int have = at.x.len - key0;
 #pragma unroll
