@@ -2,8 +2,6 @@
 #include <cmath>
 #include <limits.h>
 
-#include <cuda.h>
-
 #include "attend.cuh"
 #include "sm100_ptx.cuh"
 
@@ -272,20 +270,6 @@ int32_t check_shapes(const fastav_attend_params* p, const fastav_cache* cache) {
 }
 
 }  // namespace
-
-bool encode_pool_map(const CacheView& c, const void* pool, int box_rows, void* map) {
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  const Encode encode = reinterpret_cast<Encode>(tensor_map_encode_entry());
-  if (!encode) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)c.dim, (cuuint64_t)c.num_pages * c.hkv << c.page_shift};
-  const cuuint64_t strides[1] = {(cuuint64_t)c.dim};
-  const cuuint32_t box[2] = {(cuuint32_t)c.dim, (cuuint32_t)box_rows};
-  const cuuint32_t elem[2] = {1, 1};
-  return encode(static_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(pool), dims, strides, box, elem,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, c.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 }  // namespace fastav
 

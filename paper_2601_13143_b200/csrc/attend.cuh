@@ -58,9 +58,6 @@ cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaS
 constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4;
 cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
-// The pools as [rows of the pool, dim] bytes, boxes of box_rows rows, swizzled by the row's bytes.  `map`: a CUtensorMap.
-bool encode_pool_map(const CacheView& c, const void* pool, int box_rows, void* map);
-
 #ifdef __CUDACC__
 struct Entry {
   int row0, rows;  // query rows

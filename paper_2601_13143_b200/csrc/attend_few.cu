@@ -1,7 +1,7 @@
 // Attention over the 8-bit cache for few query rows per KV head: decoding, drafted tokens, and short questions.
 //
 // Bound by reading the cache once from HBM.  A unit is 32 keys of one KV head; every warp takes an equal run of the call's units, and has a
-// ring of its own that it fills itself with TMA (no barrier between warps until the end).  mma.sync (f16, fp32 sums) with the keys as
+// ring of its own that it fills itself (no barrier between warps until the end).  mma.sync (f16, fp32 sums) with the keys as
 // the rows: S^T = K Q^T, softmax in registers, O^T += V^T P^T, so that up to eight stacked query rows fill an instruction (sixteen: two, on the
 // same operands from the cache).  Codes become f16 exactly on their way from shared memory; a query row is scaled by a power of two first,
 // so that bf16 values are exact in f16 too; the keys' scales multiply the logits, the values' scales the weights.  The weights
@@ -10,17 +10,15 @@
 //
 // Any order of the contractions will do as long as both operands have it.  Lane 4 n + t holds, of query row n and of keys n and n + 8 of
 // sixteen, the elements DIM/4 t ..; of V the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9 and the elements DIM/8 n ..: 16-byte reads (8 for head_dim 64),
-// free of bank conflicts for head_dim 128 in the swizzle that the copies write.
+// free of bank conflicts for head_dim 128: piece p of a key's row (16 bytes) lies at p ^ (key % 8).  The ring is filled by 16-byte asynchronous
+// copies of all lanes; with TMA, four copies of one lane per unit, the issuing took a warp 900 of 4,000 cycles.
 //
 // The query rows as the rows of the instructions (half of each empty with 8 rows, 243 registers, 8 warps): 4 x 16,384 keys FIGURE_OLD us
 // instead of FIGURE_NEW.
 #include <limits.h>
 
-#include <cuda.h>
-
 #include "attend.cuh"
 #include "attend_8bit.cuh"
-#include "gather.cuh"
 #include "sm100_ptx.cuh"
 
 namespace fastav {
@@ -39,17 +37,26 @@ struct Few {
   static constexpr int kHalf = kFewKeys * DIM, kStage = 2 * kHalf;  // bytes: K or V; both
   static constexpr int kScales = 2 * kFewKeys;                      // floats of a stage
   static constexpr int kRing = kWarps * kStages * kStage;
-  static constexpr size_t smem(int entries) { return 1024 + kRing + (size_t)kWarps * kStages * kScales * 4 + (size_t)(entries + 1) * 4; }
+  static constexpr size_t smem(int entries) { return kRing + (size_t)kWarps * kStages * kScales * 4 + (size_t)(entries + 1) * 4; }
 };
 
 // A part of a job that a warp leaves for the other warps of its block.
 struct Left {
   int job_first, job_end, row0, rows, tile, head, own;
+  int in_ring;  // where: the warp's ring, else its place in global memory
 };
 
 // Where four values of a part lie in shared memory: row-major, the pieces of a row turned by the row (no two lanes on one bank).
 template <int DIM>
 __device__ __forceinline__ int part_at(int row, int piece) { return row * DIM + (piece ^ (row >> 1 & 3)) * 4; }
+
+__device__ __forceinline__ void copy_async16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>  // all but the latest N groups of this thread
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // 8 x 8 f16 values, a row per four lanes -> a column per four lanes.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
@@ -61,31 +68,20 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 // NT: groups of eight stacked rows.
 template <int DIM, bool FP8, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
-attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, AttendCall c, AttendList list) {
+attend_few_kernel(AttendCall c, AttendList list) {
   using F = Few<DIM>;
   constexpr int kTile = 8 * NT;      // stacked rows
   constexpr int kSteps = DIM / 16;   // of the contraction over head_dim, and groups of sixteen output elements
   constexpr int kRun = DIM / 8;      // output elements of a lane, per row
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t full[kWarps][F::kStages];
+  extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Left left[kWarps][2];
   __shared__ float2 left_ml[kWarps][2][kTile];
-  __shared__ int warp_sum[kWarps], abort_flag;
+  __shared__ int warp_sum[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n8 = lane >> 2, t4 = lane & 3;
-  unsigned char* const smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* const my_ring = smem + warp * F::kStages * F::kStage;
   const float* const scales = reinterpret_cast<float*>(smem + F::kRing) + warp * F::kStages * F::kScales;
   int* const ahead = reinterpret_cast<int*>(smem + F::kRing) + kWarps * F::kStages * F::kScales;
   float* const scratch = list.scratch + (long long)blockIdx.x * kWarps * kTile * DIM;  // a warp's first part
-  if (threadIdx.x == 0) {
-    abort_flag = 0;
-    ptx::prefetch_tensormap(&k_map);
-    ptx::prefetch_tensormap(&v_map);
-  }
-  if (lane == 0) {
-    for (int i = 0; i < F::kStages; ++i) ptx::mbar_init(ptx::smem_u32(&full[warp][i]), 1);
-    ptx::fence_barrier_init();
-  }
   if (lane < 2) left[warp][lane].job_first = -1;
   chain_enter_late(c);
   pdl_wait();  // everything may be what earlier work wrote
@@ -95,45 +91,57 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   const int u0 = block_u0 + run_start(warp, kWarps, block_u1 - block_u0), u1 = block_u0 + run_start(warp + 1, kWarps, block_u1 - block_u0);
 
   const uint32_t ring = ptx::smem_u32(my_ring);
-  bool ok = true;
-  int issued = 0;  // granules asked for
   Walk next;
   if (u0 < u1) next.seek(c, list, ahead, u0);
   if (u0 < u1 && next.unit < u1) {
     Walk at = next;
-    bool more = true;                                        // `next` stands at a granule of the run
-    const int box_shift = min(c.cache.page_shift, kFewKeysShift), box = 1 << box_shift;  // keys of a copy; lane i has copy i
-    int page = 0;                                                                        // of this lane's copy of the next unit
-    auto boxes = [&](const Walk& x) { return (min(kFewKeys, x.x.len - x.granule * kFewKeys) + box - 1) >> box_shift; };
-    auto look_up = [&] {
-      if (lane < boxes(next)) {
-        page = chain_load_cached(next.x.table + (next.granule * kFewKeys + lane * box >> c.cache.page_shift));
-        if ((unsigned)page >= (unsigned)c.cache.num_pages) {
-          page = 0;  // (its keys are as wrong as any)
-          if (c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
-        }
-      }
+    bool more = true;  // `next` stands at a granule of the run
+    // A unit's copies.  Lane: piece lane % kPieces of the rows lane / kPieces + kRows j; the unit's two halves of 16 keys may lie in two pages.
+    constexpr int kPieces = DIM / 16, kRows = 32 / kPieces, kCopies = kFewKeys / kRows;
+    const int row0 = lane / kPieces, piece = lane % kPieces;
+    uint32_t to[2];  // rows of even and of odd copies lie differently
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) to[odd] = ring + row0 * DIM + ((DIM == 128 ? piece ^ (row0 + odd * kRows & 7) : piece ^ (row0 >> 1 & 3)) << 4);
+    int page[2], stage_in = 0;
+    auto look_up = [&] {  // the pages of the unit that `next` stands at
+      const int key0 = next.granule * kFewKeys;
+      page[0] = chain_load_cached(next.x.table + (key0 >> c.cache.page_shift));
+      page[1] = page[0];
+      if (c.cache.page_shift == 4 && next.x.len > key0 + 16) page[1] = chain_load_cached(next.x.table + (key0 + 16 >> 4));
     };
-    auto issue = [&] {  // the unit that `next` stands at; then the one after it is looked up
-      const int stage = issued % F::kStages, count = boxes(next);
-      const uint32_t bar = ptx::smem_u32(&full[warp][stage]);
-      __syncwarp();  // what the stage held has been read
-      if (lane == 0) ptx::mbar_arrive_expect_tx(bar, count * box * 2 * (DIM + 4));
-      __syncwarp();
-      if (lane < count) {
-        const long long row = pool_row(c.cache, page, next.head, next.granule * kFewKeys + lane * box);
-        const uint32_t to = ring + stage * F::kStage + lane * box * DIM, to_scale = ptx::smem_u32(scales + stage * F::kScales + lane * box);
-        ptx::tma_load_2d(to, &k_map, 0, (int)row, bar);
-        ptx::tma_load_2d(to + F::kHalf, &v_map, 0, (int)row, bar);
-        bulk_load(to_scale, c.cache.k_scale + row, box * 4, bar);
-        bulk_load(to_scale + kFewKeys * 4, c.cache.v_scale + row, box * 4, bar);
+    auto issue = [&] {  // the copies of the unit that `next` stands at; then the one after it is looked up
+      if (more) {
+        const int key0 = next.granule * kFewKeys;
+        if ((unsigned)max(page[0], page[1]) >= (unsigned)c.cache.num_pages || (page[0] | page[1]) < 0) {
+          page[0] = page[1] = 0;  // (their keys are as wrong as any)
+          if (lane == 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+        }
+        const long long pool[2] = {pool_row(c.cache, page[0], next.head, key0), pool_row(c.cache, page[1], next.head, key0 + 16)};
+        const int have = next.x.len - key0;  // copies of rows that no page has are left out; what a page has behind the sequence's end is harmless
+        const uint32_t at_stage = stage_in * F::kStage;
+#pragma unroll
+        for (int j = 0; j < kCopies; ++j) {
+          const int second = j >= kCopies / 2 ? 1 : 0;
+          if (second && have <= 16) break;
+          const long long from = (pool[second] + row0 + (j - second * (kCopies / 2)) * kRows) * DIM + piece * 16;
+          copy_async16(to[j & 1] + at_stage + j * kRows * DIM, c.cache.k + from);
+          copy_async16(to[j & 1] + at_stage + F::kHalf + j * kRows * DIM, c.cache.v + from);
+        }
+        if (lane < 16 || have > 16) {
+          const long long row = (lane < 16 ? pool[0] : pool[1]) + (lane & 15);
+          const uint32_t at_scale = ptx::smem_u32(scales) + (stage_in * F::kScales + lane) * 4;
+          copy_async4(at_scale, c.cache.k_scale + row);
+          copy_async4(at_scale + kFewKeys * 4, c.cache.v_scale + row);
+        }
+        stage_in = stage_in + 1 == F::kStages ? 0 : stage_in + 1;
+        more = next.step(c, list, ahead, u1);
+        if (more) look_up();
       }
-      ++issued;
-      more = next.step(c, list, ahead, u1);
-      if (more) look_up();
+      copies_commit();  // (a group per unit, empty ones too)
     };
     look_up();
-    while (more && issued < F::kStages) issue();
+#pragma unroll 1
+    for (int i = 0; i < F::kStages; ++i) issue();
 
     uint32_t qf[NT][kSteps][2];
     float o[NT][kSteps][4];                                        // elements kRun n8 + 2 i + (0, 1) of rows 2 t4 + (0, 1)
@@ -185,8 +193,8 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         }
       }
       const int stage = n % F::kStages;
-      ok = ptx::mbar_wait_warp(ptx::smem_u32(&full[warp][stage]), (n / F::kStages) & 1, &abort_flag);
-      if (!ok) break;
+      copies_wait<F::kStages - 1>();
+      __syncwarp();  // ... of all lanes
       const uint32_t kt = ring + stage * F::kStage, vt = kt + F::kHalf;
       const float* const ks = scales + stage * F::kScales;
 
@@ -331,15 +339,16 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             for (int g = 0; g < NT; ++g) mma_f16(o[g][2 * j + half], a0, a1, a2, a3, weight[g][2 * h], weight[g][2 * h + 1]);
           }
       }
-      if (more) issue();
+      __syncwarp();  // the stage has been read
+      issue();
 
       const int job_first = at.job_first(), job_end = at.job_end();
       if (at.unit + 1 == u1 || at.unit + 1 == job_end) {  // the end of the job, or of the run
         const bool whole = job_first >= u0 && job_end <= u1, final = whole && c.prefixes == 0;
         const int slot = job_first < u0 ? 0 : 1;
-        // (a run's last part may lie where its ring was: nothing is in flight any more)
-        float* const part = slot == 0 ? scratch + warp * kTile * DIM : reinterpret_cast<float*>(my_ring);
-        if (!whole) __syncwarp();  // (the ring has been read)
+        // A run's last part lies where its ring was: nothing is in flight any more.
+        const bool last = at.unit + 1 + (at.unit + 1 == job_end ? list.job_cost : 0) >= u1;
+        float* const part = last ? reinterpret_cast<float*>(my_ring) : scratch + warp * kTile * DIM;
 #pragma unroll
         for (int g = 0; g < NT; ++g)
 #pragma unroll
@@ -374,21 +383,13 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
               if (n8 == 0) *(whole ? c.whole_ml + flat : &left_ml[warp][slot][row]) = make_float2(m[g][e], l[g][e]);
             }
           }
-        if (!whole && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own};
+        if (!whole && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own, last};
       }
       if (!at.step(c, list, ahead, u1)) break;
-    }
-    if (!ok) {
-      if (lane == 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_WAIT_EXPIRED);
-      // The copies in flight write into this block's shared memory: they are waited for before it may exit, also where another warp gave up.
-      int never = 0;
-      for (int n = max(0, issued - F::kStages); n < issued; ++n)
-        ptx::mbar_wait_bounded(ptx::smem_u32(&full[warp][n % F::kStages]), (n / F::kStages) & 1, &never);
     }
   }
   pdl_trigger();
   __syncthreads();
-  if (abort_flag) return;
 
   // The parts of one job that several warps left, joined in their order: to the output if the block has the whole job, else to the block's place.
   for (int i = 0; i < 2 * kWarps;) {
@@ -408,20 +409,19 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const int rows = min(kTile, job.rows * c.group - job.tile * kTile);
     for (int item = threadIdx.x; item < rows * (DIM / 4); item += kThreads) {
       const int row = item / (DIM / 4), piece = item % (DIM / 4);
-      float top = -INFINITY;
-      for (int j = i; j < end; ++j)
-        if (left[j / 2][j % 2].job_first >= 0) top = fmaxf(top, left_ml[j / 2][j % 2][row].x);
-      const float base = top == -INFINITY ? 0.f : top;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      float sum = 0.f;
+      float sum = 0.f, top = -INFINITY;
+#pragma unroll 4
       for (int j = i; j < end; ++j) {
-        if (left[j / 2][j % 2].job_first < 0) continue;
+        const Left& x = left[j / 2][j % 2];
+        if (x.job_first < 0) continue;
         const float2 ml = left_ml[j / 2][j % 2][row];
-        const float f = ptx::ex2_approx(ml.x - base);
-        const float* const part = j % 2 == 0 ? scratch + j / 2 * kTile * DIM : reinterpret_cast<float*>(smem + j / 2 * F::kStages * F::kStage);
+        const float* const part = x.in_ring ? reinterpret_cast<float*>(smem + j / 2 * F::kStages * F::kStage) : scratch + j / 2 * kTile * DIM;
         const float4 v = *reinterpret_cast<const float4*>(part + part_at<DIM>(row, piece));
-        sum += f * ml.y;
-        acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+        const float to = fmaxf(top, ml.x), base = to == -INFINITY ? 0.f : to, f0 = ptx::ex2_approx(top - base), f = ptx::ex2_approx(ml.x - base);
+        top = to;
+        sum = sum * f0 + f * ml.y;
+        acc.x = acc.x * f0 + f * v.x; acc.y = acc.y * f0 + f * v.y; acc.z = acc.z * f0 + f * v.z; acc.w = acc.w * f0 + f * v.w;
       }
       const int stacked = job.tile * kTile + row, r = stacked / c.group, head = job.head * c.group + stacked - r * c.group;
       const long long q_row = job.row0 + r, flat = (job.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
@@ -440,17 +440,17 @@ attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 }
 
 template <int DIM, bool FP8, int NT>
-cudaError_t run(const AttendCall& c, const AttendList& list, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t stream) {
+cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
   const cudaError_t e = once_per_context([] {
     return cudaFuncSetAttribute(attend_few_kernel<DIM, FP8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few<DIM>::smem(FASTAV_ATTEND_MAX_BATCH));
   });
   if (e != cudaSuccess) return e;
   count_launches(1);
-  return launch_chained(attend_few_kernel<DIM, FP8, NT>, dim3(list.grid), dim3(kThreads), Few<DIM>::smem(list.entries()), stream, k_map, v_map, c, list);
+  return launch_chained(attend_few_kernel<DIM, FP8, NT>, dim3(list.grid), dim3(kThreads), Few<DIM>::smem(list.entries()), stream, c, list);
 }
 template <int DIM, bool FP8>
-cudaError_t run(const AttendCall& c, const AttendList& list, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t stream) {
-  return list.tile_rows == 8 ? run<DIM, FP8, 1>(c, list, k_map, v_map, stream) : run<DIM, FP8, 2>(c, list, k_map, v_map, stream);
+cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
+  return list.tile_rows == 8 ? run<DIM, FP8, 1>(c, list, stream) : run<DIM, FP8, 2>(c, list, stream);
 }
 
 }  // namespace
@@ -458,11 +458,8 @@ cudaError_t run(const AttendCall& c, const AttendList& list, const CUtensorMap& 
 size_t few_scratch_floats(const AttendList& list, int dim) { return (size_t)list.grid * kWarps * list.tile_rows * dim; }
 
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
-  CUtensorMap k_map, v_map;
-  const int box = 1 << c.cache.page_shift < kFewKeys ? 1 << c.cache.page_shift : kFewKeys;
-  if (!encode_pool_map(c.cache, c.cache.k, box, &k_map) || !encode_pool_map(c.cache, c.cache.v, box, &v_map)) return cudaErrorNotSupported;
-  if (c.cache.dim == 128) return c.cache.fp8 ? run<128, true>(c, list, k_map, v_map, stream) : run<128, false>(c, list, k_map, v_map, stream);
-  return c.cache.fp8 ? run<64, true>(c, list, k_map, v_map, stream) : run<64, false>(c, list, k_map, v_map, stream);
+  if (c.cache.dim == 128) return c.cache.fp8 ? run<128, true>(c, list, stream) : run<128, false>(c, list, stream);
+  return c.cache.fp8 ? run<64, true>(c, list, stream) : run<64, false>(c, list, stream);
 }
 
 }  // namespace fastav

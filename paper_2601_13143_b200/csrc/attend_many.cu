@@ -22,8 +22,6 @@
 // O is rescaled only when a row's maximum has grown by 2^kSlack: until then its weights are larger than 2^kOffset, which f16 has room for.
 #include <limits.h>
 
-#include <cuda.h>
-
 #include "attend.cuh"
 #include "attend_8bit.cuh"
 #include "sm100_ptx.cuh"
