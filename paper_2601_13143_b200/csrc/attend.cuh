@@ -116,7 +116,7 @@ __device__ __forceinline__ int worker_of(int u, int workers, int total) {
   return u < INT_MAX / kNumSMs ? (int)(((unsigned)(u + 1) * (unsigned)workers - 1u) / (unsigned)total) : (int)(((long long)(u + 1) * workers - 1) / total);
 }
 
-// The list, all threads of the block: ahead[e] in shared memory, [entries + 1]; the total.  Block 0 leaves a copy.
+// The list, all threads of the block: ahead[e] in shared memory, [entries + 1]; the total.  Reads the index arrays only.
 template <int THREADS>
 __device__ int open_list(const AttendCall& c, const AttendList& list, int* ahead, int* warp_sum) {
   const int entries = list.entries(), each = (entries + THREADS - 1) / THREADS;
@@ -144,17 +144,17 @@ __device__ int open_list(const AttendCall& c, const AttendList& list, int* ahead
     total += warp_sum[w];
   }
 #pragma unroll 1
-  for (int e = e0; e < e1; ++e) {
-    ahead[e] += before;
-    if (blockIdx.x == 0) list.ahead[e] = ahead[e];
-  }
-  if (threadIdx.x == 0) {
-    ahead[entries] = total;
-    if (blockIdx.x == 0) list.ahead[entries] = total;
-  }
+  for (int e = e0; e < e1; ++e) ahead[e] += before;
+  if (threadIdx.x == 0) ahead[entries] = total;
   if (blockIdx.x == 0 && bad && c.device_status) atomicOr(c.device_status, FASTAV_DEV_SHAPE_MISMATCH);
   __syncthreads();
   return total;
+}
+// ... and block 0 leaves a copy for the kernel that joins (after the kernel's wait: an earlier call may still read what lies there).
+template <int THREADS>
+__device__ __forceinline__ void leave_list(const AttendList& list, const int* ahead) {
+  if (blockIdx.x == 0)
+    for (int e = threadIdx.x; e <= list.entries(); e += THREADS) list.ahead[e] = ahead[e];
 }
 
 // A walk along the list: the granule it stands at.

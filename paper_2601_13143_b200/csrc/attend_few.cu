@@ -75,7 +75,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
   constexpr int kRun = DIM / 8;      // output elements of a lane, per row
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Left left[kWarps][2];
-  __shared__ float2 left_ml[kWarps][2][kTile];
+  __shared__ float2 left_ml[kWarps][2][kTile], part_weight[2 * kWarps][kTile];
   __shared__ int warp_sum[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n8 = lane >> 2, t4 = lane & 3;
   unsigned char* const my_ring = smem + warp * F::kStages * F::kStage;
@@ -84,8 +84,9 @@ attend_few_kernel(AttendCall c, AttendList list) {
   float* const scratch = list.scratch + (long long)blockIdx.x * kWarps * kTile * DIM;  // a warp's first part
   if (lane < 2) left[warp][lane].job_first = -1;
   chain_enter_late(c);
-  pdl_wait();  // everything may be what earlier work wrote
   const int total = open_list<kThreads>(c, list, ahead, warp_sum);
+  pdl_wait();  // the rest may be what earlier work wrote
+  leave_list<kThreads>(list, ahead);
   const int workers = workers_of(list, total), block_u0 = run_start(min((int)blockIdx.x, workers), workers, total);
   const int block_u1 = run_start(min((int)blockIdx.x + 1, workers), workers, total);
   const int u0 = block_u0 + run_start(warp, kWarps, block_u1 - block_u0), u1 = block_u0 + run_start(warp + 1, kWarps, block_u1 - block_u0);
@@ -139,7 +140,22 @@ attend_few_kernel(AttendCall c, AttendList list) {
       }
       copies_commit();  // (a group per unit, empty ones too)
     };
+    // The query rows of a job: stacked row 8 g + n8, elements DIM/4 t4 ...  Asked for ahead of the first copies, whose way is as long.
+    uint32_t x[NT][kSteps * 2];
+    auto ask_queries = [&] {
+#pragma unroll
+      for (int g = 0; g < NT; ++g) {
+        const int i = at.tile * kTile + 8 * g + n8, r = i / c.group;
+        const uint4* const from = reinterpret_cast<const uint4*>(c.q + (long long)(at.x.row0 + r) * c.q_st + (long long)(at.head * c.group + i - r * c.group) * c.q_sh + t4 * (DIM / 4));
+#pragma unroll
+        for (int j = 0; j < kSteps / 2; ++j) {
+          const uint4 v = r < at.x.rows ? chain_load_cached(from + j) : make_uint4(0, 0, 0, 0);
+          x[g][4 * j] = v.x; x[g][4 * j + 1] = v.y; x[g][4 * j + 2] = v.z; x[g][4 * j + 3] = v.w;
+        }
+      }
+    };
     look_up();
+    ask_queries();
 #pragma unroll 1
     for (int i = 0; i < F::kStages; ++i) issue();
 
@@ -151,20 +167,14 @@ attend_few_kernel(AttendCall c, AttendList list) {
     for (int n = 0;; ++n) {
       const int key0 = at.granule * kFewKeys;
       if (n == 0 || at.granule == 0) {  // another job: its query rows
+        if (n > 0) ask_queries();
 #pragma unroll
         for (int g = 0; g < NT; ++g) {
           const int i = at.tile * kTile + 8 * g + n8, r = i / c.group;
           const bool there = r < at.x.rows;
-          const uint4* const from = reinterpret_cast<const uint4*>(c.q + (long long)(at.x.row0 + r) * c.q_st + (long long)(at.head * c.group + i - r * c.group) * c.q_sh + t4 * (DIM / 4));
-          uint32_t x[kSteps * 2];
-#pragma unroll
-          for (int j = 0; j < kSteps / 2; ++j) {
-            const uint4 v = there ? chain_load_cached(from + j) : make_uint4(0, 0, 0, 0);
-            x[4 * j] = v.x; x[4 * j + 1] = v.y; x[4 * j + 2] = v.z; x[4 * j + 3] = v.w;
-          }
           unsigned top = 0;  // bf16 bits of the largest magnitude; what is not a number is larger still
 #pragma unroll
-          for (int j = 0; j < kSteps * 2; ++j) top = __vmaxu2(top, x[j] & 0x7FFF7FFFu);
+          for (int j = 0; j < kSteps * 2; ++j) top = __vmaxu2(top, x[g][j] & 0x7FFF7FFFu);
           top = max(top >> 16, top & 0xFFFFu);
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
@@ -173,7 +183,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
           for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const uint32_t v = x[2 * s + half];
+              const uint32_t v = x[g][2 * s + half];
               qf[g][s][half] = two_f16(__uint_as_float(v << 16) * to, __uint_as_float(v & 0xFFFF0000u) * to);
             }
           const int own_sees = !there ? 0 : at.x.own && c.causal ? max(0, at.x.len - at.x.rows + r + 1) : at.x.len;
@@ -239,8 +249,16 @@ attend_few_kernel(AttendCall c, AttendList list) {
           for (int i = 0; i < 4; ++i) {
             float& x = z[g][i / 2][i % 2 * 2 + e];
             x *= k_scale[i];
-            if (masked && key0 + 8 * i + n8 >= sees[g][e]) x = -INFINITY;
             top = fmaxf(top, x);
+          }
+          if (masked) {
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float& x = z[g][i / 2][i % 2 * 2 + e];
+              if (key0 + 8 * i + n8 >= sees[g][e]) x = -INFINITY;
+              top = fmaxf(top, x);
+            }
           }
           over |= top * row_scale[g][e] > m[g][e] + kSlack;  // (no key yet: -inf)
         }
@@ -277,8 +295,16 @@ attend_few_kernel(AttendCall c, AttendList list) {
             const float p = ptx::ex2_approx(fmaf(x, row_scale[g][e], -base));
             l[g][e] += p;
             x = p * v_scale[i];
-            if (masked && key0 + 8 * i + n8 >= sees[g][e]) x = 0.f;  // (a place that no key fills may hold any scale)
             most = fmaxf(most, x);
+          }
+          if (masked) {  // (a place that no key fills may hold any scale)
+            most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float& x = z[g][i / 2][i % 2 * 2 + e];
+              if (key0 + 8 * i + n8 >= sees[g][e]) x = 0.f;
+              most = fmaxf(most, x);
+            }
           }
           over |= most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f);
         }
@@ -392,37 +418,50 @@ attend_few_kernel(AttendCall c, AttendList list) {
   __syncthreads();
 
   // The parts of one job that several warps left, joined in their order: to the output if the block has the whole job, else to the block's place.
-  for (int i = 0; i < 2 * kWarps;) {
-    const Left job = left[i / 2][i % 2];
-    if (job.job_first < 0) {
-      ++i;
-      continue;
+  // First what every part counts for (lane: slot), then the sums.
+  static_assert(2 * kWarps <= 32);
+  const int slot_first = lane < 2 * kWarps ? left[lane / 2][lane & 1].job_first : -1;
+  const unsigned alike = __match_any_sync(0xFFFFFFFFu, slot_first), leaders = __ballot_sync(0xFFFFFFFFu, slot_first >= 0 && __ffs(alike) - 1 == lane);
+  for (int row = warp; row < kTile; row += kWarps) {
+    const float2 ml = slot_first >= 0 ? left_ml[lane / 2][lane & 1][row] : make_float2(-INFINITY, 0.f);
+    float top = -INFINITY;  // of the lanes with the same job
+#pragma unroll 1
+    for (unsigned rest = leaders; rest; rest &= rest - 1) {
+      const unsigned group = __shfl_sync(0xFFFFFFFFu, alike, __ffs(rest) - 1);
+      float of_group = group >> lane & 1 ? ml.x : -INFINITY;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) of_group = fmaxf(of_group, __shfl_xor_sync(0xFFFFFFFFu, of_group, d));
+      if (group >> lane & 1) top = of_group;
     }
-    int end = i + 1;  // (unused slots lie between)
-    for (int j = i + 1; j < 2 * kWarps; ++j) {
-      const int start = left[j / 2][j % 2].job_first;
-      if (start >= 0 && start != job.job_first) break;
-      end = j + 1;
+    if (lane < 2 * kWarps) {
+      const float weight = ptx::ex2_approx(ml.x - (top == -INFINITY ? 0.f : top));
+      part_weight[lane][row] = make_float2(weight, weight * ml.y);
+      left_ml[lane / 2][lane & 1][row].x = top;
     }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (unsigned rest = leaders; rest; rest &= rest - 1) {
+    const int first = __ffs(rest) - 1;
+    const unsigned group = __shfl_sync(0xFFFFFFFFu, alike, first);
+    const Left job = left[first / 2][first & 1];
     const bool whole = job.job_first >= block_u0 && job.job_end <= block_u1;
     const int slot = job.job_first < block_u0 ? 0 : 1;
     const int rows = min(kTile, job.rows * c.group - job.tile * kTile);
     for (int item = threadIdx.x; item < rows * (DIM / 4); item += kThreads) {
       const int row = item / (DIM / 4), piece = item % (DIM / 4);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      float sum = 0.f, top = -INFINITY;
+      float sum = 0.f;
 #pragma unroll 4
-      for (int j = i; j < end; ++j) {
-        const Left& x = left[j / 2][j % 2];
-        if (x.job_first < 0) continue;
-        const float2 ml = left_ml[j / 2][j % 2][row];
-        const float* const part = x.in_ring ? reinterpret_cast<float*>(smem + j / 2 * F::kStages * F::kStage) : scratch + j / 2 * kTile * DIM;
+      for (unsigned of = group; of; of &= of - 1) {
+        const int j = __ffs(of) - 1;
+        const float2 w = part_weight[j][row];
+        const float* const part = left[j / 2][j & 1].in_ring ? reinterpret_cast<float*>(smem + j / 2 * F::kStages * F::kStage) : scratch + j / 2 * kTile * DIM;
         const float4 v = *reinterpret_cast<const float4*>(part + part_at<DIM>(row, piece));
-        const float to = fmaxf(top, ml.x), base = to == -INFINITY ? 0.f : to, f0 = ptx::ex2_approx(top - base), f = ptx::ex2_approx(ml.x - base);
-        top = to;
-        sum = sum * f0 + f * ml.y;
-        acc.x = acc.x * f0 + f * v.x; acc.y = acc.y * f0 + f * v.y; acc.z = acc.z * f0 + f * v.z; acc.w = acc.w * f0 + f * v.w;
+        sum += w.y;
+        acc.x = fmaf(w.x, v.x, acc.x); acc.y = fmaf(w.x, v.y, acc.y); acc.z = fmaf(w.x, v.z, acc.z); acc.w = fmaf(w.x, v.w, acc.w);
       }
+      const float top = left_ml[first / 2][first & 1][row].x;
       const int stacked = job.tile * kTile + row, r = stacked / c.group, head = job.head * c.group + stacked - r * c.group;
       const long long q_row = job.row0 + r, flat = (job.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
       if (whole && c.prefixes == 0) {
@@ -435,7 +474,6 @@ attend_few_kernel(AttendCall c, AttendList list) {
         if (piece == 0) *(whole ? c.whole_ml + flat : list.part_ml + place) = make_float2(top, sum);
       }
     }
-    i = end;
   }
 }
 

@@ -557,13 +557,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     ptx::fence_barrier_init();
   }
   chain_enter_late(c);
-  pdl_wait();  // everything may be what earlier work wrote; and tensor memory is taken when all earlier work has ended
+  const int total = open_list<kThreads>(c, list, ahead, ctl.warp_sum);
+  pdl_wait();  // the rest may be what earlier work wrote; and tensor memory is taken when all earlier work has ended
+  leave_list<kThreads>(list, ahead);
   if (warp == kIssueWarp) {
     ptx::tmem_alloc(ptx::smem_u32(&ctl.tmem_base), kTmemCols);
     ptx::tmem_relinquish();
     ptx::tc_fence_before_sync();
   }
-  const int total = open_list<kThreads>(c, list, ahead, ctl.warp_sum);  // (two block-wide barriers)
+  __syncthreads();
   ptx::tc_fence_after_sync();
   const int workers = workers_of(list, total), u0 = run_start(min((int)blockIdx.x, workers), workers, total), u1 = run_start(min((int)blockIdx.x + 1, workers), workers, total);
   if (warp < kSoftWarps) {
