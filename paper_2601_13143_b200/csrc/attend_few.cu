@@ -140,7 +140,8 @@ attend_few_kernel(AttendCall c, AttendList list) {
       }
       copies_commit();  // (a group per unit, empty ones too)
     };
-    // The query rows of a job: stacked row 8 g + n8, elements DIM/4 t4 ...  Asked for ahead of the first copies, whose way is as long.
+    // The query rows of a job: stacked row 8 g + n8, elements DIM/4 t4 ...  Asked for ahead of the first copies, whose way is as long, if
+    // there are registers for it.
     uint32_t x[NT][kSteps * 2];
     auto ask_queries = [&] {
 #pragma unroll
@@ -155,7 +156,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
       }
     };
     look_up();
-    ask_queries();
+    if (NT == 1) ask_queries();
 #pragma unroll 1
     for (int i = 0; i < F::kStages; ++i) issue();
 
@@ -167,7 +168,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
     for (int n = 0;; ++n) {
       const int key0 = at.granule * kFewKeys;
       if (n == 0 || at.granule == 0) {  // another job: its query rows
-        if (n > 0) ask_queries();
+        if (NT > 1 || n > 0) ask_queries();
 #pragma unroll
         for (int g = 0; g < NT; ++g) {
           const int i = at.tile * kTile + 8 * g + n8, r = i / c.group;
