@@ -1,8 +1,8 @@
 // K and V rows into the 8-bit cache and back (fastav_cache_write, fastav_cache_read).
 //
 // Both are bound by HBM: a row of d values moves 2 d bytes on one side and d + 4 on the other.  A block takes a few consecutive rows
-// of the packed side: one thread per token finds its sequence, its token on either side and its page; then d / 8 lanes take a (token,
-// head) row of K or V each, eight values per lane, several rows' loads in flight.
+// of the packed side: one thread per token finds its sequence, its token on either side and its page; then d / 8 lanes take a head of K
+// or V each, eight values of a row per lane, several tokens' loads in flight.
 #include <limits.h>
 
 #include "cache.cuh"
@@ -18,7 +18,6 @@ struct RowsCall {
   CacheView cache;
   int batch, total_src, total_dst, max_src;  // packed source rows; rows that move (at most); longest sequence of the source
   int table_stride, tokens;                  // tokens per block
-  unsigned per_token_magic;                  // ceil(2^32 / (2 hkv))
   long long k_st, k_sh, v_st, v_sh;          // of the bf16 side
   bool global_idx;
   int head_wait;
@@ -35,47 +34,47 @@ __device__ __forceinline__ unsigned top_of(const uint4& x) {
 // code_i = round(x_i L / top), exactly.  x_i L has at most 15 bits, so it is exact in fp32, and the quotient of a 15-bit and an
 // 8-bit number that is no tie is at least 2^-16 of itself away from one: an approximate quotient corrected once by its
 // remainder (q + (n - q t) / t, an ulp off at most, and exact where the quotient is short) rounds as the true one does.  Everything is
-// scaled by a power of two that brings `top` near 1, so that nothing overflows and 1 / top is normal.
+// scaled by a power of two that brings `top` near 1 (and leaves room for L), so that nothing overflows and 1 / top is normal.
 struct Quantiser {
-  float power, t, r;
-  __device__ explicit Quantiser(unsigned top) {
+  float2 to, less, r;  // L times the power of two; -top times it; the reciprocal of that
+  __device__ Quantiser(unsigned top, float largest) {
     const int e = (int)(top >> 7);
-    power = __uint_as_float((unsigned)min(max(254 - e, 1), 254) << 23);
-    t = top ? __uint_as_float(top << 16) * power : 1.f;
-    r = __fdividef(1.f, t);
+    const float power = __uint_as_float((unsigned)min(max(254 - e, 1), 240) << 23), t = top ? __uint_as_float(top << 16) * power : 1.f, inv = __fdividef(1.f, t);
+    to = make_float2(power * largest, power * largest);
+    less = make_float2(-t, -t);
+    r = make_float2(inv, inv);
   }
-  __device__ float code(float x, float largest) const {
-    const float n = x * power * largest, q = n * r;
-    return fmaf(fmaf(-q, t, n), r, q);
+  __device__ float2 codes(unsigned two) const {  // of two bf16 values
+    const float2 n = __fmul2_rn(make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xFFFF0000u)), to), q = __fmul2_rn(n, r);
+    return __ffma2_rn(__ffma2_rn(q, less, n), r, q);
   }
 };
-
-__device__ __forceinline__ unsigned pack_s8(float a, float b, float c, float d) {
-  constexpr float kRound = 12582912.f;  // 1.5 * 2^23: the sum's low bits are the value rounded to nearest, ties to even
-  const unsigned ab = __byte_perm(__float_as_uint(a + kRound), __float_as_uint(b + kRound), 0x0040);
-  const unsigned cd = __byte_perm(__float_as_uint(c + kRound), __float_as_uint(d + kRound), 0x0040);
-  return __byte_perm(ab, cd, 0x5410);
+// top / L, to nearest: a quotient within an ulp, corrected by its exact remainder times the nearest reciprocal (Markstein), where the remainder is normal.
+template <bool FP8>
+__device__ __forceinline__ float scale_of(unsigned top) {
+  constexpr float kLargest = FP8 ? 448.f : 127.f, kInverse = 1.f / kLargest;
+  const float t = __uint_as_float(top << 16);
+  if (top < 0x1000u) return __fdiv_rn(t, kLargest);  // below 2^-95
+  const float q = t * kInverse;
+  return fmaf(fmaf(-q, kLargest, t), kInverse, q);
 }
-__device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d) {
+
+__device__ __forceinline__ unsigned pack_s8(const float2& a, const float2& b) {
+  const float2 round = make_float2(12582912.f, 12582912.f);  // 1.5 * 2^23: the sum's low bits are the value rounded to nearest, ties to even
+  const float2 x = __fadd2_rn(a, round), y = __fadd2_rn(b, round);
+  return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
+}
+__device__ __forceinline__ unsigned pack_e4m3(const float2& a, const float2& b) {
   unsigned short lo, hi;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(a.y), "f"(a.x));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(b.y), "f"(b.x));
   return (unsigned)lo | (unsigned)hi << 16;
 }
-__device__ __forceinline__ float low_half(unsigned x) { return __uint_as_float(x << 16); }
-__device__ __forceinline__ float high_half(unsigned x) { return __uint_as_float(x & 0xFFFF0000u); }
 
 template <bool FP8>
 __device__ __forceinline__ uint2 quantise8(const uint4& x, const Quantiser& q) {
-  const unsigned w[4] = {x.x, x.y, x.z, x.w};
-  float c[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c[2 * i] = q.code(low_half(w[i]), FP8 ? 448.f : 127.f);
-    c[2 * i + 1] = q.code(high_half(w[i]), FP8 ? 448.f : 127.f);
-  }
-  return FP8 ? make_uint2(pack_e4m3(c[0], c[1], c[2], c[3]), pack_e4m3(c[4], c[5], c[6], c[7]))
-             : make_uint2(pack_s8(c[0], c[1], c[2], c[3]), pack_s8(c[4], c[5], c[6], c[7]));
+  const float2 a = q.codes(x.x), b = q.codes(x.y), c = q.codes(x.z), d = q.codes(x.w);
+  return FP8 ? make_uint2(pack_e4m3(a, b), pack_e4m3(c, d)) : make_uint2(pack_s8(a, b), pack_s8(c, d));
 }
 
 // Two e4m3 codes as floats.
@@ -154,47 +153,55 @@ cache_rows_kernel(RowsCall c, uint16_t* __restrict__ k, uint16_t* __restrict__ v
   }
   __syncthreads();
 
-  const int lane = threadIdx.x % kLanes, per_token = 2 * c.cache.hkv, work = tokens * per_token;
-  for (int base = 0; base < work; base += kRows * kUnroll) {  // (the same for all lanes: they shuffle)
-    const int e0 = base + (int)threadIdx.x / kLanes;
-    uint4 wide[kUnroll];
-    uint2 narrow[kUnroll];
-    float scale[kUnroll];
-    long long from[kUnroll], to[kUnroll];  // offsets in elements: bf16 side; row of the pool
-    bool is_v[kUnroll];
+  // A group of kLanes lanes keeps to one head of K or V and walks over the block's tokens, so that all of an address but the token's row is
+  // known beforehand; with fewer heads than groups several of these share a head's tokens.
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, heads = 2 * c.cache.hkv;
+  const int sharing = max(1, kRows / heads), step = min(kRows, heads);
+  const bool active = group < sharing * heads;
+  // (all lanes of a warp make the same number of turns: they shuffle)
+#pragma unroll 1
+  for (int h0 = 0; h0 < heads; h0 += step) {
+    const int h = h0 + group % step, first_token = group / step;
+    const bool is_v = h >= c.cache.hkv, mine = active && h < heads;
+    const int head = is_v ? h - c.cache.hkv : h;
+    uint16_t* const packed = (is_v ? v : k) + (long long)head * (is_v ? c.v_sh : c.k_sh) + lane * 8;
+    const long long stride = is_v ? c.v_st : c.k_st, head_row = (long long)head << c.cache.page_shift;
+    uint8_t* const codes = (is_v ? c.cache.v : c.cache.k) + head_row * DIM + lane * 8;
+    float* const scales = (is_v ? c.cache.v_scale : c.cache.k_scale) + head_row;
+#pragma unroll 1
+    for (int t0 = 0; t0 < tokens; t0 += sharing * kUnroll) {
+      uint4 wide[kUnroll];
+      uint2 narrow[kUnroll];
+      float scale[kUnroll];
+      long long from[kUnroll], to[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int e = e0 + u * kRows;
-      const int token = e < work ? (int)__umulhi((unsigned)e, c.per_token_magic) : 0, r = e - token * per_token;
-      is_v[u] = r >= c.cache.hkv;
-      const int head = is_v[u] ? r - c.cache.hkv : r;
-      const long long row = e < work ? packed_row[token] : -1;
-      from[u] = row < 0 ? -1 : row * (is_v[u] ? c.v_st : c.k_st) + (long long)head * (is_v[u] ? c.v_sh : c.k_sh) + lane * 8;
-      to[u] = cache_row[token] + ((long long)head << c.cache.page_shift);
-      if (from[u] < 0) continue;
-      if (WRITE) {
-        wide[u] = chain_load(reinterpret_cast<const uint4*>((is_v[u] ? v : k) + from[u]));
-      } else {
-        narrow[u] = chain_load(reinterpret_cast<const uint2*>((is_v[u] ? c.cache.v : c.cache.k) + to[u] * DIM + lane * 8));
-        scale[u] = chain_load((is_v[u] ? c.cache.v_scale : c.cache.k_scale) + to[u]);
+      for (int u = 0; u < kUnroll; ++u) {
+        const int token = t0 + first_token + u * sharing;
+        from[u] = mine && token < tokens ? packed_row[token] : -1;
+        if (from[u] < 0) continue;
+        to[u] = cache_row[token];
+        if (WRITE) {
+          wide[u] = chain_load(reinterpret_cast<const uint4*>(packed + from[u] * stride));
+        } else {
+          narrow[u] = chain_load(reinterpret_cast<const uint2*>(codes + to[u] * DIM));
+          scale[u] = chain_load(scales + to[u]);
+        }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (WRITE) {
-        unsigned top = from[u] < 0 ? 0u : top_of(wide[u]);
+      for (int u = 0; u < kUnroll; ++u) {
+        if (WRITE) {
+          unsigned top = from[u] < 0 ? 0u : top_of(wide[u]);
 #pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        if (from[u] < 0) continue;
-        const bool finite = top < 0x7F80u;  // else the codes are 0 (a NaN among them would reach rows that do not see it) and the scale is NaN
-        const uint2 codes = quantise8<FP8>(wide[u], Quantiser(top));
-        *reinterpret_cast<uint2*>((is_v[u] ? c.cache.v : c.cache.k) + to[u] * DIM + lane * 8) = finite ? codes : make_uint2(0, 0);
-        if (lane == 0)
-          (is_v[u] ? c.cache.v_scale : c.cache.k_scale)[to[u]] =
-              finite ? __fdiv_rn(__uint_as_float(top << 16), FP8 ? 448.f : 127.f) : __uint_as_float(0x7FC00000u);
-      } else {
-        if (from[u] < 0) continue;
-        *reinterpret_cast<uint4*>((is_v[u] ? v : k) + from[u]) = dequantise8<FP8>(narrow[u], scale[u]);
+          for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+          if (from[u] < 0) continue;
+          const bool finite = top < 0x7F80u;  // else the codes are 0 (a NaN among them would reach rows that do not see it) and the scale is NaN
+          const uint2 c8 = quantise8<FP8>(wide[u], Quantiser(top, FP8 ? 448.f : 127.f));
+          *reinterpret_cast<uint2*>(codes + to[u] * DIM) = finite ? c8 : make_uint2(0, 0);
+          if (lane == 0) scales[to[u]] = finite ? scale_of<FP8>(top) : __uint_as_float(0x7FC00000u);
+        } else {
+          if (from[u] < 0) continue;
+          *reinterpret_cast<uint4*>(packed + from[u] * stride) = dequantise8<FP8>(narrow[u], scale[u]);
+        }
       }
     }
   }
@@ -205,8 +212,7 @@ cudaError_t launch_rows(RowsCall c, uint16_t* k, uint16_t* v, const int32_t* cu_
                         const int32_t* start, int32_t* device_status, cudaStream_t stream) {
   // Few rows: a token per block, so that more SMs take part.  Many: 32 consecutive ones, whose scales fill whole sectors.
   c.tokens = 1;
-  while (c.tokens < kMostTokens && c.total_dst / (2 * c.tokens) >= kNumSMs * 8) c.tokens *= 2;
-  c.per_token_magic = (unsigned)((0x100000000ull + 2 * c.cache.hkv - 1) / (2 * c.cache.hkv));
+  while (c.tokens < kMostTokens && c.total_dst / (2 * c.tokens) >= kNumSMs * 2) c.tokens *= 2;
   const dim3 grid((unsigned)((c.total_dst + c.tokens - 1) / c.tokens));
   auto go = [&](auto kernel) { return launch_chained(kernel, grid, dim3(kThreads), 0, stream, c, k, v, cu_seqlens, keep_idx, cu, table, start, device_status); };
   count_launches(1);
