@@ -50,14 +50,6 @@ struct Left {
 template <int DIM>
 __device__ __forceinline__ int part_at(int row, int piece) { return row * DIM + (piece ^ (row >> 1 & 3)) * 4; }
 
-__device__ __forceinline__ void copy_async16(uint32_t to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_async4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>  // all but the latest N groups of this thread
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // 8 x 8 f16 values, a row per four lanes -> a column per four lanes.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
@@ -125,20 +117,20 @@ attend_few_kernel(AttendCall c, AttendList list) {
           const int second = j >= kCopies / 2 ? 1 : 0;
           if (second && have <= 16) break;
           const long long from = (pool[second] + row0 + (j - second * (kCopies / 2)) * kRows) * DIM + piece * 16;
-          copy_async16(to[j & 1] + at_stage + j * kRows * DIM, c.cache.k + from);
-          copy_async16(to[j & 1] + at_stage + F::kHalf + j * kRows * DIM, c.cache.v + from);
+          ptx::copy_async<16>(to[j & 1] + at_stage + j * kRows * DIM, c.cache.k + from);
+          ptx::copy_async<16>(to[j & 1] + at_stage + F::kHalf + j * kRows * DIM, c.cache.v + from);
         }
         if (lane < 16 || have > 16) {
           const long long row = (lane < 16 ? pool[0] : pool[1]) + (lane & 15);
           const uint32_t at_scale = ptx::smem_u32(scales) + (stage_in * F::kScales + lane) * 4;
-          copy_async4(at_scale, c.cache.k_scale + row);
-          copy_async4(at_scale + kFewKeys * 4, c.cache.v_scale + row);
+          ptx::copy_async<4>(at_scale, c.cache.k_scale + row);
+          ptx::copy_async<4>(at_scale + kFewKeys * 4, c.cache.v_scale + row);
         }
         stage_in = stage_in + 1 == F::kStages ? 0 : stage_in + 1;
         more = next.step(c, list, ahead, u1);
         if (more) look_up();
       }
-      copies_commit();  // (a group per unit, empty ones too)
+      ptx::copies_commit();  // (a group per unit, empty ones too)
     };
     // The query rows of a job: stacked row 8 g + n8, elements DIM/4 t4 ...  Asked for ahead of the first copies, whose way is as long, if
     // there are registers for it.
@@ -204,7 +196,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
         }
       }
       const int stage = n % F::kStages;
-      copies_wait<F::kStages - 1>();
+      ptx::copies_wait<F::kStages - 1>();
       __syncwarp();  // ... of all lanes
       const uint32_t kt = ring + stage * F::kStage, vt = kt + F::kHalf;
       const float* const ks = scales + stage * F::kScales;
