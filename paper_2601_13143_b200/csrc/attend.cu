@@ -264,8 +264,9 @@ int32_t check_shapes(const fastav_attend_params* p, const fastav_cache* cache) {
   if (p->num_prefixes < 0 || p->max_prefix_len < 0 || p->max_prefix_q < 0 || p->max_prefix_q > p->total_q) return FASTAV_ERR_INVALID_ARG;
   if (p->num_prefixes > 0 && p->prefix_table_stride < 0) return FASTAV_ERR_INVALID_ARG;
   if ((long long)p->batch + p->num_prefixes > FASTAV_ATTEND_MAX_BATCH) return FASTAV_ERR_UNSUPPORTED;
-  // a stack of query rows and the rows of all heads are 32-bit counts
-  if ((long long)p->total_q * p->num_q_heads > INT_MAX / 2) return FASTAV_ERR_UNSUPPORTED;
+  // a stack of query rows and the rows of all heads are 32-bit counts, and a stacked row times G is (query_row)
+  const long long group = p->num_q_heads / cache->num_kv_heads;
+  if ((long long)p->total_q * p->num_q_heads > INT_MAX / 2 || (double)p->total_q * group * group >= 4294967296.0) return FASTAV_ERR_UNSUPPORTED;
   return make_plan(*p, *cache).fits ? FASTAV_OK : FASTAV_ERR_UNSUPPORTED;
 }
 
@@ -302,6 +303,7 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
   AttendCall c{};
   c.cache = make_view(*cache);
   c.batch = p->batch; c.total_q = p->total_q; c.max_qlen = p->max_qlen; c.hq = p->num_q_heads; c.group = p->num_q_heads / cache->num_kv_heads;
+  c.group_magic = c.group > 1 ? (unsigned)((0x100000000ull + c.group - 1) / c.group) : 0;
   c.max_len = p->max_kv_len; c.table_stride = p->table_stride;
   c.prefixes = p->num_prefixes; c.max_prefix_len = p->max_prefix_len; c.prefix_stride = p->prefix_table_stride; c.max_prefix_q = p->max_prefix_q;
   c.q_st = p->q_stride_tok; c.q_sh = p->q_stride_head; c.o_st = p->o_stride_tok; c.o_sh = p->o_stride_head;

@@ -19,6 +19,7 @@ namespace fastav {
 struct AttendCall {
   CacheView cache;
   int batch, total_q, max_qlen, hq, group;
+  unsigned group_magic;  // ceil(2^32 / group); 0: group is 1
   int max_len, table_stride;
   int prefixes, max_prefix_len, prefix_stride, max_prefix_q;
   long long q_st, q_sh, o_st, o_sh;
@@ -59,6 +60,9 @@ constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4;
 cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 #ifdef __CUDACC__
+// The query row of a stacked row, i / group (the host sees to it that i * group < 2^32).
+__device__ __forceinline__ int query_row(const AttendCall& c, int i) { return c.group_magic ? (int)__umulhi((unsigned)i, c.group_magic) : i; }
+
 struct Entry {
   int row0, rows;  // query rows
   int len;         // keys

@@ -138,7 +138,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
     auto ask_queries = [&] {
 #pragma unroll
       for (int g = 0; g < NT; ++g) {
-        const int i = at.tile * kTile + 8 * g + n8, r = i / c.group;
+        const int i = at.tile * kTile + 8 * g + n8, r = query_row(c, i);
         const uint4* const from = reinterpret_cast<const uint4*>(c.q + (long long)(at.x.row0 + r) * c.q_st + (long long)(at.head * c.group + i - r * c.group) * c.q_sh + t4 * (DIM / 4));
 #pragma unroll
         for (int j = 0; j < kSteps / 2; ++j) {
@@ -163,7 +163,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
         if (NT > 1 || n > 0) ask_queries();
 #pragma unroll
         for (int g = 0; g < NT; ++g) {
-          const int i = at.tile * kTile + 8 * g + n8, r = i / c.group;
+          const int i = at.tile * kTile + 8 * g + n8, r = query_row(c, i);
           const bool there = r < at.x.rows;
           unsigned top = 0;  // bf16 bits of the largest magnitude; what is not a number is larger still
 #pragma unroll
@@ -374,7 +374,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
           for (int e = 0; e < 2; ++e) {
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) l[g][e] += __shfl_xor_sync(0xFFFFFFFFu, l[g][e], d);
-            const int row = 8 * g + 2 * t4 + e, i = at.tile * kTile + row, r = i / c.group;
+            const int row = 8 * g + 2 * t4 + e, i = at.tile * kTile + row, r = query_row(c, i);
             if (r >= at.x.rows) continue;
             const float back = power[g][e] == 0.f ? 0.f : 1.f / power[g][e];
             const long long q_row = at.x.row0 + r;
@@ -455,7 +455,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
         acc.x = fmaf(w.x, v.x, acc.x); acc.y = fmaf(w.x, v.y, acc.y); acc.z = fmaf(w.x, v.z, acc.z); acc.w = fmaf(w.x, v.w, acc.w);
       }
       const float top = left_ml[first / 2][first & 1][row].x;
-      const int stacked = job.tile * kTile + row, r = stacked / c.group, head = job.head * c.group + stacked - r * c.group;
+      const int stacked = job.tile * kTile + row, r = query_row(c, stacked), head = job.head * c.group + stacked - r * c.group;
       const long long q_row = job.row0 + r, flat = (job.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
       if (whole && c.prefixes == 0) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;

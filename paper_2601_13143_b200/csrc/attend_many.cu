@@ -64,6 +64,11 @@ struct Control {
   float2 row_ml[2][kSub];                                             // the streams' statistics, to be joined
 };
 
+// Whether all three phases are over (a whole warp's answer).
+__device__ __forceinline__ bool wait_all(uint32_t a, uint32_t a_parity, uint32_t b, uint32_t b_parity, uint32_t c, uint32_t c_parity) {
+  const bool x = ptx::mbar_try_wait(a, a_parity), y = ptx::mbar_try_wait(b, b_parity), z = ptx::mbar_try_wait(c, c_parity);
+  return __all_sync(0xFFFFFFFFu, x && y && z);
+}
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory"); }
 
 // What a block does of its run in one job: `tiles` tiles of keys from `first` on.
@@ -349,40 +354,45 @@ struct Place {
   int head, r;
 };
 __device__ __forceinline__ Place place_of(const AttendCall& c, const Walk& at, int tile_row) {
-  const int i = at.tile * kManyTile + tile_row, r = i / c.group;
+  const int i = at.tile * kManyTile + tile_row, r = query_row(c, i);
   return Place{(long long)at.x.row0 + r, at.head * c.group + i - r * c.group, r};
 }
 
 // A warp's 32 query rows into their operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to
-// `scale` what takes that back, times the softmax scale.
+// `scale` what takes that back, times the softmax scale.  Every lane copies its pieces to where they belong and turns them into f16 there: the
+// loads are all in flight, and the code is short (unrolled it took 7 us the first time, most of it instruction fetch).
 template <int DIM>
 __device__ __forceinline__ void load_queries(const AttendCall& c, const Walk& at, int first_row, uint32_t tile, int row_in_tile, float* scale, int lane) {
-  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kLoads = 8;  // rows of a load; loads in flight
+  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes;  // rows of a load
   const int sub = lane / kLanes, piece = lane % kLanes;
+  const uint32_t to = tile + (piece >> 3) * Many<DIM>::kHalfBytes;
 #pragma unroll 1
-  for (int j0 = 0; j0 < 32; j0 += kLoads * kRows) {
-    uint4 x[kLoads];
+  for (int j = sub; j < 32; j += kRows) {
+    const Place q = place_of(c, at, first_row + j);
+    const int row = row_in_tile + j;
+    const uint32_t at_piece = to + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+    if (q.r < at.x.rows) ptx::copy_async<16>(at_piece, c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8);
+    else ptx::st_shared4(at_piece, 0, 0, 0, 0);
+  }
+  ptx::copies_commit();
+  ptx::copies_wait<0>();
+#pragma unroll 1
+  for (int j = sub; j < 32; j += kRows) {
+    const int row = row_in_tile + j;
+    const uint32_t at_piece = to + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+    const uint4 x = ptx::ld_shared4(at_piece);
+    const unsigned m = 0x7FFF7FFFu;
+    unsigned top = __vmaxu2(__vmaxu2(x.x & m, x.y & m), __vmaxu2(x.z & m, x.w & m));  // what is not a number is larger than the rest
+    top = max(top >> 16, top & 0xFFFFu);
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const Place q = place_of(c, at, first_row + j0 + j * kRows + sub);
-      x[j] = q.r < at.x.rows ? chain_load_cached(reinterpret_cast<const uint4*>(c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8)) : make_uint4(0, 0, 0, 0);
-    }
+    for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const float by = to_one(__uint_as_float(top << 16));
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t h[4];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const unsigned m = 0x7FFF7FFFu;
-      unsigned top = __vmaxu2(__vmaxu2(x[j].x & m, x[j].y & m), __vmaxu2(x[j].z & m, x[j].w & m));  // what is not a number is larger than the rest
-      top = max(top >> 16, top & 0xFFFFu);
-#pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-      const float to = to_one(__uint_as_float(top << 16));
-      const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-      uint32_t h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xFFFF0000u) * to);
-      const int row = row_in_tile + j0 + j * kRows + sub;
-      ptx::st_shared4(tile + (piece >> 3) * Many<DIM>::kHalfBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4), h[0], h[1], h[2], h[3]);
-      if (piece == 0) scale[row] = c.scale_log2 / to;
-    }
+    for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xFFFF0000u) * by);
+    ptx::st_shared4(at_piece, h[0], h[1], h[2], h[3]);
+    if (piece == 0) scale[row] = c.scale_log2 / by;
   }
 }
 
@@ -420,8 +430,15 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     for (int v = 0; v < count; ++v, ++visits) {
       const int tile = seg.two ? v >> 1 : v, half = seg.two ? v & 1 : stream, n = done + tile, ring = n & (kScaleRing - 1);
       const Visit x{s, ctl.k_scale[ring] + half * kVisit, ctl.exponent[ring] + half * (kGroups / 2), ctl.unscale[ring] + half * (kGroups / 2)};
-      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.scale_full[ring]), (n / kScaleRing) & 1, &ctl.abort);
-      ptx::mbar_wait_warp(s_full, visits & 1, &ctl.abort);
+      const int buffer = visits & 1;
+      // The tile's scales, the logits, and that the weights two visits before have been used: looked at together (one after the other, each look
+      // is a hundred cycles and more of a visit's two thousand).
+      const uint32_t scale_full = ptx::smem_u32(&ctl.scale_full[ring]), buffer_done = pv_done + buffer * 8, done_parity = ((visits >> 1) - 1) & 1;
+      if (!wait_all(scale_full, (n / kScaleRing) & 1, s_full, visits & 1, buffer_done, done_parity)) {
+        ptx::mbar_wait_warp(scale_full, (n / kScaleRing) & 1, &ctl.abort);
+        ptx::mbar_wait_warp(s_full, visits & 1, &ctl.abort);
+        ptx::mbar_wait_warp(buffer_done, done_parity, &ctl.abort);
+      }
       ptx::tc_fence_after_sync();
       const int key0 = (seg.first + tile) * kManyKeys + half * kVisit;
       float2 t[kVisit / 2];
@@ -437,11 +454,6 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
         ptx::mbar_wait_warp(pv_done + ((visits - 1) & 1) * 8, (visits - 1) >> 1 & 1, &ctl.abort);
         ptx::tc_fence_after_sync();
         rescale_output<DIM>(outputs + stream * 128, factor);
-      }
-      const int buffer = visits & 1;
-      if (visits >= 2) {  // the weights that lay there have been used
-        ptx::mbar_wait_warp(pv_done + buffer * 8, ((visits >> 1) - 1) & 1, &ctl.abort);
-        ptx::tc_fence_after_sync();
       }
       l += visit_weights(x, weights + buffer * (kVisit / 2), row_scale, m == -INFINITY ? 0.f : m, t);
       ptx::tmem_st_wait();
