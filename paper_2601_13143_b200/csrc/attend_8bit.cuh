@@ -41,4 +41,7 @@ __device__ __forceinline__ float to_one(float magnitude) {
   return e == 255 ? 1.f : __uint_as_float((unsigned)min(max(254 - e, 1), 240) << 23);  // (room for a further factor)
 }
 
+// 1 / x of a power of two that to_one gives (times a small one).
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+
 }  // namespace fastav

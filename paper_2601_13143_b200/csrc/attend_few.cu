@@ -184,7 +184,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
           all_see = g == 0 ? least : min(all_see, least);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {  // of row n8 -> of rows 2 t4 + e
-            row_scale[g][e] = c.scale_log2 / __shfl_sync(0xFFFFFFFFu, to, 4 * (2 * t4 + e));
+            row_scale[g][e] = c.scale_log2 * inverse_power(__shfl_sync(0xFFFFFFFFu, to, 4 * (2 * t4 + e)));
             sees[g][e] = __shfl_sync(0xFFFFFFFFu, own_sees, 4 * (2 * t4 + e));
             m[g][e] = -INFINITY;
             l[g][e] = power[g][e] = 0.f;
@@ -313,7 +313,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
             factor[e] = 1.f;
             if (most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f)) {
               const float to = to_one(most) * kWeightPower;
-              factor[e] = power[g][e] == 0.f ? 0.f : to / power[g][e];
+              factor[e] = power[g][e] == 0.f ? 0.f : to * inverse_power(power[g][e]);
               power[g][e] = to;
             }
           }
@@ -376,7 +376,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
             for (int d = 4; d < 32; d <<= 1) l[g][e] += __shfl_xor_sync(0xFFFFFFFFu, l[g][e], d);
             const int row = 8 * g + 2 * t4 + e, i = at.tile * kTile + row, r = query_row(c, i);
             if (r >= at.x.rows) continue;
-            const float back = power[g][e] == 0.f ? 0.f : 1.f / power[g][e];
+            const float back = power[g][e] == 0.f ? 0.f : inverse_power(power[g][e]);
             const long long q_row = at.x.row0 + r;
             const int head = at.head * c.group + i - r * c.group;
             const long long flat = (at.x.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
