@@ -1,4 +1,5 @@
 // fastav_attend: the call's plan, and the kernel that joins the parts of its jobs.
+#include <algorithm>
 #include <cmath>
 #include <limits.h>
 
@@ -204,8 +205,10 @@ cudaError_t launch_join(const AttendCall& c, const AttendList& own, const Attend
   return flats <= 4 * room ? launch_join<DIM, 1, 1>(c, own, shared, stream) : launch_join<DIM, 1, 4>(c, own, shared, stream);
 }
 
-// The levels' entries go to the kernel that suits their rows: few (mma.sync) up to kMostFew stacked rows, else many (tcgen05).
-constexpr int kMostFew = 48;
+// The levels' entries go to the kernel that suits their stacked rows: few (mma.sync) up to 16, which it takes at once, many (tcgen05) beyond 48;
+// in between many as long as there are four of its units for every SM.  us, few / many: 28 rows, 8 x 3,000 keys of 4 heads 35.5 / 30.6, 32
+// sequences 76 / 70, one of 4,000 22.6 / 31.3, four prefixes of 3,000 32 / 36; 64 rows, 16 x 3,000 keys of 8 heads 132 / 73, 16 x 300 42.5 / 29.5.
+constexpr int kLeastMany = 17, kMostFew = 48, kManyUnits = 4 * kNumSMs;
 
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
@@ -225,15 +228,18 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   size_t off = 0;
   auto carve = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
   const long long group = p.num_q_heads / cache.num_kv_heads;
-  w.own_many = p.max_qlen * group > kMostFew;
-  w.shared_many = p.num_prefixes > 0 && p.max_prefix_q * group > kMostFew;
-  const long long few_rows = (w.own_many ? 0 : p.max_qlen * group) > (w.shared_many ? 0 : p.max_prefix_q * group) ? p.max_qlen * group : p.max_prefix_q * group;
-  w.few.tile_rows = few_rows <= 8 ? 8 : 16;
-  w.few.unit_keys = kFewKeys;
   w.many.tile_rows = kManyTile;
+  w.few.unit_keys = kFewKeys;
   w.many.unit_keys = kManyKeys;
   w.few.job_cost = kFewJobCost;
   w.many.job_cost = kManyJobCost;
+  auto takes_many = [&](long long entries, long long rows, long long len) {
+    return rows * group > kMostFew || (rows * group >= kLeastMany && most_units(p, cache, w.many, entries, rows, len) >= kManyUnits);
+  };
+  w.own_many = takes_many(p.batch, p.max_qlen, p.max_kv_len);
+  w.shared_many = p.num_prefixes > 0 && takes_many(p.num_prefixes, p.max_prefix_q, p.max_prefix_len);
+  const long long own_rows = w.own_many ? 0 : p.max_qlen * group, shared_rows = w.shared_many ? 0 : p.max_prefix_q * group;
+  w.few.tile_rows = std::max(own_rows, shared_rows) <= 8 ? 8 : 16;
   (w.own_many ? w.many : w.few).from_own = p.batch;
   (w.shared_many ? w.many : w.few).from_prefix = p.num_prefixes;
   AttendList* const lists[2] = {&w.few, &w.many};

@@ -51,7 +51,7 @@ struct AttendList {
 };
 
 // Few rows per KV head: mma.sync, a granule per warp, tiles of 8 or 16 rows (attend_few.cu).
-constexpr int kFewKeys = 32, kFewJobCost = 0;
+constexpr int kFewKeys = 32, kFewJobCost = 3;
 size_t few_scratch_floats(const AttendList& list, int dim);
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
