@@ -98,10 +98,61 @@ static PyObject* compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+/* (function, params, cache, k, v, cu_seqlens, keep_idx, cu_keep, page_table, table_stride, start, device_status, stream) */
+static PyObject* cache_write(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *c, *t[6], *start, *status, *stream;
+  if (expect("cache_write", n, 13) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) || pointers(a + 3, 6, t) ||
+      pointer(a[10], &start) || pointer(a[11], &status))
+    return NULL;
+  const long stride = PyLong_AsLong(a[9]);
+  stream = address(a[12]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_cache_write))f)(p, c, t[0], t[1], t[2], t[3], t[4], t[5], (int32_t)stride, start, status, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (function, params, cache, page_table, table_stride, start, cu_seqlens, k_out, v_out, device_status, stream) */
+static PyObject* cache_read(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *c, *table, *t[5], *stream;
+  if (expect("cache_read", n, 11) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) || pointer(a[3], &table) ||
+      pointers(a + 5, 5, t))
+    return NULL;
+  const long stride = PyLong_AsLong(a[4]);
+  stream = address(a[10]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_cache_read))f)(p, c, table, (int32_t)stride, t[0], t[1], t[2], t[3], t[4], stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (function, params, cache, q, cu_qlens, page_table, kv_lens, cu_prefix, prefix_table, prefix_lens, out, lse_out, workspace, device_status, stream) */
+static PyObject* attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *c, *t[9], *ws, *status, *stream;
+  size_t bytes;
+  if (expect("attend", n, 15) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) || pointers(a + 3, 9, t) ||
+      pointer(a[12], &ws) || size_of(a[12], &bytes) || pointer(a[13], &status))
+    return NULL;
+  stream = address(a[14]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_attend))f)(p, c, t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], t[8], ws, bytes, status, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {
     {"prune", (PyCFunction)(void (*)(void))prune, METH_FASTCALL, "fastav_prune"},
     {"select_mask", (PyCFunction)(void (*)(void))select_mask, METH_FASTCALL, "fastav_select_mask"},
     {"compact", (PyCFunction)(void (*)(void))compact, METH_FASTCALL, "fastav_compact"},
+    {"cache_write", (PyCFunction)(void (*)(void))cache_write, METH_FASTCALL, "fastav_cache_write"},
+    {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, "fastav_cache_read"},
+    {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, "fastav_attend"},
     {NULL, NULL, 0, NULL},
 };
 

@@ -385,6 +385,7 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.struct = fastav_cache(formats[k.dtype], k.shape[2], k.shape[0], k.shape[1], k.shape[3], k.data_ptr(), v.data_ptr(),
                                    k_scale.data_ptr(), v_scale.data_ptr())
+        self.address = ctypes.addressof(self.struct)
 
 
 def make_cache(num_pages: int, num_kv_heads: int, head_dim: int, page_tokens: int = 64, format: int = FASTAV_CACHE_INT8,
@@ -401,23 +402,29 @@ def _table(t: torch.Tensor | None) -> int:
     """Entries from one row of a page table to the next."""
     if t is None:
         return 0
-    if t.dim() != 2 or t.dtype != torch.int32 or (t.shape[1] > 1 and t.stride(1) != 1):
+    strides, shape = t.stride(), t.shape
+    if len(strides) != 2 or t.dtype is not torch.int32 or (strides[1] != 1 and shape[1] > 1):
         raise ValueError("expected an int32 page table [sequences, pages] with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return strides[0] if shape[0] > 1 else shape[1]
+
+
+def _struct(given, kind) -> int:
+    if not isinstance(given, kind):
+        raise TypeError(f"expected a {kind.__name__}")
+    return ctypes.addressof(given)
 
 
 def fastav_cache_write(params, cache: KvCache, k, v, cu_seqlens, keep_idx_opt, cu_keep_opt, page_table, start_opt=None, device_status=None,
                        stream=None) -> None:
     """Quantise K and V rows (the survivors of a keep list, or all of them) into the cache's pages."""
-    _check(library().fastav_cache_write(ctypes.byref(params), ctypes.byref(cache.struct), _p(k), _p(v), _p(cu_seqlens), _p(keep_idx_opt),
-                                        _p(cu_keep_opt), _p(page_table), _table(page_table), _p(start_opt), _p(device_status),
-                                        _stream(stream)), "fastav_cache_write")
+    _check(_native().cache_write(_address("fastav_cache_write"), _params(params), cache.address, k, v, cu_seqlens, keep_idx_opt, cu_keep_opt, page_table,
+                                 _table(page_table), start_opt, device_status, _stream(stream)), "fastav_cache_write")
 
 
 def fastav_cache_read(params, cache: KvCache, page_table, start_opt, cu_seqlens, k_out, v_out, device_status=None, stream=None) -> None:
     """Rows of the cache as bf16."""
-    _check(library().fastav_cache_read(ctypes.byref(params), ctypes.byref(cache.struct), _p(page_table), _table(page_table), _p(start_opt),
-                                       _p(cu_seqlens), _p(k_out), _p(v_out), _p(device_status), _stream(stream)), "fastav_cache_read")
+    _check(_native().cache_read(_address("fastav_cache_read"), _params(params), cache.address, page_table, _table(page_table), start_opt, cu_seqlens, k_out,
+                                v_out, device_status, _stream(stream)), "fastav_cache_read")
 
 
 def make_attend_params(*, batch, total_q, max_qlen, num_q_heads, max_kv_len, q, out, page_table, prefix_table=None, max_prefix_len=0,
@@ -444,10 +451,8 @@ def fastav_attend_workspace_bytes(params: fastav_attend_params, cache: KvCache) 
 def fastav_attend(params, cache: KvCache, q, cu_qlens, page_table, kv_lens, out, workspace, cu_prefix=None, prefix_table=None,
                   prefix_lens=None, lse_out_opt=None, device_status=None, stream=None) -> None:
     """Attention of q's rows over the cache: a prefix that several sequences share (optional), then each sequence's own tokens."""
-    ws, ws_bytes = _ws(workspace)
-    _check(library().fastav_attend(ctypes.byref(params), ctypes.byref(cache.struct), _p(q), _p(cu_qlens), _p(page_table), _p(kv_lens),
-                                   _p(cu_prefix), _p(prefix_table), _p(prefix_lens), _p(out), _p(lse_out_opt), ws, ws_bytes,
-                                   _p(device_status), _stream(stream)), "fastav_attend")
+    _check(_native().attend(_address("fastav_attend"), _struct(params, fastav_attend_params), cache.address, q, cu_qlens, page_table, kv_lens, cu_prefix,
+                            prefix_table, prefix_lens, out, lse_out_opt, workspace, device_status, _stream(stream)), "fastav_attend")
 
 
 def fastav_kernel_launches() -> int:

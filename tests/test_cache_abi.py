@@ -132,3 +132,22 @@ def test_python_handles_check_their_tensors():
         fastav._table(torch.zeros(4, 4))
     wide = torch.zeros(4, 10, dtype=torch.int32)
     assert fastav._table(wide[:, 2:6]) == 10 and fastav._table(wide[:1, 2:6]) == 4 and fastav._table(None) == 0
+
+
+@pytest.mark.parametrize("name,count,numbers", [("cache_write", 13, {9: 4}), ("cache_read", 11, {4: 4}), ("attend", 15, {})])
+def test_the_c_module_passes_on_what_it_is_given(lib, name, count, numbers):
+    """Marshalling: a wrong number of arguments and a params of another type are refused in Python, a call without tensors by the library."""
+    native = fastav._native()
+    function = getattr(native, name)
+    with pytest.raises(TypeError):
+        function(*range(count - 1))
+    with pytest.raises(TypeError):
+        fastav._struct(_params(), fastav.fastav_attend_params)
+    p, c = (_attend() if name == "attend" else _params()), _cache()
+    arguments = [ctypes.cast(getattr(lib, "fastav_" + name), ctypes.c_void_p).value, ctypes.addressof(p), ctypes.addressof(c)] + [None] * (count - 4) + [0]
+    for at, value in numbers.items():
+        arguments[at] = value
+    assert function(*arguments) == INVALID
+    arguments[3 if name != "cache_read" else 5] = "not a tensor"
+    with pytest.raises(AttributeError):
+        function(*arguments)
