@@ -18,9 +18,7 @@ struct Parts {
   bool whole = false;
 };
 // Part i of a row: a job's first block has it in its second place.
-__device__ __forceinline__ int part_of(const AttendList& list, const Parts& p, int i) {
-  return ((p.first + i) * 2 + (i == 0 ? 1 : 0)) * list.tile_rows + p.row;
-}
+__device__ __forceinline__ int part_of(int tile_rows, const Parts& p, int i) { return ((p.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + p.row; }
 
 // What the rows of an entry have in common.
 struct Found {
@@ -102,19 +100,19 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
     const bool there = head < c.hq, done = c.prefixes == 0 && __shfl_sync(0xFFFFFFFFu, found[0].whole, h);
     const long long flat = (long long)row * c.hq + head, flats = (long long)c.total_q * c.hq;
     float top = -INFINITY, acc[kEach] = {}, sum = 0.f;
-#pragma unroll
-    for (int l = 0; l < 2; ++l) {
-      const AttendList& list = l ? shared : own;
+#pragma unroll 1
+    for (int l = 0; l < (c.prefixes > 0 ? 2 : 1); ++l) {  // (a loop: what runs once costs its length)
       Parts p;
-      p.first = __shfl_sync(0xFFFFFFFFu, found[l].first, h);
-      p.count = __shfl_sync(0xFFFFFFFFu, found[l].count, h);
-      p.row = __shfl_sync(0xFFFFFFFFu, found[l].row, h);
+      p.first = __shfl_sync(0xFFFFFFFFu, l ? found[1].first : found[0].first, h);
+      p.count = __shfl_sync(0xFFFFFFFFu, l ? found[1].count : found[0].count, h);
+      p.row = __shfl_sync(0xFFFFFFFFu, l ? found[1].row : found[0].row, h);
       p.whole = p.count == 1;
-      const float2* const stats = p.whole ? c.whole_ml + l * flats + flat : list.part_ml;
-      const float* const outs = (p.whole ? c.whole_out + (l * flats + flat) * DIM : list.part_out) + lane * kEach;
+      const int tile_rows = l ? shared.tile_rows : own.tile_rows;
+      const float2* const stats = p.whole ? c.whole_ml + l * flats + flat : l ? shared.part_ml : own.part_ml;
+      const float* const outs = (p.whole ? c.whole_out + (l * flats + flat) * DIM : l ? shared.part_out : own.part_out) + lane * kEach;
       for (int i0 = 0; !done && i0 < p.count; i0 += 32 * WARPS) {  // a lane's part: WARPS lane + sub
         const int mine = i0 + lane * WARPS + sub;
-        const int at = p.whole ? 0 : part_of(list, p, mine);
+        const int at = p.whole ? 0 : part_of(tile_rows, p, mine);
         const float2 ml = mine < p.count ? chain_load(stats + at) : make_float2(-INFINITY, 0.f);
         float to = ml.x;
 #pragma unroll

@@ -364,6 +364,9 @@ attend_few_kernel(AttendCall c, AttendList list) {
       const int job_first = at.job_first(), job_end = at.job_end();
       if (at.unit + 1 == u1 || at.unit + 1 == job_end) {  // the end of the job, or of the run
         const bool whole = job_first >= u0 && job_end <= u1, final = whole && c.prefixes == 0;
+        // A part that no other warp of the block has a share in goes to the block's place at once.
+        const bool alone = (job_first >= u0 || u0 == block_u0) && (job_end <= u1 || u1 == block_u1);
+        const long long place = ((long long)blockIdx.x * 2 + (job_first < block_u0 ? 0 : 1)) * kTile;
         const int slot = job_first < u0 ? 0 : 1;
         // A run's last part lies where its ring was: nothing is in flight any more.
         const bool last = at.unit + 1 + (at.unit + 1 == job_end ? list.job_cost : 0) >= u1;
@@ -392,17 +395,17 @@ attend_few_kernel(AttendCall c, AttendList list) {
               }
               if (c.lse_out && n8 == 0) c.lse_out[flat] = l[g][e] == 0.f ? -INFINITY : (m[g][e] + log2f(l[g][e])) * kLn2;
             } else {
-              float* const to = whole ? c.whole_out + flat * DIM : part;
+              float* const to = whole ? c.whole_out + flat * DIM : alone ? list.part_out + (place + row) * DIM : part;
 #pragma unroll
               for (int j = 0; j < kRun / 4; ++j) {
                 const int piece = n8 * (kRun / 4) + j;
-                *reinterpret_cast<float4*>(to + (whole ? piece * 4 : part_at<DIM>(row, piece))) =
+                *reinterpret_cast<float4*>(to + (whole || alone ? piece * 4 : part_at<DIM>(row, piece))) =
                     make_float4(o[g][2 * j][e] * back, o[g][2 * j][2 + e] * back, o[g][2 * j + 1][e] * back, o[g][2 * j + 1][2 + e] * back);
               }
-              if (n8 == 0) *(whole ? c.whole_ml + flat : &left_ml[warp][slot][row]) = make_float2(m[g][e], l[g][e]);
+              if (n8 == 0) *(whole ? c.whole_ml + flat : alone ? list.part_ml + place + row : &left_ml[warp][slot][row]) = make_float2(m[g][e], l[g][e]);
             }
           }
-        if (!whole && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own, last};
+        if (!whole && !alone && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own, last};
       }
       if (!at.step(c, list, ahead, u1)) break;
     }
