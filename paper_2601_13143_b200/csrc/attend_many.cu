@@ -358,28 +358,26 @@ __device__ __forceinline__ Place place_of(const AttendCall& c, const Walk& at, i
   return Place{(long long)at.x.row0 + r, at.head * c.group + i - r * c.group, r};
 }
 
-// A warp's 32 query rows into their operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to
-// `scale` what takes that back, times the softmax scale.  Every lane copies its pieces to where they belong and turns them into f16 there: the
-// loads are all in flight, and the code is short (unrolled it took 7 us the first time, most of it instruction fetch).
+// `rows` query rows into an operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to `scale`
+// what takes that back, times the softmax scale.  Every lane copies its pieces to where they belong and turns them into f16 there: the
+// loads are all in flight, and the code is short (unrolled it took 7 us the first time, most of it instruction fetch).  Rows that do not
+// exist keep what lies there: whatever it is, it stays in their own row of S and O, which nobody reads.
 template <int DIM>
-__device__ __forceinline__ void load_queries(const AttendCall& c, const Walk& at, int first_row, uint32_t tile, int row_in_tile, float* scale, int lane) {
+__device__ __forceinline__ void load_queries(const AttendCall& c, const Walk& at, int first_row, int rows, uint32_t tile, int row_in_tile, float* scale, int lane) {
   constexpr int kLanes = DIM / 8, kRows = 32 / kLanes;  // rows of a load
   const int sub = lane / kLanes, piece = lane % kLanes;
   const uint32_t to = tile + (piece >> 3) * Many<DIM>::kHalfBytes;
 #pragma unroll 1
-  for (int j = sub; j < 32; j += kRows) {
+  for (int j = sub; j < rows; j += kRows) {
     const Place q = place_of(c, at, first_row + j);
     const int row = row_in_tile + j;
-    const uint32_t at_piece = to + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
-    if (q.r < at.x.rows) ptx::copy_async<16>(at_piece, c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8);
-    else ptx::st_shared4(at_piece, 0, 0, 0, 0);
+    if (q.r < at.x.rows) ptx::copy_async<16>(to + row * 128 + (((piece & 7) ^ (row & 7)) << 4), c.q + q.q_row * c.q_st + (long long)q.head * c.q_sh + piece * 8);
   }
   ptx::copies_commit();
   ptx::copies_wait<0>();
 #pragma unroll 4
-  for (int j0 = 0; j0 < 32; j0 += kRows) {  // (four rows' ways through the shuffles side by side: one by one they took 8,500 cycles)
-    const int j = j0 + sub;
-    const int row = row_in_tile + j;
+  for (int j0 = 0; j0 < rows; j0 += kRows) {  // (four rows' ways through the shuffles side by side: one by one they took 8,500 cycles)
+    const int row = row_in_tile + j0 + sub;
     const uint32_t at_piece = to + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
     const uint4 x = ptx::ld_shared4(at_piece);
     const unsigned m = 0x7FFF7FFFu;
@@ -412,10 +410,14 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     const Segment seg = segment_of(c, at, u1);
     // With two streams of rows a thread's row is of its stream's half; else threads of both streams have the same one.
     const int warp_row = (seg.two ? stream * kSub : 0) + quarter * 32;
-    load_queries<DIM>(c, at, warp_row, q_tiles + stream * M::kTileBytes, quarter * 32, ctl.row_scale[stream], lane);
+    {  // every row once: a stream its own, or both streams half of them each
+      const int first = seg.two ? warp_row : warp * 16, most = seg.two ? 32 : 16, rows = min(most, max(0, rows_of(c, at) - first));
+      load_queries<DIM>(c, at, first, rows, q_tiles + (seg.two ? stream : 0) * M::kTileBytes, first - (seg.two ? stream * kSub : 0), ctl.row_scale[seg.two ? stream : 0], lane);
+    }
     ptx::fence_proxy_async_smem();
     ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.q_full), lane);
-    const float row_scale = ctl.row_scale[stream][row];
+    if (!seg.two) soft_sync();
+    const float row_scale = ctl.row_scale[seg.two ? stream : 0][row];
     int sees, all_see;
     bool there;
     {
@@ -515,7 +517,7 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
         const int r = j * kRows + lane / kLanes;
         const uint4 x = ptx::ld_shared4(stage + r * (kWide * 4) + ((piece ^ (r & 7)) << 4));
         const Place q = place_of(c, at, warp_row + r);
-        if (q.r >= at.x.rows) continue;
+        if (q.r >= at.x.rows) break;
         if (final) {
           *reinterpret_cast<uint2*>(c.out + q.q_row * c.o_st + (long long)q.head * c.o_sh + d + piece * 4) =
               make_uint2(pair_bf16(__uint_as_float(x.x), __uint_as_float(x.y)), pair_bf16(__uint_as_float(x.z), __uint_as_float(x.w)));
