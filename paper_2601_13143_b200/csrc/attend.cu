@@ -207,6 +207,7 @@ cudaError_t launch_join(const AttendCall& c, const AttendList& own, const Attend
 // in between many as long as there are four of its units for every SM.  us, few / many: 28 rows, 8 x 3,000 keys of 4 heads 35.5 / 30.6, 32
 // sequences 76 / 70, one of 4,000 22.6 / 31.3, four prefixes of 3,000 32 / 36; 64 rows, 16 x 3,000 keys of 8 heads 132 / 73, 16 x 300 42.5 / 29.5.
 constexpr int kLeastMany = 17, kMostFew = 48, kManyUnits = 4 * kNumSMs;
+constexpr double kFewUnitCost = 0.13, kManyUnitCost = 2.2;  // us of an SM
 
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
@@ -241,12 +242,23 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   (w.own_many ? w.many : w.few).from_own = p.batch;
   (w.shared_many ? w.many : w.few).from_prefix = p.num_prefixes;
   AttendList* const lists[2] = {&w.few, &w.many};
+  long long units[2];
+  for (int i = 0; i < 2; ++i) {
+    units[i] = most_units(p, cache, *lists[i], lists[i]->from_own, p.max_qlen, p.max_kv_len) +
+               most_units(p, cache, *lists[i], lists[i]->from_prefix, p.max_prefix_q, p.max_prefix_len);
+    w.fits &= units[i] < INT_MAX;
+  }
+  // Where both kernels run, they do so side by side, the SMs shared out by what their units cost (one behind the other, each is a start of 6 to 8
+  // us and an end: 32 answers on a shared 16,384-token prefix FIGURE_SEQ us instead of FIGURE_BESIDE).
+  int sms[2] = {kNumSMs, kNumSMs};
+  if (units[0] > 0 && units[1] > 0) {
+    const double few = (double)units[0] * kFewUnitCost, many = (double)units[1] * kManyUnitCost;
+    sms[0] = std::min(kNumSMs - 8, std::max(8, (int)(kNumSMs * few / (few + many))));
+    sms[1] = kNumSMs - sms[0];
+  }
   for (int i = 0; i < 2; ++i) {
     AttendList& list = *lists[i];
-    const long long units = most_units(p, cache, list, list.from_own, p.max_qlen, p.max_kv_len) +
-                            most_units(p, cache, list, list.from_prefix, p.max_prefix_q, p.max_prefix_len);
-    w.fits &= units < INT_MAX;
-    list.grid = (int)(units < 1 ? 1 : units < kNumSMs ? units : kNumSMs);
+    list.grid = (int)std::max(1ll, std::min(units[i], (long long)sms[i]));
     const size_t parts = list.entries() > 0 ? (size_t)list.grid * 2 * list.tile_rows : 0;
     w.ahead[i] = carve((size_t)(list.entries() + 1) * sizeof(int32_t));
     w.out[i] = carve(parts * cache.head_dim * sizeof(float));
@@ -332,8 +344,9 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
   const AttendList &own = lists[w.own_many], &shared = lists[w.shared_many];
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (lists[1].entries() > 0) e = launch_attend_many(c, lists[1], st);
-  if (e == cudaSuccess && lists[0].entries() > 0) e = launch_attend_few(c, lists[0], st);
+  c.beside = lists[0].entries() > 0 && lists[1].entries() > 0;
+  if (lists[0].entries() > 0) e = launch_attend_few(c, lists[0], st);
+  if (e == cudaSuccess && lists[1].entries() > 0) e = launch_attend_many(c, lists[1], st);
   if (e != cudaSuccess) return cuda_failed(e);
   e = c.cache.dim == 128 ? launch_join<128>(c, own, shared, st) : launch_join<64>(c, own, shared, st);
   return e == cudaSuccess ? FASTAV_OK : cuda_failed(e);

@@ -33,6 +33,7 @@ struct AttendCall {
   // results of jobs that one block finished, where another level's are still to be joined: [2][total_q, Hq]
   float* whole_out;
   float2* whole_ml;
+  int beside;  // both kernels run, side by side on SMs of their own
   int head_wait;
 };
 inline void mark_head(AttendCall& c, bool head) { c.head_wait = head ? 1 : 0; }

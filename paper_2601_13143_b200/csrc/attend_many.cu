@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
   }
   chain_enter_late(c);
   const int total = open_list<kThreads>(c, list, ahead, ctl.warp_sum);
-  pdl_wait();  // the rest may be what earlier work wrote; and tensor memory is taken when all earlier work has ended
+  if (!c.beside) pdl_wait();  // the rest may be what earlier work wrote; and tensor memory is taken when all earlier work has ended
   leave_list<kThreads>(list, ahead);
   if (warp == kIssueWarp) {
     ptx::tmem_alloc(ptx::smem_u32(&ctl.tmem_base), kTmemCols);
@@ -600,6 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
   ptx::tc_fence_after_sync();
   if (warp == kIssueWarp) ptx::tmem_dealloc(ctl.tmem_base, kTmemCols);
   if (threadIdx.x == 0 && ctl.abort && c.device_status) atomicOr(c.device_status, FASTAV_DEV_WAIT_EXPIRED);
+  if (c.beside) pdl_wait();  // what waits for this kernel waits for the one beside it, too
 }
 
 template <int DIM>
