@@ -448,7 +448,7 @@ typedef struct fastav_attend_params {
  *   lse      = log sum_{j in V(r)} exp(scale <q[r,h,:], k_j>)
  *   out      = sum_{j in V(r)} exp(scale <q[r,h,:], k_j> - lse) v_j
  *
- * A row that sees no key gets out = 0 and lse = -inf.
+ * A row that sees no key gets out = 0 and lse = -inf; one that sees a K or V row which is not finite gets NaN (of the lse, with a V row, it may).
  *
  *   q            [total_q, Hq, head_dim] bf16
  *   cu_qlens     [B+1] int32

@@ -279,3 +279,72 @@ def test_offsets_beyond_32_bits():
     p.cache, p.tables[0] = cache, table
     p.run()
     p.check()
+
+
+def test_the_largest_batch():
+    """4,096 entries: 4,094 sequences of 0 to 6 tokens and two prefixes."""
+    lens, rows = [i % 7 for i in range(4094)], [1] * 4094
+    p = Problem(2, 1, 64, "int8", 16, lens, rows, prefix_lens=[3, 1], groups=[0, 2000, 4000], seed=14)
+    p.run()
+    p.check()
+
+
+MIXES = [  # few rows only, many rows only, both side by side, short ones, many partial results
+    dict(hq=28, hkv=4, dim=128, fmt="int8", page=64, lens=[3000, 40], rows=[1, 1]),
+    dict(hq=16, hkv=4, dim=128, fmt="fp8", page=32, lens=[700, 300], rows=[40, 64]),
+    dict(hq=32, hkv=8, dim=128, fmt="int8", page=64, lens=[30, 60, 7] * 6, rows=[1] * 18, prefix_lens=[2000], groups=[0, 18]),
+    dict(hq=8, hkv=2, dim=64, fmt="fp8", page=16, lens=[5, 70], rows=[2, 3]),
+    dict(hq=32, hkv=1, dim=64, fmt="int8", page=128, lens=[5000], rows=[4]),
+]
+
+
+@pytest.mark.parametrize("flags", [0, fastav.FASTAV_CHAIN_CALLS])
+def test_calls_one_behind_the_other_do_not_disturb_each_other(flags):
+    """The same calls alone, and in a row without a pause on one workspace, give the same bits."""
+    problems = [Problem(seed=20 + i, **m) for i, m in enumerate(MIXES)]
+    alone = []
+    for p in problems:
+        p.run()
+        p.check()
+        alone.append((p.out.clone(), p.lse.clone()))
+    params = [p.params(flags=fastav.FASTAV_CAUSAL | flags) for p in problems]
+    ws = torch.full((max(fastav.fastav_attend_workspace_bytes(q, p.cache) for p, q in zip(problems, params)),), 0xFF, dtype=torch.uint8, device="cuda")
+    dev = lambda x: torch.as_tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    arrays = [dict(cu=_cu(p.rows).cuda(), table=p.tables[0].cuda(), lens=dev(p.lens),
+                   more=dict(cu_prefix=dev(p.groups), prefix_table=p.tables[1].cuda(), prefix_lens=dev(p.prefix_lens)) if p.prefix_lens else {}) for p in problems]
+    torch.cuda.synchronize()
+    outs = []
+    for turn in range(6):
+        for i in [(3 * j + turn) % len(problems) for j in range(len(problems))]:
+            p, q, a = problems[i], params[i], arrays[i]
+            out, lse = torch.full_like(p.out, 9.0), torch.full_like(p.lse, 9.0)
+            fastav.fastav_attend(q, p.cache, p.qd, a["cu"], a["table"], a["lens"], out, ws, lse_out_opt=lse, device_status=p.status, **a["more"])
+            outs.append((i, out, lse))
+    torch.cuda.synchronize()
+    for i, out, lse in outs:
+        assert torch.equal(out, alone[i][0]) and torch.equal(lse, alone[i][1]), i
+    assert all(int(p.status) == 0 for p in problems)
+
+
+def test_lengths_and_rows_that_earlier_work_on_the_stream_writes():
+    """kv_lens, the page table and q made by kernels right before the call, on a stream of the caller's."""
+    p = Problem(28, 4, 128, "int8", 64, [900, 333], [2, 1], prefix_lens=[600], groups=[0, 2], seed=30)
+    p.run()
+    want, wlse = p.out.clone(), p.lse.clone()
+    params = p.params()
+    ws = torch.empty(fastav.fastav_attend_workspace_bytes(params, p.cache), dtype=torch.uint8, device="cuda")
+    dev = lambda x: torch.as_tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    cu, lens, groups, plens, table, ptable = _cu(p.rows).cuda(), dev(p.lens), dev(p.groups), dev(p.prefix_lens), p.tables[0].cuda(), p.tables[1].cuda()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for i in range(8):
+            p.out.fill_(0)
+            lens2, table2, q2, plens2 = lens + i, table + 0, p.qd + 0, plens - i
+            lens2 -= i
+            plens2 += i
+            fastav.fastav_attend(params, p.cache, q2, cu, table2, lens2, p.out, ws, cu_prefix=groups, prefix_table=ptable + 0, prefix_lens=plens2, lse_out_opt=p.lse,
+                                 device_status=p.status)
+            got = p.out.clone()
+            side.synchronize()
+            assert torch.equal(got, want) and torch.equal(p.lse, wlse) and int(p.status) == 0
