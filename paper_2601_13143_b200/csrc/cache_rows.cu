@@ -133,7 +133,7 @@ __device__ __forceinline__ uint4 dequantise8(const uint2& x, float scale) {
 
 // WRITE: bf16 rows -> cache; else back.  `cu`: prefix sums of the rows that move (the keep list's, or the sequences' own).
 template <int DIM, bool FP8, bool WRITE>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, WRITE ? 4 : 5)
 cache_rows_kernel(RowsCall c, uint16_t* __restrict__ k, uint16_t* __restrict__ v, const int32_t* __restrict__ cu_seqlens,
                   const int32_t* __restrict__ keep_idx, const int32_t* __restrict__ cu, const int32_t* __restrict__ table,
                   const int32_t* __restrict__ start, int32_t* device_status) {
@@ -183,7 +183,9 @@ cache_rows_kernel(RowsCall c, uint16_t* __restrict__ k, uint16_t* __restrict__ v
   __syncthreads();
 
   // A group of kLanes lanes keeps to one head of K or V and walks over the block's tokens, so that all of an address but the token's row is
-  // known beforehand; with fewer heads than groups several of these share a head's tokens.
+  // known beforehand; with fewer heads than groups several of these share a head's tokens.  (Survivors of 4 x 16,384 tokens, int8, 163 MB: 41.3
+  // us; without the arithmetic 37.  Tried: rows copied into shared memory ahead of their use, 94 us for the ragged batch instead of 65; a
+  // warp per few tokens with eight rows unrolled, 102; the scales gathered in shared memory and written head by head, 48.8.)
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, heads = 2 * c.cache.hkv;
   const int sharing = max(1, kRows / heads), step = min(kRows, heads);
   const bool active = group < sharing * heads;
@@ -240,9 +242,11 @@ cache_rows_kernel(RowsCall c, uint16_t* __restrict__ k, uint16_t* __restrict__ v
 template <bool WRITE>
 cudaError_t launch_rows(RowsCall c, uint16_t* k, uint16_t* v, const int32_t* cu_seqlens, const int32_t* keep_idx, const int32_t* cu, const int32_t* table,
                         const int32_t* start, int32_t* device_status, cudaStream_t stream) {
-  // Few rows: a token per block, so that more SMs take part.  Many: 32 consecutive ones, whose scales fill whole sectors.
+  // Few rows: a token per block, so that more SMs take part.  Many: as many as keep a group of lanes busy for four turns.
+  const int groups = kThreads / (c.cache.dim / 8), sharing = groups > 2 * c.cache.hkv ? groups / (2 * c.cache.hkv) : 1;
+  const int most = 4 * kUnroll * sharing < kMostTokens ? 4 * kUnroll * sharing : kMostTokens;
   c.tokens = 1;
-  while (c.tokens < kMostTokens && c.total_dst / (2 * c.tokens) >= kNumSMs * 2) c.tokens *= 2;
+  while (2 * c.tokens <= most && c.total_dst / (2 * c.tokens) >= kNumSMs * 2) c.tokens *= 2;
   const dim3 grid((unsigned)((c.total_dst + c.tokens - 1) / c.tokens));
   auto go = [&](auto kernel) { return launch_chained(kernel, grid, dim3(kThreads), 0, stream, c, k, v, cu_seqlens, keep_idx, cu, table, start, device_status); };
   count_launches(1);
