@@ -69,7 +69,7 @@ __device__ __forceinline__ int last_upto(const int32_t* a, int n, int x, int lan
 // Bound by latency: a few trips to memory one after the other (the row's sequence; its bounds; the parts' statistics; the parts).  So a lane
 // asks for one part's statistics each, and where rows are few and parts many, WARPS warps share those of a (row, head), eight at a time
 // each (1 x 1,024 keys, 28 heads of up to 32 parts: 7.3 us instead of 24 with a warp that went through them four at a time).  Many rows: a
-// warp takes HEADS heads of a row and finds their jobs in as many lanes (41,000 (row, head): FIGURE_JOIN us instead of 51).
+// warp takes HEADS heads of a row and finds their jobs in as many lanes (41,000 (row, head): 36 us instead of 51).
 template <int DIM, int WARPS, int HEADS>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall c, AttendList own, AttendList shared) {
   static_assert(WARPS == 1 || HEADS == 1);
@@ -249,7 +249,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
     w.fits &= units[i] < INT_MAX;
   }
   // Where both kernels run, they do so side by side, the SMs shared out by what their units cost (one behind the other, each is a start of 6 to 8
-  // us and an end: 32 answers on a shared 16,384-token prefix FIGURE_SEQ us instead of FIGURE_BESIDE).
+  // us and an end: 32 answers on a shared 16,384-token prefix 46.5 us instead of 40.4).
   int sms[2] = {kNumSMs, kNumSMs};
   if (units[0] > 0 && units[1] > 0) {
     const double few = (double)units[0] * kFewUnitCost, many = (double)units[1] * kManyUnitCost;
