@@ -20,46 +20,56 @@ struct Parts {
 // Part i of a row: a job's first block has it in its second place.
 __device__ __forceinline__ int part_of(int tile_rows, const Parts& p, int i) { return ((p.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + p.row; }
 
-// What the rows of an entry have in common.
-struct Found {
-  Entry x;
-  int granules = 0, ahead, total;
-};
-__device__ __forceinline__ Found find_entry(const AttendCall& c, const AttendList& list, int e) {
-  Found f;
-  f.ahead = chain_load_cached(list.ahead + e);  // (asked for together)
-  f.total = chain_load_cached(list.ahead + list.entries());
-  bool bad = false;
-  f.x = entry_of(c, list, e, bad);
-  f.granules = granules_of(list, f.x);
-  return f;
-}
-__device__ __forceinline__ Parts find_parts(const AttendCall& c, const AttendList& list, const Found& f, int row, int head) {
+// Where the parts of one row and head of the entry e lie: x, with `ahead` units before it of `total`.
+__device__ __forceinline__ Parts find_parts(const AttendCall& c, const AttendList& list, const Entry& x, int ahead, int total, int row, int head) {
   Parts p;
-  const int r = row - f.x.row0;
-  if (r < 0 || r >= f.x.rows || f.granules == 0) return p;
+  const int r = row - x.row0, granules = granules_of(list, x);
+  if (r < 0 || r >= x.rows || granules == 0) return p;
   const int kv = head / c.group, i = r * c.group + head - kv * c.group, tile = i / list.tile_rows;
-  const int start = f.ahead + (kv * tiles_of(c, list, f.x) + tile) * (list.job_cost + f.granules) + list.job_cost;
-  if (start < 0 || start + f.granules > f.total) return p;  // (the arrays changed meanwhile)
-  const int workers = workers_of(list, f.total);
+  const int start = ahead + (kv * tiles_of(c, list, x) + tile) * (list.job_cost + granules) + list.job_cost;
+  if (start < 0 || start + granules > total) return p;  // (the arrays changed meanwhile)
+  const int workers = workers_of(list, total);
   p.row = i - tile * list.tile_rows;
-  p.first = worker_of(start, workers, f.total);
-  p.count = worker_of(start + f.granules - 1, workers, f.total) - p.first + 1;
+  p.first = worker_of(start, workers, total);
+  p.count = worker_of(start + granules - 1, workers, total) - p.first + 1;
   p.whole = p.count == 1;
   return p;
 }
 
 // The last of n ascending numbers that is at most x (0 if none is); the whole warp, 32 looks at a time.
+template <bool CACHED>
 __device__ __forceinline__ int last_upto(const int32_t* a, int n, int x, int lane) {
   int lo = 0;
   while (n > 1) {
     const int step = (n + 31) / 32;
-    const unsigned upto = __ballot_sync(0xFFFFFFFFu, lane * step < n && chain_load_cached(a + lo + min(lane * step, n - 1)) <= x);
+    const unsigned upto = __ballot_sync(0xFFFFFFFFu, lane * step < n && index_load(a + lo + min(lane * step, n - 1), CACHED) <= x);
     const int k = upto ? 31 - __clz(upto) : 0;
     lo += k * step;
     n = min(step, n - k * step);
   }
   return lo;
+}
+
+// What a row belongs to: sequence b, and prefix a (-1: none) at the levels.
+struct Belongs {
+  int b, a;
+  bool somebody;
+  Entry x[2];
+};
+template <bool CACHED>
+__device__ __forceinline__ Belongs belongs_to(const AttendCall& c, const AttendList& own, const AttendList& shared, int row, int lane) {
+  Belongs f;
+  bool bad = false;  // (reported by open_list)
+  f.b = last_upto<CACHED>(c.cu_qlens, c.batch, row, lane);
+  f.somebody = row >= index_load(c.cu_qlens + f.b, CACHED) && row < index_load(c.cu_qlens + f.b + 1, CACHED);
+  f.x[0] = entry_of(c, own, own.from_prefix + f.b, bad, CACHED);
+  f.a = -1;
+  if (c.prefixes > 0) {
+    const int a = last_upto<CACHED>(c.cu_prefix, c.prefixes, f.b, lane);
+    if (f.b >= index_load(c.cu_prefix + a, CACHED) && f.b < index_load(c.cu_prefix + a + 1, CACHED)) f.a = a;
+    f.x[1] = entry_of(c, shared, a, bad, CACHED);
+  }
+  return f;
 }
 
 // Joins what the levels' blocks left.  With m the largest of the parts' maxima,
@@ -76,23 +86,28 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
   constexpr int kEach = DIM / 32, kHeads = kJoinWarps / WARPS * HEADS, kAtOnce = WARPS > 1 ? 8 : 2;
   __shared__ float part_acc[WARPS > 1 ? kJoinWarps : 1][DIM];
   __shared__ float2 part_ml[kJoinWarps];
+  __shared__ Belongs f;  // a block has one row
   chain_enter(c);
-  pdl_wait();
+  // Where all blocks are there at once, this is looked up while the kernel before still runs.
+  constexpr bool kEarly = HEADS == 1;
+  if (!kEarly) pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % WARPS;
   const int head_blocks = (c.hq + kHeads - 1) / kHeads, row = blockIdx.x / head_blocks, head0 = (blockIdx.x - row * head_blocks) * kHeads + warp / WARPS * HEADS;
-  const int b = last_upto(c.cu_qlens, c.batch, row, lane);
-  if (row < chain_load_cached(c.cu_qlens + b) || row >= chain_load_cached(c.cu_qlens + b + 1)) return;  // nobody's row (the whole block's answer)
+  if (warp == 0) {
+    const Belongs mine = belongs_to<!kEarly>(c, own, shared, row, lane);
+    if (lane == 0) f = mine;
+  }
+  __syncthreads();
+  if (kEarly) pdl_wait();
+  if (!f.somebody) return;
   Parts found[2];  // of head head0 + lane
   const int lane_head = head0 + lane;
   const bool lane_there = lane < HEADS && lane_head < c.hq;
-  const Found f = find_entry(c, own, own.from_prefix + b);
-  if (lane_there) found[0] = find_parts(c, own, f, row, lane_head);
-  if (c.prefixes > 0) {
-    const int a = last_upto(c.cu_prefix, c.prefixes, b, lane);
-    if (b >= chain_load_cached(c.cu_prefix + a) && b < chain_load_cached(c.cu_prefix + a + 1)) {
-      const Found g = find_entry(c, shared, a);
-      if (lane_there) found[1] = find_parts(c, shared, g, row, lane_head);
-    }
+  const int own_ahead = chain_load_cached(own.ahead + own.from_prefix + f.b), own_total = chain_load_cached(own.ahead + own.entries());
+  const int shared_ahead = f.a >= 0 ? chain_load_cached(shared.ahead + f.a) : 0, shared_total = f.a >= 0 ? chain_load_cached(shared.ahead + shared.entries()) : 0;
+  if (lane_there) {
+    found[0] = find_parts(c, own, f.x[0], own_ahead, own_total, row, lane_head);
+    if (f.a >= 0) found[1] = find_parts(c, shared, f.x[1], shared_ahead, shared_total, row, lane_head);
   }
 #pragma unroll 1
   for (int h = 0; h < HEADS; ++h) {

@@ -70,25 +70,27 @@ struct Entry {
   const int32_t* table;
   bool own;
 };
-__device__ __forceinline__ Entry entry_of(const AttendCall& c, const AttendList& list, int e, bool& bad) {
+// Reads of index arrays: after the kernel's wait through L1, ahead of it through L2.
+__device__ __forceinline__ int index_load(const int32_t* p, bool cached) { return cached ? chain_load_cached(p) : chain_load(p); }
+__device__ __forceinline__ Entry entry_of(const AttendCall& c, const AttendList& list, int e, bool& bad, bool cached = true) {
   Entry x;
   x.own = e >= list.from_prefix;
   if (x.own) {
     const int b = e - list.from_prefix;
-    const Span rows = checked_span<true>(c.cu_qlens, b, c.total_q, c.max_qlen);
+    const Span rows = checked_words(index_load(c.cu_qlens + b, cached), index_load(c.cu_qlens + b + 1, cached), c.total_q, c.max_qlen);
     x.row0 = rows.first;
     x.rows = rows.count;
-    x.len = chain_load_cached(c.lens + b);
+    x.len = index_load(c.lens + b, cached);
     x.table = c.table + (long long)b * c.table_stride;
     bad |= rows.bad;
   } else {
-    const int from = chain_load_cached(c.cu_prefix + e), to = chain_load_cached(c.cu_prefix + e + 1);
+    const int from = index_load(c.cu_prefix + e, cached), to = index_load(c.cu_prefix + e + 1, cached);
     const bool fits = from >= 0 && from <= to && to <= c.batch;
-    const Span rows = fits ? checked_words(chain_load_cached(c.cu_qlens + from), chain_load_cached(c.cu_qlens + to), c.total_q, c.max_prefix_q)
+    const Span rows = fits ? checked_words(index_load(c.cu_qlens + from, cached), index_load(c.cu_qlens + to, cached), c.total_q, c.max_prefix_q)
                            : Span{0, 0, true};
     x.row0 = rows.first;
     x.rows = rows.count;
-    x.len = chain_load_cached(c.prefix_lens + e);
+    x.len = index_load(c.prefix_lens + e, cached);
     x.table = c.prefix_table + (long long)e * c.prefix_stride;
     bad |= rows.bad;
   }
@@ -132,7 +134,7 @@ __device__ int open_list(const AttendCall& c, const AttendList& list, int* ahead
 #pragma unroll 1
   for (int e = e0; e < e1; ++e) {
     ahead[e] = sum;
-    sum += units_of(c, list, entry_of(c, list, e, bad));
+    sum += units_of(c, list, entry_of(c, list, e, bad, c.head_wait));
   }
   int upto = sum;
 #pragma unroll
