@@ -36,6 +36,15 @@ __device__ __forceinline__ Parts find_parts(const AttendCall& c, const AttendLis
   return p;
 }
 
+__device__ __forceinline__ Parts from_lane(const Parts& mine, int lane) {
+  Parts p;
+  p.first = __shfl_sync(0xFFFFFFFFu, mine.first, lane);
+  p.count = __shfl_sync(0xFFFFFFFFu, mine.count, lane);
+  p.row = __shfl_sync(0xFFFFFFFFu, mine.row, lane);
+  p.whole = p.count == 1;
+  return p;
+}
+
 // The last of n ascending numbers that is at most x (0 if none is); the whole warp, 32 looks at a time.
 template <bool CACHED>
 __device__ __forceinline__ int last_upto(const int32_t* a, int n, int x, int lane) {
@@ -115,54 +124,54 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
     const bool there = head < c.hq, done = c.prefixes == 0 && __shfl_sync(0xFFFFFFFFu, found[0].whole, h);
     const long long flat = (long long)row * c.hq + head, flats = (long long)c.total_q * c.hq;
     float top = -INFINITY, acc[kEach] = {}, sum = 0.f;
+    // The parts of both levels are one list, own first.
+    const Parts p0 = from_lane(found[0], h), p1 = from_lane(found[1], h);
+    const int parts_all = done ? 0 : p0.count + p1.count;
 #pragma unroll 1
-    for (int l = 0; l < (c.prefixes > 0 ? 2 : 1); ++l) {  // (a loop: what runs once costs its length)
+    for (int i0 = 0; i0 < parts_all; i0 += 32 * WARPS) {  // a lane's part: WARPS lane + sub
+      const int mine = i0 + lane * WARPS + sub;
+      const bool is_shared = mine >= p0.count;
+      const bool whole = is_shared ? p1.whole : p0.whole;
       Parts p;
-      p.first = __shfl_sync(0xFFFFFFFFu, l ? found[1].first : found[0].first, h);
-      p.count = __shfl_sync(0xFFFFFFFFu, l ? found[1].count : found[0].count, h);
-      p.row = __shfl_sync(0xFFFFFFFFu, l ? found[1].row : found[0].row, h);
-      p.whole = p.count == 1;
-      const int tile_rows = l ? shared.tile_rows : own.tile_rows;
-      const float2* const stats = p.whole ? c.whole_ml + l * flats + flat : l ? shared.part_ml : own.part_ml;
-      const float* const outs = (p.whole ? c.whole_out + (l * flats + flat) * DIM : l ? shared.part_out : own.part_out) + lane * kEach;
-      for (int i0 = 0; !done && i0 < p.count; i0 += 32 * WARPS) {  // a lane's part: WARPS lane + sub
-        const int mine = i0 + lane * WARPS + sub;
-        const int at = p.whole ? 0 : part_of(tile_rows, p, mine);
-        const float2 ml = mine < p.count ? chain_load(stats + at) : make_float2(-INFINITY, 0.f);
-        float to = ml.x;
+      p.first = is_shared ? p1.first : p0.first;
+      p.row = is_shared ? p1.row : p0.row;
+      const long long at = whole ? (is_shared ? flats : 0) + flat
+                                 : part_of(is_shared ? shared.tile_rows : own.tile_rows, p, mine - (is_shared ? p0.count : 0));
+      const float2 ml = mine < parts_all ? chain_load((whole ? c.whole_ml : is_shared ? shared.part_ml : own.part_ml) + at) : make_float2(-INFINITY, 0.f);
+      const float* const outs = (whole ? c.whole_out : is_shared ? shared.part_out : own.part_out) + at * DIM;
+      float to = ml.x;
 #pragma unroll
-        for (int d = 16; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, d));
-        to = fmaxf(to, top);
-        const float base = to == -INFINITY ? 0.f : to, before = exp2f(top - base), weight = exp2f(ml.x - base);
-        top = to;
-        sum = sum * before + weight * ml.y;  // (a lane's own; added up below)
+      for (int d = 16; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, d));
+      to = fmaxf(to, top);
+      const float base = to == -INFINITY ? 0.f : to, before = exp2f(top - base), weight = exp2f(ml.x - base);
+      top = to;
+      sum = sum * before + weight * ml.y;  // (a lane's own; added up below)
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) acc[e] *= before;
-        const int parts = min(32, (p.count - i0 - sub + WARPS - 1) / WARPS);  // of this warp
-        for (int j0 = 0; j0 < parts; j0 += kAtOnce) {
-          float v[kAtOnce][kEach];
+      for (int e = 0; e < kEach; ++e) acc[e] *= before;
+      const int parts = min(32, (parts_all - i0 - sub + WARPS - 1) / WARPS);  // of this warp
+      for (int j0 = 0; j0 < parts; j0 += kAtOnce) {
+        float v[kAtOnce][kEach];
 #pragma unroll
-          for (int j = 0; j < kAtOnce; ++j) {
-            const int from = __shfl_sync(0xFFFFFFFFu, at, (j0 + j) & 31);
+        for (int j = 0; j < kAtOnce; ++j) {
+          const float* const from = reinterpret_cast<const float*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(outs), (j0 + j) & 31)) + lane * kEach;
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) v[j][e] = 0.f;
-            if (j0 + j < parts) {
-              if (kEach == 4) {
-                const float4 x = chain_load(reinterpret_cast<const float4*>(outs + (long long)from * DIM));
-                v[j][0] = x.x; v[j][1] = x.y; v[j][2 % kEach] = x.z; v[j][3 % kEach] = x.w;
-              } else {
-                const float2 x = chain_load(reinterpret_cast<const float2*>(outs + (long long)from * DIM));
-                v[j][0] = x.x; v[j][1] = x.y;
-              }
+          for (int e = 0; e < kEach; ++e) v[j][e] = 0.f;
+          if (j0 + j < parts) {
+            if (kEach == 4) {
+              const float4 x = chain_load(reinterpret_cast<const float4*>(from));
+              v[j][0] = x.x; v[j][1] = x.y; v[j][2 % kEach] = x.z; v[j][3 % kEach] = x.w;
+            } else {
+              const float2 x = chain_load(reinterpret_cast<const float2*>(from));
+              v[j][0] = x.x; v[j][1] = x.y;
             }
           }
+        }
 #pragma unroll
-          for (int j = 0; j < kAtOnce; ++j) {
-            const float w = __shfl_sync(0xFFFFFFFFu, weight, (j0 + j) & 31);
-            if (j0 + j < parts)
+        for (int j = 0; j < kAtOnce; ++j) {
+          const float w = __shfl_sync(0xFFFFFFFFu, weight, (j0 + j) & 31);
+          if (j0 + j < parts)
 #pragma unroll
-              for (int e = 0; e < kEach; ++e) acc[e] = fmaf(w, v[j][e], acc[e]);
-          }
+            for (int e = 0; e < kEach; ++e) acc[e] = fmaf(w, v[j][e], acc[e]);
         }
       }
     }
