@@ -220,10 +220,11 @@ cudaError_t launch_join(const AttendCall& c, const AttendList& own, const Attend
 }
 template <int DIM>
 cudaError_t launch_join(const AttendCall& c, const AttendList& own, const AttendList& shared, cudaStream_t stream) {
-  // As many warps per row and head as are resident at once (two blocks an SM); many rows: several heads per warp.
+  // As many warps per row and head as are resident at once (two blocks an SM; two warps: four blocks, 64 answers on a shared prefix 43.1 us
+  // instead of 45.1; four warps were no quicker than two); many rows: several heads per warp.
   const long long flats = (long long)c.total_q * c.hq, room = kNumSMs * 2 * kJoinWarps;
   if (flats * 8 <= room) return launch_join<DIM, 8, 1>(c, own, shared, stream);
-  if (flats * 2 <= room) return launch_join<DIM, 2, 1>(c, own, shared, stream);
+  if (flats <= room) return launch_join<DIM, 2, 1>(c, own, shared, stream);
   return flats <= 4 * room ? launch_join<DIM, 1, 1>(c, own, shared, stream) : launch_join<DIM, 1, 4>(c, own, shared, stream);
 }
 

@@ -77,9 +77,12 @@ attend_few_kernel(AttendCall c, AttendList list) {
   float* const scratch = list.scratch + (long long)blockIdx.x * kWarps * kTile * DIM;  // a warp's first part
   if (lane < 2) left[warp][lane].job_first = -1;
   chain_enter_late(c);
+  if (c.beside) {
+    pdl_wait();
+    pdl_trigger();  // the kernel for many rows starts beside this one; that earlier work has ended holds for it, too
+  }
   const int total = open_list<kThreads>(c, list, ahead, warp_sum);
   pdl_wait();  // the rest may be what earlier work wrote
-  if (c.beside) pdl_trigger();  // the kernel for many rows starts beside this one; that earlier work has ended holds for it, too
   leave_list<kThreads>(list, ahead);
   const int workers = workers_of(list, total), block_u0 = run_start(min((int)blockIdx.x, workers), workers, total);
   const int block_u1 = run_start(min((int)blockIdx.x + 1, workers), workers, total);
