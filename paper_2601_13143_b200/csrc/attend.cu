@@ -237,7 +237,7 @@ constexpr double kFewUnitCost = 0.13, kManyUnitCost = 2.2;  // us of an SM
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
   bool own_many, shared_many;
-  size_t ahead[2], out[2], ml[2], scratch, whole_out, whole_ml, total = 0;  // offsets into the workspace: few, many
+  size_t ahead[2], out[2], ml[2], scratch, copies, whole_out, whole_ml, total = 0;  // offsets into the workspace: few, many
   bool fits = true;
 };
 
@@ -289,6 +289,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
     w.out[i] = carve(parts * cache.head_dim * sizeof(float));
     w.ml[i] = carve(parts * sizeof(float2));
   }
+  w.copies = carve(w.many.entries() > kManyListed ? (size_t)w.many.grid * (w.many.entries() + 1) * sizeof(int32_t) : 0);
   w.scratch = carve(w.few.entries() > 0 ? few_scratch_floats(w.few, cache.head_dim) * sizeof(float) : 0);
   const size_t rows = p.num_prefixes > 0 ? (size_t)2 * p.total_q * p.num_q_heads : 0;
   w.whole_out = carve(rows * cache.head_dim * sizeof(float));
@@ -366,6 +367,7 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
     lists[i].part_ml = reinterpret_cast<float2*>(ws + w.ml[i]);
   }
   lists[0].scratch = reinterpret_cast<float*>(ws + w.scratch);
+  lists[1].copies = reinterpret_cast<int32_t*>(ws + w.copies);
   const AttendList &own = lists[w.own_many], &shared = lists[w.shared_many];
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;

@@ -48,6 +48,7 @@ struct AttendList {
   float* part_out;           // [grid][2][tile_rows][dim]
   float2* part_ml;           // [grid][2][tile_rows]: running maximum (base 2), sum
   float* scratch;            // few: parts that warps of one block exchange
+  int32_t* copies;           // many: the blocks' own `ahead`, where there are more entries than shared memory has room for
   __host__ __device__ int entries() const { return from_prefix + from_own; }
 };
 
@@ -57,7 +58,7 @@ size_t few_scratch_floats(const AttendList& list, int dim);
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 // Many: tcgen05, a granule per step of a block (attend_many.cu).
-constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4;
+constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4, kManyListed = 3000;  // (entries whose `ahead` is in shared memory)
 cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 #ifdef __CUDACC__

@@ -6,8 +6,10 @@
 //   warps 0-7    softmax, a thread per row.  Warps 0-3 and 4-7 are two STREAMS with an S, an O and two P of their own.  With more than 128
 //                rows the streams are the two halves of the rows and share every key; with fewer they take 64 keys of every tile each and
 //                their sums are joined at the end.  A VISIT is 64 keys of a stream.
-//   warps 8-15   codes -> f16, 16 keys of every tile each: straight from global memory (one tile ahead in registers) to the operand
-//                tiles in shared memory
+//   warps 8-15   codes -> f16, 16 keys of every tile each, to the operand tiles in shared memory.  What a tile ahead is asked for stays in
+//                flight: K's codes in 16 KB of shared memory (asynchronous copies), V's in registers, and V's rows are called into L2 when
+//                K's are.  (Both in registers: each was asked for only half a tile ahead, 2.4 us a tile from HBM instead of 1.65;
+//                16 sequences of 3,000 keys, 64 rows: 71 us instead of 60.)
 //   warps 16-19  issue the MMAs: the S of a stream's next visit as soon as the logits of this one are in registers, PV when its weights are
 //                there
 //
@@ -50,6 +52,7 @@ struct Many {
   static constexpr int kHalfBytes = 128 * 128;           // 128 rows of 128 bytes
   static constexpr int kTileBytes = kHalves * kHalfBytes;
   static constexpr int kOperands = 6 * kTileBytes;       // Q twice, K twice, V twice
+  static constexpr int kCodes = kManyKeys * DIM;         // K's codes of the tile after
 };
 
 struct Control {
@@ -125,14 +128,15 @@ __device__ __forceinline__ void convert_piece(const uint4& x, uint32_t at, uint3
 }
 
 template <int DIM, bool FP8>
-__device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t k_tiles, uint32_t v_tiles, int u0,
-                                             int u1, int warp, int lane) {
+__device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendList& list, const int* ahead, Control& ctl, uint32_t k_tiles, uint32_t v_tiles, uint32_t codes_at,
+                                             int u0, int u1, int warp, int lane) {
   using P = Piece<DIM>;
   const P mine(warp, lane);
   Walk at;
   at.seek(c, list, ahead, u0);
   if (at.unit >= u1) return;
-  uint4 k[P::kLoads], v[P::kLoads];
+  uint4 v[P::kLoads];
+  const uint32_t my_codes = codes_at + warp * P::kLoads * 512 + lane * 16;  // of K: what a lane copies there is what it reads
   float ks = 0.f, vs = 0.f;  // of key `lane` of this warp's 16
   int pool = 0;              // row of the pool of the first of them
   int have = 0;              // how many exist
@@ -156,13 +160,19 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
 #pragma unroll
     for (int j = 0; j < P::kLoads; ++j) to[j] = chain_load(reinterpret_cast<const uint4*>(from + j * P::kRows * DIM));
   };
+  auto copy_keys = [&] {
+    const uint8_t* const from = c.cache.k + (long long)pool * DIM + mine.row * DIM + mine.piece * 16;
+#pragma unroll
+    for (int j = 0; j < P::kLoads; ++j) ptx::copy_async<16>(my_codes + j * 512, from + j * P::kRows * DIM);
+    ptx::copies_commit();
+  };
   auto ask_scales = [&] {
     ks = lane < have ? chain_load(c.cache.k_scale + pool + lane) : 0.f;
     vs = lane < have ? chain_load(c.cache.v_scale + pool + lane) : 0.f;
   };
   find_page();
   find_keys();
-  ask(c.cache.k, k);
+  copy_keys();
   ask_scales();
   ask(c.cache.v, v);
   bool more = at.step(c, list, ahead, u1);
@@ -187,9 +197,10 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
       ctl.exponent[ring][warp] = (float)e;
       ctl.unscale[ring][warp] = __uint_as_float((unsigned)(127 - e - kOffset) << 23);
     }
+    ptx::copies_wait<0>();
 #pragma unroll
     for (int j = 0; j < P::kLoads; ++j)
-      convert_piece<FP8, false>(k[j], k_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, 0);
+      convert_piece<FP8, false>(ptx::ld_shared4(my_codes + j * 512), k_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, 0);
     ptx::fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
@@ -198,8 +209,9 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     }
     if (more) {
       find_keys();
-      ask(c.cache.k, k);
+      copy_keys();
       ask_scales();
+      if (lane < 16) ptx::prefetch_l2(c.cache.v + (long long)(pool + lane) * DIM);
     }
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.v_empty[slot]), free_parity, &ctl.abort);
     if (exist < 16)
@@ -543,7 +555,8 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
   }
 }
 
-template <int DIM, bool FP8>
+// LISTED: the list's entries have room in shared memory (all others go through global memory: 500 -> 511 us with the choice made at run time).
+template <int DIM, bool FP8, bool LISTED>
 __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, AttendList list) {
   using M = Many<DIM>;
   extern __shared__ unsigned char smem_raw[];
@@ -551,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned char* const smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t q_tiles = ptx::smem_u32(smem), k_tiles = q_tiles + 2 * M::kTileBytes, v_tiles = k_tiles + 2 * M::kTileBytes;
-  int* const ahead = reinterpret_cast<int*>(smem + M::kOperands);
+  int* const ahead = LISTED ? reinterpret_cast<int*>(smem + M::kOperands + M::kCodes) : list.copies + (long long)blockIdx.x * (list.entries() + 1);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.k_full[i]), kConvWarps);
@@ -572,6 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     ptx::fence_barrier_init();
   }
   chain_enter_late(c);
+  if (!LISTED && !c.beside) pdl_wait();  // (earlier work may still read what lies there)
   const int total = open_list<kThreads>(c, list, ahead, ctl.warp_sum);
   if (!c.beside) pdl_wait();  // the rest may be what earlier work wrote; and tensor memory is taken when all earlier work has ended
   leave_list<kThreads>(list, ahead);
@@ -588,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     if (u0 < u1) softmax<DIM>(c, list, ahead, ctl, q_tiles, u0, u1, warp, lane);
   } else if (warp < kIssueWarp) {
     ptx::fewer_registers<kConvRegs>();
-    if (u0 < u1) convert_keys<DIM, FP8>(c, list, ahead, ctl, k_tiles, v_tiles, u0, u1, warp - kSoftWarps, lane);
+    if (u0 < u1) convert_keys<DIM, FP8>(c, list, ahead, ctl, k_tiles, v_tiles, v_tiles + 2 * M::kTileBytes, u0, u1, warp - kSoftWarps, lane);
   } else {
     ptx::fewer_registers<kIssueRegs>();
     if (u0 < u1 && warp < kIssueWarp + 2) issue_mmas<DIM, true>(c, list, ahead, ctl, q_tiles, k_tiles, v_tiles, u0, u1, warp & 1);
@@ -604,27 +618,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
 }
 
 template <int DIM>
-size_t many_smem(int entries) { return 1024 + Many<DIM>::kOperands + (size_t)(entries + 1) * 4; }
+size_t many_smem(int entries) { return 1024 + Many<DIM>::kOperands + Many<DIM>::kCodes + (entries <= kManyListed ? (size_t)(entries + 1) * 4 : 0); }
 
-template <int DIM, bool FP8>
+template <int DIM, bool FP8, bool LISTED>
 cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
   const cudaError_t e = once_per_context([] {
     cudaFuncAttributes a;
-    const cudaError_t got = cudaFuncGetAttributes(&a, attend_many_kernel<DIM, FP8>);
+    const cudaError_t got = cudaFuncGetAttributes(&a, attend_many_kernel<DIM, FP8, LISTED>);
     if (got != cudaSuccess) return got;
     if (a.numRegs * kThreads < kRegsNeeded) return cudaErrorInvalidConfiguration;  // the softmax's warps would wait for registers for ever
-    return cudaFuncSetAttribute(attend_many_kernel<DIM, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many_smem<DIM>(FASTAV_ATTEND_MAX_BATCH));
+    return cudaFuncSetAttribute(attend_many_kernel<DIM, FP8, LISTED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many_smem<DIM>(kManyListed));
   });
   if (e != cudaSuccess) return e;
   count_launches(1);
-  return launch_chained(attend_many_kernel<DIM, FP8>, dim3(list.grid), dim3(kThreads), many_smem<DIM>(list.entries()), stream, c, list);
+  return launch_chained(attend_many_kernel<DIM, FP8, LISTED>, dim3(list.grid), dim3(kThreads), many_smem<DIM>(list.entries()), stream, c, list);
+}
+
+template <bool LISTED>
+cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
+  if (c.cache.dim == 128) return c.cache.fp8 ? run<128, true, LISTED>(c, list, stream) : run<128, false, LISTED>(c, list, stream);
+  return c.cache.fp8 ? run<64, true, LISTED>(c, list, stream) : run<64, false, LISTED>(c, list, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
-  if (c.cache.dim == 128) return c.cache.fp8 ? run<128, true>(c, list, stream) : run<128, false>(c, list, stream);
-  return c.cache.fp8 ? run<64, true>(c, list, stream) : run<64, false>(c, list, stream);
+  return list.entries() <= kManyListed ? run<true>(c, list, stream) : run<false>(c, list, stream);
 }
 
 }  // namespace fastav

@@ -289,6 +289,15 @@ def test_the_largest_batch():
     p.check()
 
 
+@pytest.mark.parametrize("entries", [2998, 3002])
+def test_many_rows_of_more_sequences_than_a_block_lists_in_shared_memory(entries):
+    """Two rows of 32 heads on one KV head each; up to 3,000 entries are listed in shared memory."""
+    lens, rows = [i % 9 for i in range(entries - 1)], [2] * (entries - 1)
+    p = Problem(32, 1, 64, "fp8", 16, lens, rows, prefix_lens=[5], groups=[3, 2001], seed=15)
+    p.run()
+    p.check()
+
+
 MIXES = [  # few rows only, many rows only, both side by side, short ones, many partial results
     dict(hq=28, hkv=4, dim=128, fmt="int8", page=64, lens=[3000, 40], rows=[1, 1]),
     dict(hq=16, hkv=4, dim=128, fmt="fp8", page=32, lens=[700, 300], rows=[40, 64]),
