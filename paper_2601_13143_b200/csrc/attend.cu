@@ -228,11 +228,12 @@ cudaError_t launch_join(const AttendCall& c, const AttendList& own, const Attend
   return flats <= 4 * room ? launch_join<DIM, 1, 1>(c, own, shared, stream) : launch_join<DIM, 1, 4>(c, own, shared, stream);
 }
 
-// The levels' entries go to the kernel that suits their stacked rows: few (mma.sync) up to 16, which it takes at once, many (tcgen05) beyond 48;
-// in between many as long as there are four of its units for every SM.  us, few / many: 28 rows, 8 x 3,000 keys of 4 heads 35.5 / 30.6, 32
-// sequences 76 / 70, one of 4,000 22.6 / 31.3, four prefixes of 3,000 32 / 36; 64 rows, 16 x 3,000 keys of 8 heads 132 / 73, 16 x 300 42.5 / 29.5.
-constexpr int kLeastMany = 17, kMostFew = 48, kManyUnits = 4 * kNumSMs;
-constexpr double kFewUnitCost = 0.13, kManyUnitCost = 2.2;  // us of an SM
+// The levels' entries go to the kernel that suits their stacked rows: few (mma.sync) up to 16, which an instruction pair takes at once, many (tcgen05)
+// beyond.  us, few / many: one sequence of 60 keys of 8 heads, 48 rows 15.3 / 13.5, of 1,000, 24 rows 17.9 / 16.0; 28 rows on 4 heads: 4,000 keys
+// 19.8 / 17.5, 8 x 3,000 keys 35.5 / 26.3, a prefix of 4,000 for seven rows each of four sequences with few rows of their own 21.2 / 22.5;
+// 8 sequences of 500 to 744 keys, up to 32 rows on 2 heads of 64, 14.4 / 14.9; 16 rows of 8 heads, 16 x 2,000 keys 39.3 / 43.3, one of 4,000 19.9 / 18.7.
+constexpr int kMostFew = 16;
+constexpr double kFewUnitCost = 0.13, kManyUnitCost = 1.7;  // us of an SM (many at 1.2 / 1.7 / 2.2 / 3: 32 answers 37.7 / 37.5 / 38.9 / 42.8, 64 44.4 / 42.0 / 42.2 / 40.5)
 
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
@@ -257,11 +258,9 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   w.many.unit_keys = kManyKeys;
   w.few.job_cost = kFewJobCost;
   w.many.job_cost = kManyJobCost;
-  auto takes_many = [&](long long entries, long long rows, long long len) {
-    return rows * group > kMostFew || (rows * group >= kLeastMany && most_units(p, cache, w.many, entries, rows, len) >= kManyUnits);
-  };
-  w.own_many = takes_many(p.batch, p.max_qlen, p.max_kv_len);
-  w.shared_many = p.num_prefixes > 0 && takes_many(p.num_prefixes, p.max_prefix_q, p.max_prefix_len);
+  auto takes_many = [&](long long rows) { return rows * group > kMostFew; };
+  w.own_many = takes_many(p.max_qlen);
+  w.shared_many = p.num_prefixes > 0 && takes_many(p.max_prefix_q);
   const long long own_rows = w.own_many ? 0 : p.max_qlen * group, shared_rows = w.shared_many ? 0 : p.max_prefix_q * group;
   w.few.tile_rows = std::max(own_rows, shared_rows) <= 8 ? 8 : 16;
   (w.own_many ? w.many : w.few).from_own = p.batch;
@@ -274,7 +273,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
     w.fits &= units[i] < INT_MAX;
   }
   // Where both kernels run, they do so side by side, the SMs shared out by what their units cost (one behind the other, each is a start of 6 to 8
-  // us and an end: 32 answers on a shared 16,384-token prefix 46.5 us instead of 40.4).
+  // us and an end: 32 answers on a shared 16,384-token prefix 46.5 us instead of 40.4; 37.5 since).
   int sms[2] = {kNumSMs, kNumSMs};
   if (units[0] > 0 && units[1] > 0) {
     const double few = (double)units[0] * kFewUnitCost, many = (double)units[1] * kManyUnitCost;
