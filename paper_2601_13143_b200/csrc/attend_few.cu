@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache for few query rows per KV head: decoding, drafted tokens, and short questions.
+// Attention over the 8-bit cache for few query rows per KV head (up to 16): decoding, a few drafted tokens.
 //
 // Bound by reading the cache once from HBM.  A unit is 32 keys of one KV head; every warp takes an equal run of the call's units, and has a
 // ring of its own that it fills itself (no barrier between warps until the end).  mma.sync (f16, fp32 sums) with the keys as
@@ -14,8 +14,8 @@
 // copies of all lanes; with TMA, four copies of one lane per unit, the issuing took a warp 900 of 4,000 cycles.
 //
 // The query rows as the rows of the instructions (half of each empty with 8 rows, 243 registers, 8 warps): 4 x 16,384 keys 48.9 us
-// instead of 46.2 at that step.  Now: 37.4 us (138 MB, 3.7 TB/s; the loop about half of that time, at the copy's rate, the start of a block, its
-// warps' join and the join kernel the rest), 32 sequences of 512 to 4,096 keys 29.4 us (83 MB).
+// instead of 46.2 at that step.  Now: 36.6 us (138 MB, 3.8 TB/s; the loop about half of that time, at the copy's rate, the start of a block, its
+// warps' join and the join kernel the rest), 32 sequences of 512 to 4,096 keys 28.5 us (83 MB).
 #include <limits.h>
 
 #include "attend.cuh"

