@@ -44,4 +44,24 @@ __device__ __forceinline__ float to_one(float magnitude) {
 // 1 / x of a power of two that to_one gives (times a small one).
 __device__ __forceinline__ float inverse_power(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
 
+// A query row as f16.  It is multiplied by a power of two that lays its largest magnitude on 2^15 .. 2^16 (bf16's largest mantissa there is
+// 65,280; f16 ends at 65,504).  Elements of 2^-32 of the largest and more are exact then; f16's last step being 2^-24, smaller ones are off by at
+// most 2^-40 of it.  (Laid on 1 .. 2, those below 2^-17 lost bits, and that showed wherever no key answers the largest element.)
+//
+// A logit is (sum of query and code) * (the key's scale 2^-kLogitBits) * (softmax scale 2^kLogitBits / the power of two): the first two factors stay
+// below 2^127 for every scale that a bf16 row can have.
+constexpr int kQueryBits = 15, kLogitBits = 24;
+constexpr float kKeyScaleFactor = 1.f / (1 << kLogitBits);
+
+// ... that power of two, for the largest magnitude's bf16 bits (1 where it is 0 or not finite).
+__device__ __forceinline__ float query_power(unsigned top) {
+  const int e = (int)(top >> 7);
+  return top == 0 || e == 255 ? 1.f : __uint_as_float((unsigned)min(254 + kQueryBits - e, 253) << 23);
+}
+// ... and what takes it back, times the softmax scale (base 2): never 0, or a hidden key's -inf times it would not be -inf.
+__device__ __forceinline__ float query_scale(float scale_log2, float power) {
+  const int e = 254 + kLogitBits - (int)(__float_as_uint(power) >> 23);
+  return fmaxf(scale_log2 * __uint_as_float((unsigned)min(e, 254) << 23), 1.4e-45f);
+}
+
 }  // namespace fastav

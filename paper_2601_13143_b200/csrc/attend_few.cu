@@ -3,8 +3,8 @@
 // Bound by reading the cache once from HBM.  A unit is 32 keys of one KV head; every warp takes an equal run of the call's units, and has a
 // ring of its own that it fills itself (no barrier between warps until the end).  mma.sync (f16, fp32 sums) with the keys as
 // the rows: S^T = K Q^T, softmax in registers, O^T += V^T P^T, so that up to eight stacked query rows fill an instruction (sixteen: two, on the
-// same operands from the cache).  Codes become f16 exactly on their way from shared memory; a query row is scaled by a power of two first,
-// so that bf16 values are exact in f16 too; the keys' scales multiply the logits, the values' scales the weights.  The weights
+// same operands from the cache).  Codes become f16 exactly on their way from shared memory; a query row is scaled by a power of two first
+// and exact in f16 down to 2^-32 of its largest element (query_power); the keys' scales multiply the logits, the values' scales the weights.  The weights
 // 2^(z - m) vs are rounded to f16 (11 bits; the output has 8) after another power of two per row.  Running maxima move only when a logit
 // is 2^8 above them, so that the sums are hardly ever rescaled.
 //
@@ -176,7 +176,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
           top = max(top >> 16, top & 0xFFFFu);
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
           top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-          const float to = to_one(__uint_as_float(top << 16));
+          const float to = query_power(top);
 #pragma unroll
           for (int s = 0; s < kSteps; ++s)
 #pragma unroll
@@ -189,7 +189,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
           all_see = g == 0 ? least : min(all_see, least);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {  // of row n8 -> of rows 2 t4 + e
-            row_scale[g][e] = c.scale_log2 * inverse_power(__shfl_sync(0xFFFFFFFFu, to, 4 * (2 * t4 + e)));
+            row_scale[g][e] = query_scale(c.scale_log2, __shfl_sync(0xFFFFFFFFu, to, 4 * (2 * t4 + e)));
             sees[g][e] = __shfl_sync(0xFFFFFFFFu, own_sees, 4 * (2 * t4 + e));
             m[g][e] = -INFINITY;
             l[g][e] = power[g][e] = 0.f;
@@ -233,7 +233,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
       float k_scale[4], v_scale[4];  // of keys n8, n8 + 8, n8 + 16, n8 + 24
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        k_scale[i] = ks[8 * i + n8];
+        k_scale[i] = ks[8 * i + n8] * kKeyScaleFactor;
         v_scale[i] = ks[kFewKeys + 8 * i + n8];
       }
       // The maxima and the powers of two are moved only when a lane meets a value above what they allow; only then the lanes of a row compare theirs.

@@ -192,7 +192,7 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     const int e = top > 0.f ? min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 118) : 0;  // top <= 2^e (lanes 0 to 15)
     const float times = good ? vs * __uint_as_float((unsigned)(127 + kValuePower - e) << 23) : 0.f;
     const uint32_t factor = two_f16(times, times);
-    const float key_scale = good ? ks : __uint_as_float(0x7FC00000u);
+    const float key_scale = good ? ks * kKeyScaleFactor : __uint_as_float(0x7FC00000u);
     const int exist = have;
 
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), free_parity, &ctl.abort);  // (a wait that gives up only marks the results as invalid)
@@ -374,8 +374,8 @@ __device__ __forceinline__ Place place_of(const AttendCall& c, const Walk& at, i
   return Place{(long long)at.x.row0 + r, at.head * c.group + i - r * c.group, r};
 }
 
-// `rows` query rows into an operand tile, DIM / 8 lanes to a row, scaled by a power of two that makes their bf16 values exact in f16; to `scale`
-// what takes that back, times the softmax scale.  Every lane copies its pieces to where they belong and turns them into f16 there: the
+// `rows` query rows into an operand tile, DIM / 8 lanes to a row, scaled by a power of two each (query_power); to `scale` what takes that back, times
+// the softmax scale.  Every lane copies its pieces to where they belong and turns them into f16 there: the
 // loads are all in flight, and the code is short (unrolled it took 7 us the first time, most of it instruction fetch).  Rows that do not
 // exist keep what lies there: whatever it is, it stays in their own row of S and O, which nobody reads.
 template <int DIM>
@@ -401,13 +401,13 @@ __device__ __forceinline__ void load_queries(const AttendCall& c, const Walk& at
     top = max(top >> 16, top & 0xFFFFu);
 #pragma unroll
     for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    const float by = to_one(__uint_as_float(top << 16));
+    const float by = query_power(top);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     uint32_t h[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = two_f16(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xFFFF0000u) * by);
     ptx::st_shared4(at_piece, h[0], h[1], h[2], h[3]);
-    if (piece == 0) scale[row] = c.scale_log2 * inverse_power(by);
+    if (piece == 0) scale[row] = query_scale(c.scale_log2, by);
   }
 }
 

@@ -1,0 +1,51 @@
+"""fastav_attend where queries, keys or values differ very much in size, for each of its kernels.  Tolerances as derived in test_gpu_attend.py."""
+import pytest
+import torch
+
+from attend_shapes import ROWS, long_problem, place, set_queries
+
+pytestmark = pytest.mark.gpu
+
+
+def _normal(p, n, seed=7):
+    return torch.randn(n, p.hkv, p.dim, generator=torch.Generator().manual_seed(seed))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("exponent", [-100, -40, 40, 100, 120])
+def test_large_keys_with_small_queries_and_the_reverse(rows, exponent, fmt):
+    p = long_problem(rows, fmt, n=600)
+    n = p.lens[0]
+    q = torch.randn(p.total, p.hq, p.dim, generator=torch.Generator().manual_seed(8))
+    set_queries(p, q * 2.0 ** -exponent)
+    place(p, 0, k=_normal(p, n).clamp(-3.9, 3.9) * 2.0 ** exponent)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("bits", [16, 20, 24])
+def test_small_elements_of_a_query_beside_a_large_one_that_no_key_answers(rows, bits, fmt):
+    """The largest element of a query row meets zeros in every key; those that count are 2^-bits of it."""
+    p = long_problem(rows, fmt, n=600)
+    n = p.lens[0]
+    q = torch.randn(p.total, p.hq, p.dim, generator=torch.Generator().manual_seed(8)).clamp(-4, 4) * 2.0 ** -bits
+    q[..., 3] = 1.5
+    set_queries(p, q)
+    k = _normal(p, n) * 2.0 ** bits
+    k[..., 3] = 0
+    place(p, 0, k=k)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("query", [0.0, 2.0 ** -120])
+def test_logits_that_are_almost_nothing(rows, query):
+    """Equal weights: a query row of zeros or of tiny values, and a softmax scale that takes their product below fp32's numbers."""
+    p = long_problem(rows, n=333, scale=1e-14)
+    set_queries(p, torch.full((p.dim,), query))
+    p.run()
+    p.check()
