@@ -27,9 +27,9 @@ namespace {
 
 constexpr int kWarps = 12, kThreads = 32 * kWarps, kFewKeysShift = 5;
 static_assert(1 << kFewKeysShift == kFewKeys);
-constexpr float kSlack = 8.f;        // log2 of what a weight may reach before the maximum is moved
-// A row's weights 2^(z - m) vs times a power of two that brings the largest to 2,048 .. 4,096, and moved when one is above 32,768 (f16 ends at
-// 65,504): what lies under f16's normal numbers is less than 2^-25 of the largest.
+constexpr float kSlack = 6.f;        // log2 of what a weight may reach before the maximum is moved (times the largest scale it is below 2^128)
+// A row's weights 2^(z - m) vs times a power of two that brings the largest to 2,048 .. 4,096; lowered when one is above 32,768 (f16 ends at
+// 65,504), raised when the maximum moves.  So the largest so far has 2,048 at least, and f16's last step, 2^-24, is 2^-35 of it.
 constexpr float kWeightPower = 2048, kMostWeight = 32768;
 
 template <int DIM>
@@ -263,16 +263,24 @@ attend_few_kernel(AttendCall c, AttendList list) {
       if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
         for (int g = 0; g < NT; ++g) {
-          float factor[2];
+          float factor[2];  // of what has been summed up
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float top = fmaxf(fmaxf(z[g][0][e], z[g][0][2 + e]), fmaxf(z[g][1][e], z[g][1][2 + e])) * row_scale[g][e];
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            top = fmaxf(top, m[g][e]);
-            factor[e] = m[g][e] == -INFINITY ? 0.f : ptx::ex2_approx(m[g][e] - top);
-            m[g][e] = top;
+            // By whole bits, and the power of two goes up by what the weights so far go down by: the largest of these stays where it was, and nothing drifts.
+            // (Else the power would remain that of values which count for nothing any more.)  What this unit's weights make of it is seen to below.
+            const float before = m[g][e], to = before == -INFINITY ? top : before + fmaxf(ceilf(top - before), 0.f), by = to - before;
+            factor[e] = before == -INFINITY ? 0.f : ptx::ex2_approx(-by);
             l[g][e] *= factor[e];
+            if (before > -INFINITY && power[g][e] > 0.f) {
+              const unsigned bits = __float_as_uint(power[g][e]);
+              const int up = min((int)rintf(fminf(by, 300.f)), 251 - (int)(bits >> 23));
+              power[g][e] = __uint_as_float(bits + ((unsigned)up << 23));
+              factor[e] = ptx::ex2_approx((float)up - by);
+            }
+            m[g][e] = to;
           }
 #pragma unroll
           for (int j = 0; j < kSteps; ++j)

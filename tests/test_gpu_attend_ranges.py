@@ -2,13 +2,29 @@
 import pytest
 import torch
 
-from attend_shapes import ROWS, long_problem, place, set_queries
+from attend_shapes import ROWS, along, direction, long_problem, place, set_queries
 
 pytestmark = pytest.mark.gpu
 
 
 def _normal(p, n, seed=7):
     return torch.randn(n, p.hkv, p.dim, generator=torch.Generator().manual_seed(seed))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("bits", [24, 36, 44])
+@pytest.mark.parametrize("block", [32, 128])
+def test_large_values_that_lose_their_weight(rows, bits, block, fmt):
+    """Blocks of keys in turn: values of 1 with logits of 0, then values of 2^-bits with logits of 90 (base 2), which have all the weight."""
+    p = long_problem(rows, fmt, n=9000 if rows == 1 else 6000, causal=False)
+    n = p.lens[0]
+    late = torch.arange(n) // block % 2 == 1
+    set_queries(p, direction(p.dim))
+    place(p, 0, along(torch.where(late, 90.0, 0.0) + torch.rand(n, generator=p.gen), p.dim)[:, None].expand(-1, p.hkv, -1),
+          _normal(p, n) * torch.where(late, 2.0 ** -bits, 1.0)[:, None, None])
+    p.run()
+    p.check()
 
 
 @pytest.mark.parametrize("fmt", ["int8", "fp8"])
