@@ -10,6 +10,7 @@ namespace fastav {
 namespace {
 
 constexpr int kJoinWarps = 8;
+constexpr float kShare = 1.f / 1024;  // on every weight: the sum of some hundred parts near bf16's largest value stays in fp32
 
 // The parts of one row and head at one level: which job, which blocks.
 struct Parts {
@@ -81,8 +82,8 @@ __device__ __forceinline__ Belongs belongs_to(const AttendCall& c, const AttendL
   return f;
 }
 
-// Joins what the levels' blocks left.  With m the largest of the parts' maxima,
-//   out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i,  lse = ln 2 (m + log2 sum).
+// Joins what the levels' blocks left.  With m the largest of the parts' log-sum-exps (base 2),
+//   out = sum_i 2^(lse_i - m) out_i / sum_i 2^(lse_i - m),  lse = ln 2 (m + log2 sum).
 // Rows of one level that one block finished are there already; a row that sees no key gets 0 and -inf.
 //
 // Bound by latency: a few trips to memory one after the other (the row's sequence; its bounds; the parts' statistics; the parts).  So a lane
@@ -94,7 +95,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
   static_assert(WARPS == 1 || HEADS == 1);
   constexpr int kEach = DIM / 32, kHeads = kJoinWarps / WARPS * HEADS, kAtOnce = WARPS > 1 ? 8 : 2;
   __shared__ float part_acc[WARPS > 1 ? kJoinWarps : 1][DIM];
-  __shared__ float2 part_ml[kJoinWarps];
+  __shared__ float2 part_sum[kJoinWarps];  // their maximum and sum
   __shared__ Belongs f;  // a block has one row
   chain_enter(c);
   // Where all blocks are there at once, this is looked up while the kernel before still runs.
@@ -137,15 +138,15 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
       p.row = is_shared ? p1.row : p0.row;
       const long long at = whole ? (is_shared ? flats : 0) + flat
                                  : part_of(is_shared ? shared.tile_rows : own.tile_rows, p, mine - (is_shared ? p0.count : 0));
-      const float2 ml = mine < parts_all ? chain_load((whole ? c.whole_ml : is_shared ? shared.part_ml : own.part_ml) + at) : make_float2(-INFINITY, 0.f);
+      const float lse = mine < parts_all ? chain_load((whole ? c.whole_lse : is_shared ? shared.part_lse : own.part_lse) + at) : -INFINITY;
       const float* const outs = (whole ? c.whole_out : is_shared ? shared.part_out : own.part_out) + at * DIM;
-      float to = ml.x;
+      float to = lse;
 #pragma unroll
       for (int d = 16; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, d));
       to = fmaxf(to, top);
-      const float base = to == -INFINITY ? 0.f : to, before = exp2f(top - base), weight = exp2f(ml.x - base);
+      const float base = to == -INFINITY ? 0.f : to, before = exp2f(top - base), weight = exp2f(lse - base) * kShare;
       top = to;
-      sum = sum * before + weight * ml.y;  // (a lane's own; added up below)
+      sum = sum * before + weight;  // (a lane's own; added up below)
 #pragma unroll
       for (int e = 0; e < kEach; ++e) acc[e] *= before;
       const int parts = min(32, (parts_all - i0 - sub + WARPS - 1) / WARPS);  // of this warp
@@ -180,12 +181,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
     if (WARPS > 1) {
 #pragma unroll
       for (int e = 0; e < kEach; ++e) part_acc[warp][lane * kEach + e] = acc[e];
-      if (lane == 0) part_ml[warp] = make_float2(top, sum);
+      if (lane == 0) part_sum[warp] = make_float2(top, sum);
       __syncthreads();
       if (sub != 0) return;
       float to = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) to = fmaxf(to, part_ml[warp + w].x);
+      for (int w = 0; w < WARPS; ++w) to = fmaxf(to, part_sum[warp + w].x);
       const float base = to == -INFINITY ? 0.f : to;
       top = to;
       sum = 0.f;
@@ -193,8 +194,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
       for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
-        const float weight = exp2f(part_ml[warp + w].x - base);
-        sum += weight * part_ml[warp + w].y;
+        const float weight = exp2f(part_sum[warp + w].x - base);
+        sum += weight * part_sum[warp + w].y;
 #pragma unroll
         for (int e = 0; e < kEach; ++e) acc[e] = fmaf(weight, part_acc[warp + w][lane * kEach + e], acc[e]);
       }
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
     uint16_t* const to = c.out + (long long)row * c.o_st + (long long)head * c.o_sh + lane * kEach;
     if (kEach == 4) *reinterpret_cast<uint2*>(to) = make_uint2(packed[0], packed[kEach / 2 - 1]);
     else *reinterpret_cast<uint32_t*>(to) = packed[0];
-    if (c.lse_out && lane == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (c.lse_out && lane == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum * (1.f / kShare))) * kLn2;
   }
 }
 
@@ -238,7 +239,7 @@ constexpr double kFewUnitCost = 0.13, kManyUnitCost = 1.7;  // us of an SM (many
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
   bool own_many, shared_many;
-  size_t ahead[2], out[2], ml[2], scratch, copies, whole_out, whole_ml, total = 0;  // offsets into the workspace: few, many
+  size_t ahead[2], out[2], lse[2], scratch, copies, whole_out, whole_lse, total = 0;  // offsets into the workspace: few, many
   bool fits = true;
 };
 
@@ -286,13 +287,13 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
     const size_t parts = list.entries() > 0 ? (size_t)list.grid * 2 * list.tile_rows : 0;
     w.ahead[i] = carve((size_t)(list.entries() + 1) * sizeof(int32_t));
     w.out[i] = carve(parts * cache.head_dim * sizeof(float));
-    w.ml[i] = carve(parts * sizeof(float2));
+    w.lse[i] = carve(parts * sizeof(float));
   }
   w.copies = carve(w.many.entries() > kManyListed ? (size_t)w.many.grid * (w.many.entries() + 1) * sizeof(int32_t) : 0);
   w.scratch = carve(w.few.entries() > 0 ? few_scratch_floats(w.few, cache.head_dim) * sizeof(float) : 0);
   const size_t rows = p.num_prefixes > 0 ? (size_t)2 * p.total_q * p.num_q_heads : 0;
   w.whole_out = carve(rows * cache.head_dim * sizeof(float));
-  w.whole_ml = carve(rows * sizeof(float2));
+  w.whole_lse = carve(rows * sizeof(float));
   w.total = off;
   return w;
 }
@@ -358,12 +359,12 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
   c.device_status = device_status;
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
   c.whole_out = reinterpret_cast<float*>(ws + w.whole_out);
-  c.whole_ml = reinterpret_cast<float2*>(ws + w.whole_ml);
+  c.whole_lse = reinterpret_cast<float*>(ws + w.whole_lse);
   AttendList lists[2] = {w.few, w.many};
   for (int i = 0; i < 2; ++i) {
     lists[i].ahead = reinterpret_cast<int32_t*>(ws + w.ahead[i]);
     lists[i].part_out = reinterpret_cast<float*>(ws + w.out[i]);
-    lists[i].part_ml = reinterpret_cast<float2*>(ws + w.ml[i]);
+    lists[i].part_lse = reinterpret_cast<float*>(ws + w.lse[i]);
   }
   lists[0].scratch = reinterpret_cast<float*>(ws + w.scratch);
   lists[1].copies = reinterpret_cast<int32_t*>(ws + w.copies);

@@ -4,8 +4,8 @@
 // sequence with the sequence's own tokens, or the rows of all sequences that share a prefix with the prefix.  Its query rows times the
 // G query heads of a KV head are stacked (row i of the stack: query row i / G, head i % G) and cut into tiles; a JOB is one (entry, KV head,
 // tile), its keys cut into granules, the UNITS.  All units of a launch form one list, keys innermost, and every worker takes an equal run
-// of it, whatever the lengths.  A run that begins or ends inside a job leaves a part (running maximum, sum and weighted values); the
-// parts of a job lie with consecutive blocks, and the kernel that joins them works out which from the list alone.  A job begins with
+// of it, whatever the lengths.  A run that begins or ends inside a job leaves a part (its keys' log-sum-exp in base 2, and the output they alone would
+// give: sums that are not divided yet pass fp32's range where values are near bf16's); the parts of a job lie with consecutive blocks, and the kernel that joins them works out which from the list alone.  A job begins with
 // `job_cost` units that hold nothing: what its queries, its output and its first logits cost, in granules; short jobs would else
 // all fall to a few workers.
 #pragma once
@@ -32,7 +32,7 @@ struct AttendCall {
   int32_t* device_status;
   // results of jobs that one block finished, where another level's are still to be joined: [2][total_q, Hq]
   float* whole_out;
-  float2* whole_ml;
+  float* whole_lse;
   int beside;  // both kernels run, side by side on SMs of their own
   int head_wait;
 };
@@ -46,7 +46,7 @@ struct AttendList {
   int grid;                  // blocks that share the list
   int32_t* ahead;            // [entries + 1] units before an entry, left for the kernel that joins
   float* part_out;           // [grid][2][tile_rows][dim]
-  float2* part_ml;           // [grid][2][tile_rows]: running maximum (base 2), sum
+  float* part_lse;           // [grid][2][tile_rows], base 2
   float* scratch;            // few: parts that warps of one block exchange
   int32_t* copies;           // many: the blocks' own `ahead`, where there are more entries than shared memory has room for
   __host__ __device__ int entries() const { return from_prefix + from_own; }

@@ -31,6 +31,7 @@ constexpr float kSlack = 6.f;        // log2 of what a weight may reach before t
 // A row's weights 2^(z - m) vs times a power of two that brings the largest to 2,048 .. 4,096; lowered when one is above 32,768 (f16 ends at
 // 65,504), raised when the maximum moves.  So the largest so far has 2,048 at least, and f16's last step, 2^-24, is 2^-35 of it.
 constexpr float kWeightPower = 2048, kMostWeight = 32768;
+constexpr float kShare = 1.f / 32;   // on the weights of a block's parts, 24 at most: their sum stays in fp32 where values are near bf16's largest
 
 template <int DIM>
 struct Few {
@@ -68,7 +69,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
   constexpr int kRun = DIM / 8;      // output elements of a lane, per row
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Left left[kWarps][2];
-  __shared__ float2 left_ml[kWarps][2][kTile], part_weight[2 * kWarps][kTile];
+  __shared__ float left_lse[kWarps][2][kTile], part_weight[2 * kWarps][kTile];
   __shared__ int warp_sum[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n8 = lane >> 2, t4 = lane & 3;
   unsigned char* const my_ring = smem + warp * F::kStages * F::kStage;
@@ -392,30 +393,35 @@ attend_few_kernel(AttendCall c, AttendList list) {
             for (int d = 4; d < 32; d <<= 1) l[g][e] += __shfl_xor_sync(0xFFFFFFFFu, l[g][e], d);
             const int row = 8 * g + 2 * t4 + e, i = at.tile * kTile + row, r = query_row(c, i);
             if (r >= at.x.rows) continue;
-            const float back = power[g][e] == 0.f ? 0.f : inverse_power(power[g][e]);
+            const float back = power[g][e] == 0.f ? 0.f : inverse_power(power[g][e]), inv = l[g][e] == 0.f ? 0.f : 1.f / l[g][e];
+            const float lse = l[g][e] == 0.f ? -INFINITY : m[g][e] + log2f(l[g][e]);
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {  // (in this order no product leaves fp32's range)
+              o[g][j][e] = o[g][j][e] * inv * back;
+              o[g][j][2 + e] = o[g][j][2 + e] * inv * back;
+            }
             const long long q_row = at.x.row0 + r;
             const int head = at.head * c.group + i - r * c.group;
             const long long flat = (at.x.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
             if (final) {
-              const float inv = l[g][e] == 0.f ? 0.f : back / l[g][e];
               uint16_t* const to = c.out + q_row * c.o_st + (long long)head * c.o_sh + n8 * kRun;
 #pragma unroll
               for (int j = 0; j < kRun / 8; ++j) {
                 uint32_t x[4];
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) x[i4] = pair_bf16(o[g][4 * j + i4][e] * inv, o[g][4 * j + i4][2 + e] * inv);
+                for (int i4 = 0; i4 < 4; ++i4) x[i4] = pair_bf16(o[g][4 * j + i4][e], o[g][4 * j + i4][2 + e]);
                 *reinterpret_cast<uint4*>(to + 8 * j) = make_uint4(x[0], x[1], x[2], x[3]);
               }
-              if (c.lse_out && n8 == 0) c.lse_out[flat] = l[g][e] == 0.f ? -INFINITY : (m[g][e] + log2f(l[g][e])) * kLn2;
+              if (c.lse_out && n8 == 0) c.lse_out[flat] = lse * kLn2;
             } else {
               float* const to = whole ? c.whole_out + flat * DIM : alone ? list.part_out + (place + row) * DIM : part;
 #pragma unroll
               for (int j = 0; j < kRun / 4; ++j) {
                 const int piece = n8 * (kRun / 4) + j;
                 *reinterpret_cast<float4*>(to + (whole || alone ? piece * 4 : part_at<DIM>(row, piece))) =
-                    make_float4(o[g][2 * j][e] * back, o[g][2 * j][2 + e] * back, o[g][2 * j + 1][e] * back, o[g][2 * j + 1][2 + e] * back);
+                    make_float4(o[g][2 * j][e], o[g][2 * j][2 + e], o[g][2 * j + 1][e], o[g][2 * j + 1][2 + e]);
               }
-              if (n8 == 0) *(whole ? c.whole_ml + flat : alone ? list.part_ml + place + row : &left_ml[warp][slot][row]) = make_float2(m[g][e], l[g][e]);
+              if (n8 == 0) *(whole ? c.whole_lse + flat : alone ? list.part_lse + place + row : &left_lse[warp][slot][row]) = lse;
             }
           }
         if (!whole && !alone && lane == 0) left[warp][slot] = Left{job_first, job_end, at.x.row0, at.x.rows, at.tile, at.head, at.x.own, last};
@@ -432,20 +438,19 @@ attend_few_kernel(AttendCall c, AttendList list) {
   const int slot_first = lane < 2 * kWarps ? left[lane / 2][lane & 1].job_first : -1;
   const unsigned alike = __match_any_sync(0xFFFFFFFFu, slot_first), leaders = __ballot_sync(0xFFFFFFFFu, slot_first >= 0 && __ffs(alike) - 1 == lane);
   for (int row = warp; row < kTile; row += kWarps) {
-    const float2 ml = slot_first >= 0 ? left_ml[lane / 2][lane & 1][row] : make_float2(-INFINITY, 0.f);
+    const float lse = slot_first >= 0 ? left_lse[lane / 2][lane & 1][row] : -INFINITY;
     float top = -INFINITY;  // of the lanes with the same job
 #pragma unroll 1
     for (unsigned rest = leaders; rest; rest &= rest - 1) {
       const unsigned group = __shfl_sync(0xFFFFFFFFu, alike, __ffs(rest) - 1);
-      float of_group = group >> lane & 1 ? ml.x : -INFINITY;
+      float of_group = group >> lane & 1 ? lse : -INFINITY;
 #pragma unroll
       for (int d = 16; d; d >>= 1) of_group = fmaxf(of_group, __shfl_xor_sync(0xFFFFFFFFu, of_group, d));
       if (group >> lane & 1) top = of_group;
     }
     if (lane < 2 * kWarps) {
-      const float weight = ptx::ex2_approx(ml.x - (top == -INFINITY ? 0.f : top));
-      part_weight[lane][row] = make_float2(weight, weight * ml.y);
-      left_ml[lane / 2][lane & 1][row].x = top;
+      part_weight[lane][row] = ptx::ex2_approx(lse - (top == -INFINITY ? 0.f : top)) * kShare;
+      left_lse[lane / 2][lane & 1][row] = top;
     }
   }
   __syncthreads();
@@ -464,23 +469,23 @@ attend_few_kernel(AttendCall c, AttendList list) {
 #pragma unroll 4
       for (unsigned of = group; of; of &= of - 1) {
         const int j = __ffs(of) - 1;
-        const float2 w = part_weight[j][row];
+        const float w = part_weight[j][row];
         const float* const part = left[j / 2][j & 1].in_ring ? reinterpret_cast<float*>(smem + j / 2 * F::kStages * F::kStage) : scratch + j / 2 * kTile * DIM;
         const float4 v = *reinterpret_cast<const float4*>(part + part_at<DIM>(row, piece));
-        sum += w.y;
-        acc.x = fmaf(w.x, v.x, acc.x); acc.y = fmaf(w.x, v.y, acc.y); acc.z = fmaf(w.x, v.z, acc.z); acc.w = fmaf(w.x, v.w, acc.w);
+        sum += w;
+        acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
       }
-      const float top = left_ml[first / 2][first & 1][row].x;
+      const float lse = sum == 0.f ? -INFINITY : left_lse[first / 2][first & 1][row] + log2f(sum * (1.f / kShare)), inv = sum == 0.f ? 0.f : 1.f / sum;
+      acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
       const int stacked = job.tile * kTile + row, r = query_row(c, stacked), head = job.head * c.group + stacked - r * c.group;
       const long long q_row = job.row0 + r, flat = (job.own ? 0ll : (long long)c.total_q * c.hq) + q_row * c.hq + head;
       if (whole && c.prefixes == 0) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        *reinterpret_cast<uint2*>(c.out + q_row * c.o_st + (long long)head * c.o_sh + piece * 4) = make_uint2(pair_bf16(acc.x * inv, acc.y * inv), pair_bf16(acc.z * inv, acc.w * inv));
-        if (c.lse_out && piece == 0) c.lse_out[flat] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+        *reinterpret_cast<uint2*>(c.out + q_row * c.o_st + (long long)head * c.o_sh + piece * 4) = make_uint2(pair_bf16(acc.x, acc.y), pair_bf16(acc.z, acc.w));
+        if (c.lse_out && piece == 0) c.lse_out[flat] = lse * kLn2;
       } else {
         const long long place = ((long long)blockIdx.x * 2 + slot) * kTile + row;
         *reinterpret_cast<float4*>((whole ? c.whole_out + flat * DIM : list.part_out + place * DIM) + piece * 4) = acc;
-        if (piece == 0) *(whole ? c.whole_ml + flat : list.part_ml + place) = make_float2(top, sum);
+        if (piece == 0) *(whole ? c.whole_lse + flat : list.part_lse + place) = lse;
       }
     }
   }

@@ -498,11 +498,9 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     const bool whole = at.job_first() >= u0 && at.job_end() <= u1, final = whole && c.prefixes == 0;
     const long long level = at.x.own ? 0ll : (long long)c.total_q * c.hq;
     const long long part = ((long long)blockIdx.x * 2 + (at.job_first() < u0 ? 0 : 1)) * kManyTile;  // the block's place for what it did not finish
-    if (final) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      back *= inv;
-      other *= inv;
-    }
+    const float inv = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + log2f(l);
+    back *= inv;
+    other *= inv;
     // A stream writes its rows; where both have the same ones, half of the columns each.  By kWide columns through shared memory (the query
     // tiles, which nobody needs any more), so that rows are written in whole lines.
     constexpr int kWide = DIM / 2, kLanes = kWide / 4, kRows = 32 / kLanes;
@@ -547,9 +545,9 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     if (there && (seg.two || stream == 0)) {
       const Place q = place_of(c, at, warp_row + lane);
       if (final) {
-        if (c.lse_out) c.lse_out[q.q_row * c.hq + q.head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (c.lse_out) c.lse_out[q.q_row * c.hq + q.head] = lse * kLn2;
       } else {
-        *(whole ? c.whole_ml + level + q.q_row * c.hq + q.head : list.part_ml + part + warp_row + lane) = make_float2(m, l);
+        *(whole ? c.whole_lse + level + q.q_row * c.hq + q.head : list.part_lse + part + warp_row + lane) = lse;
       }
     }
     ptx::tc_fence_before_sync();

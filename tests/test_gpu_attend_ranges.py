@@ -28,6 +28,17 @@ def test_large_values_that_lose_their_weight(rows, bits, block, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS[:1])
+@pytest.mark.parametrize("exponent", [-60, 100, 116, 120, 122, 124])
+def test_values_of_one_extreme_size(rows, exponent, fmt):
+    """Up to near the largest bf16: scales of up to 2^119 (e4m3) and 2^121 (int8), in parts that several blocks leave."""
+    p = long_problem(rows, fmt, n=2500)
+    place(p, 0, v=_normal(p, p.lens[0]).clamp(-3.9, 3.9) * 2.0 ** exponent)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
 @pytest.mark.parametrize("rows", ROWS)
 @pytest.mark.parametrize("exponent", [-100, -40, 40, 100, 120])
 def test_large_keys_with_small_queries_and_the_reverse(rows, exponent, fmt):
@@ -63,5 +74,16 @@ def test_logits_that_are_almost_nothing(rows, query):
     """Equal weights: a query row of zeros or of tiny values, and a softmax scale that takes their product below fp32's numbers."""
     p = long_problem(rows, n=333, scale=1e-14)
     set_queries(p, torch.full((p.dim,), query))
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("rows", ROWS[:1])
+def test_values_near_the_largest_bf16_under_a_growing_maximum(rows):
+    """Logits that rise by a few bits from key to key: sums run above their maximum for a while, and nothing may pass fp32's range."""
+    p = long_problem(rows, n=2000, causal=False)
+    n = p.lens[0]
+    set_queries(p, direction(p.dim))
+    place(p, 0, along(torch.arange(n) % 64 * 0.9, p.dim)[:, None].expand(-1, p.hkv, -1), _normal(p, n).clamp(-1.9, 1.9) * 2.0 ** 126)
     p.run()
     p.check()
