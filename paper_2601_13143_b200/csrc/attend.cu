@@ -289,7 +289,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
     w.out[i] = carve(parts * cache.head_dim * sizeof(float));
     w.lse[i] = carve(parts * sizeof(float));
   }
-  w.copies = carve(w.many.entries() > kManyListed ? (size_t)w.many.grid * (w.many.entries() + 1) * sizeof(int32_t) : 0);
+  w.copies = carve(w.many.entries() > many_listed(cache.head_dim) ? (size_t)w.many.grid * (w.many.entries() + 1) * sizeof(int32_t) : 0);
   w.scratch = carve(w.few.entries() > 0 ? few_scratch_floats(w.few, cache.head_dim) * sizeof(float) : 0);
   const size_t rows = p.num_prefixes > 0 ? (size_t)2 * p.total_q * p.num_q_heads : 0;
   w.whole_out = carve(rows * cache.head_dim * sizeof(float));

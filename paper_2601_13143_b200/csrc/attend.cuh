@@ -58,7 +58,8 @@ size_t few_scratch_floats(const AttendList& list, int dim);
 cudaError_t launch_attend_few(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 // Many: tcgen05, a granule per step of a block (attend_many.cu).
-constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4, kManyListed = 3000;  // (entries whose `ahead` is in shared memory)
+constexpr int kManyTile = 256, kManyKeys = 128, kManyJobCost = 4;
+constexpr int many_listed(int dim) { return dim == 128 ? 2000 : 3000; }  // entries whose `ahead` has room in shared memory
 cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream);
 
 #ifdef __CUDACC__

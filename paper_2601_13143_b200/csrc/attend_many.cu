@@ -17,15 +17,22 @@
 // wait for PV, and a stream stood still for the way to the issuing warp, PV, QK and back; 16 questions on 16,384 keys, Mistral-7B shapes,
 // 597 us instead of 579 at that step.)  Registers move from the warps that need few to the softmax's, which hold a visit's logits.
 //
-// A value's scale is folded into its f16 operand relative to the power of two E of the largest scale of 16 keys, and E joins the exponent:
-// w = 2^(z + E - m + kOffset) is rounded to f16 for the matrix pipe, l = sum w 2^(-E - kOffset) stays in fp32.  So no weight is
-// multiplied by a scale, and values of very different size keep their bits.  The keys' scales multiply the logits in fp32.
+// The keys' scales multiply the logits in fp32.  The values' scales are looked at sixteen keys at a time.  Where they lie within a factor of 2^kEven of
+// each other (EVEN groups), a value's operand is code * scale / 2^E * 2^kValuePower, rounded once, with 2^E the least power of two above all sixteen, and E
+// joins the exponent: w = 2^(z + E - m + kOffset) is rounded to f16 for the matrix pipe, l = sum w 2^(-E - kOffset) stays in fp32.  m is the row's largest
+// z + E.  So f16 sees one rounding of the weight and one of the value (2^-11 each), and what it cannot hold, 2^-25 of a unit, is 2^-36 of the row's
+// largest product of weight and scale where the scales of sixteen neighbours are alike, 2^-30 where they differ by 2^kEven.
 //
-// 16 questions of 64 to 128 tokens on 16,384 keys (346 GFLOP): 502 us, 0.69 PFLOP/s.  Bound by the chains of the converting and softmax warps per
-// tile (5,000 cycles, of which the MMAs take 2,600 and the exponentials 2,000): a scheduler issues 0.54 instructions a cycle.  Taking the weights
-// with the maximum so far first, and a new one only where f16 overflows, spills: 619 us.
+// Other groups (a row of zeros, an outlier, a hidden key's large value) would lose the smaller values that way: f16 has no room for both.  There
+// a value's operand is its code alone, log2 of its scale joins its own logit, and the weights are summed up ahead of that.  That takes the
+// exponentials twice: 16 questions on 16,384 keys with every eighth group uneven 611 us instead of 527 at that step.  (The scales multiplying
+// the weights in fp32 in every group: 607 us.  What it takes is not the products, 12 us, but two 16-byte loads per eight logits, which every lane of a warp gets.)
 //
-// O is rescaled only when a row's maximum has grown by 2^kSlack: until then its weights are larger than 2^kOffset, which f16 has room for.
+// 16 questions of 64 to 128 tokens on 16,384 keys (346 GFLOP): 521 us, 0.66 PFLOP/s.  Bound by the chains of the converting and softmax warps per
+// tile (5,200 cycles, of which the MMAs take 2,600 and the exponentials 2,000).  Taking the weights with the maximum so far first, and a new one
+// only where f16 overflows, spills: 619 us instead of 500 at that step.
+//
+// O is rescaled only when a row's maximum has grown by kSlack: until then its weights are larger than 2^kOffset, which f16 has room for.
 #include <limits.h>
 
 #include "attend.cuh"
@@ -44,9 +51,13 @@ constexpr int kSoftRegs = 144, kConvRegs = 72, kIssueRegs = 48;
 constexpr int kRegsNeeded = 32 * (kSoftWarps * kSoftRegs + kConvWarps * kConvRegs + 4 * kIssueRegs);
 constexpr int kGroups = kManyKeys / 16;          // of 16 keys: a converting warp's
 constexpr int kScaleRing = 4;
-constexpr int kOffset = 11;                      // the largest weight of a row's first visit is 2^kOffset ...
-constexpr float kSlack = 4.f;                    // ... and the maximum is moved when a logit is this much above it (f16 ends at 2^16)
-constexpr int kValuePower = 7;                   // a value operand is code * (scale / 2^E) * 2^kValuePower, below 2^16
+constexpr int kValuePower = 7;                   // a value operand is below 2^16
+constexpr int kEven = 6;
+constexpr int kOffset = 12;                      // the largest weight of a row's first visit is up to 2^kOffset ...
+constexpr float kSlack = 3.9f;                   // ... and the maximum is moved when one would be this much (log2) above that (f16 ends at 2^16)
+// Bounds of the exponents.  A key's from kLeastExponent on: 2^(z - m) stays below 2^74 (value rows that are smaller, 10^-19 and less, keep fewer bits).
+// E of an uneven group: its weights without their scales stay below 2^116, and above 2^-80 where all scales are as large as can be.
+constexpr int kLeastExponent = -70, kLeastGroup = -16, kMostGroup = 30;
 constexpr int kTmemCols = 512, kWeightsAt = 2 * kVisit, kOutputAt = kWeightsAt + 4 * (kVisit / 2);  // columns: S, P, O
 static_assert(kConvWarps == kGroups && kOutputAt + 2 * 128 <= kTmemCols);
 
@@ -66,7 +77,10 @@ struct Control {
   int abort;
   int warp_sum[kWarps];
   alignas(16) float k_scale[kScaleRing][kManyKeys];
-  float exponent[kScaleRing][kGroups], unscale[kScaleRing][kGroups];  // E; 2^(-E - kOffset)
+  alignas(16) float v_exponent[kScaleRing][kManyKeys], v_log[kScaleRing][kManyKeys];  // of values in groups that are not even: e, the least with scale <= 2^e; log2 scale - E
+  float exponent[kScaleRing][kGroups];                                                // E
+  float bound[kScaleRing][kGroups], unscale[kScaleRing][kGroups];                     // of even groups E and 2^(-E - kOffset), else -inf and 0
+  alignas(4) uint8_t even[kScaleRing][kGroups];
   float row_scale[2][kSub];                                           // of a stream's query rows
   float2 row_ml[2][kSub];                                             // the streams' statistics, to be joined
 };
@@ -94,6 +108,9 @@ __device__ __forceinline__ bool skip(const AttendCall& c, const AttendList& list
   return at.step(c, list, ahead, u1);
 }
 
+// 2^e for e of -126 and more, up to 127.
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }
+
 // ---- codes to f16 ----------------------------------------------------------------------------------------------------
 // One warp's 16 keys of a tile, 16 codes per lane and load.  DIM 128: a load is 4 keys of 8 pieces; lane bits 0, 1 and 3 name the piece, 2 and 4 the
 // key, so that the eight lanes of a phase store to eight different banks' quarters.  DIM 64: 8 keys of 4 pieces.
@@ -114,18 +131,21 @@ struct Piece {
   __device__ __forceinline__ int key(int j) const { return j * kRows + row; }
 };
 
-// 16 codes -> 32 bytes of a swizzled operand row.  `times`: f16x2 factor (values only).
+// 16 codes -> 32 bytes of a swizzled operand row.  Values only: times a factor in two f16 parts (twice each), rounded once.
 template <bool FP8, bool VALUES>
-__device__ __forceinline__ void convert_piece(const uint4& x, uint32_t at, uint32_t times) {
+__device__ __forceinline__ void convert_piece(const uint4& x, uint32_t at, uint32_t times, uint32_t rest) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t h[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     four_codes<FP8>(w[i], h[2 * i], h[2 * i + 1]);
-    if (VALUES) {
-      asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h[2 * i]) : "r"(times));
-      asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h[2 * i + 1]) : "r"(times));
-    }
+    if (VALUES)
+#pragma unroll
+      for (int j = 2 * i; j < 2 * i + 2; ++j) {
+        uint32_t small;
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(small) : "r"(h[j]), "r"(rest));
+        asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(h[j]) : "r"(times), "r"(small));
+      }
   }
   ptx::st_shared4(at, h[0], h[1], h[2], h[3]);
   ptx::st_shared4(at ^ 16, h[4], h[5], h[6], h[7]);
@@ -184,47 +204,55 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
   for (int i = 0;; ++i) {  // `at` stands a tile further on
     const int slot = i & 1, ring = i & (kScaleRing - 1);
     const uint32_t free_parity = ((i >> 1) & 1) ^ 1u;
-    // values' scales: a value row that is not finite makes the weights of the rows that see it NaN, not everybody's sums
-    const bool good = fabsf(vs) < INFINITY;
-    float top = good ? fabsf(vs) : 0.f;
-#pragma unroll
-    for (int d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    const int e = top > 0.f ? min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 118) : 0;  // top <= 2^e (lanes 0 to 15)
-    const float times = good ? vs * __uint_as_float((unsigned)(127 + kValuePower - e) << 23) : 0.f;
-    const uint32_t factor = two_f16(times, times);
-    const float key_scale = good ? ks * kKeyScaleFactor : __uint_as_float(0x7FC00000u);
-    const int exist = have;
-
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), free_parity, &ctl.abort);  // (a wait that gives up only marks the results as invalid)
-    if (lane < 16) ctl.k_scale[ring][16 * warp + lane] = key_scale;
-    if (lane == 0) {
-      ctl.exponent[ring][warp] = (float)e;
-      ctl.unscale[ring][warp] = __uint_as_float((unsigned)(127 - e - kOffset) << 23);
-    }
     ptx::copies_wait<0>();
 #pragma unroll
     for (int j = 0; j < P::kLoads; ++j)
-      convert_piece<FP8, false>(ptx::ld_shared4(my_codes + j * 512), k_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, 0);
+      convert_piece<FP8, false>(ptx::ld_shared4(my_codes + j * 512), k_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, 0, 0);
     ptx::fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      ptx::mbar_arrive(ptx::smem_u32(&ctl.scale_full[ring]));
-      ptx::mbar_arrive(ptx::smem_u32(&ctl.k_full[slot]));
-    }
+    ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.k_full[slot]), lane);
+    const float key = ks, value = vs;  // the scales are looked at when what comes next is under way: nobody needs them before the logits
+    const int exist = have;
     if (more) {
       find_keys();
       copy_keys();
       ask_scales();
       if (lane < 16) ptx::prefetch_l2(c.cache.v + (long long)(pool + lane) * DIM);
     }
+    // values' scales: a value row that is not finite makes the weights of the rows that see it NaN, not everybody's sums
+    const bool good = fabsf(value) < INFINITY;
+    const int own = max(good ? (int)(__float_as_uint(fabsf(value)) >> 23) - 126 : kLeastExponent, kLeastExponent);  // |value| <= 2^own
+    unsigned both = (unsigned)own << 16 | (lane < exist ? -own : -1000) & 0xFFFF;  // the largest; the least, negated
+#pragma unroll
+    for (int d = 8; d; d >>= 1) both = __vmaxs2(both, __shfl_xor_sync(0xFFFFFFFFu, both, d));
+    const int largest = (int)both >> 16;
+    const bool even = largest + (int)(short)both <= kEven;  // (lanes 0 to 15)
+    const int e = even ? largest : min(max(largest, kLeastGroup), kMostGroup);
+    const float factor = !good ? 0.f : even ? value * power_of_two(kValuePower - e) : copysignf(1 << kValuePower, value), coarse = __uint_as_float(__float_as_uint(factor) & 0xFFFFE000u);
+    const uint32_t factors = two_f16(coarse, factor - coarse);
+    const float key_scale = good ? key * kKeyScaleFactor : __uint_as_float(0x7FC00000u);
+    if (lane < 16) ctl.k_scale[ring][16 * warp + lane] = key_scale;
+    if (!even && lane < 16) {
+      ctl.v_exponent[ring][16 * warp + lane] = (float)own;
+      ctl.v_log[ring][16 * warp + lane] = good ? log2f(fabsf(value)) - (float)e : 0.f;
+    }
+    if (lane == 0) {
+      ctl.exponent[ring][warp] = (float)e;
+      ctl.even[ring][warp] = even;
+      ctl.bound[ring][warp] = even ? (float)e : -INFINITY;
+      ctl.unscale[ring][warp] = even ? power_of_two(-e) * (1.f / (1 << kOffset)) : 0.f;
+    }
+    ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.scale_full[ring]), lane);
     ptx::mbar_wait_warp(ptx::smem_u32(&ctl.v_empty[slot]), free_parity, &ctl.abort);
     if (exist < 16)
 #pragma unroll
       for (int j = 0; j < P::kLoads; ++j)
-        if (mine.key(j) >= exist) v[j] = make_uint4(0, 0, 0, 0);  // (e4m3 has NaN, which a factor of 0 does not take away)
+        if (mine.key(j) >= exist) v[j] = make_uint4(0, 0, 0, 0);  // (e4m3 has NaN, which a weight of 0 does not take away)
 #pragma unroll
-    for (int j = 0; j < P::kLoads; ++j)
-      convert_piece<FP8, true>(v[j], v_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, __shfl_sync(0xFFFFFFFFu, factor, mine.key(j)));
+    for (int j = 0; j < P::kLoads; ++j) {
+      const uint32_t two = __shfl_sync(0xFFFFFFFFu, factors, mine.key(j));
+      convert_piece<FP8, true>(v[j], v_tiles + slot * Many<DIM>::kTileBytes + mine.to[j & 1] + j * P::kRows * 128, __byte_perm(two, two, 0x1010), __byte_perm(two, two, 0x3232));
+    }
     ptx::fence_proxy_async_smem();
     ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.v_full[slot]), lane);
     if (!more) break;
@@ -293,11 +321,11 @@ __device__ __forceinline__ void issue_mmas(const AttendCall& c, const AttendList
 // ---- softmax ------------------------------------------------------------------------------------------------------------
 struct Visit {
   uint32_t s;       // tensor memory address of the logits
-  const float* ks;  // scales of the keys, exponents of the groups, and what undoes them
-  const float *exponent, *unscale;
+  const float *ks, *ve, *log_vs, *bound, *exponent, *unscale;  // as in Control
+  const uint8_t* even_at;
 };
 
-// A visit's logits times the scales of their keys (and not yet of the row), and the largest z + E of them; `limit`: columns from there on are hidden.
+// A visit's logits times the scales of their keys (and not yet of the row), and the largest z + e of the groups whose scales are even; `limit`: columns from there on are hidden.
 __device__ __forceinline__ float visit_logits(const Visit& x, float row_scale, bool masked, int limit, float2 (&t)[kVisit / 2]) {
   uint32_t (&v)[kVisit / 32][32] = reinterpret_cast<uint32_t(&)[kVisit / 32][32]>(t);
 #pragma unroll
@@ -323,19 +351,54 @@ __device__ __forceinline__ float visit_logits(const Visit& x, float row_scale, b
     float most = -INFINITY;
 #pragma unroll
     for (int j = g * 8; j < g * 8 + 8; ++j) most = ptx::max3(most, t[j].x, t[j].y);
-    top = fmaxf(top, fmaf(most, row_scale, x.exponent[g]));
+    top = fmaxf(top, fmaf(most, row_scale, x.bound[g]));
   }
   return top;
 }
-// Their weights with the maximum `m` (base 2) as f16 pairs to tensor memory; the fp32 sum.
-__device__ __forceinline__ float visit_weights(const Visit& x, uint32_t to, float row_scale, float m, float2 (&t)[kVisit / 2]) {
+// ... and of the others.
+__device__ __forceinline__ float uneven_top(const Visit& x, uint32_t even, float row_scale, float top, const float2 (&t)[kVisit / 2]) {
+  const float2 rs = make_float2(row_scale, row_scale);
+#pragma unroll
+  for (int g = 0; g < kVisit / 16; ++g) {
+    if (even >> 8 * g & 1) continue;
+#pragma unroll
+    for (int j = g * 8; j < g * 8 + 8; j += 2) {
+      const float4 ve = *reinterpret_cast<const float4*>(x.ve + 2 * j);
+      const float2 a = __ffma2_rn(t[j], rs, make_float2(ve.x, ve.y)), b = __ffma2_rn(t[j + 1], rs, make_float2(ve.z, ve.w));
+      top = ptx::max3(ptx::max3(top, a.x, a.y), b.x, b.y);
+    }
+  }
+  return top;
+}
+// For these, ahead of the weights: their fp32 sum; and the logits, times the row's scale, get the logarithms of their values' scales.
+__device__ __forceinline__ float uneven_weights(const Visit& x, uint32_t even, float row_scale, float m, float2 (&t)[kVisit / 2]) {
   float l = 0.f;
   const float2 rs = make_float2(row_scale, row_scale);
+#pragma unroll
+  for (int g = 0; g < kVisit / 16; ++g) {
+    if (even >> 8 * g & 1) continue;
+    const float add = x.exponent[g] - m;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = g * 8; j < g * 8 + 8; j += 2) {
+      const float4 log_vs = *reinterpret_cast<const float4*>(x.log_vs + 2 * j);
+      sum += ptx::ex2_approx(fmaf(t[j].x, row_scale, add)) + ptx::ex2_approx(fmaf(t[j].y, row_scale, add)) + ptx::ex2_approx(fmaf(t[j + 1].x, row_scale, add)) +
+             ptx::ex2_approx(fmaf(t[j + 1].y, row_scale, add));
+      t[j] = __ffma2_rn(t[j], rs, make_float2(log_vs.x, log_vs.y));
+      t[j + 1] = __ffma2_rn(t[j + 1], rs, make_float2(log_vs.z, log_vs.w));
+    }
+    l = fmaf(sum, power_of_two(-(int)x.exponent[g]), l);
+  }
+  return l;
+}
+// The weights of a visit with the maximum `m` (base 2) as f16 pairs to tensor memory; the fp32 sum of the even groups'.
+__device__ __forceinline__ float visit_weights(const Visit& x, uint32_t even, uint32_t to, float row_scale, float m, float2 (&t)[kVisit / 2]) {
+  float l = 0.f;
   uint32_t p[kVisit / 2];
 #pragma unroll
   for (int g = 0; g < kVisit / 16; ++g) {
-    const float add = x.exponent[g] - m + kOffset;
-    const float2 plus = make_float2(add, add);
+    const float add = x.exponent[g] - m + kOffset, r = even >> 8 * g & 1 ? row_scale : 1.f;
+    const float2 plus = make_float2(add, add), rs = make_float2(r, r);
     float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = g * 8; j < g * 8 + 8; ++j) {
@@ -448,7 +511,8 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
 #pragma unroll 1
     for (int v = 0; v < count; ++v, ++visits) {
       const int tile = seg.two ? v >> 1 : v, half = seg.two ? v & 1 : stream, n = done + tile, ring = n & (kScaleRing - 1);
-      const Visit x{s, ctl.k_scale[ring] + half * kVisit, ctl.exponent[ring] + half * (kGroups / 2), ctl.unscale[ring] + half * (kGroups / 2)};
+      const Visit x{s, ctl.k_scale[ring] + half * kVisit, ctl.v_exponent[ring] + half * kVisit, ctl.v_log[ring] + half * kVisit, ctl.bound[ring] + half * (kGroups / 2),
+                    ctl.exponent[ring] + half * (kGroups / 2), ctl.unscale[ring] + half * (kGroups / 2), ctl.even[ring] + half * (kGroups / 2)};
       const int buffer = visits & 1;
       // The tile's scales, the logits, and that the weights two visits before have been used: looked at together (one after the other, each look
       // is a hundred cycles and more of a visit's two thousand).
@@ -461,20 +525,25 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
       ptx::tc_fence_after_sync();
       const int key0 = (seg.first + tile) * kManyKeys + half * kVisit;
       float2 t[kVisit / 2];
-      const float top = visit_logits(x, row_scale, key0 + kVisit > all_see, sees - key0, t);
+      const uint32_t even_groups = *reinterpret_cast<const uint32_t*>(x.even_at);  // a byte each
+      const bool even = even_groups == 0x01010101u;
+      float top = visit_logits(x, row_scale, key0 + kVisit > all_see, sees - key0, t);
+      if (!even) top = uneven_top(x, even_groups, row_scale, top, t);
       ptx::tc_fence_before_sync();
       ptx::mbar_arrive_warp(s_free, lane);
       if (v == 0) {
         m = top;
       } else if (__any_sync(0xFFFFFFFFu, there && (top > m + kSlack || (m == -INFINITY && top > m)))) {  // the sums so far
-        const float to = fmaxf(top, m), factor = m == -INFINITY ? 0.f : ptx::ex2_approx(m - to);
-        l *= factor;
+        const float to = fmaxf(top, m), by = m == -INFINITY ? -INFINITY : m - to, factor = ptx::ex2_approx(by), root = ptx::ex2_approx(0.5f * by);
+        l = l * root * root;  // (l may be as large as 2^74: it is not yet 0 where the factor is)
         m = to;
         ptx::mbar_wait_warp(pv_done + ((visits - 1) & 1) * 8, (visits - 1) >> 1 & 1, &ctl.abort);
         ptx::tc_fence_after_sync();
         rescale_output<DIM>(outputs + stream * 128, factor);
       }
-      l += visit_weights(x, weights + buffer * (kVisit / 2), row_scale, m == -INFINITY ? 0.f : m, t);
+      const float base = m == -INFINITY ? 0.f : m;
+      if (!even) l += uneven_weights(x, even_groups, row_scale, base, t);
+      l += visit_weights(x, even_groups, weights + buffer * (kVisit / 2), row_scale, base, t);
       ptx::tmem_st_wait();
       ptx::tc_fence_before_sync();
       ptx::mbar_arrive_warp(p_full + buffer * 8, lane);
@@ -486,14 +555,14 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     ptx::tc_fence_before_sync();
     soft_sync();
     ptx::tc_fence_after_sync();
-    float other = 0.f, back = __uint_as_float((unsigned)(127 - kOffset - kValuePower) << 23);
+    float other = 0.f, back = power_of_two(-kOffset - kValuePower);
     if (!seg.two) {
       const float2 a = ctl.row_ml[0][row], b = ctl.row_ml[1][row];
       m = fmaxf(a.x, b.x);
-      const float base = m == -INFINITY ? 0.f : m, f0 = ptx::ex2_approx(a.x - base), f1 = ptx::ex2_approx(b.x - base);
-      l = a.y * f0 + b.y * f1;
-      other = back * f1;
-      back *= f0;
+      const float base = m == -INFINITY ? 0.f : m, f0 = ptx::ex2_approx(0.5f * (a.x - base)), f1 = ptx::ex2_approx(0.5f * (b.x - base));
+      l = a.y * f0 * f0 + b.y * f1 * f1;  // (roots, as above)
+      other = back * f1 * f1;
+      back *= f0 * f0;
     }
     const bool whole = at.job_first() >= u0 && at.job_end() <= u1, final = whole && c.prefixes == 0;
     const long long level = at.x.own ? 0ll : (long long)c.total_q * c.hq;
@@ -620,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
 }
 
 template <int DIM>
-size_t many_smem(int entries) { return 1024 + Many<DIM>::kOperands + Many<DIM>::kCodes + (entries <= kManyListed ? (size_t)(entries + 1) * 4 : 0); }
+size_t many_smem(int entries) { return 1024 + Many<DIM>::kOperands + Many<DIM>::kCodes + (entries <= many_listed(DIM) ? (size_t)(entries + 1) * 4 : 0); }
 
 template <int DIM, bool FP8, bool LISTED>
 cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
@@ -629,7 +698,7 @@ cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream
     const cudaError_t got = cudaFuncGetAttributes(&a, attend_many_kernel<DIM, FP8, LISTED>);
     if (got != cudaSuccess) return got;
     if (a.numRegs * kThreads < kRegsNeeded) return cudaErrorInvalidConfiguration;  // the softmax's warps would wait for registers for ever
-    return cudaFuncSetAttribute(attend_many_kernel<DIM, FP8, LISTED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many_smem<DIM>(kManyListed));
+    return cudaFuncSetAttribute(attend_many_kernel<DIM, FP8, LISTED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many_smem<DIM>(many_listed(DIM)));
   });
   if (e != cudaSuccess) return e;
   count_launches(1);
@@ -645,7 +714,7 @@ cudaError_t run(const AttendCall& c, const AttendList& list, cudaStream_t stream
 }  // namespace
 
 cudaError_t launch_attend_many(const AttendCall& c, const AttendList& list, cudaStream_t stream) {
-  return list.entries() <= kManyListed ? run<true>(c, list, stream) : run<false>(c, list, stream);
+  return list.entries() <= many_listed(c.cache.dim) ? run<true>(c, list, stream) : run<false>(c, list, stream);
 }
 
 }  // namespace fastav

@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from attend_shapes import ROWS, along, direction, long_problem, place, set_queries
+from attend_shapes import GROUP, ROWS, along, direction, long_problem, place, set_queries
+from test_gpu_attend import Problem
 
 pytestmark = pytest.mark.gpu
 
@@ -28,7 +29,48 @@ def test_large_values_that_lose_their_weight(rows, bits, block, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["int8", "fp8"])
-@pytest.mark.parametrize("rows", ROWS[:1])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("bits", [24, 32, 44])
+def test_a_small_value_with_all_the_weight_among_large_ones(rows, bits, fmt):
+    """Of sixteen neighbours one has all the weight, and values of 2^-bits of the others'."""
+    p = long_problem(rows, fmt, n=1500, causal=False)
+    n = p.lens[0]
+    heavy = torch.arange(n) % 16 == 5
+    set_queries(p, direction(p.dim))
+    place(p, 0, along(torch.where(heavy, 80.0, 0.0) + torch.rand(n, generator=p.gen), p.dim)[:, None].expand(-1, p.hkv, -1),
+          _normal(p, n) * torch.where(heavy, 2.0 ** -bits, 1.0)[:, None, None])
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS[1:])
+@pytest.mark.parametrize("size", [2.0 ** 24, 2.0 ** 40, 1e30])
+def test_hidden_keys_with_large_values_do_not_matter(rows, size, fmt):
+    """Values of the keys that a causal row does not see are larger by `size`; the last row sees them."""
+    p = Problem(8 * GROUP, 8, 128, fmt, 64, [700, rows + 3], [rows, rows], seed=3)
+    for b, n in enumerate(p.lens):
+        v = _normal(p, n)
+        v[n - rows + 1:] *= size
+        place(p, b, v=v)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("size", [1e-9, 2.0 ** -60])
+def test_groups_of_zero_values_among_small_ones(rows, size, fmt):
+    """Every other 16 keys have values of exactly 0, the rest small ones."""
+    p = long_problem(rows, fmt, n=2000)
+    n = p.lens[0]
+    place(p, 0, v=_normal(p, n) * torch.where(torch.arange(n) // 16 % 2 == 0, 0.0, size)[:, None, None])
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS)
 @pytest.mark.parametrize("exponent", [-60, 100, 116, 120, 122, 124])
 def test_values_of_one_extreme_size(rows, exponent, fmt):
     """Up to near the largest bf16: scales of up to 2^119 (e4m3) and 2^121 (int8), in parts that several blocks leave."""
@@ -78,12 +120,21 @@ def test_logits_that_are_almost_nothing(rows, query):
     p.check()
 
 
-@pytest.mark.parametrize("rows", ROWS[:1])
+@pytest.mark.parametrize("rows", ROWS)
 def test_values_near_the_largest_bf16_under_a_growing_maximum(rows):
     """Logits that rise by a few bits from key to key: sums run above their maximum for a while, and nothing may pass fp32's range."""
     p = long_problem(rows, n=2000, causal=False)
     n = p.lens[0]
     set_queries(p, direction(p.dim))
     place(p, 0, along(torch.arange(n) % 64 * 0.9, p.dim)[:, None].expand(-1, p.hkv, -1), _normal(p, n).clamp(-1.9, 1.9) * 2.0 ** 126)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("entries", [1999, 2003])
+def test_lists_of_more_entries_than_shared_memory_has_room_for(entries):
+    """Two rows of 16 heads on one KV head each, head_dim 128: up to 2,000 entries are listed in shared memory."""
+    lens, rows = [i % 9 for i in range(entries - 1)], [2] * (entries - 1)
+    p = Problem(16, 1, 128, "int8", 16, lens, rows, prefix_lens=[5], groups=[3, 1501], seed=16)
     p.run()
     p.check()
