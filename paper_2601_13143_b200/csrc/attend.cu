@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall
   }
   __syncthreads();
   if (kEarly) pdl_wait();
+  if (c.beside && blockIdx.x == 0 && threadIdx.x == 0) *c.ended = 0;
   if (!f.somebody) return;
   Parts found[2];  // of head head0 + lane
   const int lane_head = head0 + lane;
@@ -239,7 +240,7 @@ constexpr double kFewUnitCost = 0.13, kManyUnitCost = 1.7;  // us of an SM (many
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
   bool own_many, shared_many;
-  size_t ahead[2], out[2], lse[2], scratch, copies, whole_out, whole_lse, total = 0;  // offsets into the workspace: few, many
+  size_t ahead[2], out[2], lse[2], scratch, copies, whole_out, whole_lse, ended, total = 0;  // offsets into the workspace: few, many
   bool fits = true;
 };
 
@@ -294,6 +295,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   const size_t rows = p.num_prefixes > 0 ? (size_t)2 * p.total_q * p.num_q_heads : 0;
   w.whole_out = carve(rows * cache.head_dim * sizeof(float));
   w.whole_lse = carve(rows * sizeof(float));
+  w.ended = carve(sizeof(uint64_t));
   w.total = off;
   return w;
 }
@@ -372,6 +374,9 @@ extern "C" int32_t fastav_attend(const fastav_attend_params* p, const fastav_cac
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   c.beside = lists[0].entries() > 0 && lists[1].entries() > 0;
+  lists[1].through_l2 = c.beside;
+  c.ended = reinterpret_cast<uint64_t*>(ws + w.ended);
+  c.ticket = 0xFA57A77E00000000ull + (uint64_t)fastav_kernel_launches();  // another for every call
   if (lists[0].entries() > 0) e = launch_attend_few(c, lists[0], st);
   if (e == cudaSuccess && lists[1].entries() > 0) e = launch_attend_many(c, lists[1], st);
   if (e != cudaSuccess) return cuda_failed(e);

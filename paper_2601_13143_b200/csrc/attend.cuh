@@ -34,6 +34,10 @@ struct AttendCall {
   float* whole_out;
   float* whole_lse;
   int beside;  // both kernels run, side by side on SMs of their own
+  // ... and how the second knows that earlier work has ended, of which its own wait (for the first kernel's end) comes too late to tell it: the first
+  // kernel writes the call's ticket here behind its wait and ahead of letting the second start; the join takes it away.
+  uint64_t* ended;
+  uint64_t ticket;
   int head_wait;
 };
 inline void mark_head(AttendCall& c, bool head) { c.head_wait = head ? 1 : 0; }
@@ -49,6 +53,7 @@ struct AttendList {
   float* part_lse;           // [grid][2][tile_rows], base 2
   float* scratch;            // few: parts that warps of one block exchange
   int32_t* copies;           // many: the blocks' own `ahead`, where there are more entries than shared memory has room for
+  int through_l2;            // index arrays always: the kernel has no wait of its own ahead of its reads
   __host__ __device__ int entries() const { return from_prefix + from_own; }
 };
 
@@ -72,7 +77,7 @@ struct Entry {
   const int32_t* table;
   bool own;
 };
-// Reads of index arrays: after the kernel's wait through L1, ahead of it through L2.
+// Reads of index arrays: after the kernel's wait through L1, ahead of it (or without one, AttendList::through_l2) through L2.
 __device__ __forceinline__ int index_load(const int32_t* p, bool cached) { return cached ? chain_load_cached(p) : chain_load(p); }
 __device__ __forceinline__ Entry entry_of(const AttendCall& c, const AttendList& list, int e, bool& bad, bool cached = true) {
   Entry x;
@@ -136,7 +141,7 @@ __device__ int open_list(const AttendCall& c, const AttendList& list, int* ahead
 #pragma unroll 1
   for (int e = e0; e < e1; ++e) {
     ahead[e] = sum;
-    sum += units_of(c, list, entry_of(c, list, e, bad, c.head_wait));
+    sum += units_of(c, list, entry_of(c, list, e, bad, c.head_wait && !list.through_l2));
   }
   int upto = sum;
 #pragma unroll
@@ -176,7 +181,7 @@ struct Walk {
   __device__ __forceinline__ int job_end() const { return unit - granule + granules; }
   __device__ __forceinline__ void load(const AttendCall& c, const AttendList& list) {
     bool bad = false;  // (reported by open_list)
-    x = entry_of(c, list, e, bad);
+    x = entry_of(c, list, e, bad, !list.through_l2);
     tiles = tiles_of(c, list, x);
     granules = granules_of(list, x);
   }

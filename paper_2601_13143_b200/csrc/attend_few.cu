@@ -80,7 +80,11 @@ attend_few_kernel(AttendCall c, AttendList list) {
   chain_enter_late(c);
   if (c.beside) {
     pdl_wait();
-    pdl_trigger();  // the kernel for many rows starts beside this one; that earlier work has ended holds for it, too
+    if (blockIdx.x == 0) {
+      if (threadIdx.x == 0) ptx::st_release_gpu(c.ended, c.ticket);
+      __syncthreads();  // (ahead of any thread's trigger)
+    }
+    pdl_trigger();  // the kernel for many rows starts beside this one
   }
   const int total = open_list<kThreads>(c, list, ahead, warp_sum);
   pdl_wait();  // the rest may be what earlier work wrote

@@ -167,7 +167,7 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
   int page = 0;              // the page of the tile that `at` stands at, asked for a tile ahead of its keys
   auto find_page = [&] {
     const int key0 = at.granule * kManyKeys + 16 * warp;
-    if (key0 < at.x.len) page = chain_load_cached(at.x.table + (key0 >> c.cache.page_shift));
+    if (key0 < at.x.len) page = index_load(at.x.table + (key0 >> c.cache.page_shift), !list.through_l2);
   };
   auto find_keys = [&] {
     const int key0 = at.granule * kManyKeys + 16 * warp;
@@ -656,6 +656,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(AttendCall c, 
     ptx::fence_barrier_init();
   }
   chain_enter_late(c);
+  // Beside the kernel for few rows: where its ticket is seen, so is all that the work before it wrote.  (It was written ahead of this kernel's start, so
+  // it is seen; if not, this kernel waits until the other has ended, as any would.  Nothing spins.)
+  if (c.beside && !__syncthreads_or(threadIdx.x == 0 && ptx::ld_acquire_gpu(c.ended) == c.ticket)) pdl_wait();
   if (!LISTED && !c.beside) pdl_wait();  // (earlier work may still read what lies there)
   const int total = open_list<kThreads>(c, list, ahead, ctl.warp_sum);
   if (!c.beside) pdl_wait();  // the rest may be what earlier work wrote; and tensor memory is taken when all earlier work has ended

@@ -111,6 +111,14 @@ __device__ __forceinline__ void st_shared4(uint32_t at, uint32_t a, uint32_t b, 
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
+// ---- between kernels of one device: what is seen by whoever writes is seen by whoever then reads this value --------------
+__device__ __forceinline__ void st_release_gpu(uint64_t* at, uint64_t v) { asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(at), "l"(v) : "memory"); }
+__device__ __forceinline__ uint64_t ld_acquire_gpu(const uint64_t* at) {
+  uint64_t v;
+  asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(at) : "memory");
+  return v;
+}
+
 // ---- proxies and fences ------------------------------------------------------------------------
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
