@@ -306,7 +306,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
             const float p = ptx::ex2_approx(fmaf(x, row_scale[g][e], -base));
             l[g][e] += p;
             x = p * v_scale[i];
-            most = fmaxf(most, x);
+            most = fmaxf(most, fabsf(x));
           }
           if (masked) {  // (a place that no key fills may hold any scale)
             most = 0.f;
@@ -314,7 +314,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
             for (int i = 0; i < 4; ++i) {
               float& x = z[g][i / 2][i % 2 * 2 + e];
               if (key0 + 8 * i + n8 >= sees[g][e]) x = 0.f;
-              most = fmaxf(most, x);
+              most = fmaxf(most, fabsf(x));
             }
           }
           over |= most * power[g][e] > kMostWeight || (power[g][e] == 0.f && most > 0.f);
@@ -325,7 +325,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
           float factor[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float most = fmaxf(fmaxf(z[g][0][e], z[g][0][2 + e]), fmaxf(z[g][1][e], z[g][1][2 + e]));
+            float most = fmaxf(fmaxf(fabsf(z[g][0][e]), fabsf(z[g][0][2 + e])), fmaxf(fabsf(z[g][1][e]), fabsf(z[g][1][2 + e])));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
             factor[e] = 1.f;

@@ -138,3 +138,17 @@ def test_lists_of_more_entries_than_shared_memory_has_room_for(entries):
     p = Problem(16, 1, 128, "int8", 16, lens, rows, prefix_lens=[5], groups=[3, 1501], seed=16)
     p.run()
     p.check()
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("some", [False, True])
+def test_a_value_is_its_code_times_its_scale_whatever_the_sign(rows, some):
+    """Scales that are negative, all of them or every third one; values of a cache that others filled."""
+    p = long_problem(rows, n=700)
+    t = torch.arange(700)
+    to, slot, flip = p.tables[0][0].long()[t // 64], t % 64, torch.where((t % 3 == 0) | (not some), -1.0, 1.0)
+    for scales, which in ((p.cache.k_scale, 0), (p.cache.v_scale, 1)):
+        scales[to.cuda(), :, slot.cuda()] *= flip[:, None].cuda()
+        p.tokens[0][which] *= flip[:, None, None]
+    p.run()
+    p.check()
