@@ -263,7 +263,7 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
   auto takes_many = [&](long long rows) { return rows * group > kMostFew; };
   w.own_many = takes_many(p.max_qlen);
   w.shared_many = p.num_prefixes > 0 && takes_many(p.max_prefix_q);
-  const long long own_rows = w.own_many ? 0 : p.max_qlen * group, shared_rows = w.shared_many ? 0 : p.max_prefix_q * group;
+  const long long own_rows = w.own_many ? 0 : p.max_qlen * group, shared_rows = p.num_prefixes == 0 || w.shared_many ? 0 : p.max_prefix_q * group;
   w.few.tile_rows = std::max(own_rows, shared_rows) <= 8 ? 8 : 16;
   (w.own_many ? w.many : w.few).from_own = p.batch;
   (w.shared_many ? w.many : w.few).from_prefix = p.num_prefixes;
