@@ -222,7 +222,7 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     // values' scales: a value row that is not finite makes the weights of the rows that see it NaN, not everybody's sums
     const bool good = fabsf(value) < INFINITY;
     const int own = max(good ? (int)(__float_as_uint(fabsf(value)) >> 23) - 126 : kLeastExponent, kLeastExponent);  // |value| <= 2^own
-    unsigned both = (unsigned)own << 16 | (lane < exist ? -own : -1000) & 0xFFFF;  // the largest; the least, negated
+    unsigned both = (unsigned)own << 16 | (lane < exist && good ? -own : -1000) & 0xFFFF;  // the largest; the least, negated
 #pragma unroll
     for (int d = 8; d; d >>= 1) both = __vmaxs2(both, __shfl_xor_sync(0xFFFFFFFFu, both, d));
     const int largest = (int)both >> 16;
