@@ -388,7 +388,7 @@ typedef struct fastav_cache { /* host memory; read at call time */
   int32_t page_tokens;        /* 16, 32, 64, 128 or 256 */
   int32_t num_pages;          /* >= 1 */
   int32_t num_kv_heads, head_dim; /* as in fastav_params; head_dim 64 or 128 */
-  void *k, *v;                /* device, 128-byte aligned */
+  void *k, *v;                /* device, 128-byte aligned (rows in whole lines) */
   float *k_scale, *v_scale;   /* device, 16-byte aligned */
 } fastav_cache;
 
@@ -422,7 +422,7 @@ int32_t fastav_cache_read(const fastav_params* params, const fastav_cache* cache
                           void* stream);
 
 /* Shapes of one fastav_attend call (host memory). */
-typedef struct fastav_attend_params {
+typedef struct fastav_attend_params { /* bounds: loose ones change no result, but they choose the kernel and how the SMs are shared out */
   int32_t batch;               /* B >= 1; batch + num_prefixes <= FASTAV_ATTEND_MAX_BATCH */
   int32_t total_q, max_qlen;   /* sum_b R_b = cu_qlens[B]; max_b R_b (upper bounds are fine) */
   int32_t num_q_heads;         /* a multiple of the cache's num_kv_heads */

@@ -88,8 +88,9 @@ __device__ __forceinline__ Belongs belongs_to(const AttendCall& c, const AttendL
 //
 // Bound by latency: a few trips to memory one after the other (the row's sequence; its bounds; the parts' statistics; the parts).  So a lane
 // asks for one part's statistics each, and where rows are few and parts many, WARPS warps share those of a (row, head), eight at a time
-// each (1 x 1,024 keys, 28 heads of up to 32 parts: 7.3 us instead of 24 with a warp that went through them four at a time).  Many rows: a
-// warp takes HEADS heads of a row and finds their jobs in as many lanes (41,000 (row, head): 36 us instead of 51).
+// each (1 x 1,024 keys, 28 heads of up to 32 parts: the call in 13.3 us instead of 23.7 with a warp that went through them four at a time, in a step that
+// also spared 64-bit divisions).  Many rows: a warp takes HEADS heads of a row and finds their jobs in as many lanes (41,000 (row, head): 36 us
+// instead of 51).
 template <int DIM, int WARPS, int HEADS>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendCall c, AttendList own, AttendList shared) {
   static_assert(WARPS == 1 || HEADS == 1);
@@ -231,11 +232,11 @@ cudaError_t launch_join(const AttendCall& c, const AttendList& own, const Attend
 }
 
 // The levels' entries go to the kernel that suits their stacked rows: few (mma.sync) up to 16, which an instruction pair takes at once, many (tcgen05)
-// beyond.  us, few / many: one sequence of 60 keys of 8 heads, 48 rows 15.3 / 13.5, of 1,000, 24 rows 17.9 / 16.0; 28 rows on 4 heads: 4,000 keys
+// beyond.  us, few / many, when the rule was made: one sequence of 60 keys of 8 heads, 48 rows 15.3 / 13.5, of 1,000, 24 rows 17.9 / 16.0; 28 rows on 4 heads: 4,000 keys
 // 19.8 / 17.5, 8 x 3,000 keys 35.5 / 26.3, a prefix of 4,000 for seven rows each of four sequences with few rows of their own 21.2 / 22.5;
 // 8 sequences of 500 to 744 keys, up to 32 rows on 2 heads of 64, 14.4 / 14.9; 16 rows of 8 heads, 16 x 2,000 keys 39.3 / 43.3, one of 4,000 19.9 / 18.7.
 constexpr int kMostFew = 16;
-constexpr double kFewUnitCost = 0.13, kManyUnitCost = 1.7;  // us of an SM (many at 1.2 / 1.7 / 2.2 / 3: 32 answers 37.7 / 37.5 / 38.9 / 42.8, 64 44.4 / 42.0 / 42.2 / 40.5)
+constexpr double kFewUnitCost = 0.13, kManyUnitCost = 1.7;  // us of an SM (many at 1.2 / 1.7 / 2.2 / 3, then: 32 answers 37.7 / 37.5 / 38.9 / 42.8, 64 44.4 / 42.0 / 42.2 / 40.5)
 
 struct Plan {
   AttendList few{}, many{};   // lists of the two kernels; without entries: not launched
@@ -274,8 +275,8 @@ Plan make_plan(const fastav_attend_params& p, const fastav_cache& cache) {
                most_units(p, cache, *lists[i], lists[i]->from_prefix, p.max_prefix_q, p.max_prefix_len);
     w.fits &= units[i] < INT_MAX;
   }
-  // Where both kernels run, they do so side by side, the SMs shared out by what their units cost (one behind the other, each is a start of 6 to 8
-  // us and an end: 32 answers on a shared 16,384-token prefix 46.5 us instead of 40.4; 37.5 since).
+  // Where both kernels run, they do so side by side, the SMs shared out by what their units cost by the host's bounds (one behind the other, each is a start of
+  // 6 to 8 us and an end: 32 answers on a shared 16,384-token prefix 46.5 us instead of 40.4 at that step; 41.6 now).
   int sms[2] = {kNumSMs, kNumSMs};
   if (units[0] > 0 && units[1] > 0) {
     const double few = (double)units[0] * kFewUnitCost, many = (double)units[1] * kManyUnitCost;

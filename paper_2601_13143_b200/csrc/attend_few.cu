@@ -15,7 +15,7 @@
 //
 // The query rows as the rows of the instructions (half of each empty with 8 rows, 243 registers, 8 warps): 4 x 16,384 keys 48.9 us
 // instead of 46.2 at that step.  Now: 36.6 us (138 MB, 3.8 TB/s; the loop about half of that time, at the copy's rate, the start of a block, its
-// warps' join and the join kernel the rest), 32 sequences of 512 to 4,096 keys 28.5 us (83 MB).
+// warps' join and the join kernel the rest), 32 sequences of 512 to 4,096 keys 29.0 us (83 MB).
 #include <limits.h>
 
 #include "attend.cuh"

@@ -28,7 +28,7 @@
 // exponentials twice: 16 questions on 16,384 keys with every eighth group uneven 611 us instead of 527 at that step.  (The scales multiplying
 // the weights in fp32 in every group: 607 us.  What it takes is not the products, 12 us, but two 16-byte loads per eight logits, which every lane of a warp gets.)
 //
-// 16 questions of 64 to 128 tokens on 16,384 keys (346 GFLOP): 521 us, 0.66 PFLOP/s.  Bound by the chains of the converting and softmax warps per
+// 16 questions of 64 to 128 tokens on 16,384 keys (346 GFLOP): 523 us, 0.66 PFLOP/s.  Bound by the chains of the converting and softmax warps per
 // tile (5,200 cycles, of which the MMAs take 2,600 and the exponentials 2,000).  Taking the weights with the maximum so far first, and a new one
 // only where f16 overflows, spills: 619 us instead of 500 at that step.
 //

@@ -183,8 +183,9 @@ cache_rows_kernel(RowsCall c, uint16_t* __restrict__ k, uint16_t* __restrict__ v
   __syncthreads();
 
   // A group of kLanes lanes keeps to one head of K or V and walks over the block's tokens, so that all of an address but the token's row is
-  // known beforehand; with fewer heads than groups several of these share a head's tokens.  (Survivors of 4 x 16,384 tokens, int8, 163 MB: 41.3
-  // us; without the arithmetic 37.  Tried: rows copied into shared memory ahead of their use, 94 us for the ragged batch instead of 65; a
+  // known beforehand; with fewer heads than groups several of these share a head's tokens.  (Survivors of 4 x 16,384 tokens, int8, 163 MB: 40.5
+  // us; without the arithmetic 37: what takes the time is issued per row and address, 0.7 instructions a cycle and scheduler, some 140 of a warp for two
+  // rows of 128.  Tried: rows copied into shared memory ahead of their use, 94 us for the ragged batch instead of 65; a
   // warp per few tokens with eight rows unrolled, 102; the scales gathered in shared memory and written head by head, 48.8.)
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, heads = 2 * c.cache.hkv;
   const int sharing = max(1, kRows / heads), step = min(kRows, heads);
@@ -278,8 +279,9 @@ int32_t check_cache(const fastav_cache* c) {
   if (c->format != FASTAV_CACHE_INT8 && c->format != FASTAV_CACHE_FP8) return FASTAV_ERR_UNSUPPORTED;
   if (c->head_dim != 64 && c->head_dim != 128) return FASTAV_ERR_UNSUPPORTED;
   if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return FASTAV_ERR_UNSUPPORTED;
+  // (128 bytes: a row of codes lies in one line, which fastav_attend calls into L2 by one prefetch per row)
   if (!aligned(c->k, 128) || !aligned(c->v, 128) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)) return FASTAV_ERR_UNSUPPORTED;
-  // a row of the pool is a 32-bit coordinate of the copies that fastav_attend reads it with; a block's rows one of this file's
+  // fastav_attend's kernel for many rows counts rows of the pool in 32 bits; with the heads bounded no product of counts here overflows
   if (c->num_kv_heads > 1024 || (long long)c->num_pages * c->num_kv_heads * c->page_tokens > INT_MAX) return FASTAV_ERR_UNSUPPORTED;
   return FASTAV_OK;
 }
