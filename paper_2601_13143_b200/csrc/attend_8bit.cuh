@@ -44,6 +44,15 @@ __device__ __forceinline__ float to_one(float magnitude) {
 // 1 / x of a power of two that to_one gives (times a small one).
 __device__ __forceinline__ float inverse_power(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
 
+// m + log2(l), -inf for l = 0.  m and log2(l) may be large where their sum is not (m holds the exponents of values' scales), so l's exponent goes to m
+// first, exactly: 70 + log2f(2^-70) alone is off by 2^-18.
+__device__ __forceinline__ float plus_log2(float m, float l) {
+  if (l == 0.f) return -INFINITY;
+  if (!(l < INFINITY)) return l;
+  const int bits = (int)__float_as_uint(l), k = (bits >> 23) - 127;
+  return m + (float)k + log2f(__uint_as_float((unsigned)(bits - (k << 23))));
+}
+
 // A query row as f16.  It is multiplied by a power of two that lays its largest magnitude on 2^15 .. 2^16 (bf16's largest mantissa there is
 // 65,280; f16 ends at 65,504).  Elements of 2^-32 of the largest and more are exact then; f16's last step being 2^-24, smaller ones are off by at
 // most 2^-40 of it.  (Laid on 1 .. 2, those below 2^-17 lost bits, and that showed wherever no key answers the largest element.)

@@ -398,7 +398,7 @@ attend_few_kernel(AttendCall c, AttendList list) {
             const int row = 8 * g + 2 * t4 + e, i = at.tile * kTile + row, r = query_row(c, i);
             if (r >= at.x.rows) continue;
             const float back = power[g][e] == 0.f ? 0.f : inverse_power(power[g][e]), inv = l[g][e] == 0.f ? 0.f : 1.f / l[g][e];
-            const float lse = l[g][e] == 0.f ? -INFINITY : m[g][e] + log2f(l[g][e]);
+            const float lse = plus_log2(m[g][e], l[g][e]);
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {  // (in this order no product leaves fp32's range)
               o[g][j][e] = o[g][j][e] * inv * back;

@@ -56,8 +56,8 @@ constexpr int kEven = 6;
 constexpr int kOffset = 12;                      // the largest weight of a row's first visit is up to 2^kOffset ...
 constexpr float kSlack = 3.9f;                   // ... and the maximum is moved when one would be this much (log2) above that (f16 ends at 2^16)
 // Bounds of the exponents.  A key's from kLeastExponent on: 2^(z - m) stays below 2^74 (value rows that are smaller, 10^-19 and less, keep fewer bits).
-// E of an uneven group: its weights without their scales stay below 2^116, and above 2^-80 where all scales are as large as can be.
-constexpr int kLeastExponent = -70, kLeastGroup = -16, kMostGroup = 30;
+// E of an uneven group up to kMostGroup: its weights without their scales stay below 2^116, and above 2^-80 where all scales are as large as can be.
+constexpr int kLeastExponent = -70, kMostGroup = 30;
 constexpr int kTmemCols = 512, kWeightsAt = 2 * kVisit, kOutputAt = kWeightsAt + 4 * (kVisit / 2);  // columns: S, P, O
 static_assert(kConvWarps == kGroups && kOutputAt + 2 * 128 <= kTmemCols);
 
@@ -227,7 +227,7 @@ __device__ __forceinline__ void convert_keys(const AttendCall& c, const AttendLi
     for (int d = 8; d; d >>= 1) both = __vmaxs2(both, __shfl_xor_sync(0xFFFFFFFFu, both, d));
     const int largest = (int)both >> 16;
     const bool even = largest + (int)(short)both <= kEven;  // (lanes 0 to 15)
-    const int e = even ? largest : min(max(largest, kLeastGroup), kMostGroup);
+    const int e = even ? largest : min(largest, kMostGroup);
     const float factor = !good ? 0.f : even ? value * power_of_two(kValuePower - e) : copysignf(1 << kValuePower, value), coarse = __uint_as_float(__float_as_uint(factor) & 0xFFFFE000u);
     const uint32_t factors = two_f16(coarse, factor - coarse);
     const float key_scale = good ? key * kKeyScaleFactor : __uint_as_float(0x7FC00000u);
@@ -567,7 +567,7 @@ __device__ __forceinline__ void softmax(const AttendCall& c, const AttendList& l
     const bool whole = at.job_first() >= u0 && at.job_end() <= u1, final = whole && c.prefixes == 0;
     const long long level = at.x.own ? 0ll : (long long)c.total_q * c.hq;
     const long long part = ((long long)blockIdx.x * 2 + (at.job_first() < u0 ? 0 : 1)) * kManyTile;  // the block's place for what it did not finish
-    const float inv = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + log2f(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l, lse = plus_log2(m, l);
     back *= inv;
     other *= inv;
     // A stream writes its rows; where both have the same ones, half of the columns each.  By kWide columns through shared memory (the query

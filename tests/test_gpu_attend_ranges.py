@@ -152,3 +152,15 @@ def test_a_value_is_its_code_times_its_scale_whatever_the_sign(rows, some):
         p.tokens[0][which] *= flip[:, None, None]
     p.run()
     p.check()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("size", [0.0, 2.0 ** -62, 1e-9, 1e9, 2.0 ** 110])
+def test_log_sum_exps_near_zero_beside_values_of_any_size(rows, size, fmt):
+    """A few keys, logits of a few bits: the log-sum-exp is small and the exponents of the values' scales are not."""
+    p = Problem(8 * GROUP, 8, 64, fmt, 64, [1, 2, 3, 5], [rows] * 4, causal=False, seed=17)
+    for b, n in enumerate(p.lens):
+        place(p, b, v=_normal(p, n, seed=18 + b) * size)
+    p.run()
+    p.check()
