@@ -452,7 +452,7 @@ typedef struct fastav_attend_params { /* bounds: loose ones change no result, bu
  *
  * Sums, maxima and statistics are fp32; weights are rounded to 11 bits (f16) for the matrix pipe, and so are values with their scales where more than
  * 16 rows (query rows times G) go together.  Elements of a query row below 2^-32 of its largest are rounded to 2^-39 of it.  Values may be of any size up to the
- * largest bf16 and are mixed as they come; V rows below 1e-19 keep fewer bits with more than 16 rows, and where V rows that a query row sees differ in size by
+ * largest bf16 and are mixed as they come; V rows and outputs below 1e-19 keep fewer bits with more than 16 rows, and where V rows that a query row sees differ in size by
  * more than 2^100 the smaller ones' share may be lost.
  *
  *   q            [total_q, Hq, head_dim] bf16
