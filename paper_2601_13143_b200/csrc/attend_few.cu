@@ -6,7 +6,7 @@
 // same operands from the cache).  Codes become f16 exactly on their way from shared memory; a query row is scaled by a power of two first
 // and exact in f16 down to 2^-32 of its largest element (query_power); the keys' scales multiply the logits, the values' scales the weights.  The weights
 // 2^(z - m) vs are rounded to f16 (11 bits; the output has 8) after another power of two per row.  Running maxima move only when a logit
-// is 2^8 above them, so that the sums are hardly ever rescaled.
+// is 6 above them, so that the sums are hardly ever rescaled.
 //
 // Any order of the contractions will do as long as both operands have it.  Lane 4 n + t holds, of query row n and of keys n and n + 8 of
 // sixteen, the elements DIM/4 t ..; of V the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9 and the elements DIM/8 n ..: 16-byte reads (8 for head_dim 64),

@@ -24,8 +24,8 @@
 // largest product of weight and scale where the scales of sixteen neighbours are alike, 2^-30 where they differ by 2^kEven.
 //
 // Other groups (a row of zeros, an outlier, a hidden key's large value) would lose the smaller values that way: f16 has no room for both.  There
-// a value's operand is its code alone, log2 of its scale joins its own logit, and the weights are summed up ahead of that.  That takes the
-// exponentials twice: 16 questions on 16,384 keys with every eighth group uneven 611 us instead of 527 at that step.  (The scales multiplying
+// a value's operand is its code alone, its own scale's exponent e counts for m, log2 of the scale joins its logit, and the weights are summed up ahead of that.  That
+// takes the exponentials twice: 16 questions on 16,384 keys with every eighth group uneven 611 us instead of 527 at that step.  (The scales multiplying
 // the weights in fp32 in every group: 607 us.  What it takes is not the products, 12 us, but two 16-byte loads per eight logits, which every lane of a warp gets.)
 //
 // 16 questions of 64 to 128 tokens on 16,384 keys (346 GFLOP): 523 us, 0.66 PFLOP/s.  Bound by the chains of the converting and softmax warps per
