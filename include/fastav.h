@@ -13,7 +13,8 @@
  *     fastav_prune    all three in one enqueue
  *
  * and beside it what its survivors are kept and used with: an 8-bit cache and the attention over it (fastav_cache_write,
- * fastav_cache_read, fastav_attend).
+ * fastav_cache_read, fastav_attend), how new tokens come there (fastav_rotate, fastav_rotate_write) and how the cache is pruned while answers
+ * are written (fastav_cache_weigh, fastav_cache_evict).
  *
  * Conventions shared by every call
  *   - Plain C.  No CUDA types: `stream` is a cudaStream_t passed as void*.
@@ -471,6 +472,125 @@ int32_t fastav_attend(const fastav_attend_params* params, const fastav_cache* ca
                       const int32_t* page_table, const int32_t* kv_lens, const int32_t* cu_prefix, const int32_t* prefix_table,
                       const int32_t* prefix_lens, void* out, float* lse_out_opt, void* workspace, size_t workspace_bytes,
                       int32_t* device_status, void* stream);
+
+/*
+ * ---- Queries and keys in their positions, new tokens straight into the cache --------------------------------
+ *
+ * What lies between a layer's projection and the calls above: every head's row of q and k may be normed, and is rotated by its token's
+ * position, on one axis or on several (time, height and width of audio-visual prompts):
+ *
+ *     fastav_rotate        q and k of a prompt (then scored, pruned, written by their keep list, or attended to)
+ *     fastav_rotate_write  new tokens: q as above, K (rotated) and V quantised into the cache's pages in the same pass
+ *
+ * A row x of head_dim elements becomes
+ *
+ *     y_i  = x_i w_i / sqrt(mean_j x_j^2 + norm_eps)                          where the side has norm weights w, else x_i
+ *     pair p of rotary_dim / 2: (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),   t = pos[axis[p]] * frequency[p]
+ *
+ * with (a, b) = (p, p + rotary_dim / 2), or (2 p, 2 p + 1) under FASTAV_ROTATE_INTERLEAVED; elements from rotary_dim on are not rotated.
+ * t is taken modulo a turn in 64-bit integers (the error of a position far out is that of frequency's own last bit), sines, cosines, the
+ * norm and the rotation are fp32, and the result is rounded once: to bf16, or for K in the cache straight to its code (not to bf16 first).
+ */
+#define FASTAV_ROTATE_INTERLEAVED 0x2000u
+#define FASTAV_ROTATE_MAX_PAIRS 64
+#define FASTAV_ROTATE_MAX_AXES 4
+
+typedef struct fastav_rotate_params { /* host memory; read at call time */
+  int32_t batch;                      /* fastav_rotate_write: B >= 1.  fastav_rotate does not read it */
+  int32_t total_tokens;               /* N (fastav_rotate_write: cu_seqlens[B], an upper bound is fine) */
+  int32_t num_q_heads, num_kv_heads, head_dim; /* any counts >= 1; head_dim 64 or 128 */
+  int32_t rotary_dim;                 /* a multiple of 16 up to head_dim; 0: no rotation (pos may be NULL) */
+  int32_t num_axes;                   /* 1 to 4 */
+  float norm_eps;                     /* 1e-20 or more where norm weights are given (squares below 2^-126 are lost beside it) */
+  uint32_t flags;                     /* FASTAV_ROTATE_INTERLEAVED, FASTAV_CHAIN_CALLS (here: pos, the norm weights, cu_seqlens, the page table
+                                         and start_opt were complete before the preceding work) */
+  int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head;
+  int64_t qo_stride_tok, qo_stride_head, ko_stride_tok, ko_stride_head;
+  int64_t pos_stride_tok, pos_stride_axis;   /* pos[axis * pos_stride_axis + token * pos_stride_tok] */
+  uint8_t axis[FASTAV_ROTATE_MAX_PAIRS];     /* of each pair, below num_axes */
+  double frequency[FASTAV_ROTATE_MAX_PAIRS]; /* of each pair, radians per position; finite */
+} fastav_rotate_params;
+
+/*
+ *   q, k        [N, Hq, head_dim], [N, Hkv, head_dim] bf16; either may be NULL with its output and is skipped
+ *   pos         int32, strides from params; any value
+ *   q_norm_opt, k_norm_opt  [head_dim] bf16 or NULL (that side is not normed)
+ *   q_out, k_out  the same shapes; may be q and k themselves (with their strides), must not overlap them otherwise
+ */
+int32_t fastav_rotate(const fastav_rotate_params* params, const void* q, const void* k, const int32_t* pos, const void* q_norm_opt,
+                      const void* k_norm_opt, void* q_out, void* k_out, void* stream);
+
+/*
+ * Sequence b's new tokens are cu_seqlens[b] ... of q, k, v and pos, and become tokens start_opt[b], start_opt[b] + 1, ... of the cached
+ * sequence (NULL: 0, 1, ...), laid down as fastav_cache_write lays rows down (its rules for rows without a place hold).  q and q_out may be
+ * NULL.  Rows of q_out behind cu_seqlens[B] are left as they are.  ko_ strides are not read.
+ */
+int32_t fastav_rotate_write(const fastav_rotate_params* params, const fastav_cache* cache, const void* q, const void* k, const void* v,
+                            const int32_t* pos, const void* q_norm_opt, const void* k_norm_opt, const int32_t* cu_seqlens,
+                            const int32_t* page_table, int32_t table_stride, const int32_t* start_opt, void* q_out, int32_t* device_status,
+                            void* stream);
+
+/*
+ * ---- Pruning the cache while answers are written -------------------------------------------------------------
+ *
+ * Section 2.2's rule (what gets the least attention goes) for a cache that grows: the attention that each cached token gets is summed up
+ * per KV head, and the lightest tokens are evicted.
+ *
+ *     fastav_cache_weigh   adds what a call's query rows pay to each token
+ *     fastav_cache_evict   keeps the heaviest tokens, in order, in place or in other pages
+ *
+ * Weights are a pool of their own beside the scales: [num_pages, num_kv_heads, page_tokens] fp32, 16-byte aligned.
+ */
+
+/*
+ * For sequence b with n_b = kv_lens[b] tokens, KV head h and token j < n_b:
+ *
+ *   weights[j, h] = decay * (j < weighed_lens_opt[b] ? weights[j, h] : 0) + sum_{r: j in V(r)} sum_{heads g of h} exp(scale <q[r,g,:], k_j> - lse[r, g])
+ *
+ * V(r) as in fastav_attend: all n_b tokens, or j <= n_b - R_b + r under FASTAV_CAUSAL.  lse is what fastav_attend returned for these rows (a
+ * prefix's share in it, too); a row whose lse is -inf pays nothing.  weighed_lens_opt: tokens from there on (new ones) have no weight yet and
+ * their places are not read; NULL: all have.  With decay 0 none is read.
+ *
+ * Of params: batch, total_q, max_qlen, num_q_heads, max_kv_len, table_stride, the strides of q, softmax_scale, FASTAV_CAUSAL, FASTAV_CHAIN_CALLS
+ * (here: cu_qlens, kv_lens, weighed_lens_opt and the page table).  The params of the attention's own call serve; its prefixes are not read: their
+ * tokens are weighed by a call of their own, with the prefixes as sequences, the rows that share one as its rows (cu_qlens at its sequences' edges) and without
+ * FASTAV_CAUSAL.
+ *
+ * Sums are fp32, in a fixed order; parts below 2^-126 count as 0.  No two sequences may have a token in the same place.  A sequence without query rows gets decay * weights.  An entry
+ * of the table that names no page sets FASTAV_DEV_BAD_INDEX, and its tokens are left out.  decay: finite, >= 0.
+ */
+int32_t fastav_cache_weigh(const fastav_attend_params* params, const fastav_cache* cache, float* weights, float decay, const void* q,
+                           const float* lse, const int32_t* cu_qlens, const int32_t* page_table, const int32_t* kv_lens,
+                           const int32_t* weighed_lens_opt, int32_t* device_status, void* stream);
+
+#define FASTAV_EVICT_JOINT 0x4000u /* one set of tokens for all KV heads of a sequence, by the sum of their weights (in 64 bits, rounded to fp32) */
+
+typedef struct fastav_evict_params { /* host memory */
+  int32_t batch, max_kv_len, max_keep;        /* B >= 1; max_b n_b, max_b k_b (upper bounds are fine) */
+  int32_t table_stride, out_table_stride;     /* entries per row */
+  int32_t first, recent;                      /* so many tokens at a sequence's front and end always stay (and count toward k_b) */
+  uint32_t flags;                             /* FASTAV_EVICT_JOINT, FASTAV_CHAIN_CALLS (here: kv_lens, keep_counts and the page tables) */
+} fastav_evict_params;
+
+/*
+ * Per sequence b and KV head, of n_b = kv_lens[b] tokens the k_b = keep_counts[b] heaviest stay; equal weights go to the lower index, the
+ * first and the recent ones rank above every weight, NaN below.  Survivors move together without changing their order: codes, scales and weights of
+ * the i-th become those of token i.  k_b outside [0, n_b] is clamped (FASTAV_DEV_K_CLAMPED); more first and recent tokens than k_b: the
+ * lowest-index ones stay (FASTAV_DEV_PROTECT_OVERFLOW).
+ *
+ *   out_table_opt    [B, out_table_stride] int32: pages where the survivors go, none of which holds a token of the call.  NULL: in place; no two
+ *                    sequences may share a page then.
+ *   kv_lens_out      [B] int32: k_b.  Must not be kv_lens.
+ *   keep_idx_out_opt [B, Hkv, max_keep] int32 or NULL: where survivor i was; places behind k_b are left as they are
+ *   workspace        fastav_evict_workspace_bytes() bytes, 256-byte aligned
+ *
+ * Places of the cache behind the survivors are left as they are.  A token whose entry in the table names no page of the pool ranks lowest; such
+ * rows, and rows that an entry of out_table_opt sends to no page, are left out (FASTAV_DEV_BAD_INDEX).
+ */
+int32_t fastav_evict_workspace_bytes(const fastav_evict_params* params, const fastav_cache* cache, size_t* out_bytes);
+int32_t fastav_cache_evict(const fastav_evict_params* params, const fastav_cache* cache, float* weights, const int32_t* page_table,
+                           const int32_t* kv_lens, const int32_t* keep_counts, const int32_t* out_table_opt, int32_t* kv_lens_out,
+                           int32_t* keep_idx_out_opt, void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream);
 
 /*
  * Number of kernels this library has launched in this process so far (a diagnostic counter).

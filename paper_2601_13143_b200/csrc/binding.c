@@ -146,6 +146,79 @@ static PyObject* attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+/* A pool of weights beside a cache's scales: as many bytes as those. */
+static int weights_of(PyObject* o, PyObject* scales, void** out) {
+  size_t bytes, want;
+  if (size_of(o, &bytes) || size_of(scales, &want)) return -1;
+  if (bytes != want) {
+    PyErr_SetString(PyExc_ValueError, "expected fp32 weights [pages, KV heads, page tokens], as the cache's scales");
+    return -1;
+  }
+  return pointer(o, out);
+}
+
+/* (function, params, q, k, pos, q_norm, k_norm, q_out, k_out, stream) */
+static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *t[7], *stream;
+  if (expect("rotate", n, 10) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || pointers(a + 2, 7, t)) return NULL;
+  stream = address(a[9]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_rotate))f)(p, t[0], t[1], t[2], t[3], t[4], t[5], t[6], stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (function, params, cache, q, k, v, pos, q_norm, k_norm, cu_seqlens, page_table, table_stride, start, q_out, device_status, stream) */
+static PyObject* rotate_write(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *c, *t[8], *u[3], *stream;
+  if (expect("rotate_write", n, 16) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) ||
+      pointers(a + 3, 8, t) || pointers(a + 12, 3, u))
+    return NULL;
+  const long stride = PyLong_AsLong(a[11]);
+  stream = address(a[15]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_rotate_write))f)(p, c, t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], (int32_t)stride, u[0], u[1], u[2], stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (function, params, cache, the cache's scales, weights, decay, q, lse, cu_qlens, page_table, kv_lens, weighed_lens, device_status, stream) */
+static PyObject* cache_weigh(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *c, *w, *t[7], *stream;
+  if (expect("cache_weigh", n, 14) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) ||
+      weights_of(a[4], a[3], &w) || pointers(a + 6, 7, t))
+    return NULL;
+  const double decay = PyFloat_AsDouble(a[5]);
+  stream = address(a[13]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_cache_weigh))f)(p, c, w, (float)decay, t[0], t[1], t[2], t[3], t[4], t[5], t[6], stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (function, params, cache, the cache's scales, weights, page_table, kv_lens, keep_counts, out_table, kv_lens_out, keep_idx_out, workspace, device_status,
+   stream) */
+static PyObject* cache_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *f, *p, *c, *w, *t[6], *ws, *status, *stream;
+  size_t bytes;
+  if (expect("cache_evict", n, 14) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) ||
+      weights_of(a[4], a[3], &w) || pointers(a + 5, 6, t) || pointer(a[11], &ws) || size_of(a[11], &bytes) || pointer(a[12], &status))
+    return NULL;
+  stream = address(a[13]);
+  if (PyErr_Occurred()) return NULL;
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((__typeof__(&fastav_cache_evict))f)(p, c, w, t[0], t[1], t[2], t[3], t[4], t[5], ws, bytes, status, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {
     {"prune", (PyCFunction)(void (*)(void))prune, METH_FASTCALL, "fastav_prune"},
     {"select_mask", (PyCFunction)(void (*)(void))select_mask, METH_FASTCALL, "fastav_select_mask"},
@@ -153,6 +226,10 @@ static PyMethodDef methods[] = {
     {"cache_write", (PyCFunction)(void (*)(void))cache_write, METH_FASTCALL, "fastav_cache_write"},
     {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, "fastav_cache_read"},
     {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, "fastav_attend"},
+    {"rotate", (PyCFunction)(void (*)(void))rotate, METH_FASTCALL, "fastav_rotate"},
+    {"rotate_write", (PyCFunction)(void (*)(void))rotate_write, METH_FASTCALL, "fastav_rotate_write"},
+    {"cache_weigh", (PyCFunction)(void (*)(void))cache_weigh, METH_FASTCALL, "fastav_cache_weigh"},
+    {"cache_evict", (PyCFunction)(void (*)(void))cache_evict, METH_FASTCALL, "fastav_cache_evict"},
     {NULL, NULL, 0, NULL},
 };
 

@@ -18,6 +18,8 @@ FASTAV_PROTECT_QUERY_ROWS = 2
 FASTAV_KEEP_IDX_GLOBAL = 4
 FASTAV_SELECT_LOWEST = 0x800
 FASTAV_CHAIN_CALLS = 0x1000
+FASTAV_ROTATE_INTERLEAVED = 0x2000
+FASTAV_EVICT_JOINT = 0x4000
 
 FASTAV_SCORE_PATH_GENERIC = 0x100
 FASTAV_SCORE_PATH_NARROW = 0x200
@@ -46,7 +48,9 @@ EXPORTS = ("fastav_version", "fastav_status_string", "fastav_last_cuda_error", "
            "fastav_prune_host", "fastav_kernel_launches", "fastav_select_noalloc", "fastav_select_mask", "fastav_selftest_bounded_wait",
            "fastav_rollout_state_bytes", "fastav_rollout_workspace_bytes", "fastav_rollout_begin", "fastav_rollout_layer",
            "fastav_rollout_read", "fastav_rollout_threshold", "fastav_cache_write", "fastav_cache_read", "fastav_attend_workspace_bytes",
-           "fastav_attend")
+           "fastav_attend", "fastav_rotate", "fastav_rotate_write", "fastav_cache_weigh", "fastav_evict_workspace_bytes", "fastav_cache_evict")
+
+ROTATE_MAX_PAIRS = 64
 
 
 class fastav_params(ctypes.Structure):
@@ -86,6 +90,33 @@ class fastav_attend_params(ctypes.Structure):
         ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
         ("o_stride_tok", ctypes.c_int64), ("o_stride_head", ctypes.c_int64),
         ("softmax_scale", ctypes.c_float),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class fastav_rotate_params(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("total_tokens", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+        ("norm_eps", ctypes.c_float),
+        ("flags", ctypes.c_uint32),
+        ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+        ("k_stride_tok", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+        ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+        ("qo_stride_tok", ctypes.c_int64), ("qo_stride_head", ctypes.c_int64),
+        ("ko_stride_tok", ctypes.c_int64), ("ko_stride_head", ctypes.c_int64),
+        ("pos_stride_tok", ctypes.c_int64), ("pos_stride_axis", ctypes.c_int64),
+        ("axis", ctypes.c_uint8 * ROTATE_MAX_PAIRS),
+        ("frequency", ctypes.c_double * ROTATE_MAX_PAIRS),
+    ]
+
+
+class fastav_evict_params(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("max_kv_len", ctypes.c_int32), ("max_keep", ctypes.c_int32),
+        ("table_stride", ctypes.c_int32), ("out_table_stride", ctypes.c_int32),
+        ("first", ctypes.c_int32), ("recent", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
     ]
 
@@ -180,6 +211,17 @@ def library() -> ctypes.CDLL:
         lib.fastav_attend_workspace_bytes.argtypes = [ap, cp, szp]
         lib.fastav_attend.restype = ctypes.c_int32
         lib.fastav_attend.argtypes = [ap, cp, vp, i32p, i32p, i32p, i32p, i32p, i32p, vp, vp, vp, ctypes.c_size_t, i32p, vp]
+        rp, ep = ctypes.POINTER(fastav_rotate_params), ctypes.POINTER(fastav_evict_params)
+        lib.fastav_rotate.restype = ctypes.c_int32
+        lib.fastav_rotate.argtypes = [rp, vp, vp, i32p, vp, vp, vp, vp, vp]
+        lib.fastav_rotate_write.restype = ctypes.c_int32
+        lib.fastav_rotate_write.argtypes = [rp, cp, vp, vp, vp, i32p, vp, vp, i32p, i32p, ctypes.c_int32, i32p, vp, i32p, vp]
+        lib.fastav_cache_weigh.restype = ctypes.c_int32
+        lib.fastav_cache_weigh.argtypes = [ap, cp, vp, ctypes.c_float, vp, vp, i32p, i32p, i32p, i32p, i32p, vp]
+        lib.fastav_evict_workspace_bytes.restype = ctypes.c_int32
+        lib.fastav_evict_workspace_bytes.argtypes = [ep, cp, szp]
+        lib.fastav_cache_evict.restype = ctypes.c_int32
+        lib.fastav_cache_evict.argtypes = [ep, cp, vp, i32p, i32p, i32p, i32p, i32p, i32p, vp, ctypes.c_size_t, i32p, vp]
         _lib = lib
     return _lib
 
@@ -453,6 +495,84 @@ def fastav_attend(params, cache: KvCache, q, cu_qlens, page_table, kv_lens, out,
     """Attention of q's rows over the cache: a prefix that several sequences share (optional), then each sequence's own tokens."""
     _check(_native().attend(_address("fastav_attend"), _struct(params, fastav_attend_params), cache.address, q, cu_qlens, page_table, kv_lens, cu_prefix,
                             prefix_table, prefix_lens, out, lse_out_opt, workspace, device_status, _stream(stream)), "fastav_attend")
+
+
+# ---- queries and keys in their positions, and the cache pruned while it grows: argument marshalling only ---------------
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0) -> list[float]:
+    """Radians per position of each pair: base^(-2 i / rotary_dim)."""
+    return [base ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)]
+
+
+def make_rotate_params(*, q=None, k=None, v=None, q_out=None, k_out=None, pos=None, frequencies=(), axis=None, interleaved=False, norm_eps=1e-6, batch=1,
+                       flags=0) -> fastav_rotate_params:
+    """Fill a ``fastav_rotate_params`` from the tensors whose shapes and strides it records: q, k (and v, outputs) [tokens, heads, head_dim], ``pos``
+    [tokens], or [axes, tokens].  ``frequencies``: radians per position of each pair (their number is half of rotary_dim); ``axis``: the
+    row of ``pos`` that turns each pair (None: the first)."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("expected q or k")
+    p = fastav_rotate_params()
+    p.batch, p.total_tokens, p.head_dim = batch, some.shape[0], some.shape[2]
+    p.num_q_heads, p.num_kv_heads = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    for name, t, like in (("q", q, q), ("k", k, k), ("v", v, k), ("qo", q_out, q), ("ko", k_out, k)):
+        if t is not None and (like is None or t.shape != like.shape or t.dtype is not torch.bfloat16 or t.shape[0] != p.total_tokens or t.shape[2] != p.head_dim):
+            raise ValueError("expected bf16 tensors [tokens, heads, head_dim], outputs and v shaped as q and k")
+        tok, head = _strides3(t, 1 if like is None else like.shape[1], p.head_dim)
+        setattr(p, name + "_stride_tok", tok)
+        setattr(p, name + "_stride_head", head)
+    if len(frequencies) > ROTATE_MAX_PAIRS:
+        raise ValueError(f"at most {ROTATE_MAX_PAIRS} pairs")
+    p.rotary_dim, p.num_axes = 2 * len(frequencies), 1
+    if pos is not None:
+        if pos.dtype is not torch.int32 or pos.dim() not in (1, 2) or pos.shape[-1] != p.total_tokens:
+            raise ValueError("expected int32 positions [tokens] or [axes, tokens]")
+        if pos.dim() == 2:
+            p.num_axes = pos.shape[0]
+        p.pos_stride_tok, p.pos_stride_axis = pos.stride(-1), pos.stride(0) if pos.dim() == 2 else 0
+    for i, f in enumerate(frequencies):
+        p.frequency[i] = f
+        p.axis[i] = 0 if axis is None else axis[i]
+    p.norm_eps, p.flags = float(norm_eps), int(flags) | (FASTAV_ROTATE_INTERLEAVED if interleaved else 0)
+    return p
+
+
+def fastav_rotate(params, q, k, pos, q_out, k_out, q_norm_opt=None, k_norm_opt=None, stream=None) -> None:
+    """Norm per head (optional) and rotation by position of a prompt's queries and keys; either side may be None."""
+    _check(_native().rotate(_address("fastav_rotate"), _struct(params, fastav_rotate_params), q, k, pos, q_norm_opt, k_norm_opt, q_out, k_out, _stream(stream)),
+           "fastav_rotate")
+
+
+def fastav_rotate_write(params, cache: KvCache, q, k, v, pos, cu_seqlens, page_table, start_opt, q_out, q_norm_opt=None, k_norm_opt=None, device_status=None,
+                        stream=None) -> None:
+    """The same for new tokens: queries to ``q_out``, rotated keys and values straight into the cache's pages."""
+    _check(_native().rotate_write(_address("fastav_rotate_write"), _struct(params, fastav_rotate_params), cache.address, q, k, v, pos, q_norm_opt, k_norm_opt,
+                                  cu_seqlens, page_table, _table(page_table), start_opt, q_out, device_status, _stream(stream)), "fastav_rotate_write")
+
+
+def fastav_cache_weigh(params: fastav_attend_params, cache: KvCache, weights, q, lse, cu_qlens, page_table, kv_lens, weighed_lens_opt=None, decay=1.0,
+                       device_status=None, stream=None) -> None:
+    """Add the attention that q's rows pay to each cached token (``lse`` as fastav_attend returns it) to ``weights``, shaped as the cache's scales."""
+    _check(_native().cache_weigh(_address("fastav_cache_weigh"), _struct(params, fastav_attend_params), cache.address, cache.k_scale, weights, decay, q, lse,
+                                 cu_qlens, page_table, kv_lens, weighed_lens_opt, device_status, _stream(stream)), "fastav_cache_weigh")
+
+
+def make_evict_params(*, batch, max_kv_len, max_keep, page_table, out_table=None, first=0, recent=0, flags=0) -> fastav_evict_params:
+    """Fill a ``fastav_evict_params``."""
+    return fastav_evict_params(batch, max_kv_len, max_keep, _table(page_table), _table(out_table), first, recent, int(flags))
+
+
+def fastav_evict_workspace_bytes(params: fastav_evict_params, cache: KvCache) -> int:
+    out = ctypes.c_size_t(0)
+    _check(library().fastav_evict_workspace_bytes(ctypes.byref(params), ctypes.byref(cache.struct), ctypes.byref(out)), "fastav_evict_workspace_bytes")
+    return int(out.value)
+
+
+def fastav_cache_evict(params, cache: KvCache, weights, page_table, kv_lens, keep_counts, kv_lens_out, workspace, out_table_opt=None, keep_idx_out_opt=None,
+                       device_status=None, stream=None) -> None:
+    """Keep the heaviest tokens of each sequence and KV head, in place or in the pages of ``out_table_opt``."""
+    _check(_native().cache_evict(_address("fastav_cache_evict"), _struct(params, fastav_evict_params), cache.address, cache.k_scale, weights, page_table, kv_lens,
+                                 keep_counts, out_table_opt, kv_lens_out, keep_idx_out_opt, workspace, device_status, _stream(stream)), "fastav_cache_evict")
 
 
 def fastav_kernel_launches() -> int:
