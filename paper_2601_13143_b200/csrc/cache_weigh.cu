@@ -13,6 +13,7 @@
 namespace fastav {
 namespace {
 
+constexpr int kMostFew = 16;  // stacked rows; beyond, the kernel for many
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = 32;  // keys of a unit
 
 // Up to 16 stacked rows (query rows times G) at once, more by turns.  A warp has a run of units of one KV head; mma.sync with the keys as rows, S^T = K Q^T, the codes
@@ -189,6 +190,9 @@ extern "C" int32_t fastav_cache_weigh(const fastav_attend_params* p, const fasta
   c.device_status = device_status;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const long long stacked = (long long)c.max_qlen * c.group;
-  const cudaError_t e = stacked <= 8 ? launch_few<1>(c, st) : launch_few<2>(c, st);
+  cudaError_t e = cudaSuccess;
+  bool used = false;
+  if (stacked > kMostFew && weigh_many_applies(c)) e = launch_weigh_many(c, st, &used);
+  if (!used) e = stacked <= 8 ? launch_few<1>(c, st) : launch_few<2>(c, st);
   return e == cudaSuccess ? FASTAV_OK : cuda_failed(e);
 }

@@ -1,0 +1,436 @@
+// fastav_cache_weigh for many query rows: a question's tokens at once, all rows that share a prefix.
+//
+// More than 16 stacked rows (query rows times G).  S^T = K Q^T on the fifth-generation tensor cores (tcgen05.mma, bf16 operands, fp32 sums in tensor memory) with the KEYS as the
+// accumulator's lanes: a token's weight is then a sum over one lane's columns, which one thread adds up by itself, and nothing is joined.  Codes are exact
+// in bf16 (int8 and e4m3 have at most eight significant bits), so queries go to the matrix pipe as they are, by TMA from the caller's tensor.
+//
+// A block, one per SM, takes an equal run of units (128 keys of a KV head, against all stacked rows of their sequence, 128 at a time), one or two units together:
+//
+//   warps 0-7   two groups of four, a thread per key: exponentials of 128 columns at a time from tensor memory, twice buffered, summed in a register.  With
+//               two units each group has one of them, with one they take turns with the row tiles.
+//   warps 8-15  codes -> bf16 operand tiles in shared memory, a group of units ahead
+//   warp 16     query rows by TMA, and their log-sum-exps and masks
+//   warp 17     issues the MMAs
+//
+// Bound by the exponentials: 16 per clock and SM, while the MMAs of the same elements take half that time.
+#include <cuda.h>
+#include <limits.h>
+
+#include "attend_8bit.cuh"
+#include "weigh.cuh"
+
+namespace fastav {
+namespace {
+
+constexpr int kTile = 128;  // keys of a unit; stacked rows of a row tile, at most
+constexpr int kSumWarps = 8, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kIssueWarp = kLoadWarp + 1, kWarps = kIssueWarp + 1, kThreads = 32 * kWarps;
+constexpr int kStages = 2, kRowSlots = 4;
+constexpr int kTmemCols = 512;
+constexpr int kHalfBytes = 128 * 128;  // 128 rows of 128 bytes: 64 elements
+
+template <int DIM>
+struct Many {
+  static constexpr int kTileBytes = DIM / 64 * kHalfBytes;
+  static constexpr int kOperands = (4 + kStages) * kTileBytes;  // K: two units, twice; Q
+};
+
+struct RowSlot {
+  alignas(16) float neg_lse[kTile];  // -log2(e) lse
+  alignas(16) int sees[kTile];       // keys that the row sees; 0: it pays nothing
+  int least[kTile / 32];             // the least of 32 of them
+};
+struct Control {
+  uint64_t k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[2][2], s_empty[2][2];
+  RowSlot rows[kRowSlots];
+  float join[2][kTile];
+  long long warp_sum[kWarps];
+  int first[2], unit[2];  // where the block's run begins and ends: sequence, unit of it
+  uint32_t tmem_base;
+  int abort;
+};
+
+struct ManyCall {
+  WeighCall w;
+  int rows_per_tile;  // query rows (not stacked) of a row tile
+};
+inline void mark_head(ManyCall& c, bool head) { c.w.head_wait = head ? 1 : 0; }
+
+// A block's run, walked by every role for itself.
+struct Run {
+  int b, u, end_b, end_u;
+  WeighSpan s;
+  int key_tiles = -1, row_tiles, head, tile, units;  // units: 1 or 2 from `tile` on
+  __device__ __forceinline__ Run(const Control& ctl) : b(ctl.first[0]), u(ctl.unit[0]), end_b(ctl.first[1]), end_u(ctl.unit[1]) {}
+  __device__ __forceinline__ bool next(const ManyCall& c) {
+    for (;;) {
+      if (b > end_b || (b == end_b && u >= end_u)) return false;
+      if (key_tiles < 0) {
+        s = weigh_span(c.w, b);
+        key_tiles = (s.len + kTile - 1) / kTile;
+        row_tiles = (s.rows + c.rows_per_tile - 1) / c.rows_per_tile;
+      }
+      const int limit = b == end_b ? end_u : key_tiles * c.w.cache.hkv;
+      if (u < limit) {
+        head = u / key_tiles;
+        tile = u - head * key_tiles;
+        units = min(2, min(key_tiles - tile, limit - u));
+        u += units;
+        return true;
+      }
+      ++b;
+      u = 0;
+      key_tiles = -1;
+    }
+  }
+  __device__ __forceinline__ int stacked(const ManyCall& c, int row_tile) const {  // rows of a row tile
+    return min(c.rows_per_tile, s.rows - row_tile * c.rows_per_tile) * c.w.group;
+  }
+};
+
+// What a sequence costs per unit: its row tiles, and about as much as one more for what is done once.
+__device__ __forceinline__ int unit_cost(const ManyCall& c, const WeighSpan& s) { return (s.rows + c.rows_per_tile - 1) / c.rows_per_tile + 1; }
+
+// Finds the block's run: the units whose start, in the call's total cost, lies in the block's share.
+__device__ __forceinline__ void find_run(const ManyCall& c, Control& ctl) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = c.w.batch;
+  long long total = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    long long ahead = 0;
+    const long long from = pass ? total * blockIdx.x / gridDim.x : 0, to = pass ? total * (blockIdx.x + 1) / gridDim.x : 0;
+    for (int b0 = 0; b0 < batch; b0 += kThreads) {
+      const int b = b0 + tid;
+      int cost = 0, units = 0;
+      if (b < batch) {
+        const WeighSpan s = weigh_span(c.w, b);
+        if (s.bad && pass == 0 && blockIdx.x == 0 && c.w.device_status) atomicOr(c.w.device_status, FASTAV_DEV_SHAPE_MISMATCH);
+        units = (s.len + kTile - 1) / kTile * c.w.cache.hkv;
+        cost = unit_cost(c, s);
+      }
+      const long long own = (long long)units * cost;
+      long long incl = own;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, d);
+        if (lane >= d) incl += x;
+      }
+      if (lane == 31) ctl.warp_sum[warp] = incl;
+      __syncthreads();
+      long long start = ahead + incl - own;
+      for (int i = 0; i < kWarps; ++i) {
+        if (i < warp) start += ctl.warp_sum[i];
+        ahead += ctl.warp_sum[i];
+      }
+      // An edge's unit is the first one that starts there or behind: of the least sequence whose last unit does.
+      const long long last = start + (long long)(units - 1) * cost;
+      if (pass && units > 0)
+        for (int e = 0; e < 2; ++e)
+          if ((e ? to : from) <= last) atomicMin(&ctl.first[e], b);
+      __syncthreads();
+      if (pass && units > 0) {
+        for (int e = 0; e < 2; ++e) {
+          const long long edge = e ? to : from;
+          if (ctl.first[e] == b) ctl.unit[e] = edge <= start ? 0 : (int)((edge - start + cost - 1) / cost);
+        }
+      }
+    }
+    total = ahead;
+  }
+  __syncthreads();
+}
+
+// 16 codes -> 32 bytes of a swizzled bf16 operand row.
+template <bool FP8>
+__device__ __forceinline__ void codes_to_bf16(const uint4& x, uint32_t at) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t h[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (FP8) {
+      // s eeee mmm as the sign and the low end of bf16's exponent and mantissa is the value times 2^-120 (subnormals, too); exact
+      const uint32_t a = __byte_perm(w[i], 0, 0x1404), b = __byte_perm(w[i], 0, 0x3424);  // a code in the upper byte of each half
+      const uint32_t la = ((a >> 4) & 0x07F007F0u) | (a & 0x80008000u), lb = ((b >> 4) & 0x07F007F0u) | (b & 0x80008000u), up = 0x7B807B80u;  // 2^120, twice
+      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[2 * i]) : "r"(la), "r"(up));
+      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[2 * i + 1]) : "r"(lb), "r"(up));
+    } else {
+      // the code plus 128 as the low bits of 2^23, less 2^23 + 128: a whole number of at most eight bits, whose float ends in sixteen zeros
+      const uint32_t u = w[i] ^ 0x80808080u;
+      const float2 less = make_float2(-8388736.f, -8388736.f);
+      const float2 a = __fadd2_rn(make_float2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7441))), less);
+      const float2 b = __fadd2_rn(make_float2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7442)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7443))), less);
+      h[2 * i] = __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x7632);
+      h[2 * i + 1] = __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x7632);
+    }
+  }
+  ptx::st_shared4(at, h[0], h[1], h[2], h[3]);
+  ptx::st_shared4(at ^ 16, h[4], h[5], h[6], h[7]);
+}
+
+template <int DIM, bool FP8>
+__global__ void __launch_bounds__(kThreads, 1)
+weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ManyCall c) {
+  using M = Many<DIM>;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t k_tiles = base, q_tiles = base + 4 * M::kTileBytes;
+  Control& ctl = *reinterpret_cast<Control*>(smem_raw + (base - ptx::smem_u32(smem_raw)) + M::kOperands);
+  volatile int* abort = &ctl.abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const WeighCall& w = c.w;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.k_full[i]), kConvWarps);
+      ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 1);
+      for (int j = 0; j < 2; ++j) {
+        ptx::mbar_init(ptx::smem_u32(&ctl.s_full[i][j]), 1);
+        ptx::mbar_init(ptx::smem_u32(&ctl.s_empty[i][j]), kSumWarps / 2);
+      }
+      ctl.first[i] = w.batch;
+      ctl.unit[i] = 0;
+    }
+    for (int i = 0; i < kStages; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.q_full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.q_empty[i]), 1);
+    }
+    for (int i = 0; i < kRowSlots; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.rows_full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.rows_empty[i]), kSumWarps);
+    }
+    ctl.abort = 0;
+    ptx::fence_barrier_init();
+    ptx::prefetch_tensormap(&q_map);
+  }
+  if (w.head_wait) pdl_wait();
+  pdl_trigger();
+  pdl_wait();
+  __syncthreads();
+  find_run(c, ctl);
+  if (warp == kIssueWarp) {
+    ptx::tmem_alloc(ptx::smem_u32(&ctl.tmem_base), kTmemCols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = ctl.tmem_base;
+  Run run(ctl);
+
+  // (A wait that gives up changes nothing in the way a warp goes: it only marks the results as invalid.)
+  if (warp < kSumWarps) {
+    const int half = warp >> 2, in_tile = threadIdx.x & (kTile - 1);
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + half * 2 * kTile;
+    int tiles_seen = 0, mine_seen = 0, group = 0;
+    bool more = run.next(c);
+    // The thread's key: place in the pool, scale, weight before; asked for a group ahead.
+    struct Key { long long at; float scale, before; };
+    auto ask = [&] {
+      Key k{-1, 0.f, 0.f};
+      const int key = (run.tile + (run.units == 2 ? half : 0)) * kTile + in_tile;
+      if (key < run.s.len) {
+        const int page = page_of(w.cache, w.table, w.table_stride, run.b, key);
+        if (page >= 0) {
+          k.at = pool_row(w.cache, page, run.head, key);
+          k.scale = chain_load(w.cache.k_scale + k.at) * w.scale_log2;
+          const int fresh = w.decay == 0.f ? 0 : w.weighed ? chain_load_cached(w.weighed + run.b) : INT_MAX;
+          if (key < fresh) k.before = chain_load(w.weights + k.at);
+        } else if (w.device_status) {
+          atomicOr(w.device_status, FASTAV_DEV_BAD_INDEX);
+        }
+      }
+      return k;
+    };
+    Key next{-1, 0.f, 0.f};
+    if (more) next = ask();
+    while (more) {
+      const Key mine = next;
+      const int key0 = (run.tile + (run.units == 2 ? half : 0)) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
+      const bool pair = run.units == 2;
+      const Run here = run;
+      more = run.next(c);
+      if (more) next = ask();
+      const float2 scale = make_float2(mine.scale, mine.scale);
+      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      for (int t = 0; t < row_tiles; ++t, ++tiles_seen) {
+        const int slot = tiles_seen % kRowSlots;
+        RowSlot& rows = ctl.rows[slot];
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_full[slot]), tiles_seen / kRowSlots & 1, abort);
+        if (pair || (t & 1) == half) {
+          const int buffer = mine_seen & 1;
+          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[half][buffer]), mine_seen >> 1 & 1, abort);
+          ptx::tc_fence_after_sync();
+          const int columns = here.stacked(c, t);
+          for (int c0 = 0; c0 < columns; c0 += 32) {
+            uint32_t v[32];
+            ptx::tmem_ld32(lanes + buffer * kTile + c0, v);
+            ptx::tmem_ld_wait_for(v);
+            const float4* const nl = reinterpret_cast<const float4*>(rows.neg_lse + c0);
+            if (rows.least[c0 >> 5] >= key_end) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const float4 l = nl[j];
+                const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), scale, make_float2(l.x, l.y));
+                const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), scale, make_float2(l.z, l.w));
+                sum[0] = __fadd2_rn(sum[0], make_float2(ptx::ex2_approx(a.x), ptx::ex2_approx(a.y)));
+                sum[1] = __fadd2_rn(sum[1], make_float2(ptx::ex2_approx(b.x), ptx::ex2_approx(b.y)));
+              }
+            } else {  // a mask's edge, rows that pay nothing or do not exist (what stands in their columns may be anything)
+              const int4* const sees = reinterpret_cast<const int4*>(rows.sees + c0);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const float4 l = nl[j];
+                const int4 n = sees[j];
+                const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), scale, make_float2(l.x, l.y));
+                const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), scale, make_float2(l.z, l.w));
+                sum[0] = __fadd2_rn(sum[0], make_float2(key < n.x ? ptx::ex2_approx(a.x) : 0.f, key < n.y ? ptx::ex2_approx(a.y) : 0.f));
+                sum[1] = __fadd2_rn(sum[1], make_float2(key < n.z ? ptx::ex2_approx(b.x) : 0.f, key < n.w ? ptx::ex2_approx(b.y) : 0.f));
+              }
+            }
+            __syncwarp();
+          }
+          ptx::tc_fence_before_sync();
+          ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.s_empty[half][buffer]), lane);
+          ++mine_seen;
+        }
+        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_empty[slot]), lane);
+      }
+      float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+      if (!pair) {  // the second group's row tiles
+        if (half == 1) ctl.join[group & 1][in_tile] = total;
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
+        if (half == 0) total += ctl.join[group & 1][in_tile];
+        ++group;
+      }
+      if (mine.at >= 0 && (pair || half == 0)) w.weights[mine.at] = fmaf(w.decay, mine.before, total);
+    }
+  } else if (warp < kLoadWarp) {
+    // Loads of 4 keys of 8 pieces (head_dim 64: 8 of 4); the eight lanes of a phase store to eight different quarters of the banks.
+    constexpr int kLoads = DIM / 32, kRows = 16 / kLoads;
+    const int cw = warp - kSumWarps;
+    const int piece = DIM == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = DIM == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    for (int group = 0; run.next(c);) {
+      if (run.row_tiles == 0) continue;
+      const int slot = group & 1;
+      uint4 x[2][kLoads];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // 16 keys each, in one page
+        const int key0 = run.tile * kTile + (cw * run.units + i) * 16;
+        if (i >= run.units || key0 >= run.s.len) continue;
+        const int page = max(0, page_of(w.cache, w.table, w.table_stride, run.b, key0));  // (the weights of a page that is none are left out)
+        const uint8_t* const from = w.cache.k + (pool_row(w.cache, page, run.head, key0) + row) * DIM + piece * 16;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kRows * DIM));
+      }
+      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), (group >> 1 & 1) ^ 1u, abort);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int in_group = (cw * run.units + i) * 16;
+        if (i >= run.units || run.tile * kTile + in_group >= run.s.len) continue;
+        const uint32_t tile = k_tiles + (2 * slot + in_group / kTile) * M::kTileBytes + (piece >> 2) * kHalfBytes;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const int r = in_group % kTile + j * kRows + row;
+          codes_to_bf16<FP8>(x[i][j], tile + r * 128 + (((2 * (piece & 3)) ^ (r & 7)) << 4));
+        }
+      }
+      ptx::fence_proxy_async_smem();
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.k_full[slot]), lane);
+      ++group;
+    }
+  } else if (warp == kLoadWarp) {
+    int tiles = 0;
+    const uint32_t box_bytes = (uint32_t)(c.rows_per_tile * w.group) * 128u;
+    while (run.next(c))
+      for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
+        const int stage = tiles % kStages, slot = tiles % kRowSlots;
+        const int row0 = run.s.row0 + t * c.rows_per_tile;
+        const uint32_t bar = ptx::smem_u32(&ctl.q_full[stage]);
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_empty[stage]), (tiles / kStages & 1) ^ 1u, abort);
+        ptx::mbar_expect_tx_warp(bar, box_bytes * (DIM / 64));
+#pragma unroll
+        for (int sub = 0; sub < DIM / 64; ++sub)
+          ptx::tma_load_3d_warp(q_tiles + stage * M::kTileBytes + sub * kHalfBytes, &q_map, sub * 64, run.head * w.group, row0, bar);
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_empty[slot]), (tiles / kRowSlots & 1) ^ 1u, abort);
+        const int stacked = run.stacked(c, t);
+#pragma unroll
+        for (int i = 0; i < kTile / 32; ++i) {
+          const int x = 32 * i + lane, r = x / w.group, head = run.head * w.group + x - r * w.group;
+          float lse = -INFINITY;
+          if (x < stacked) lse = chain_load(w.lse + (long long)(row0 + r) * w.hq + head);
+          const int sees = lse == -INFINITY ? 0 : w.causal ? max(0, run.s.len - run.s.rows + t * c.rows_per_tile + r + 1) : run.s.len;
+          ctl.rows[slot].neg_lse[x] = -lse * kLog2e;
+          ctl.rows[slot].sees[x] = sees;
+          const int least = __reduce_min_sync(0xFFFFFFFFu, sees);
+          if (lane == 0) ctl.rows[slot].least[i] = least;
+        }
+        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_full[slot]), lane);
+      }
+    // The copies write into this block's shared memory: they have to be waited for before it may exit.
+    int never = 0;
+    for (int i = max(0, tiles - kStages); i < tiles; ++i) ptx::mbar_wait_bounded(ptx::smem_u32(&ctl.q_full[i % kStages]), i / kStages & 1, &never);
+    __syncwarp();
+  } else {
+    int tiles = 0, issued[2] = {0, 0};
+    for (int group = 0; run.next(c);) {
+      if (run.row_tiles == 0) continue;
+      const int slot = group & 1;
+      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_full[slot]), group >> 1 & 1, abort);
+      for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
+        const int stage = tiles % kStages;
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full[stage]), tiles / kStages & 1, abort);
+        const uint32_t idesc = ptx::umma_idesc_bf16(kTile, (run.stacked(c, t) + 15) / 16 * 16);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (run.units == 1 && (t & 1) != half) continue;
+          const int n = issued[half]++, buffer = n & 1;
+          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_empty[half][buffer]), (n >> 1 & 1) ^ 1u, abort);
+          ptx::tc_fence_after_sync();
+          ptx::umma_bf16_steps<DIM / 16, kHalfBytes, kHalfBytes>(tmem + (2 * half + buffer) * kTile, ptx::umma_desc_sw128(k_tiles + (2 * slot + (run.units == 2 ? half : 0)) * M::kTileBytes, 0),
+                                                                 ptx::umma_desc_sw128(q_tiles + stage * M::kTileBytes, 0), idesc, false);
+          ptx::umma_commit(ptx::smem_u32(&ctl.s_full[half][buffer]));
+        }
+        ptx::umma_commit(ptx::smem_u32(&ctl.q_empty[stage]));
+      }
+      ptx::umma_commit(ptx::smem_u32(&ctl.k_empty[slot]));
+      ++group;
+    }
+    if (tiles > 0) {  // the columns are given back below: not before the last MMA is done
+      int never = 0;
+      ptx::mbar_wait_bounded(ptx::smem_u32(&ctl.q_empty[(tiles - 1) % kStages]), (tiles - 1) / kStages & 1, &never);
+      __syncwarp();
+    }
+  }
+
+  // ---- everybody meets here, whatever happened above ----
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kIssueWarp) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, kTmemCols);
+  }
+  if (threadIdx.x == 0 && ctl.abort && w.device_status) atomicOr(w.device_status, FASTAV_DEV_WAIT_EXPIRED);
+}
+
+template <int DIM, bool FP8>
+cudaError_t launch(const ManyCall& c, const CUtensorMap& map, cudaStream_t stream) {
+  constexpr size_t kSmem = Many<DIM>::kOperands + sizeof(Control) + 1024;
+  const cudaError_t e = once_per_context([&] { return cudaFuncSetAttribute(weigh_many_kernel<DIM, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem); });
+  if (e != cudaSuccess) return e;
+  const long long units = (long long)c.w.batch * c.w.cache.hkv * ((c.w.max_len + kTile - 1) / kTile);
+  count_launches(1);
+  return launch_chained(weigh_many_kernel<DIM, FP8>, dim3((unsigned)(units < kNumSMs ? units : kNumSMs)), dim3(kThreads), kSmem, stream, map, c);
+}
+
+}  // namespace
+
+bool weigh_many_applies(const WeighCall& c) { return c.group <= kTile; }
+
+cudaError_t launch_weigh_many(const WeighCall& w, cudaStream_t stream, bool* used) {
+  ManyCall c{w, kTile / w.group};
+  if (c.rows_per_tile > w.max_qlen) c.rows_per_tile = w.max_qlen;
+  CUtensorMap map;
+  *used = encode_rows_map(w.q, w.cache.dim, w.hq, w.total_q, w.q_st, w.q_sh, w.group, c.rows_per_tile, &map);
+  if (!*used) return cudaSuccess;
+  if (w.cache.dim == 128) return w.cache.fp8 ? launch<128, true>(c, map, stream) : launch<128, false>(c, map, stream);
+  return w.cache.fp8 ? launch<64, true>(c, map, stream) : launch<64, false>(c, map, stream);
+}
+
+}  // namespace fastav

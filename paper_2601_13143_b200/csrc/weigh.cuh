@@ -22,6 +22,10 @@ struct WeighCall {
 };
 inline void mark_head(WeighCall& c, bool head) { c.head_wait = head ? 1 : 0; }
 
+// The kernel for many stacked rows.  `*used` is false when the queries could not be described to the tensor-memory-accelerator; nothing was launched then.
+bool weigh_many_applies(const WeighCall& c);
+cudaError_t launch_weigh_many(const WeighCall& c, cudaStream_t stream, bool* used);
+
 #ifdef __CUDACC__
 // A sequence's query rows and tokens, cut down to what the host promised.
 struct WeighSpan {
