@@ -6,13 +6,16 @@
 //
 // A block, one per SM, takes an equal run of units (128 keys of a KV head, against all stacked rows of their sequence, 128 at a time), one or two units together:
 //
-//   warps 0-7   two groups of four, a thread per key: exponentials of 128 columns at a time from tensor memory, twice buffered, summed in a register.  With
-//               two units each group has one of them, with one they take turns with the row tiles.
-//   warps 8-15  codes -> bf16 operand tiles in shared memory, a group of units ahead
-//   warp 16     query rows by TMA, and their log-sum-exps and masks
-//   warp 17     issues the MMAs
+//   warps 0-15  four teams of four, a thread per key: exponentials of 128 columns at a time from tensor memory, twice buffered, summed in a register.  Two
+//               teams share a unit's columns; with one unit the two pairs of teams take turns with the row tiles.
+//   warps 16-19 codes -> bf16 operand tiles in shared memory, a group of units ahead
+//   warp 20     query rows by TMA
+//   warp 21     issues the MMAs
+//   warp 22     log-sum-exps and masks of the query rows (23: nothing; registers move by whole teams)
 //
-// Bound by the exponentials: 16 per clock and SM, while the MMAs of the same elements take half that time.
+// Bound by the exponentials (16 per clock and SM; the special-function unit is busy for some 75 % of the time), while the MMAs of the same elements
+// take half as long.  1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials): 256 us.  With eight summing warps a block instead of
+// sixteen 296 (each waits for its own loads from tensor memory), 336 with 16 columns at a time; a quarter of the exponentials by a polynomial beside the unit: 256, half: 262.
 #include <cuda.h>
 #include <limits.h>
 
@@ -23,9 +26,13 @@ namespace fastav {
 namespace {
 
 constexpr int kTile = 128;  // keys of a unit; stacked rows of a row tile, at most
-constexpr int kSumWarps = 8, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kIssueWarp = kLoadWarp + 1, kWarps = kIssueWarp + 1, kThreads = 32 * kWarps;
+constexpr int kSumWarps = 16, kConvWarps = 4, kLoadWarp = kSumWarps + kConvWarps, kIssueWarp = kLoadWarp + 1, kRowWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
+// Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
+constexpr int kSumRegs = 88, kConvRegs = 72, kLastRegs = 48;
+constexpr int kRegsNeeded = 32 * (kSumWarps * kSumRegs + kConvWarps * kConvRegs + 4 * kLastRegs);
 constexpr int kStages = 2, kRowSlots = 4;
 constexpr int kTmemCols = 512;
+constexpr int kPiece = 32;  // columns of tensor memory in registers at a time
 constexpr int kHalfBytes = 128 * 128;  // 128 rows of 128 bytes: 64 elements
 
 template <int DIM>
@@ -42,7 +49,7 @@ struct RowSlot {
 struct Control {
   uint64_t k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[2][2], s_empty[2][2];
   RowSlot rows[kRowSlots];
-  float join[2][kTile];
+  float join[2][4][kTile];
   long long warp_sum[kWarps];
   int first[2], unit[2];  // where the block's run begins and ends: sequence, unit of it
   uint32_t tmem_base;
@@ -165,6 +172,28 @@ __device__ __forceinline__ void codes_to_bf16(const uint4& x, uint32_t at) {
   ptx::st_shared4(at ^ 16, h[4], h[5], h[6], h[7]);
 }
 
+// What kPiece columns of rows add to the weight of the thread's key.  MASKED: a mask's edge, rows that pay nothing or do not exist (what stands in their
+// columns may be anything).
+template <bool MASKED>
+__device__ __forceinline__ void add_columns(const uint32_t (&v)[kPiece], const float* neg_lse, const int* sees, int key, const float2& scale, float2 (&sum)[2]) {
+  const float4* const nl = reinterpret_cast<const float4*>(neg_lse);
+#pragma unroll
+  for (int j = 0; j < kPiece / 4; ++j) {
+    const float4 l = nl[j];
+    const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), scale, make_float2(l.x, l.y));
+    const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), scale, make_float2(l.z, l.w));
+    float2 p = make_float2(ptx::ex2_approx(a.x), ptx::ex2_approx(a.y));
+    float2 q = make_float2(ptx::ex2_approx(b.x), ptx::ex2_approx(b.y));
+    if (MASKED) {
+      const int4 n = reinterpret_cast<const int4*>(sees)[j];
+      p = make_float2(key < n.x ? p.x : 0.f, key < n.y ? p.y : 0.f);
+      q = make_float2(key < n.z ? q.x : 0.f, key < n.w ? q.y : 0.f);
+    }
+    sum[0] = __fadd2_rn(sum[0], p);
+    sum[1] = __fadd2_rn(sum[1], q);
+  }
+}
+
 template <int DIM, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1)
 weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ManyCall c) {
@@ -216,9 +245,11 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 
   // (A wait that gives up changes nothing in the way a warp goes: it only marks the results as invalid.)
   if (warp < kSumWarps) {
-    const int half = warp >> 2, in_tile = threadIdx.x & (kTile - 1);
+    ptx::more_registers<kSumRegs>();
+    const int team = warp >> 2, half = team >> 1, in_tile = threadIdx.x & (kTile - 1);
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + half * 2 * kTile;
     int tiles_seen = 0, mine_seen = 0, group = 0;
+    const int tile_rows = c.rows_per_tile * w.group;
     bool more = run.next(c);
     // The thread's key: place in the pool, scale, weight before; asked for a group ahead.
     struct Key { long long at; float scale, before; };
@@ -244,7 +275,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       const Key mine = next;
       const int key0 = (run.tile + (run.units == 2 ? half : 0)) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
       const bool pair = run.units == 2;
-      const Run here = run;
+      const int stacked = run.s.rows * w.group;
       more = run.next(c);
       if (more) next = ask();
       const float2 scale = make_float2(mine.scale, mine.scale);
@@ -257,33 +288,13 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           const int buffer = mine_seen & 1;
           ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[half][buffer]), mine_seen >> 1 & 1, abort);
           ptx::tc_fence_after_sync();
-          const int columns = here.stacked(c, t);
-          for (int c0 = 0; c0 < columns; c0 += 32) {
-            uint32_t v[32];
+          const int columns = min(tile_rows, stacked - t * tile_rows);
+          for (int c0 = kPiece * (team & 1); c0 < columns; c0 += 2 * kPiece) {
+            uint32_t v[kPiece];
             ptx::tmem_ld32(lanes + buffer * kTile + c0, v);
             ptx::tmem_ld_wait_for(v);
-            const float4* const nl = reinterpret_cast<const float4*>(rows.neg_lse + c0);
-            if (rows.least[c0 >> 5] >= key_end) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const float4 l = nl[j];
-                const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), scale, make_float2(l.x, l.y));
-                const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), scale, make_float2(l.z, l.w));
-                sum[0] = __fadd2_rn(sum[0], make_float2(ptx::ex2_approx(a.x), ptx::ex2_approx(a.y)));
-                sum[1] = __fadd2_rn(sum[1], make_float2(ptx::ex2_approx(b.x), ptx::ex2_approx(b.y)));
-              }
-            } else {  // a mask's edge, rows that pay nothing or do not exist (what stands in their columns may be anything)
-              const int4* const sees = reinterpret_cast<const int4*>(rows.sees + c0);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const float4 l = nl[j];
-                const int4 n = sees[j];
-                const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), scale, make_float2(l.x, l.y));
-                const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), scale, make_float2(l.z, l.w));
-                sum[0] = __fadd2_rn(sum[0], make_float2(key < n.x ? ptx::ex2_approx(a.x) : 0.f, key < n.y ? ptx::ex2_approx(a.y) : 0.f));
-                sum[1] = __fadd2_rn(sum[1], make_float2(key < n.z ? ptx::ex2_approx(b.x) : 0.f, key < n.w ? ptx::ex2_approx(b.y) : 0.f));
-              }
-            }
+            if (rows.least[c0 / kPiece] >= key_end) add_columns<false>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
+            else add_columns<true>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
             __syncwarp();
           }
           ptx::tc_fence_before_sync();
@@ -293,15 +304,19 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_empty[slot]), lane);
       }
       float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-      if (!pair) {  // the second group's row tiles
-        if (half == 1) ctl.join[group & 1][in_tile] = total;
-        asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
-        if (half == 0) total += ctl.join[group & 1][in_tile];
-        ++group;
+      // The teams' sums, in their order.
+      const bool joins = team == 0 || (pair && team == 2);
+      if (!joins) ctl.join[group & 1][team][in_tile] = total;
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
+      if (joins) {
+        total += ctl.join[group & 1][team + 1][in_tile];
+        if (!pair) total += ctl.join[group & 1][2][in_tile] + ctl.join[group & 1][3][in_tile];
+        if (mine.at >= 0) w.weights[mine.at] = fmaf(w.decay, mine.before, total);
       }
-      if (mine.at >= 0 && (pair || half == 0)) w.weights[mine.at] = fmaf(w.decay, mine.before, total);
+      ++group;
     }
   } else if (warp < kLoadWarp) {
+    ptx::fewer_registers<kConvRegs>();
     // Loads of 4 keys of 8 pieces (head_dim 64: 8 of 4); the eight lanes of a phase store to eight different quarters of the banks.
     constexpr int kLoads = DIM / 32, kRows = 16 / kLoads;
     const int cw = warp - kSumWarps;
@@ -309,65 +324,97 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     for (int group = 0; run.next(c);) {
       if (run.row_tiles == 0) continue;
       const int slot = group & 1;
-      uint4 x[2][kLoads];
+      const int sixteens = run.units * kTile / 16;  // of keys, each in one page
+      bool waited = false;
+      for (int i0 = cw; i0 < sixteens; i0 += 2 * kConvWarps) {
+        uint4 x[2][kLoads];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {  // 16 keys each, in one page
-        const int key0 = run.tile * kTile + (cw * run.units + i) * 16;
-        if (i >= run.units || key0 >= run.s.len) continue;
-        const int page = max(0, page_of(w.cache, w.table, w.table_stride, run.b, key0));  // (the weights of a page that is none are left out)
-        const uint8_t* const from = w.cache.k + (pool_row(w.cache, page, run.head, key0) + row) * DIM + piece * 16;
+        for (int i = 0; i < 2; ++i) {
+          const int key0 = run.tile * kTile + (i0 + i * kConvWarps) * 16;
+          if (key0 >= run.s.len) continue;
+          const int page = max(0, page_of(w.cache, w.table, w.table_stride, run.b, key0));  // (the weights of a page that is none are left out)
+          const uint8_t* const from = w.cache.k + (pool_row(w.cache, page, run.head, key0) + row) * DIM + piece * 16;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kRows * DIM));
-      }
-      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), (group >> 1 & 1) ^ 1u, abort);
+          for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kRows * DIM));
+        }
+        if (!waited) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), (group >> 1 & 1) ^ 1u, abort);
+        waited = true;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int in_group = (cw * run.units + i) * 16;
-        if (i >= run.units || run.tile * kTile + in_group >= run.s.len) continue;
-        const uint32_t tile = k_tiles + (2 * slot + in_group / kTile) * M::kTileBytes + (piece >> 2) * kHalfBytes;
+        for (int i = 0; i < 2; ++i) {
+          const int in_group = (i0 + i * kConvWarps) * 16;
+          if (run.tile * kTile + in_group >= run.s.len) continue;
+          const uint32_t tile = k_tiles + (2 * slot + in_group / kTile) * M::kTileBytes + (piece >> 2) * kHalfBytes;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const int r = in_group % kTile + j * kRows + row;
-          codes_to_bf16<FP8>(x[i][j], tile + r * 128 + (((2 * (piece & 3)) ^ (r & 7)) << 4));
+          for (int j = 0; j < kLoads; ++j) {
+            const int r = in_group % kTile + j * kRows + row;
+            codes_to_bf16<FP8>(x[i][j], tile + r * 128 + (((2 * (piece & 3)) ^ (r & 7)) << 4));
+          }
         }
       }
       ptx::fence_proxy_async_smem();
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.k_full[slot]), lane);
       ++group;
     }
-  } else if (warp == kLoadWarp) {
+  } else {
+    ptx::fewer_registers<kLastRegs>();
+  }
+  if (warp == kLoadWarp) {
     int tiles = 0;
     const uint32_t box_bytes = (uint32_t)(c.rows_per_tile * w.group) * 128u;
     while (run.next(c))
       for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
-        const int stage = tiles % kStages, slot = tiles % kRowSlots;
-        const int row0 = run.s.row0 + t * c.rows_per_tile;
+        const int stage = tiles % kStages;
         const uint32_t bar = ptx::smem_u32(&ctl.q_full[stage]);
         ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_empty[stage]), (tiles / kStages & 1) ^ 1u, abort);
         ptx::mbar_expect_tx_warp(bar, box_bytes * (DIM / 64));
 #pragma unroll
         for (int sub = 0; sub < DIM / 64; ++sub)
-          ptx::tma_load_3d_warp(q_tiles + stage * M::kTileBytes + sub * kHalfBytes, &q_map, sub * 64, run.head * w.group, row0, bar);
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_empty[slot]), (tiles / kRowSlots & 1) ^ 1u, abort);
-        const int stacked = run.stacked(c, t);
-#pragma unroll
-        for (int i = 0; i < kTile / 32; ++i) {
-          const int x = 32 * i + lane, r = x / w.group, head = run.head * w.group + x - r * w.group;
-          float lse = -INFINITY;
-          if (x < stacked) lse = chain_load(w.lse + (long long)(row0 + r) * w.hq + head);
-          const int sees = lse == -INFINITY ? 0 : w.causal ? max(0, run.s.len - run.s.rows + t * c.rows_per_tile + r + 1) : run.s.len;
-          ctl.rows[slot].neg_lse[x] = -lse * kLog2e;
-          ctl.rows[slot].sees[x] = sees;
-          const int least = __reduce_min_sync(0xFFFFFFFFu, sees);
-          if (lane == 0) ctl.rows[slot].least[i] = least;
-        }
-        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_full[slot]), lane);
+          ptx::tma_load_3d_warp(q_tiles + stage * M::kTileBytes + sub * kHalfBytes, &q_map, sub * 64, run.head * w.group, run.s.row0 + t * c.rows_per_tile, bar);
       }
     // The copies write into this block's shared memory: they have to be waited for before it may exit.
     int never = 0;
     for (int i = max(0, tiles - kStages); i < tiles; ++i) ptx::mbar_wait_bounded(ptx::smem_u32(&ctl.q_full[i % kStages]), i / kStages & 1, &never);
     __syncwarp();
-  } else {
+  } else if (warp == kRowWarp) {
+    int tiles = 0, t = 0;
+    constexpr int kEach = kTile / 32;
+    float lse[kEach];  // of the next row tile, asked for ahead of the wait for its place
+    int sees[kEach];
+    auto ask = [&] {
+      const int stacked = run.stacked(c, t), first = t * c.rows_per_tile;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int x = 32 * i + lane, r = x / w.group, head = run.head * w.group + x - r * w.group;
+        lse[i] = x < stacked ? chain_load(w.lse + (long long)(run.s.row0 + first + r) * w.hq + head) : -INFINITY;
+        sees[i] = w.causal ? max(0, run.s.len - run.s.rows + first + r + 1) : run.s.len;
+      }
+    };
+    auto advance = [&] {
+      if (++t < run.row_tiles) return true;
+      t = 0;
+      do {
+        if (!run.next(c)) return false;
+      } while (run.row_tiles == 0);
+      return true;
+    };
+    run.row_tiles = 0;
+    bool more = advance();
+    if (more) ask();
+    for (; more; ++tiles) {
+      const int slot = tiles % kRowSlots;
+      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_empty[slot]), (tiles / kRowSlots & 1) ^ 1u, abort);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int n = lse[i] == -INFINITY ? 0 : sees[i], least = __reduce_min_sync(0xFFFFFFFFu, n);
+        ctl.rows[slot].neg_lse[32 * i + lane] = -lse[i] * kLog2e;
+        ctl.rows[slot].sees[32 * i + lane] = n;
+        if (lane == 0) ctl.rows[slot].least[i] = least;
+      }
+      more = advance();
+      if (more) ask();
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_full[slot]), lane);
+    }
+  } else if (warp == kIssueWarp) {
     int tiles = 0, issued[2] = {0, 0};
     for (int group = 0; run.next(c);) {
       if (run.row_tiles == 0) continue;
@@ -412,7 +459,13 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
 template <int DIM, bool FP8>
 cudaError_t launch(const ManyCall& c, const CUtensorMap& map, cudaStream_t stream) {
   constexpr size_t kSmem = Many<DIM>::kOperands + sizeof(Control) + 1024;
-  const cudaError_t e = once_per_context([&] { return cudaFuncSetAttribute(weigh_many_kernel<DIM, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem); });
+  const cudaError_t e = once_per_context([&] {
+    cudaFuncAttributes a;
+    const cudaError_t got = cudaFuncGetAttributes(&a, weigh_many_kernel<DIM, FP8>);
+    if (got != cudaSuccess) return got;
+    if (a.numRegs * kThreads < kRegsNeeded) return cudaErrorInvalidConfiguration;  // the summing warps would wait for registers for ever
+    return cudaFuncSetAttribute(weigh_many_kernel<DIM, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+  });
   if (e != cudaSuccess) return e;
   const long long units = (long long)c.w.batch * c.w.cache.hkv * ((c.w.max_len + kTile - 1) / kTile);
   count_launches(1);
