@@ -1,13 +1,17 @@
 // fastav_cache_evict: the lightest tokens of a cached sequence go, the others move together.
 //
-// A thread-block cluster per sequence and KV head does both steps in one launch; one set for all heads is selected by a cluster per sequence first, since rows that
-// move in place take their weights with them.  Selection: the k-th largest weight by its 32-bit key, 8 bits at a time, each block
-// counting a slice of the tokens into a histogram of its own that all blocks of the cluster then add up; ranks by one sum over threads and blocks; the
-// survivors' list goes to the workspace.  Moving: rounds of kMoved rows a block, in the survivors' order.  Bound by the rows that move (codes and scales of K and V, weights:
-// 2 (d + 4) + 4 bytes each way), for one sequence by the selection's chain.
+// Selection: a thread-block cluster per sequence and KV head (or per sequence, for one set of all heads), a slice of the tokens per block, their keys in registers.  The
+// k-th largest weight by its 32-bit key, 8 bits at a time: each block counts its keys into a histogram and sends it to all blocks of the cluster, where one warp adds
+// them up and finds the digit.  Ranks from ballots; the survivors' list goes to the workspace.  (Keys in shared memory, sums over all 1,024 threads
+// of a block and histograms fetched from the others: 2 us a digit instead of 0.7.)
+//
+// Moving: the same clusters go on with it in place and where there is little to move (one launch), in rounds of kMoved rows a block in the survivors' order; else a
+// kernel with a block per kChunk rows, that many in flight.  Bound by the rows that move (codes and scales of K and V, weights: 2 (d + 4) + 4 bytes each
+// way), for one sequence by the selection's chain.
 //
 // In place.  Survivor i comes from a place >= i, and sources ascend.  So a round's rows may be written as soon as all of that round have been read: what later
-// rounds read lies behind their own targets.
+// rounds read lies behind their own targets.  (The rows of the round after are asked for ahead of that.)  One set for all heads is selected by a launch of its own, since rows
+// that move take the weights with them.
 #include <limits.h>
 
 #include "cache.cuh"
@@ -17,7 +21,15 @@ namespace fastav {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kHeld = 8192;  // keys that a block holds in shared memory; those of a longer slice are looked up again
+constexpr int kChunk = 128, kChunkThreads = 256;  // rows of a block that only moves
+constexpr int kStripes = 8, kHeld = kStripes * kThreads;  // keys that a block holds, kThreads tokens a stripe; those of a longer slice are looked up again
+
+// Tokens of a block's slice, at least: a cluster of blocks is 0.5 us a digit slower than one block, which takes 1,024 tokens in hardly more time than 256 (1 x 300 tokens
+// 16 -> 12 us alone, in clusters from 256 and from 1,024 on).
+constexpr int kLeastSlice = 1024;
+// A block's survivors up to which the selecting clusters move them, one round of theirs; beyond, another launch with more blocks is quicker (819 of 1,024 tokens,
+// 4 heads: 8.1 us instead of 12.2).
+constexpr int kFewRows = 256;
 
 struct EvictCall {
   CacheView cache;
@@ -38,25 +50,36 @@ __device__ __forceinline__ unsigned key_of(float w) {
   return bits ^ (bits >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-template <int DIM, bool SELECT, bool MOVE>
-__global__ void __launch_bounds__(kThreads)
+template <int DIM, bool SELECT, bool MOVE, bool JOINT>
+__global__ void __launch_bounds__(kThreads, 1)
 evict_kernel(EvictCall c) {
-  constexpr int kPieces = DIM / 16, kAtOnce = kThreads / kPieces, kUnroll = 2;  // 16-byte pieces of a row; rows that the threads take at once
+  constexpr int kPieces = DIM / 16, kAtOnce = kThreads / kPieces, kUnroll = 4;  // 16-byte pieces of a row; rows that the threads take at once
   constexpr int kMoved = kAtOnce * kUnroll;                                     // rows of a round
-  constexpr int kSmall = (3 * kMoved + kThreads - 1) / kThreads;                // scales and weights of a round, per thread
-  extern __shared__ unsigned held[];  // [kHeld]
+  static_assert(kMoved <= kThreads);
+  __shared__ int pages[kHeld / 16 + 1];                              // of the first kHeld tokens of the slice; -1: none
+  __shared__ int2 places[2][MOVE ? kMoved : 1];
   __shared__ unsigned hist[2][256];
-  __shared__ unsigned warp_a[kWarps], warp_b[kWarps], found[4];
-  __shared__ unsigned counts[2];  // of this block: keys above the threshold, keys equal to it
+  __shared__ __align__(16) unsigned inbox[2][kPortableCluster][256];  // the histograms of all blocks
+  __shared__ unsigned counted[kStripes * kWarps], totals[2], found[2][3];  // totals: of the blocks before this one, keys above the threshold and equal to it
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
-  constexpr bool kJoint = SELECT && !MOVE;  // one set for all heads: a cluster per sequence here
-  const int blocks = c.blocks, rank = blocks > 1 ? (int)cluster_rank() : 0, job = blockIdx.x / blocks, b = kJoint ? job : job / c.cache.hkv;
-  const int head = kJoint ? 0 : job - b * c.cache.hkv;
+  constexpr bool kPerSequence = JOINT && SELECT;  // one set for all heads
+  static_assert(!(JOINT && SELECT && MOVE));
+  const int blocks = c.blocks, rank = blocks > 1 ? (int)cluster_rank() : 0, job = blockIdx.x / blocks, b = kPerSequence ? job : job / c.cache.hkv;
+  const int head = kPerSequence ? 0 : job - b * c.cache.hkv;
   auto sync_all = [&] { if (blocks > 1) cluster_sync(); else __syncthreads(); };
+  if constexpr (SELECT) {
+    if (tid < 2) totals[tid] = 0;
+    if (blocks > 1) cluster_arrive();  // "this block runs": waited for before the first remote access
+  }
   if (c.head_wait) pdl_wait();
   pdl_trigger();
   pdl_wait();
 
+  if constexpr (SELECT) {
+    if (tid < 256) hist[0][tid] = hist[1][tid] = 0;
+    if (blocks == 1)  // (the slice is known; entries behind the sequence's end are looked at and not used)
+      for (int p = tid; p << c.cache.page_shift < min(c.max_len, kHeld); p += kThreads) pages[p] = page_of(c.cache, c.table, c.table_stride, b, p << c.cache.page_shift);
+  }
   const int given_len = chain_load_cached(c.lens + b), given_keep = chain_load_cached(c.counts + b);
   const int n = min(max(given_len, 0), c.max_len), wanted = min(max(given_keep, 0), n), k = min(wanted, c.max_keep);
   const bool all = k == n;
@@ -67,174 +90,342 @@ evict_kernel(EvictCall c) {
                      (stay > k ? FASTAV_DEV_PROTECT_OVERFLOW : 0);
     if (bits && c.device_status) atomicOr(c.device_status, bits);
   }
-  int32_t* const list = c.list + (long long)(MOVE && !SELECT ? b : job) * c.max_keep;  // rows of the pool, of head 0; -1: in no page
+  int32_t* const list = c.list + (long long)(JOINT ? b : job) * c.max_keep;  // rows of the pool, of head 0; -1: in no page
   if constexpr (SELECT) {
   const int slice = (n + blocks - 1) / blocks, t0 = min(n, rank * slice), t1 = min(n, t0 + slice);
-
-  auto look_up = [&](int t) {
-    const int page = page_of(c.cache, c.table, c.table_stride, b, t);
-    unsigned key = 0;
-    if (page >= 0) {
-      float w;
-      if (kJoint) {
-        double sum = 0.;
-        for (int h = 0; h < c.cache.hkv; ++h) sum += (double)chain_load(c.weights + pool_row(c.cache, page, h, t));
-        w = (float)sum;
-      } else {
-        w = chain_load(c.weights + pool_row(c.cache, page, head, t));
-      }
-      key = key_of(w);
-    } else if (c.device_status) {
-      atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
-    }
-    return t < c.first || t >= n - c.recent ? kStays : key;
+  const int shift = c.cache.page_shift, first_page = t0 >> shift;
+  if (blocks > 1)
+    for (int p = first_page + tid; p <= (min(t1, t0 + kHeld) - 1) >> shift; p += kThreads) pages[p - first_page] = page_of(c.cache, c.table, c.table_stride, b, p << shift);
+  __syncthreads();
+  auto page_at = [&](int t) { return t - t0 < kHeld ? pages[(t >> shift) - first_page] : page_of(c.cache, c.table, c.table_stride, b, t); };
+  auto weight_at = [&](int page, int t) {
+    if (!kPerSequence) return chain_load(c.weights + pool_row(c.cache, page, head, t));
+    double sum = 0.;
+#pragma unroll 4
+    for (int h = 0; h < c.cache.hkv; ++h) sum += (double)chain_load(c.weights + pool_row(c.cache, page, h, t));
+    return (float)sum;
   };
-  auto key_at = [&](int t) { return t - t0 < kHeld ? held[t - t0] : look_up(t); };
+  auto key_from = [&](int page, float w, int t) { return t < c.first || t >= n - c.recent ? kStays : page < 0 ? 0u : key_of(w); };
+
+  // ---- keys, all of a thread's loads at once ----
+  unsigned keys[kStripes];
+  {
+    float w[kStripes];
+    int page[kStripes];
+#pragma unroll
+    for (int i = 0; i < kStripes; ++i) {
+      const int t = t0 + i * kThreads + tid;
+      page[i] = t < t1 ? page_at(t) : -1;
+      if (!kPerSequence) w[i] = page[i] < 0 ? 0.f : weight_at(page[i], t);
+    }
+    if (kPerSequence) {  // all stripes of a head, then the next
+      double sum[kStripes];
+#pragma unroll
+      for (int i = 0; i < kStripes; ++i) sum[i] = 0.;
+#pragma unroll 4
+      for (int h = 0; h < c.cache.hkv; ++h)
+#pragma unroll
+        for (int i = 0; i < kStripes; ++i)
+          if (page[i] >= 0) sum[i] += (double)chain_load(c.weights + pool_row(c.cache, page[i], h, t0 + i * kThreads + tid));
+#pragma unroll
+      for (int i = 0; i < kStripes; ++i) w[i] = (float)sum[i];
+    }
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kStripes; ++i) {
+      const int t = t0 + i * kThreads + tid;
+      bad |= t < t1 && page[i] < 0;
+      keys[i] = key_from(page[i], w[i], t);
+    }
+    if (bad && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+  }
+  auto look_up = [&](int t) {
+    const int page = page_at(t);
+    if (page < 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+    return key_from(page, page < 0 ? 0.f : weight_at(page, t), t);
+  };
+
+  if (blocks > 1) cluster_wait();
 
   // ---- the threshold: the k-th largest key, and how many of those equal to it stay (the first ones) ----
-  unsigned threshold = 0, equal_stay = 0;
-  for (int t = t0 + tid; t < min(t1, t0 + kHeld); t += kThreads) held[t - t0] = look_up(t);
-  if (tid < 256) hist[0][tid] = 0;
-  __syncthreads();
+  unsigned threshold = all ? 0 : kStays, equal_stay = 0;
+  bool from_threshold = all;  // every key from the threshold on stays
   if (!all && k > 0) {
     unsigned remaining = k, prefix = 0;
     for (int pass = 0; pass < 4; ++pass) {
-      const int shift = 24 - 8 * pass;
-      unsigned* const mine = hist[pass & 1];
-      for (int t = t0 + tid; t < t1; t += kThreads) {
-        const unsigned key = key_at(t);
-        if (pass == 0 || key >> (shift + 8) == prefix) atomicAdd(&mine[key >> shift & 255u], 1u);
+      const int low = 24 - 8 * pass, buffer = pass & 1;
+      auto count = [&](unsigned key) {
+        if (pass == 0 || key >> (low + 8) == prefix) atomicAdd(&hist[buffer][key >> low & 255u], 1u);
+      };
+#pragma unroll
+      for (int i = 0; i < kStripes; ++i)
+        if (t0 + i * kThreads + tid < t1) count(keys[i]);
+      for (int t = t0 + kHeld + tid; t < t1; t += kThreads) count(look_up(t));
+      __syncthreads();
+      if (tid < 256) {
+        const unsigned mine = hist[buffer][tid];
+        hist[buffer][tid] = 0;  // for the pass after the next
+        if (blocks == 1) inbox[buffer][0][tid] = mine;
+        else
+          for (int r = 0; r < blocks; ++r) remote_store(remote(&inbox[buffer][rank][tid], r), mine);
       }
       sync_all();
-      if (tid < 256) hist[pass & 1 ^ 1][tid] = 0;  // (everybody has read it: ahead of the barrier)
-      unsigned total = 0;
-      const int digit = 255 - tid;  // thread 0 has the highest
-      if (tid < 256) {
-        if (blocks == 1) total = mine[digit];
-        else
-          for (int r = 0; r < blocks; ++r) {
-            unsigned v;
-            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote(&mine[digit], r)) : "memory");
-            total += v;
+      if (warp == 0) {  // lane l has the digits 255 - 8 l - j
+        unsigned bins[8], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bins[j] = 0;
+        for (int r = 0; r < blocks; ++r) {
+          const uint4 lo = reinterpret_cast<const uint4*>(inbox[buffer][r])[62 - 2 * lane], hi = reinterpret_cast<const uint4*>(inbox[buffer][r])[63 - 2 * lane];
+          bins[0] += hi.w; bins[1] += hi.z; bins[2] += hi.y; bins[3] += hi.x;
+          bins[4] += lo.w; bins[5] += lo.z; bins[6] += lo.y; bins[7] += lo.x;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += bins[j];
+        unsigned above = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const unsigned x = __shfl_up_sync(0xFFFFFFFFu, above, d);
+          if (lane >= d) above += x;
+        }
+        above -= sum;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (above < remaining && remaining <= above + bins[j]) {
+            found[buffer][0] = 255 - 8 * lane - j;
+            found[buffer][1] = remaining - above;
+            found[buffer][2] = bins[j];
           }
-      }
-      const unsigned above = sum_before<kWarps>(total, pass & 1 ? warp_b : warp_a, lane, warp);
-      if (tid < 256 && above < remaining && remaining <= above + total) {
-        found[0] = digit;
-        found[1] = remaining - above;
-        found[2] = total;
-      }
-      __syncthreads();
-      prefix = prefix << 8 | found[0];
-      remaining = found[1];
-      if (remaining == found[2]) {  // all of them stay: no need to tell them apart
-        threshold = shift == 0 ? prefix : prefix << shift;
-        equal_stay = 0xFFFFFFFFu;
-        break;
-      }
-      threshold = prefix;
-      equal_stay = remaining;
-      __syncthreads();  // `found` is written again
-    }
-  } else if (all) {
-    equal_stay = 0xFFFFFFFFu;
-  } else {
-    threshold = kStays;  // nobody stays
-    equal_stay = 0;
-  }
-  const bool from_threshold = equal_stay == 0xFFFFFFFFu;  // every key from the threshold on stays
-
-  // ---- the survivors' list ----
-  const int each = (t1 - t0 + kThreads - 1) / kThreads, mine0 = min(t1, t0 + tid * each), mine1 = min(t1, mine0 + each);
-  unsigned above = 0, equal = 0;
-  for (int t = mine0; t < mine1; ++t) {
-    const unsigned key = key_at(t);
-    above += from_threshold ? key >= threshold : key > threshold;
-    equal += !from_threshold && key == threshold;
-  }
-  __syncthreads();
-  const unsigned above_before = sum_before<kWarps>(above, warp_a, lane, warp), equal_before = sum_before<kWarps>(equal, warp_b, lane, warp);
-  if (tid == kThreads - 1) {
-    counts[0] = above_before + above;
-    counts[1] = equal_before + equal;
-  }
-  sync_all();
-  unsigned above_ahead = 0, equal_ahead = 0;
-  for (int r = 0; r < rank; ++r) {
-    unsigned x, y;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(remote(&counts[0], r)) : "memory");
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(remote(&counts[1], r)) : "memory");
-    above_ahead += x;
-    equal_ahead += y;
-  }
-  {
-    int32_t* const idx = c.keep_idx ? c.keep_idx + (long long)job * (kJoint ? c.cache.hkv : 1) * c.max_keep : nullptr;
-    unsigned a = above_ahead + above_before, e = equal_ahead + equal_before;
-    for (int t = mine0; t < mine1; ++t) {
-      const unsigned key = key_at(t);
-      const bool over = from_threshold ? key >= threshold : key > threshold, same = !from_threshold && key == threshold;
-      if (over || (same && e < equal_stay)) {
-        const unsigned at = a + min(e, from_threshold ? 0u : equal_stay);
-        if (at < (unsigned)k) {
-          const int page = page_of(c.cache, c.table, c.table_stride, b, t);
-          list[at] = page < 0 ? -1 : (int)pool_row(c.cache, page, 0, t);
-          if (idx)
-            for (int h = 0; h < (kJoint ? c.cache.hkv : 1); ++h) idx[(long long)h * c.max_keep + at] = t;
+          above += bins[j];
         }
       }
-      a += over;
-      e += same;
+      __syncthreads();
+      prefix = prefix << 8 | found[buffer][0];
+      remaining = found[buffer][1];
+      threshold = prefix << low;
+      equal_stay = remaining;
+      from_threshold = remaining == found[buffer][2];  // all of them stay: no need to tell them apart
+      if (from_threshold) break;
     }
   }
-  sync_all();  // the list is there for all blocks; nobody's shared memory is read by another any more
+  auto is_above = [&](unsigned key) { return from_threshold ? key >= threshold : key > threshold; };
+  auto is_equal = [&](unsigned key) { return !from_threshold && key == threshold; };
+
+  // ---- what the blocks before this one keep ----
+  unsigned above_ahead = all ? t0 : 0, equal_ahead = 0;
+  if (blocks > 1 && !all && k > 0) {
+    unsigned both_above = 0, both_equal = 0;
+#pragma unroll
+    for (int i = 0; i < kStripes; ++i)
+      if (t0 + i * kThreads + tid < t1) both_above += is_above(keys[i]), both_equal += is_equal(keys[i]);
+    for (int t = t0 + kHeld + tid; t < t1; t += kThreads) {
+      const unsigned key = look_up(t);
+      both_above += is_above(key);
+      both_equal += is_equal(key);
+    }
+    both_above = __reduce_add_sync(0xFFFFFFFFu, both_above);
+    both_equal = __reduce_add_sync(0xFFFFFFFFu, both_equal);
+    if (lane < blocks && lane > rank) {
+      asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(remote(&totals[0], lane)), "r"(both_above) : "memory");
+      asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(remote(&totals[1], lane)), "r"(both_equal) : "memory");
+    }
+    cluster_sync();
+    above_ahead = totals[0];
+    equal_ahead = totals[1];
+  }
+
+  // ---- the survivors' list, kStripes stripes at a time ----
+  int32_t* const idx = c.keep_idx ? c.keep_idx + (long long)job * (kPerSequence ? c.cache.hkv : 1) * c.max_keep : nullptr;
+  for (int g0 = t0; g0 < t1; g0 += kHeld) {
+    if (g0 > t0) {
+#pragma unroll
+      for (int i = 0; i < kStripes; ++i) {
+        const int t = g0 + i * kThreads + tid;
+        if (t < t1) keys[i] = look_up(t);
+      }
+      __syncthreads();
+    }
+    unsigned masks_above[kStripes], masks_equal[kStripes];
+#pragma unroll
+    for (int i = 0; i < kStripes; ++i) {
+      const bool there = g0 + i * kThreads + tid < t1;
+      masks_above[i] = masks_equal[i] = 0;
+      if (g0 + i * kThreads < t1) {
+        masks_above[i] = __ballot_sync(0xFFFFFFFFu, there && is_above(keys[i]));
+        masks_equal[i] = __ballot_sync(0xFFFFFFFFu, there && is_equal(keys[i]));
+      }
+      if (lane == 0) counted[i * kWarps + warp] = __popc(masks_above[i]) | __popc(masks_equal[i]) << 16;
+    }
+    __syncthreads();
+    if (warp == 0) {  // prefix sums of 4 counts a lane
+      constexpr int kEach = kStripes * kWarps / 32;
+      unsigned own[kEach], sum = 0;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        own[j] = counted[lane * kEach + j];
+        sum += own[j];
+      }
+      unsigned before = sum;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned x = __shfl_up_sync(0xFFFFFFFFu, before, d);
+        if (lane >= d) before += x;
+      }
+      if (lane == 31) found[0][0] = before;  // of all stripes
+      before -= sum;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        counted[lane * kEach + j] = before;
+        before += own[j];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kStripes; ++i) {
+      const int t = g0 + i * kThreads + tid;
+      if (t >= t1) break;
+      const unsigned bit = 1u << lane, before = counted[i * kWarps + warp];
+      const unsigned a = above_ahead + (before & 0xFFFFu) + __popc(masks_above[i] & (bit - 1)), e = equal_ahead + (before >> 16) + __popc(masks_equal[i] & (bit - 1));
+      const bool over = masks_above[i] & bit, same = masks_equal[i] & bit;
+      if (!over && !(same && e < equal_stay)) continue;
+      const unsigned at = a + (from_threshold ? 0u : min(e, equal_stay));
+      if (at >= (unsigned)k) continue;
+      const int page = page_at(t);
+      list[at] = page < 0 ? -1 : (int)pool_row(c.cache, page, 0, t);
+      if (idx)
+        for (int h = 0; h < (kPerSequence ? c.cache.hkv : 1); ++h) idx[(long long)h * c.max_keep + at] = t;
+    }
+    above_ahead += found[0][0] & 0xFFFFu;
+    equal_ahead += found[0][0] >> 16;
+  }
+  sync_all();  // the list is there for all blocks; nobody's shared memory is written by another any more
   }
   if constexpr (!MOVE) return;
 
   // ---- the rows ----
   const int32_t* const to_table = c.out_table ? c.out_table : c.table;
   const int to_stride = c.out_table ? c.out_stride : c.table_stride, of_head = head << c.cache.page_shift;
-  // Survivor i comes from `from` and goes to `to`; false: it stays where it is, or is left out.
-  auto moves = [&](int i, int& from, int& to) {
-    if (i >= k) return false;
-    from = chain_load(list + i);
-    const int page = page_of(c.cache, to_table, to_stride, b, i);
-    if (page < 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
-    if (from < 0 || page < 0) return false;
-    from += of_head;
-    to = (int)pool_row(c.cache, page, head, i);
-    return from != to;
+  const int piece = tid % kPieces, row_of = tid / kPieces, step = blocks * kMoved;
+  // Thread t < kMoved finds where row t of a round comes from and goes to; -1: it stays where it is, is left out, or does not exist.
+  auto locate = [&](int r0) {
+    const int i = r0 + rank * kMoved + tid;
+    int from = -1, to = -1;
+    if (i < k) {
+      from = chain_load(list + i);
+      const int page = page_of(c.cache, to_table, to_stride, b, i);
+      if (page < 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+      to = page < 0 ? -1 : (int)pool_row(c.cache, page, head, i);
+      if (from >= 0) from += of_head;
+      if (from < 0 || to < 0 || from == to) from = to = -1;
+    }
+    return make_int2(from, to);
   };
-  const int piece = tid % kPieces, row_of = tid / kPieces;
-  for (int r0 = 0; r0 < k; r0 += blocks * kMoved) {
-    const int i0 = r0 + rank * kMoved;
+  struct Round {
     uint4 x[kUnroll], y[kUnroll];
-    int to[kUnroll], small_to[kSmall];
-    float value[kSmall];
+    int to[kUnroll], small_to;
+    float ks, vs, w;
+  };
+  auto read = [&](const int2* places, Round& r) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      int from;
-      if (!moves(i0 + u * kAtOnce + row_of, from, to[u])) { to[u] = -1; continue; }
-      x[u] = chain_load(reinterpret_cast<const uint4*>(c.cache.k + (long long)from * DIM) + piece);
-      y[u] = chain_load(reinterpret_cast<const uint4*>(c.cache.v + (long long)from * DIM) + piece);
+      const int2 at = places[u * kAtOnce + row_of];
+      r.to[u] = at.y;
+      if (at.y < 0) continue;
+      r.x[u] = chain_load(reinterpret_cast<const uint4*>(c.cache.k + (long long)at.x * DIM) + piece);
+      r.y[u] = chain_load(reinterpret_cast<const uint4*>(c.cache.v + (long long)at.x * DIM) + piece);
     }
-    auto small_pool = [&](int j) { const int which = (j * kThreads + tid) / kMoved; return which == 0 ? c.cache.k_scale : which == 1 ? c.cache.v_scale : c.weights; };
-#pragma unroll
-    for (int j = 0; j < kSmall; ++j) {
-      const int item = j * kThreads + tid;
-      int from;
-      if (item >= 3 * kMoved || !moves(i0 + item % kMoved, from, small_to[j])) { small_to[j] = -1; continue; }
-      value[j] = chain_load(small_pool(j) + from);
+    r.small_to = -1;
+    if (tid < kMoved) {
+      const int2 at = places[tid];
+      r.small_to = at.y;
+      if (at.y >= 0) {
+        r.ks = chain_load(c.cache.k_scale + at.x);
+        r.vs = chain_load(c.cache.v_scale + at.x);
+        r.w = chain_load(c.weights + at.x);
+      }
     }
-    if (!c.out_table) sync_all();
+  };
+  auto write = [&](const Round& r) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-      if (to[u] >= 0) {
-        reinterpret_cast<uint4*>(c.cache.k + (long long)to[u] * DIM)[piece] = x[u];
-        reinterpret_cast<uint4*>(c.cache.v + (long long)to[u] * DIM)[piece] = y[u];
+      if (r.to[u] >= 0) {
+        reinterpret_cast<uint4*>(c.cache.k + (long long)r.to[u] * DIM)[piece] = r.x[u];
+        reinterpret_cast<uint4*>(c.cache.v + (long long)r.to[u] * DIM)[piece] = r.y[u];
       }
+    if (r.small_to >= 0) {
+      c.cache.k_scale[r.small_to] = r.ks;
+      c.cache.v_scale[r.small_to] = r.vs;
+      c.weights[r.small_to] = r.w;
+    }
+  };
+  if (k == 0) return;  // (all blocks of the cluster)
+  Round now, next;
+  if (tid < kMoved) places[0][tid] = locate(0);
+  if (tid < kMoved) places[1][tid] = locate(step);
+  __syncthreads();
+  read(places[0], now);
+  int buffer = 0;
+  for (int r0 = 0; r0 < k; r0 += step, buffer ^= 1) {
+    sync_all();  // this round's rows have been read, and the next one's are located
+    if (r0 + step < k) read(places[buffer ^ 1], next);
+    if (r0 + 2 * step < k && tid < kMoved) places[buffer][tid] = locate(r0 + 2 * step);
+    write(now);
+    now = next;
+  }
+}
+
+// Rows to pages of their own, kChunk survivors of a sequence's KV head a block.
+template <int DIM>
+__global__ void __launch_bounds__(kChunkThreads)
+evict_rows_kernel(EvictCall c, int chunks, bool joint) {
+  constexpr int kPieces = DIM / 16, kAtOnce = kChunkThreads / kPieces, kUnroll = kChunk / kAtOnce;
+  __shared__ int source[kChunk], place[kChunk];  // rows of the pool; -1: left out
+  const int job = blockIdx.x / chunks, b = job / c.cache.hkv, head = job - b * c.cache.hkv, i0 = (blockIdx.x - job * chunks) * kChunk, tid = threadIdx.x;
+  if (c.head_wait) pdl_wait();
+  pdl_trigger();
+  pdl_wait();
+  const int n = min(max(chain_load_cached(c.lens + b), 0), c.max_len), k = min(min(max(chain_load_cached(c.counts + b), 0), n), c.max_keep);
+  if (i0 >= k) return;
+  float ks = 0.f, vs = 0.f, w = 0.f;
+  int from = -1, to = -1;
+  if (tid < kChunk) {
+    const int i = i0 + tid;
+    if (i < k) {
+      from = chain_load(c.list + (long long)(joint ? b : job) * c.max_keep + i);
+      const int page = page_of(c.cache, c.out_table, c.out_stride, b, i);
+      if (page >= 0) to = (int)pool_row(c.cache, page, head, i);
+      else if (c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+      if (from < 0 || to < 0) from = to = -1;
+      else from += head << c.cache.page_shift;
+    }
+    source[tid] = from;
+    place[tid] = to;
+  }
+  __syncthreads();
+  if (to >= 0) {
+    ks = chain_load(c.cache.k_scale + from);
+    vs = chain_load(c.cache.v_scale + from);
+    w = chain_load(c.weights + from);
+  }
+  const int piece = tid % kPieces, row_of = tid / kPieces;
+  uint4 x[kUnroll], y[kUnroll];
 #pragma unroll
-    for (int j = 0; j < kSmall; ++j)
-      if (small_to[j] >= 0) small_pool(j)[small_to[j]] = value[j];
+  for (int u = 0; u < kUnroll; ++u) {
+    const int at = source[u * kAtOnce + row_of];
+    if (at < 0) continue;
+    x[u] = chain_load(reinterpret_cast<const uint4*>(c.cache.k + (long long)at * DIM) + piece);
+    y[u] = chain_load(reinterpret_cast<const uint4*>(c.cache.v + (long long)at * DIM) + piece);
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int at = place[u * kAtOnce + row_of];
+    if (at < 0) continue;
+    reinterpret_cast<uint4*>(c.cache.k + (long long)at * DIM)[piece] = x[u];
+    reinterpret_cast<uint4*>(c.cache.v + (long long)at * DIM)[piece] = y[u];
+  }
+  if (to >= 0) {
+    c.cache.k_scale[to] = ks;
+    c.cache.v_scale[to] = vs;
+    c.weights[to] = w;
   }
 }
 
@@ -282,19 +473,26 @@ extern "C" int32_t fastav_cache_evict(const fastav_evict_params* p, const fastav
   c.lens_out = kv_lens_out; c.keep_idx = keep_idx_out_opt; c.list = static_cast<int32_t*>(workspace);
   c.device_status = device_status;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  auto go = [&](auto kernel, int jobs, size_t smem) {
-    c.blocks = cluster_blocks(jobs, p->max_kv_len, 256, kPortableCluster);
+  auto go = [&](auto kernel, int jobs) {
+    c.blocks = cluster_blocks(jobs, p->max_kv_len, kLeastSlice, kPortableCluster);
     count_launches(1);
-    return launch_chained_cluster(kernel, dim3((unsigned)(jobs * c.blocks)), dim3(kThreads), c.blocks > 1 ? c.blocks : 0, smem, st, c);
+    return launch_chained_cluster(kernel, dim3((unsigned)(jobs * c.blocks)), dim3(kThreads), c.blocks > 1 ? c.blocks : 0, 0, st, c);
   };
-  constexpr size_t kKeys = kHeld * sizeof(unsigned);
-  const int heads = p->batch * cache->num_kv_heads;
+  const bool joint = (p->flags & FASTAV_EVICT_JOINT) != 0, wide = c.cache.dim == 128;
+  const int jobs = p->batch * cache->num_kv_heads;
+  const long long chunks = (p->max_keep + kChunk - 1) / kChunk;
+  const bool apart = out_table_opt && p->max_keep > 0 && chunks * jobs <= INT_MAX && (joint || p->max_keep > kFewRows * cluster_blocks(jobs, p->max_kv_len, kLeastSlice, kPortableCluster));
   cudaError_t e;
-  if (p->flags & FASTAV_EVICT_JOINT) {
-    e = go(evict_kernel<64, true, false>, p->batch, kKeys);
-    if (e == cudaSuccess) e = c.cache.dim == 128 ? go(evict_kernel<128, false, true>, heads, 0) : go(evict_kernel<64, false, true>, heads, 0);
-  } else {
-    e = c.cache.dim == 128 ? go(evict_kernel<128, true, true>, heads, kKeys) : go(evict_kernel<64, true, true>, heads, kKeys);
+  if (joint) e = go(evict_kernel<64, true, false, true>, p->batch);
+  else if (apart) e = go(evict_kernel<64, true, false, false>, jobs);
+  else e = wide ? go(evict_kernel<128, true, true, false>, jobs) : go(evict_kernel<64, true, true, false>, jobs);
+  if (e == cudaSuccess && apart) {
+    count_launches(1);
+    const dim3 grid((unsigned)(chunks * jobs));
+    e = wide ? launch_chained(evict_rows_kernel<128>, grid, dim3(kChunkThreads), 0, st, c, (int)chunks, joint)
+             : launch_chained(evict_rows_kernel<64>, grid, dim3(kChunkThreads), 0, st, c, (int)chunks, joint);
+  } else if (e == cudaSuccess && joint) {
+    e = wide ? go(evict_kernel<128, false, true, true>, jobs) : go(evict_kernel<64, false, true, true>, jobs);
   }
   return e == cudaSuccess ? FASTAV_OK : cuda_failed(e);
 }
