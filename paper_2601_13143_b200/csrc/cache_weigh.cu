@@ -16,142 +16,234 @@ namespace {
 constexpr int kMostFew = 16;  // stacked rows; beyond, the kernel for many
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = 32;  // keys of a unit
 
-// Up to 16 stacked rows (query rows times G) at once, more by turns.  A warp has a run of units of one KV head; mma.sync with the keys as rows, S^T = K Q^T, the codes
-// from global memory straight to the registers of the operand: the contraction may run over head_dim in any order, so lane 4 n + t holds, of query row
-// n and of keys n and n + 8, the elements DIM / 4 t ..
-template <int DIM, bool FP8, int NT>
-__global__ void __launch_bounds__(kThreads)
-weigh_few_kernel(WeighCall c, int run) {
+// Up to 16 stacked rows (query rows times G) at once, more by turns.  mma.sync with the keys as rows, S^T = K Q^T, the codes from global memory straight to
+// the registers of the operand: the contraction may run over head_dim in any order, so lane 4 n + t holds, of query row n and of keys n and n + 8, the
+// elements DIM / 4 t ..
+//
+// A TASK is a run of units of one KV head; every warp has one (or, with many short sequences, several).  How long a run has to be for all of them to fit into one wave of
+// blocks comes from the lengths themselves: by the host's bounds, ragged sequences leave warps without work (32 of 512 to 4,096 tokens: 12.6 us).
+template <int DIM>
+constexpr int kBlocksPerSm = DIM == 128 ? 3 : 4;  // (4 and 5 of up to 8 rows: no quicker, and registers spill)
+
+// ONE_LOOK: 32 sequences or fewer, whose bounds a warp looks at once.
+template <int DIM, bool FP8, int NT, bool ONE_LOOK>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm<DIM>)
+weigh_few_kernel(WeighCall c) {
   constexpr int kSteps = DIM / 16, kPieces = DIM / 64, kTile = 8 * NT;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n8 = lane >> 2, t4 = lane & 3;
-  const int b = blockIdx.z, head = blockIdx.y;
-  if (c.head_wait) pdl_wait();
-  pdl_trigger();
-  pdl_wait();
-  const WeighSpan s = weigh_span(c, b);
-  if (s.bad && blockIdx.x == 0 && head == 0 && threadIdx.x == 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_SHAPE_MISMATCH);
-  const int u0 = (blockIdx.x * kWarps + warp) * run, u1 = min(u0 + run, (s.len + kUnit - 1) / kUnit);
-  if (u0 >= u1) return;
-  const int stacked = s.rows * c.group;
-  const int fresh = c.decay == 0.f ? 0 : c.weighed ? chain_load_cached(c.weighed + b) : s.len;  // tokens from here on have no weight yet
+  pdl_wait();  // everything may be what earlier work wrote
 
-  for (int row0 = 0; row0 == 0 || row0 < stacked; row0 += kTile) {
-    uint32_t qf[NT][kSteps][2];
-    float row_scale[NT][2], lse[NT][2];  // of rows 2 t4 + (0, 1)
-    int sees[NT][2];
+  // ---- the tasks: every warp finds its own, a lane per sequence, 32 sequences at a time ----
+  auto units_at = [&](int b) { return b < c.batch ? (min(max(chain_load_cached(c.lens + b), 0), c.max_len) + kUnit - 1) / kUnit : 0; };
+  auto fresh_at = [&](int b) { return c.decay == 0.f ? 0 : c.weighed ? chain_load_cached(c.weighed + b) : INT_MAX; };  // tokens from here on have no weight yet
+  WeighSpan seq{0, 0, 0, false};  // up to 32 sequences: of sequence `lane`, asked for beside its length
+  int seq_fresh = 0;
+  if (ONE_LOOK && lane < c.batch) {
+    seq = weigh_span(c, lane);
+    seq_fresh = fresh_at(lane);
+  }
+  int units = ONE_LOOK ? (seq.len + kUnit - 1) / kUnit : units_at(lane);
+  long long all = units;
+  if (!ONE_LOOK)
+#pragma unroll 4
+    for (int b = 32 + lane; b < c.batch; b += 32) all += units_at(b);
 #pragma unroll
-    for (int g = 0; g < NT; ++g) {
-      const int i = row0 + 8 * g + n8;
-      const bool there = i < stacked;
-      const int r = there ? i / c.group : 0, query_head = head * c.group + i - r * c.group;
-      uint32_t x[kSteps * 2];
-      const uint4* const from = reinterpret_cast<const uint4*>(c.q + (long long)(s.row0 + r) * c.q_st + (long long)query_head * c.q_sh + t4 * (DIM / 4));
-      unsigned top = 0;  // bf16 bits of the largest magnitude; what is not a number is larger still
+  for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, d);
+  if (blockIdx.x == 0 && warp == 0) {
+    bool bad = seq.bad;
+    if (!ONE_LOOK)
+      for (int b = lane; b < c.batch; b += 32) bad |= weigh_span(c, b).bad;
+    if (bad && c.device_status) atomicOr(c.device_status, FASTAV_DEV_SHAPE_MISMATCH);
+  }
+  const long long warps = (long long)gridDim.x * kWarps, room = max(warps - (long long)c.batch * c.cache.hkv, (warps + 1) / 2);
+  const int run = (int)max(1ll, (all * c.cache.hkv + room - 1) / room);  // tasks: units / run, and less than one more for each sequence and head
+  int b0 = 0, ahead = 0;  // tasks of the sequences before b0
+  for (int task = blockIdx.x * kWarps + warp;; task += gridDim.x * kWarps) {
+    int own_tasks, upto;
+    unsigned behind;
+    for (;;) {  // to the 32 sequences one of which has the task
+      own_tasks = c.cache.hkv * ((units + run - 1) / run);
+      upto = own_tasks;
 #pragma unroll
-      for (int j = 0; j < kSteps / 2; ++j) {
-        const uint4 v = there ? chain_load(from + j) : make_uint4(0, 0, 0, 0);
-        x[4 * j] = v.x; x[4 * j + 1] = v.y; x[4 * j + 2] = v.z; x[4 * j + 3] = v.w;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += x;
       }
-#pragma unroll
-      for (int j = 0; j < kSteps * 2; ++j) top = __vmaxu2(top, x[j] & 0x7FFF7FFFu);
-      top = max(top >> 16, top & 0xFFFFu);
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      const float to = query_power(top);
-#pragma unroll
-      for (int k = 0; k < kSteps; ++k)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t v = x[2 * k + half];
-          qf[g][k][half] = two_f16(__uint_as_float(v << 16) * to, __uint_as_float(v & 0xFFFF0000u) * to);
-        }
-      const float own_lse = there ? chain_load(c.lse + (long long)(s.row0 + r) * c.hq + query_head) : -INFINITY;
-      const int own_sees = own_lse == -INFINITY ? 0 : c.causal ? max(0, s.len - s.rows + r + 1) : s.len;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {  // of row n8 -> of rows 2 t4 + e
-        const int of = 4 * (2 * t4 + e);
-        row_scale[g][e] = query_scale(c.scale_log2, __shfl_sync(0xFFFFFFFFu, to, of));
-        lse[g][e] = __shfl_sync(0xFFFFFFFFu, own_lse, of) * kLog2e;
-        sees[g][e] = __shfl_sync(0xFFFFFFFFu, own_sees, of);
-      }
+      behind = __ballot_sync(0xFFFFFFFFu, ahead + upto > task);
+      if (behind) break;
+      ahead += __shfl_sync(0xFFFFFFFFu, upto, 31);
+      b0 += 32;
+      if (ONE_LOOK || b0 >= c.batch) return;
+      units = units_at(b0 + lane);
     }
+    const int at = __ffs(behind) - 1, b = b0 + at;
+    WeighSpan s{__shfl_sync(0xFFFFFFFFu, seq.row0, at), __shfl_sync(0xFFFFFFFFu, seq.rows, at), __shfl_sync(0xFFFFFFFFu, seq.len, at), false};
+    int fresh = __shfl_sync(0xFFFFFFFFu, seq_fresh, at);
+    if (!ONE_LOOK) {
+      s = weigh_span(c, b);
+      fresh = fresh_at(b);
+    }
+    const int all_units = __shfl_sync(0xFFFFFFFFu, units, at), per_head = (all_units + run - 1) / run, in_seq = task - ahead - __shfl_sync(0xFFFFFFFFu, upto - own_tasks, at);
+    const int head = in_seq / per_head, u0 = (in_seq - head * per_head) * run, u1 = min(u0 + run, all_units);
+    pdl_trigger();
+    const int stacked = s.rows * c.group;
 
-    for (int u = u0; u < u1; ++u) {
-      const int key0 = u * kUnit;
-      // Lane's key is key0 + lane for page, scale and weight; pages hold 16 tokens or more, so sixteen lanes have one page.
-      const bool mine = key0 + lane < s.len;
-      const int page = mine ? page_of(c.cache, c.table, c.table_stride, b, key0 + lane) : -1;
-      if (mine && page < 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
-      const long long at = page < 0 ? 0 : pool_row(c.cache, page, head, key0 + lane);
-      const float own_scale = page < 0 ? 0.f : chain_load(c.cache.k_scale + at) * kKeyScaleFactor;
-      const float before = page >= 0 && (row0 > 0 || key0 + lane < fresh) ? chain_load(c.weights + at) : 0.f;
-      const long long half_row[2] = {__shfl_sync(0xFFFFFFFFu, at, 0), __shfl_sync(0xFFFFFFFFu, at, 16)};
+    // Lane's key of a unit is key0 + lane for page, scale and weight; pages hold 16 tokens or more, so sixteen lanes have one page.
+    struct Unit {
       uint4 a[2][kPieces], d[2][kPieces];  // of 16 keys h: key n8, key n8 + 8
+      long long at;                        // row of the pool; -1: none
+      float scale, before;
+    };
+    const int32_t* const pages = c.table + (long long)b * c.table_stride;
+    auto page_entry = [&](int u) { return u < u1 && u * kUnit + lane < s.len ? chain_load_cached(pages + (u * kUnit + lane >> c.cache.page_shift)) : -1; };
+    auto ask = [&](int u, int page, bool again, Unit& x) {
+      const int key = u * kUnit + lane;
+      const bool there = (unsigned)page < (unsigned)c.cache.num_pages;
+      if (!there && key < s.len && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+      x.at = there ? pool_row(c.cache, page, head, key) : -1;
+      const long long at = there ? x.at : 0;  // (keys that are none read the pool's first rows: in bounds)
+      x.scale = chain_load(c.cache.k_scale + at);
+      x.before = there && (again || key < fresh) ? chain_load(c.weights + at) : 0.f;
+      const long long half_row[2] = {__shfl_sync(0xFFFFFFFFu, at, 0), __shfl_sync(0xFFFFFFFFu, at, 16)};
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
           const uint8_t* const from = c.cache.k + (half_row[h] + n8) * DIM + (t4 * kPieces + p) * 16;
-          a[h][p] = chain_load(reinterpret_cast<const uint4*>(from));
-          d[h][p] = chain_load(reinterpret_cast<const uint4*>(from + 8 * DIM));
+          x.a[h][p] = chain_load(reinterpret_cast<const uint4*>(from));
+          x.d[h][p] = chain_load(reinterpret_cast<const uint4*>(from + 8 * DIM));
         }
-      float z[NT][2][4];
+    };
+
+    for (int row0 = 0; row0 == 0 || row0 < stacked; row0 += kTile) {
+      int page = page_entry(u0);
+      // The query rows, asked for beside the first page; the first keys are on their way while they become operands.
+      uint32_t x[NT][kSteps * 2];
+      float own_lse[NT];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int g = 0; g < NT; ++g) {
+        const int i = row0 + 8 * g + n8;
+        const bool there = i < stacked;
+        const int r = there ? i / c.group : 0, query_head = head * c.group + i - r * c.group;
+        const uint4* const from = reinterpret_cast<const uint4*>(c.q + (long long)(s.row0 + r) * c.q_st + (long long)query_head * c.q_sh + t4 * (DIM / 4));
 #pragma unroll
-        for (int g = 0; g < NT; ++g)
+        for (int j = 0; j < kSteps / 2; ++j) {
+          const uint4 v = there ? chain_load(from + j) : make_uint4(0, 0, 0, 0);
+          x[g][4 * j] = v.x; x[g][4 * j + 1] = v.y; x[g][4 * j + 2] = v.z; x[g][4 * j + 3] = v.w;
+        }
+        own_lse[g] = there ? chain_load(c.lse + (long long)(s.row0 + r) * c.hq + query_head) : -INFINITY;
+      }
+      Unit now, next;
+      ask(u0, page, row0 > 0, now);
+      page = page_entry(u0 + 1);
+      uint32_t qf[NT][kSteps][2];
+      float row_scale[NT][2], lse[NT][2];  // of rows 2 t4 + (0, 1)
+      int sees[NT][2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) z[g][h][i] = 0.f;
+      for (int g = 0; g < NT; ++g) {
+        const int i = row0 + 8 * g + n8, r = i < stacked ? i / c.group : 0;
+        unsigned top = 0;  // bf16 bits of the largest magnitude; what is not a number is larger still
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-          const uint32_t wa[4] = {a[h][p].x, a[h][p].y, a[h][p].z, a[h][p].w}, wb[4] = {d[h][p].x, d[h][p].y, d[h][p].z, d[h][p].w};
+        for (int j = 0; j < kSteps * 2; ++j) top = __vmaxu2(top, x[g][j] & 0x7FFF7FFFu);
+        top = max(top >> 16, top & 0xFFFFu);
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const float to = query_power(top);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t a0, a1, a2, a3;
-            four_codes<FP8>(wa[i], a0, a2);
-            four_codes<FP8>(wb[i], a1, a3);
+        for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-            for (int g = 0; g < NT; ++g) mma_f16(z[g][h], a0, a1, a2, a3, qf[g][4 * p + i][0], qf[g][4 * p + i][1]);
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t v = x[g][2 * k + half];
+            qf[g][k][half] = two_f16(__uint_as_float(v << 16) * to, __uint_as_float(v & 0xFFFF0000u) * to);
+          }
+        const int own_sees = own_lse[g] == -INFINITY ? 0 : c.causal ? max(0, s.len - s.rows + r + 1) : s.len;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {  // of row n8 -> of rows 2 t4 + e
+          const int of = 4 * (2 * t4 + e);
+          row_scale[g][e] = query_scale(c.scale_log2, __shfl_sync(0xFFFFFFFFu, to, of));
+          lse[g][e] = __shfl_sync(0xFFFFFFFFu, own_lse[g], of) * kLog2e;
+          sees[g][e] = __shfl_sync(0xFFFFFFFFu, own_sees, of);
+        }
+      }
+
+      auto weigh = [&](int u, const Unit& k) {
+        const int key0 = u * kUnit;
+        float z[NT][2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int g = 0; g < NT; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[g][h][i] = 0.f;
+#pragma unroll
+          for (int p = 0; p < kPieces; ++p) {
+            const uint32_t wa[4] = {k.a[h][p].x, k.a[h][p].y, k.a[h][p].z, k.a[h][p].w}, wb[4] = {k.d[h][p].x, k.d[h][p].y, k.d[h][p].z, k.d[h][p].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t a0, a1, a2, a3;
+              four_codes<FP8>(wa[i], a0, a2);
+              four_codes<FP8>(wb[i], a1, a3);
+#pragma unroll
+              for (int g = 0; g < NT; ++g) mma_f16(z[g][h], a0, a1, a2, a3, qf[g][4 * p + i][0], qf[g][4 * p + i][1]);
+            }
           }
         }
+        const float own_scale = k.scale * kKeyScaleFactor;
+        float paid[4];  // to keys n8 + 8 i by the rows of this lane
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float scale = __shfl_sync(0xFFFFFFFFu, own_scale, 8 * i + n8);
+          paid[i] = 0.f;
+#pragma unroll
+          for (int g = 0; g < NT; ++g)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float p = ptx::ex2_approx(fmaf(z[g][i / 2][i % 2 * 2 + e] * scale, row_scale[g][e], -lse[g][e]));
+              paid[i] += key0 + 8 * i + n8 < sees[g][e] ? p : 0.f;
+            }
+          paid[i] += __shfl_xor_sync(0xFFFFFFFFu, paid[i], 1);
+          paid[i] += __shfl_xor_sync(0xFFFFFFFFu, paid[i], 2);
+        }
+        // lane 4 n + t has the sums of keys n + 8 i: lane 8 i + n takes its own from lane 4 n
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = __shfl_sync(0xFFFFFFFFu, paid[i], 4 * (lane & 7));
+          if (lane >> 3 == i) sum = x;
+        }
+        if (k.at >= 0) c.weights[k.at] = fmaf(row0 > 0 ? 1.f : c.decay, k.before, sum);
+      };
+      // A unit is asked for while the one before is weighed, its page a unit earlier still.
+      for (int u = u0;;) {
+        if (u + 1 < u1) {
+          ask(u + 1, page, row0 > 0, next);
+          page = page_entry(u + 2);
+        }
+        weigh(u, now);
+        if (++u >= u1) break;
+        if (u + 1 < u1) {
+          ask(u + 1, page, row0 > 0, now);
+          page = page_entry(u + 2);
+        }
+        weigh(u, next);
+        if (++u >= u1) break;
       }
-      float paid[4];  // to keys n8 + 8 i by the rows of this lane
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float scale = __shfl_sync(0xFFFFFFFFu, own_scale, 8 * i + n8);
-        paid[i] = 0.f;
-#pragma unroll
-        for (int g = 0; g < NT; ++g)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float p = ptx::ex2_approx(fmaf(z[g][i / 2][i % 2 * 2 + e] * scale, row_scale[g][e], -lse[g][e]));
-            paid[i] += key0 + 8 * i + n8 < sees[g][e] ? p : 0.f;
-          }
-        paid[i] += __shfl_xor_sync(0xFFFFFFFFu, paid[i], 1);
-        paid[i] += __shfl_xor_sync(0xFFFFFFFFu, paid[i], 2);
-      }
-      // lane 4 n + t has the sums of keys n + 8 i: lane 8 i + n takes its own from lane 4 n
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = __shfl_sync(0xFFFFFFFFu, paid[i], 4 * (lane & 7));
-        if (lane >> 3 == i) sum = x;
-      }
-      if (page >= 0) c.weights[at] = fmaf(row0 > 0 ? 1.f : c.decay, before, sum);
     }
   }
 }
 
+template <int DIM, bool FP8, int NT>
+cudaError_t launch_few(const WeighCall& c, cudaStream_t stream) {
+  const long long units = (c.max_len + kUnit - 1) / kUnit, blocks = (units * c.cache.hkv * c.batch + kWarps - 1) / kWarps, most = (long long)kNumSMs * kBlocksPerSm<DIM>;
+  count_launches(1);
+  const dim3 grid((unsigned)(blocks < most ? blocks : most));
+  return c.batch <= 32 ? launch_chained(weigh_few_kernel<DIM, FP8, NT, true>, grid, dim3(kThreads), 0, stream, c)
+                       : launch_chained(weigh_few_kernel<DIM, FP8, NT, false>, grid, dim3(kThreads), 0, stream, c);
+}
 template <int NT>
 cudaError_t launch_few(const WeighCall& c, cudaStream_t stream) {
-  // Runs as short as fill the SMs with 16 warps each.
-  const long long units = (c.max_len + kUnit - 1) / kUnit, all = units * c.cache.hkv * c.batch;
-  const int run = (int)max(1ll, min(all / (kNumSMs * 16), 64ll));
-  const dim3 grid((unsigned)((units + (long long)run * kWarps - 1) / ((long long)run * kWarps)), c.cache.hkv, c.batch);
-  auto go = [&](auto kernel) { return launch_chained(kernel, grid, dim3(kThreads), 0, stream, c, run); };
-  count_launches(1);
-  if (c.cache.dim == 128) return c.cache.fp8 ? go(weigh_few_kernel<128, true, NT>) : go(weigh_few_kernel<128, false, NT>);
-  return c.cache.fp8 ? go(weigh_few_kernel<64, true, NT>) : go(weigh_few_kernel<64, false, NT>);
+  if (c.cache.dim == 128) return c.cache.fp8 ? launch_few<128, true, NT>(c, stream) : launch_few<128, false, NT>(c, stream);
+  return c.cache.fp8 ? launch_few<64, true, NT>(c, stream) : launch_few<64, false, NT>(c, stream);
 }
 
 }  // namespace
