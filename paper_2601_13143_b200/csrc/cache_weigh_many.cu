@@ -8,10 +8,10 @@
 //
 //   warps 0-15  four teams of four, a thread per key: exponentials of 128 columns at a time from tensor memory, twice buffered, summed in a register.  Two
 //               teams share a unit's columns; with one unit the two pairs of teams take turns with the row tiles.
-//   warps 16-19 codes -> bf16 operand tiles in shared memory, a group of units ahead
-//   warp 20     query rows by TMA
-//   warp 21     issues the MMAs
-//   warp 22     log-sum-exps and masks of the query rows (23: nothing; registers move by whole teams)
+//   warps 16-23 codes -> bf16 operand tiles in shared memory, scales and weights so far beside them, a group of units ahead
+//   warp 24     query rows by TMA
+//   warp 25     issues the MMAs
+//   warp 26     log-sum-exps and masks of the query rows (27: nothing; registers move by whole teams)
 //
 // Bound by the exponentials (16 per clock and SM; the special-function unit is busy for some 75 % of the time), while the MMAs of the same elements
 // take half as long.  1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials): 256 us.  With eight summing warps a block instead of
@@ -26,11 +26,11 @@ namespace fastav {
 namespace {
 
 constexpr int kTile = 128;  // keys of a unit; stacked rows of a row tile, at most
-constexpr int kSumWarps = 16, kConvWarps = 4, kLoadWarp = kSumWarps + kConvWarps, kIssueWarp = kLoadWarp + 1, kRowWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
+constexpr int kSumWarps = 16, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kIssueWarp = kLoadWarp + 1, kRowWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
 // Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
-constexpr int kSumRegs = 88, kConvRegs = 72, kLastRegs = 48;
+constexpr int kSumRegs = 80, kConvRegs = 64, kLastRegs = 48;
 constexpr int kRegsNeeded = 32 * (kSumWarps * kSumRegs + kConvWarps * kConvRegs + 4 * kLastRegs);
-constexpr int kStages = 2, kRowSlots = 4;
+constexpr int kStages = 2, kRowSlots = 4, kKeySlots = 4;
 constexpr int kTmemCols = 512;
 constexpr int kPiece = 32;  // columns of tensor memory in registers at a time
 constexpr int kHalfBytes = 128 * 128;  // 128 rows of 128 bytes: 64 elements
@@ -46,8 +46,13 @@ struct RowSlot {
   alignas(16) int sees[kTile];       // keys that the row sees; 0: it pays nothing
   int least[kTile / 32];             // the least of 32 of them
 };
+struct KeySlot {  // of a group of units
+  int row[2 * kTile];  // of the pool; -1: no key, or in no page
+  float scale[2 * kTile], before[2 * kTile];  // (of such, too: 0)
+};
 struct Control {
-  uint64_t k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[2][2], s_empty[2][2];
+  KeySlot keys[kKeySlots];
+  uint64_t keys_full[kKeySlots], keys_empty[kKeySlots], k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[2][2], s_empty[2][2];
   RowSlot rows[kRowSlots];
   float join[2][4][kTile];
   long long warp_sum[kWarps];
@@ -64,30 +69,35 @@ inline void mark_head(ManyCall& c, bool head) { c.w.head_wait = head ? 1 : 0; }
 
 // A block's run, walked by every role for itself.
 struct Run {
-  int b, u, end_b, end_u;
+  int b, end_b, end_u, start_u;
   WeighSpan s;
-  int key_tiles = -1, row_tiles, head, tile, units;  // units: 1 or 2 from `tile` on
-  __device__ __forceinline__ Run(const Control& ctl) : b(ctl.first[0]), u(ctl.unit[0]), end_b(ctl.first[1]), end_u(ctl.unit[1]) {}
+  int row_tiles, head, tile, units;  // units: 1 or 2 from `tile` on
+  int key_tiles = -1, left = 0;      // left: units of the sequence that are still to come
+  __device__ __forceinline__ Run(const Control& ctl) : b(ctl.first[0]), end_b(ctl.first[1]), end_u(ctl.unit[1]), start_u(ctl.unit[0]) {}
+  // To the next group; what it finds is meant to be short, every role goes through it once a group.
   __device__ __forceinline__ bool next(const ManyCall& c) {
-    for (;;) {
-      if (b > end_b || (b == end_b && u >= end_u)) return false;
-      if (key_tiles < 0) {
+    if (left > 0) {
+      tile += units;
+      if (tile >= key_tiles) {
+        tile = 0;
+        ++head;
+      }
+    } else {
+      for (;; ++b, start_u = 0, key_tiles = -1) {
+        if (key_tiles >= 0) continue;  // this one is done
+        if (b > end_b || (b == end_b && start_u >= end_u)) return false;
         s = weigh_span(c.w, b);
         key_tiles = (s.len + kTile - 1) / kTile;
         row_tiles = (s.rows + c.rows_per_tile - 1) / c.rows_per_tile;
+        left = (b == end_b ? end_u : key_tiles * c.w.cache.hkv) - start_u;
+        if (left > 0) break;
       }
-      const int limit = b == end_b ? end_u : key_tiles * c.w.cache.hkv;
-      if (u < limit) {
-        head = u / key_tiles;
-        tile = u - head * key_tiles;
-        units = min(2, min(key_tiles - tile, limit - u));
-        u += units;
-        return true;
-      }
-      ++b;
-      u = 0;
-      key_tiles = -1;
+      head = start_u / key_tiles;
+      tile = start_u - head * key_tiles;
     }
+    units = min(2, min(key_tiles - tile, left));
+    left -= units;
+    return true;
   }
   __device__ __forceinline__ int stacked(const ManyCall& c, int row_tile) const {  // rows of a row tile
     return min(c.rows_per_tile, s.rows - row_tile * c.rows_per_tile) * c.w.group;
@@ -224,6 +234,10 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       ptx::mbar_init(ptx::smem_u32(&ctl.rows_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.rows_empty[i]), kSumWarps);
     }
+    for (int i = 0; i < kKeySlots; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.keys_full[i]), kConvWarps);
+      ptx::mbar_init(ptx::smem_u32(&ctl.keys_empty[i]), kSumWarps);
+    }
     ctl.abort = 0;
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&q_map);
@@ -250,35 +264,15 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + half * 2 * kTile;
     int tiles_seen = 0, mine_seen = 0, group = 0;
     const int tile_rows = c.rows_per_tile * w.group;
-    bool more = run.next(c);
-    // The thread's key: place in the pool, scale, weight before; asked for a group ahead.
-    struct Key { long long at; float scale, before; };
-    auto ask = [&] {
-      Key k{-1, 0.f, 0.f};
-      const int key = (run.tile + (run.units == 2 ? half : 0)) * kTile + in_tile;
-      if (key < run.s.len) {
-        const int page = page_of(w.cache, w.table, w.table_stride, run.b, key);
-        if (page >= 0) {
-          k.at = pool_row(w.cache, page, run.head, key);
-          k.scale = chain_load(w.cache.k_scale + k.at) * w.scale_log2;
-          const int fresh = w.decay == 0.f ? 0 : w.weighed ? chain_load_cached(w.weighed + run.b) : INT_MAX;
-          if (key < fresh) k.before = chain_load(w.weights + k.at);
-        } else if (w.device_status) {
-          atomicOr(w.device_status, FASTAV_DEV_BAD_INDEX);
-        }
-      }
-      return k;
-    };
-    Key next{-1, 0.f, 0.f};
-    if (more) next = ask();
-    while (more) {
-      const Key mine = next;
-      const int key0 = (run.tile + (run.units == 2 ? half : 0)) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
+    while (run.next(c)) {
       const bool pair = run.units == 2;
-      const int stacked = run.s.rows * w.group;
-      more = run.next(c);
-      if (more) next = ask();
-      const float2 scale = make_float2(mine.scale, mine.scale);
+      const int key0 = (run.tile + (pair ? half : 0)) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
+      const int stacked = run.s.rows * w.group, of_group = (pair ? half * kTile : 0) + in_tile, keys = group % kKeySlots;
+      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.keys_full[keys]), group / kKeySlots & 1, abort);
+      const int mine = ctl.keys[keys].row[of_group];
+      const float own_scale = ctl.keys[keys].scale[of_group], before = ctl.keys[keys].before[of_group];
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.keys_empty[keys]), lane);
+      const float2 scale = make_float2(own_scale, own_scale);
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int t = 0; t < row_tiles; ++t, ++tiles_seen) {
         const int slot = tiles_seen % kRowSlots;
@@ -311,7 +305,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       if (joins) {
         total += ctl.join[group & 1][team + 1][in_tile];
         if (!pair) total += ctl.join[group & 1][2][in_tile] + ctl.join[group & 1][3][in_tile];
-        if (mine.at >= 0) w.weights[mine.at] = fmaf(w.decay, mine.before, total);
+        if (mine >= 0) w.weights[mine] = fmaf(w.decay, before, total);
       }
       ++group;
     }
@@ -321,28 +315,77 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     constexpr int kLoads = DIM / 32, kRows = 16 / kLoads;
     const int cw = warp - kSumWarps;
     const int piece = DIM == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = DIM == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
-    for (int group = 0; run.next(c);) {
-      if (run.row_tiles == 0) continue;
-      const int slot = group & 1;
-      const int sixteens = run.units * kTile / 16;  // of keys, each in one page
-      bool waited = false;
-      for (int i0 = cw; i0 < sixteens; i0 += 2 * kConvWarps) {
-        uint4 x[2][kLoads];
+    // A warp has two sixteens of a group's keys, each in one page.  A group is asked for as soon as the one before is in the tiles, its pages a group earlier.
+    struct Group { int head, len, key0, units, row_tiles, fresh; const int32_t* pages; };  // key0: the warp's first
+    int fresh = 0, fresh_of = -1;  // tokens of a sequence from there on have no weight yet
+    auto next_group = [&](Group& g) {
+      if (!run.next(c)) return false;
+      if (run.b != fresh_of) {
+        fresh_of = run.b;
+        fresh = w.decay == 0.f ? 0 : w.weighed ? chain_load_cached(w.weighed + run.b) : INT_MAX;
+      }
+      g = Group{run.head, run.s.len, run.tile * kTile + cw * run.units * 16, run.units, run.row_tiles, fresh, w.table + (long long)run.b * w.table_stride};
+      return true;
+    };
+    auto page_entry = [&](const Group& g, int i) {
+      const int key0 = g.key0 + i * 16;
+      return i < g.units && key0 < g.len ? chain_load_cached(g.pages + (key0 >> w.cache.page_shift)) : 0;
+    };
+    uint4 x[2][kLoads];
+    int at = -1;  // of key `lane` of the 32 (16)
+    float scale = 0.f, before = 0.f;
+    const uint8_t* const codes = w.cache.k + row * DIM + piece * 16;
+    auto ask = [&](const Group& g, const int (&pages)[2]) {
+      const int key = g.key0 + lane, in_page = (1 << w.cache.page_shift) - 1;
+      int first[2];  // the sixteens' rows of the pool (which has fewer than 2^31); -1: the page is none
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        first[i] = (unsigned)pages[i] < (unsigned)w.cache.num_pages ? (pages[i] * w.cache.hkv + g.head << w.cache.page_shift) + (g.key0 + i * 16 & in_page) : -1;
+      const bool there = lane < 16 * g.units && key < g.len;
+      const int mine = lane < 16 ? first[0] : first[1];
+      if (there && mine < 0 && w.device_status) atomicOr(w.device_status, FASTAV_DEV_BAD_INDEX);
+      at = there && mine >= 0 ? mine + (lane & 15) : -1;
+      scale = at >= 0 ? chain_load(w.cache.k_scale + at) : 0.f;
+      before = at >= 0 && key < g.fresh ? chain_load(w.weights + at) : 0.f;
+      if (g.row_tiles == 0) return;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (i >= g.units || g.key0 + i * 16 >= g.len) continue;
+        const uint8_t* const from = codes + (long long)max(first[i], 0) * DIM;  // (the weights of a page that is none are left out)
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kRows * DIM));
+      }
+    };
+    Group now, next;
+    bool more = next_group(now);
+    int pages[2] = {0, 0};
+    if (more) {
+      pages[0] = page_entry(now, 0);
+      pages[1] = page_entry(now, 1);
+      ask(now, pages);
+    }
+    for (int group = 0, converted = 0; more; ++group) {
+      more = next_group(next);
+      if (more) {
+        pages[0] = page_entry(next, 0);
+        pages[1] = page_entry(next, 1);
+      }
+      const int keys = group % kKeySlots;
+      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.keys_empty[keys]), (group / kKeySlots & 1) ^ 1u, abort);
+      if (lane < 16 * now.units) {
+        const int of_group = cw * now.units * 16 + lane;
+        ctl.keys[keys].row[of_group] = at;
+        ctl.keys[keys].scale[of_group] = scale * w.scale_log2;
+        ctl.keys[keys].before[of_group] = before;
+      }
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.keys_full[keys]), lane);
+      if (now.row_tiles > 0) {
+        const int slot = converted & 1;
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), (converted >> 1 & 1) ^ 1u, abort);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int key0 = run.tile * kTile + (i0 + i * kConvWarps) * 16;
-          if (key0 >= run.s.len) continue;
-          const int page = max(0, page_of(w.cache, w.table, w.table_stride, run.b, key0));  // (the weights of a page that is none are left out)
-          const uint8_t* const from = w.cache.k + (pool_row(w.cache, page, run.head, key0) + row) * DIM + piece * 16;
-#pragma unroll
-          for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kRows * DIM));
-        }
-        if (!waited) ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), (group >> 1 & 1) ^ 1u, abort);
-        waited = true;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int in_group = (i0 + i * kConvWarps) * 16;
-          if (run.tile * kTile + in_group >= run.s.len) continue;
+          const int in_group = (cw * now.units + i) * 16;
+          if (i >= now.units || now.key0 + i * 16 >= now.len) continue;
           const uint32_t tile = k_tiles + (2 * slot + in_group / kTile) * M::kTileBytes + (piece >> 2) * kHalfBytes;
 #pragma unroll
           for (int j = 0; j < kLoads; ++j) {
@@ -350,10 +393,12 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             codes_to_bf16<FP8>(x[i][j], tile + r * 128 + (((2 * (piece & 3)) ^ (r & 7)) << 4));
           }
         }
+        ptx::fence_proxy_async_smem();
+        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.k_full[slot]), lane);
+        ++converted;
       }
-      ptx::fence_proxy_async_smem();
-      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.k_full[slot]), lane);
-      ++group;
+      now = next;
+      if (more) ask(now, pages);
     }
   } else {
     ptx::fewer_registers<kLastRegs>();
