@@ -514,7 +514,7 @@ typedef struct fastav_rotate_params { /* host memory; read at call time */
 /*
  *   q, k        [N, Hq, head_dim], [N, Hkv, head_dim] bf16; either may be NULL with its output and is skipped
  *   pos         int32, strides from params; any value
- *   q_norm_opt, k_norm_opt  [head_dim] bf16 or NULL (that side is not normed)
+ *   q_norm_opt, k_norm_opt  [head_dim] bf16, 16-byte aligned, or NULL (that side is not normed)
  *   q_out, k_out  the same shapes; may be q and k themselves (with their strides), must not overlap them otherwise
  */
 int32_t fastav_rotate(const fastav_rotate_params* params, const void* q, const void* k, const int32_t* pos, const void* q_norm_opt,

@@ -70,6 +70,11 @@ __device__ __forceinline__ unsigned pack_e4m3(const float2& a, const float2& b) 
   return (unsigned)lo | (unsigned)hi << 16;
 }
 
+__device__ __forceinline__ unsigned two_bf16(float lo, float hi) {
+  unsigned r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
 __device__ __forceinline__ float2 both(unsigned two) { return make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xFFFF0000u)); }
 template <bool FP8>
 __device__ __forceinline__ uint2 quantise8(const uint4& x, unsigned top) {

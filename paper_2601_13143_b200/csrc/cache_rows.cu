@@ -33,11 +33,6 @@ __device__ __forceinline__ float2 two_e4m3(unsigned short pair) {
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(h));
   return make_float2(lo, hi);
 }
-__device__ __forceinline__ unsigned two_bf16(float lo, float hi) {
-  unsigned r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 template <bool FP8>
 __device__ __forceinline__ uint4 dequantise8(const uint2& x, float scale) {
   unsigned out[4];

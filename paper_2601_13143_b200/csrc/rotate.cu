@@ -2,8 +2,10 @@
 //
 // y = x w / sqrt(mean x^2 + eps) per head, then pairs of elements turned by the angle position * frequency.  Bound by HBM: a row of d values is read and
 // written once (2 d bytes each way; d + 4 bytes to the cache).  A block takes a few consecutive tokens.  Their sines and cosines depend on token and pair only,
-// so they are made once into shared memory, in the order in which lanes read them; then d / 16 lanes take a head's row each, a lane two pieces of 8
-// elements: pieces that hold the two halves of the same pairs, so that a rotation needs no other lane.
+// so they are made once into shared memory, in the order in which lanes read them.  d / 16 lanes take a row, a lane two pieces of 8
+// elements: pieces that hold the two halves of the same pairs, so that a rotation needs no other lane.  A group of lanes keeps to one head and walks over
+// the block's tokens, so that addresses, the norm's weights and what becomes of the row are known beforehand, and a block has as many threads as that
+// takes.  (Groups that walk over the heads of a token: 324 instructions of a warp for four rows instead of 170, 16 x 900 tokens into the cache 102 us.)
 //
 // Angles.  frequency / (2 pi) as a 64-bit binary fraction of a turn times the position, modulo 2^64, IS the angle modulo a turn: integers wrap where floats
 // lose bits (fp32 is 0.06 rad off at position 10^6).
@@ -14,17 +16,19 @@
 
 #include "cache.cuh"
 #include "cache_quantise.cuh"
+#include "sm100_ptx.cuh"
 
 namespace fastav {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMostTokens = 8;  // of a block
+constexpr int kMostThreads = 256;
+constexpr int kMostTokens = 4;  // of a block: what all blocks have in flight should lie close together (65,536 tokens of 40 rows: 4 or 8 tokens 223 and 229 us, 16 249, 32 272)
 constexpr int kPairs = FASTAV_ROTATE_MAX_PAIRS;
 
 struct RotateCall {
   CacheView cache;
   int batch, total, hq, hkv, rows;   // rows of a token: query heads, then K heads, then (to the cache) V heads
+  int heads, at_once;                // rows that a block's groups take in one pass, tokens at a time
   int rotary, table_stride, tokens;  // tokens per block
   bool interleaved;
   float eps;
@@ -41,53 +45,39 @@ inline void mark_head(RotateCall& c, bool head) { c.head_wait = head ? 1 : 0; }
 
 enum { kToRows, kToInt8, kToFp8 };
 
-__device__ __forceinline__ float max_nan2(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
+// Sixteen values of a row as pairs, and the row's place.
+struct Row {
+  uint4 lo, hi;
+};
 
-__device__ __forceinline__ uint4 to_bf16(const float* x) {
-  uint4 r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x[1]), "f"(x[0]));
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.y) : "f"(x[3]), "f"(x[2]));
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.z) : "f"(x[5]), "f"(x[4]));
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w) : "f"(x[7]), "f"(x[6]));
-  return r;
-}
-__device__ __forceinline__ void to_floats(const uint4& x, float* f) {
-  const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
-}
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
 
-// Eight codes of a row whose largest magnitude is laid on L: x * power is exact (a power of two that brings the largest into [1, 2)), times L / that.
+// Eight codes of a row whose largest magnitude is laid on L, given factor = L / that.
 template <bool FP8>
-__device__ __forceinline__ uint2 codes_of(const float* x, float power, float factor) {
+__device__ __forceinline__ uint2 codes_of(const float2* x, float factor) {
   float2 y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = make_float2(x[2 * i] * power * factor, x[2 * i + 1] * power * factor);
   if (FP8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __fmul2_rn(x[i], two(factor));
     return make_uint2(pack_e4m3(y[0], y[1]), pack_e4m3(y[2], y[3]));
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = make_float2(y[i].x + 12582912.f, y[i].y + 12582912.f);  // 1.5 * 2^23: the code in the low bits
+    for (int i = 0; i < 4; ++i) y[i] = __ffma2_rn(x[i], two(factor), two(12582912.f));  // 1.5 * 2^23: the code in the low bits
     return make_uint2(low_bytes(y[0], y[1]), low_bytes(y[2], y[3]));
   }
 }
 
-template <int DIM, int TO>
-__global__ void __launch_bounds__(kThreads, 3)
+template <int DIM, int TO, bool NORMED, bool INTERLEAVED>
+__global__ void __launch_bounds__(kMostThreads, 4)
 rotate_kernel(const __grid_constant__ RotateCall c) {
-  constexpr int kLanes = DIM / 16, kGroups = kThreads / kLanes, kUnroll = 2;
+  constexpr int kLanes = DIM / 16;
   constexpr bool kFp8 = TO == kToFp8;
-  __shared__ __align__(16) float2 table[kMostTokens][kPairs];  // (cos, sin): of lane l's i-th pair at ((i / 2) * 8 + l) * 2 + i % 2
-  __shared__ __align__(16) float norm[2][DIM];                 // of lane l's i-th element at ((i / 4) * kLanes + l) * 4 + i % 4
-  __shared__ long long place[kMostTokens];                     // row of the pool, head 0; -1: left out
-  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  // Halves: (cos, cos, sin, sin) of lane l's pairs 2 j and 2 j + 1 at [j * 8 + l]; neighbours: (cos, cos, -sin, sin) of its j-th.
+  __shared__ __align__(16) float4 table[kMostTokens][INTERLEAVED ? kPairs : kPairs / 2];
+  __shared__ __align__(16) float4 weights[NORMED ? 2 : 1][NORMED ? DIM / 4 : 1];  // the norm's, of lane l's four j at [j * kLanes + l]
+  __shared__ long long place[kMostTokens];  // row of the pool, head 0; -1: left out
+  const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const unsigned mates = (kLanes == 32 ? 0xFFFFFFFFu : (1u << kLanes) - 1u) << (threadIdx.x & 31 & ~(kLanes - 1));  // the group's lanes of the warp
   const int turned = c.rotary / 16;  // lanes whose pieces are turned
   const int piece0 = lane < turned ? lane : 2 * lane, piece1 = lane < turned ? lane + turned : piece0 + 1;
 
@@ -96,170 +86,211 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
   pdl_wait();
   const int first = blockIdx.x * c.tokens, listed = TO == kToRows ? c.total : min(c.total, chain_load_cached(c.cu + c.batch));
   const int tokens = max(0, min(c.tokens, listed - first));
-  if (TO != kToRows && blockIdx.x == 0 && threadIdx.x == 0 && c.device_status && chain_load_cached(c.cu + c.batch) > c.total)
+  if (TO != kToRows && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0 && c.device_status && chain_load_cached(c.cu + c.batch) > c.total)
     atomicOr(c.device_status, FASTAV_DEV_SHAPE_MISMATCH);
-  const int total_rows = tokens * c.rows;
 
+  // The rows that this group takes in a pass: where the first one lies, and how far apart they are.
+  struct Head {
+    const uint16_t *from, *norm;
+    long long step;
+  };
+  const int phase = group / c.heads;
+  auto head_of = [&](int h) {
+    Head x;
+    if (h < c.hq) x = Head{c.q + (first + phase) * c.q_st + h * c.q_sh, c.q_norm, c.q_st};
+    else if (TO == kToRows || h < c.hq + c.hkv) x = Head{c.k + (first + phase) * c.k_st + (h - c.hq) * c.k_sh, c.k_norm, c.k_st};
+    else x = Head{c.v + (first + phase) * c.v_st + (h - c.hq - c.hkv) * c.v_sh, nullptr, c.v_st};
+    x.step *= c.at_once;
+    return x;
+  };
+  Row next;
+  auto ask = [&](Head& x, int token) {
+    if (token < tokens) {
+      next.lo = chain_load(reinterpret_cast<const uint4*>(x.from) + piece0);
+      next.hi = chain_load(reinterpret_cast<const uint4*>(x.from) + piece1);
+    }
+    x.from += x.step;
+  };
+  // The first rows are on their way while the table is made.
+  const bool active = group < c.heads * c.at_once;
+  int h = active ? blockIdx.y * c.heads + group - phase * c.heads : c.rows;
+  Head head{};
+  if (h < c.rows) {
+    head = head_of(h);
+    ask(head, phase);
+  }
+
+  if (NORMED)
+    for (int i = threadIdx.x; i < 2 * DIM; i += blockDim.x) {
+      const uint16_t* const w = i < DIM ? c.q_norm : c.k_norm;
+      const int at = i % DIM, piece = at / 8, second = piece < 2 * turned ? piece >= turned : piece & 1;
+      const int l = piece < 2 * turned ? piece - (second ? turned : 0) : piece / 2, j = second * 8 + at % 8;
+      reinterpret_cast<float*>(&weights[i / DIM][(j >> 2) * kLanes + l])[j & 3] = w ? __uint_as_float((unsigned)chain_load(w + at) << 16) : 1.f;
+    }
   const int half = c.rotary / 2;
-  for (int e = threadIdx.x; e < tokens * half; e += kThreads) {
+  for (int e = threadIdx.x; e < tokens * half; e += blockDim.x) {
     const int token = e / half, slot = e - token * half, l = slot / 8, i = slot % 8;
-    const int pair = !c.interleaved ? slot : i < 4 ? 4 * l + i : 4 * (l + turned) + i - 4;
+    const int pair = !INTERLEAVED ? slot : i < 4 ? 4 * l + i : 4 * (l + turned) + i - 4;
     const int pos = chain_load(c.pos + (first + token) * c.pos_st + c.axis[pair] * c.pos_sa);
     const unsigned long long angle = c.turn[pair] * (unsigned long long)(long long)pos;
     float s, co;
     sincospif((float)(int)(angle >> 32) * (1.f / 2147483648.f), &s, &co);
-    table[token][((i >> 1) * 8 + l) * 2 + (i & 1)] = make_float2(co, s);
-  }
-  if (threadIdx.x < 2 * DIM) {
-    const int side = threadIdx.x / DIM, at = threadIdx.x % DIM, piece = at / 8;
-    const int l = piece < 2 * turned ? piece % max(turned, 1) : turned + (piece - 2 * turned) / 2;
-    const int i = (piece < 2 * turned ? piece / max(turned, 1) : (piece - 2 * turned) % 2) * 8 + at % 8;
-    const uint16_t* const w = side ? c.k_norm : c.q_norm;
-    norm[side][((i >> 2) * kLanes + l) * 4 + (i & 3)] = w ? __uint_as_float((unsigned)chain_load(w + at) << 16) : 1.f;
-  }
-  if (TO != kToRows && (int)threadIdx.x < tokens) {
-    const int row = first + threadIdx.x;
-    int lo = 0, hi = c.batch;  // largest b with cu[b] <= row
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (chain_load_cached(c.cu + mid) <= row) lo = mid; else hi = mid;
-    }
-    const int i = row - chain_load_cached(c.cu + lo);
-    const long long token = (long long)(c.start ? chain_load_cached(c.start + lo) : 0) + i;
-    int bad = 0;
-    long long at = -1;
-    if (i < 0 || token < 0 || token >= (long long)c.table_stride << c.cache.page_shift || token > INT_MAX) {
-      bad = FASTAV_DEV_SHAPE_MISMATCH;
+    if (INTERLEAVED) {
+      table[token][i * 8 + l] = make_float4(co, co, -s, s);
     } else {
-      const int page = page_of(c.cache, c.table, c.table_stride, lo, (int)token);
-      if (page < 0) bad = FASTAV_DEV_BAD_INDEX;
-      else at = pool_row(c.cache, page, 0, (int)token);
+      float* const at = reinterpret_cast<float*>(&table[token][(i >> 1) * 8 + l]) + (i & 1);
+      at[0] = co;
+      at[2] = s;
     }
-    place[threadIdx.x] = at;
-    if (bad && c.device_status) atomicOr(c.device_status, bad);
   }
+  if (TO != kToRows)
+    for (int t = threadIdx.x; t < tokens; t += blockDim.x) {
+      const int row = first + t;
+      int lo = 0, hi = c.batch;  // largest b with cu[b] <= row
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (chain_load_cached(c.cu + mid) <= row) lo = mid; else hi = mid;
+      }
+      const int i = row - chain_load_cached(c.cu + lo);
+      const long long token = (long long)(c.start ? chain_load_cached(c.start + lo) : 0) + i;
+      int bad = 0;
+      long long at = -1;
+      if (i < 0 || token < 0 || token >= (long long)c.table_stride << c.cache.page_shift || token > INT_MAX) {
+        bad = FASTAV_DEV_SHAPE_MISMATCH;
+      } else {
+        const int page = page_of(c.cache, c.table, c.table_stride, lo, (int)token);
+        if (page < 0) bad = FASTAV_DEV_BAD_INDEX;
+        else at = pool_row(c.cache, page, 0, (int)token);
+      }
+      place[t] = at;
+      if (bad && c.device_status) atomicOr(c.device_status, bad);
+    }
   __syncthreads();
 
-  int token = group / c.rows, head = group - token * c.rows;
-  const int token_step = kGroups / c.rows, head_step = kGroups - token_step * c.rows;
-  // (all lanes of a warp make the same number of turns: they shuffle)
-#pragma unroll 1
-  for (int r0 = 0; r0 < total_rows; r0 += kGroups * kUnroll) {
-    uint4 in0[kUnroll], in1[kUnroll];
-    int of_token[kUnroll], of_head[kUnroll];
+  // A row normed and rotated, as pairs of neighbours: x[0..3] the first piece, x[4..7] the second.
+  auto turn = [&](const Row& r, int token, bool normed, int side, float2 (&x)[8]) {
+    const unsigned in[8] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w, r.hi.x, r.hi.y, r.hi.z, r.hi.w};
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      of_token[u] = token;
-      of_head[u] = head;
-      in0[u] = in1[u] = make_uint4(0, 0, 0, 0);
-      if (token < tokens) {
-        const long long row = first + token;
-        const uint16_t* const from = head < c.hq ? c.q + row * c.q_st + head * c.q_sh
-                                     : TO == kToRows || head < c.hq + c.hkv ? c.k + row * c.k_st + (head - c.hq) * c.k_sh
-                                                                           : c.v + row * c.v_st + (head - c.hq - c.hkv) * c.v_sh;
-        in0[u] = chain_load(reinterpret_cast<const uint4*>(from + piece0 * 8));
-        in1[u] = chain_load(reinterpret_cast<const uint4*>(from + piece1 * 8));
+    for (int i = 0; i < 8; ++i) x[i] = both(in[i]);
+    if (NORMED && normed) {
+      float2 squares = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) squares = __ffma2_rn(x[i], x[i], squares);
+      float sum = squares.x + squares.y;
+#pragma unroll
+      for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
+      float inverse = rsqrtf(fmaf(sum, 1.f / DIM, c.eps));
+      if (!(sum < INFINITY)) {  // squares beyond fp32 (the whole group's): once more, of what is 2^-64 as large (eps is nothing beside them)
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 small = __fmul2_rn(x[i], two(0x1p-64f));
+          sum = fmaf(small.x, small.x, fmaf(small.y, small.y, sum));
+        }
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
+        inverse = rsqrtf(sum * (1.f / DIM)) * 0x1p-64f;
       }
-      token += token_step;
-      head += head_step;
-      if (head >= c.rows) { head -= c.rows; ++token; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 w = weights[NORMED ? side : 0][NORMED ? i * kLanes + lane : 0];
+        x[2 * i] = __fmul2_rn(x[2 * i], __fmul2_rn(make_float2(w.x, w.y), two(inverse)));
+        x[2 * i + 1] = __fmul2_rn(x[2 * i + 1], __fmul2_rn(make_float2(w.z, w.w), two(inverse)));
+      }
     }
+    if (lane >= turned) return;
+    const float4* const t = table[token] + lane;
+    if (INTERLEAVED) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const bool there = of_token[u] < tokens, is_q = of_head[u] < c.hq, is_v = TO != kToRows && of_head[u] >= c.hq + c.hkv;
-      const long long row = first + of_token[u];
-      float x[16];
-      to_floats(in0[u], x);
-      to_floats(in1[u], x + 8);
-      if (c.q_norm || c.k_norm) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
-#pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        if (__any_sync(0xFFFFFFFFu, !(sum < INFINITY))) {  // squares beyond fp32: once more, of what is 2^-64 as large (eps is nothing beside them)
-          float small = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) small = fmaf(x[i] * 0x1p-64f, x[i] * 0x1p-64f, small);
-#pragma unroll
-          for (int d = 1; d < kLanes; d <<= 1) small += __shfl_xor_sync(0xFFFFFFFFu, small, d);
-          sum = sum < INFINITY ? rsqrtf(fmaf(sum, 1.f / DIM, c.eps)) : rsqrtf(small * (1.f / DIM)) * 0x1p-64f;
-        } else {
-          sum = rsqrtf(fmaf(sum, 1.f / DIM, c.eps));
-        }
-        if (!is_v && (is_q ? c.q_norm : c.k_norm)) {
-          const float4* const w = reinterpret_cast<const float4*>(norm[is_q ? 0 : 1]) + lane;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 f = w[i * kLanes];
-            x[4 * i] *= sum * f.x;
-            x[4 * i + 1] *= sum * f.y;
-            x[4 * i + 2] *= sum * f.z;
-            x[4 * i + 3] *= sum * f.w;
-          }
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float4 f = t[i * 8];
+        x[i] = __ffma2_rn(x[i], make_float2(f.x, f.y), __fmul2_rn(make_float2(x[i].y, x[i].x), make_float2(f.z, f.w)));
       }
-      if (lane < turned && there && !is_v) {
-        const float4* const t = reinterpret_cast<const float4*>(table[of_token[u]]) + lane;
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 f = t[i * 8];  // (cos, sin) of two pairs
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float co = j ? f.z : f.x, s = j ? f.w : f.y;
-            const int p = 2 * i + j;
-            if (c.interleaved) {
-              const float y = x[2 * p], z = x[2 * p + 1];
-              x[2 * p] = y * co - z * s;
-              x[2 * p + 1] = z * co + y * s;
-            } else {
-              const float y = x[p], z = x[p + 8];
-              x[p] = y * co - z * s;
-              x[p + 8] = z * co + y * s;
-            }
-          }
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float4 f = t[i * 8];
+        const float2 co = make_float2(f.x, f.y), s = make_float2(f.z, f.w), a = x[i], b = x[i + 4];
+        x[i] = __ffma2_rn(a, co, __fmul2_rn(b, __fmul2_rn(s, two(-1.f))));
+        x[i + 4] = __ffma2_rn(b, co, __fmul2_rn(a, s));
       }
-      if (TO == kToRows || is_q) {
-        if (there) {
-          uint16_t* const to = is_q ? c.q_out + row * c.qo_st + of_head[u] * c.qo_sh : c.k_out + row * c.ko_st + (of_head[u] - c.hq) * c.ko_sh;
-          *reinterpret_cast<uint4*>(to + piece0 * 8) = to_bf16(x);
-          *reinterpret_cast<uint4*>(to + piece1 * 8) = to_bf16(x + 8);
-        }
-      }
-      if (TO != kToRows) {
+    }
+  };
+  auto put_rows = [&](uint16_t* to, const float2 (&x)[8]) {
+    *reinterpret_cast<uint4*>(to + piece0 * 8) = make_uint4(two_bf16(x[0].x, x[0].y), two_bf16(x[1].x, x[1].y), two_bf16(x[2].x, x[2].y), two_bf16(x[3].x, x[3].y));
+    *reinterpret_cast<uint4*>(to + piece1 * 8) = make_uint4(two_bf16(x[4].x, x[4].y), two_bf16(x[5].x, x[5].y), two_bf16(x[6].x, x[6].y), two_bf16(x[7].x, x[7].y));
+  };
+  // Codes and scale of a row of K or V; what is not finite: codes 0 and a scale that is NaN, as fastav_cache_write leaves them.
+  auto put_codes = [&](uint8_t* pool, float* scales, long long row, uint2 c0, uint2 c1, float scale, bool finite) {
+    uint8_t* const to = pool + row * DIM;
+    *reinterpret_cast<uint2*>(to + piece0 * 8) = finite ? c0 : make_uint2(0, 0);
+    *reinterpret_cast<uint2*>(to + piece1 * 8) = finite ? c1 : make_uint2(0, 0);
+    if (lane == 0) scales[row] = finite ? scale : __uint_as_float(0x7FC00000u);
+  };
+
+  // f(row, token) for the group's rows, the next one asked for ahead.
+  auto walk = [&](auto f) {
+    for (int token = phase; token < tokens; token += c.at_once) {
+      const Row now = next;
+      ask(head, token + c.at_once);
+      f(now, token);
+    }
+  };
+  while (h < c.rows) {
+    if (h < c.hq || TO == kToRows) {
+      const bool is_q = h < c.hq, normed = head.norm != nullptr;
+      uint16_t* const out = is_q ? c.q_out + first * c.qo_st + h * c.qo_sh : c.k_out + first * c.ko_st + (h - c.hq) * c.ko_sh;
+      const long long stride = is_q ? c.qo_st : c.ko_st;
+      walk([&](const Row& r, int token) {
+        float2 x[8];
+        turn(r, token, normed, is_q ? 0 : 1, x);
+        put_rows(out + token * stride, x);
+      });
+    } else if (h < c.hq + c.hkv) {
+      const bool normed = head.norm != nullptr;
+      const long long of_head = (long long)(h - c.hq) << c.cache.page_shift;
+      walk([&](const Row& r, int token) {
+        float2 x[8];
+        turn(r, token, normed, 1, x);
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = max_nan2(top, fabsf(x[i]));
+        for (int i = 0; i < 8; ++i) top = ptx::max_nan(top, fabsf(x[i].x), fabsf(x[i].y));
 #pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) top = max_nan2(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        const long long at = there ? place[of_token[u]] : -1;
-        if (!is_q && at >= 0) {
-          const int kv = of_head[u] - c.hq - (is_v ? c.hkv : 0);
-          const long long to = at + ((long long)kv << c.cache.page_shift);
-          uint8_t* const codes = (is_v ? c.cache.v : c.cache.k) + to * DIM;
-          const bool finite = top < INFINITY;  // else the codes are 0 and the scale is NaN, as fastav_cache_write leaves them
-          uint2 c0, c1;
-          float scale;
-          if (is_v) {  // exactly as fastav_cache_write rounds
-            const unsigned bits = __float_as_uint(top) >> 16;
-            c0 = quantise8<kFp8>(in0[u], bits);
-            c1 = quantise8<kFp8>(in1[u], bits);
-            scale = scale_of<kFp8>(bits);
-          } else {
-            constexpr float kLargest = kFp8 ? 448.f : 127.f;
-            const int e = (int)(__float_as_uint(top) >> 23);
-            const float power = __uint_as_float((unsigned)min(max(254 - e, 1), 253) << 23), t = top * power;
-            const float factor = t > 0.f ? __fdiv_rn(kLargest, t) : 0.f;
-            c0 = codes_of<kFp8>(x, power, factor);
-            c1 = codes_of<kFp8>(x + 8, power, factor);
-            scale = __fdiv_rn(top, kLargest);
-          }
-          *reinterpret_cast<uint2*>(codes + piece0 * 8) = finite ? c0 : make_uint2(0, 0);
-          *reinterpret_cast<uint2*>(codes + piece1 * 8) = finite ? c1 : make_uint2(0, 0);
-          if (lane == 0) (is_v ? c.cache.v_scale : c.cache.k_scale)[to] = finite ? scale : __uint_as_float(0x7FC00000u);
+        for (int d = 1; d < kLanes; d <<= 1) {
+          const float other = __shfl_xor_sync(mates, top, d);
+          top = ptx::max_nan(top, other, other);
         }
-      }
+        const long long at = place[token];
+        if (at < 0) return;
+        constexpr float kLargest = kFp8 ? 448.f : 127.f;
+        float factor = __fdividef(kLargest, top);
+        if (top < 0x1p-100f) {  // L / top leaves fp32: everything by 2^100 first (exact)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __fmul2_rn(x[i], two(0x1p100f));
+          factor = top > 0.f ? __fdividef(kLargest, top * 0x1p100f) : 0.f;
+        } else if (top > 0x1p100f) {  // (an approximate quotient is 0 for divisors near fp32's end)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __fmul2_rn(x[i], two(0x1p-60f));
+          factor = __fdividef(kLargest, top * 0x1p-60f);
+        }
+        put_codes(c.cache.k, c.cache.k_scale, at + of_head, codes_of<kFp8>(x, factor), codes_of<kFp8>(x + 4, factor), __fdiv_rn(top, kLargest), top < INFINITY);
+      });
+    } else {
+      const long long of_head = (long long)(h - c.hq - c.hkv) << c.cache.page_shift;
+      walk([&](const Row& r, int token) {  // exactly as fastav_cache_write rounds
+        unsigned top = larger(top_of(r.lo), top_of(r.hi));
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) top = larger(top, __shfl_xor_sync(mates, top, d));
+        top = larger(top, __byte_perm(top, top, 0x1032)) & 0xFFFFu;
+        const long long at = place[token];
+        if (at < 0) return;
+        put_codes(c.cache.v, c.cache.v_scale, at + of_head, quantise8<kFp8>(r.lo, top), quantise8<kFp8>(r.hi, top), scale_of<kFp8>(top), top < 0x7F80u);
+      });
+    }
+    h += c.heads * gridDim.y;
+    if (h < c.rows) {
+      head = head_of(h);
+      ask(head, phase);
     }
   }
 }
@@ -292,12 +323,13 @@ int32_t check_side(const void* in, const void* out, int64_t in_st, int64_t in_sh
 }
 
 // What both entry points ask of the rotation.
-int32_t check_turns(const fastav_rotate_params* p, const int32_t* pos, bool normed) {
+int32_t check_turns(const fastav_rotate_params* p, const int32_t* pos, const void* q_norm, const void* k_norm) {
   if (!p || p->total_tokens < 0) return FASTAV_ERR_INVALID_ARG;
   if (p->head_dim != 64 && p->head_dim != 128) return FASTAV_ERR_UNSUPPORTED;
   if (p->rotary_dim < 0 || p->rotary_dim > p->head_dim) return FASTAV_ERR_INVALID_ARG;
   if (p->rotary_dim % 16 != 0) return FASTAV_ERR_UNSUPPORTED;
-  if (normed && !(p->norm_eps >= 1e-20f && std::isfinite(p->norm_eps))) return FASTAV_ERR_INVALID_ARG;
+  if ((q_norm || k_norm) && !(p->norm_eps >= 1e-20f && std::isfinite(p->norm_eps))) return FASTAV_ERR_INVALID_ARG;
+  if (!aligned(q_norm, 16) || !aligned(k_norm, 16)) return FASTAV_ERR_UNSUPPORTED;
   if (p->rotary_dim == 0) return FASTAV_OK;
   if (p->num_axes < 1 || p->num_axes > FASTAV_ROTATE_MAX_AXES || (p->total_tokens > 0 && !pos)) return FASTAV_ERR_INVALID_ARG;
   if (!aligned(pos, 4)) return FASTAV_ERR_UNSUPPORTED;
@@ -331,13 +363,27 @@ RotateCall make_call(const fastav_rotate_params& p, const void* q, const void* k
 
 template <int TO>
 int32_t launch(RotateCall& c, int dim, cudaStream_t stream) {
-  // Few tokens: one per block, so that more SMs take part.  Many: the block's start is shared by more rows.
-  c.tokens = 1;
-  while (2 * c.tokens <= kMostTokens && c.total / (2 * c.tokens) >= kNumSMs * 3) c.tokens *= 2;
-  const dim3 grid((unsigned)((c.total + c.tokens - 1) / c.tokens));
+  const int lanes = dim / 16, passes = (c.rows * lanes + kMostThreads - 1) / kMostThreads;
+  c.heads = (c.rows + passes - 1) / passes;
+  c.at_once = kMostThreads / (c.heads * lanes);
+  c.at_once = c.at_once < 1 ? 1 : c.at_once < kMostTokens ? c.at_once : kMostTokens;
+  const int threads = (c.heads * c.at_once * lanes + 31) / 32 * 32;
+  // Few tokens: one per block (or as many as it takes at once), so that more SMs take part.  Many: the block's start is shared by more rows; in
+  // whole waves of blocks, four to an SM.
+  const int resident = kNumSMs * 4, waves = (c.total + resident * kMostTokens - 1) / (resident * kMostTokens);
+  c.tokens = (c.total + resident * waves - 1) / (resident * waves);
+  if (c.tokens < c.at_once) c.tokens = c.at_once;
+  // The passes over a token's rows: one behind the other, or side by side where that leaves no SM without room (32 tokens of 36 rows 6.1 -> 4.9 us).
+  const int blocks = (c.total + c.tokens - 1) / c.tokens;
+  const dim3 grid((unsigned)blocks, (long long)blocks * passes <= resident ? passes : 1);
   count_launches(1);
-  const cudaError_t e = dim == 128 ? launch_chained(rotate_kernel<128, TO>, grid, dim3(kThreads), 0, stream, c)
-                                   : launch_chained(rotate_kernel<64, TO>, grid, dim3(kThreads), 0, stream, c);
+  auto go = [&](auto kernel) { return launch_chained(kernel, grid, dim3(threads), 0, stream, c); };
+  const bool normed = c.q_norm || c.k_norm;
+  cudaError_t e;
+  if (dim == 128) e = c.interleaved ? (normed ? go(rotate_kernel<128, TO, true, true>) : go(rotate_kernel<128, TO, false, true>))
+                                    : (normed ? go(rotate_kernel<128, TO, true, false>) : go(rotate_kernel<128, TO, false, false>));
+  else e = c.interleaved ? (normed ? go(rotate_kernel<64, TO, true, true>) : go(rotate_kernel<64, TO, false, true>))
+                         : (normed ? go(rotate_kernel<64, TO, true, false>) : go(rotate_kernel<64, TO, false, false>));
   return e == cudaSuccess ? FASTAV_OK : cuda_failed(e);
 }
 
@@ -348,7 +394,7 @@ using namespace fastav;
 
 extern "C" int32_t fastav_rotate(const fastav_rotate_params* p, const void* q, const void* k, const int32_t* pos, const void* q_norm_opt, const void* k_norm_opt,
                                  void* q_out, void* k_out, void* stream) {
-  int32_t rc = check_turns(p, pos, (q && q_norm_opt) || (k && k_norm_opt));
+  int32_t rc = check_turns(p, pos, q ? q_norm_opt : nullptr, k ? k_norm_opt : nullptr);
   if (rc != FASTAV_OK) return rc;
   if ((rc = check_side(q, q_out, p->q_stride_tok, p->q_stride_head, p->qo_stride_tok, p->qo_stride_head, p->num_q_heads, p->head_dim)) != FASTAV_OK) return rc;
   if ((rc = check_side(k, k_out, p->k_stride_tok, p->k_stride_head, p->ko_stride_tok, p->ko_stride_head, p->num_kv_heads, p->head_dim)) != FASTAV_OK) return rc;
@@ -365,7 +411,7 @@ extern "C" int32_t fastav_rotate(const fastav_rotate_params* p, const void* q, c
 extern "C" int32_t fastav_rotate_write(const fastav_rotate_params* p, const fastav_cache* cache, const void* q, const void* k, const void* v, const int32_t* pos,
                                        const void* q_norm_opt, const void* k_norm_opt, const int32_t* cu_seqlens, const int32_t* page_table, int32_t table_stride,
                                        const int32_t* start_opt, void* q_out, int32_t* device_status, void* stream) {
-  int32_t rc = check_turns(p, pos, (q && q_norm_opt) || k_norm_opt);
+  int32_t rc = check_turns(p, pos, q ? q_norm_opt : nullptr, k_norm_opt);
   if (rc != FASTAV_OK) return rc;
   if ((rc = check_cache(cache)) != FASTAV_OK) return rc;
   if (p->batch < 1 || p->num_kv_heads != cache->num_kv_heads || p->head_dim != cache->head_dim) return FASTAV_ERR_INVALID_ARG;

@@ -70,6 +70,7 @@ def test_rotate_refuses_bad_arguments(lib):
     assert call(q=None) == INVALID and call(ko=None) == INVALID and call(pos=None) == INVALID and call(pos=FAKE + 2) == UNSUPPORTED
     assert call(q=None, k=None, qo=None, ko=None) == INVALID
     assert call(q=FAKE + 8) == UNSUPPORTED and call(ko=FAKE + 2) == UNSUPPORTED
+    assert lib.fastav_rotate(ctypes.byref(_rotate()), FAKE, FAKE, FAKE, FAKE, FAKE + 8, 2 * FAKE, 2 * FAKE, None) == UNSUPPORTED
     assert call(p=_rotate(qo_stride_tok=1024), qo=FAKE) == INVALID          # in place, with other strides
     assert call(p=_rotate(total_tokens=0), q=None, k=None, qo=None, ko=None, pos=None) == fastav.FASTAV_OK
     assert lib.fastav_rotate(None, FAKE, FAKE, FAKE, None, None, FAKE, FAKE, None) == INVALID
