@@ -1,9 +1,10 @@
 // fastav_cache_evict: the lightest tokens of a cached sequence go, the others move together.
 //
-// Selection: a thread-block cluster per sequence and KV head (or per sequence, for one set of all heads), a slice of the tokens per block, their keys in registers.  The
+// Selection: a thread-block cluster per sequence and KV head (or per sequence, for one set of all heads), a slice of the tokens per block, eight in a row per thread (which lie in one
+// page: one look-up, two loads), their keys in registers.  The
 // k-th largest weight by its 32-bit key, 8 bits at a time: each block counts its keys into a histogram and sends it to all blocks of the cluster, where one warp adds
-// them up and finds the digit.  Ranks from ballots; the survivors' list goes to the workspace.  (Keys in shared memory, sums over all 1,024 threads
-// of a block and histograms fetched from the others: 2 us a digit instead of 0.7.)
+// them up and finds the digit.  Ranks by one sum over threads and blocks; the survivors' list goes to the workspace.  (Sums over all 1,024 threads of a block for
+// each digit, histograms fetched from the others: 2 us a digit instead of 0.7; tokens kThreads apart per thread, ranks from ballots: 2.3 us for the list.)
 //
 // Moving: the same clusters go on with it in place and where there is little to move (one launch), in rounds of kMoved rows a block in the survivors' order; else a
 // kernel with a block per kChunk rows, that many in flight.  Bound by the rows that move (codes and scales of K and V, weights: 2 (d + 4) + 4 bytes each
@@ -22,8 +23,7 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kChunk = 128, kChunkThreads = 256;  // rows of a block that only moves
-constexpr int kStripes = 8, kHeld = kStripes * kThreads;  // keys that a block holds, kThreads tokens a stripe; those of a longer slice are looked up again
-
+constexpr int kEach = 8, kHeld = kEach * kThreads;  // keys that a thread, a block holds; those of a longer slice are looked up again
 // Tokens of a block's slice, at least: a cluster of blocks is 0.5 us a digit slower than one block, which takes 1,024 tokens in hardly more time than 256 (1 x 300 tokens
 // 16 -> 12 us alone, in clusters from 256 and from 1,024 on).
 constexpr int kLeastSlice = 1024;
@@ -60,7 +60,7 @@ evict_kernel(EvictCall c) {
   __shared__ int2 places[2][MOVE ? kMoved : 1];
   __shared__ unsigned hist[2][256];
   __shared__ __align__(16) unsigned inbox[2][kPortableCluster][256];  // the histograms of all blocks
-  __shared__ unsigned counted[kStripes * kWarps], totals[2], found[2][3];  // totals: of the blocks before this one, keys above the threshold and equal to it
+  __shared__ unsigned warp_a[kWarps], totals[2], found[2][3];  // totals: of the blocks before this one, keys above the threshold and equal to it
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
   constexpr bool kPerSequence = JOINT && SELECT;  // one set for all heads
   static_assert(!(JOINT && SELECT && MOVE));
@@ -92,59 +92,71 @@ evict_kernel(EvictCall c) {
   }
   int32_t* const list = c.list + (long long)(JOINT ? b : job) * c.max_keep;  // rows of the pool, of head 0; -1: in no page
   if constexpr (SELECT) {
-  const int slice = (n + blocks - 1) / blocks, t0 = min(n, rank * slice), t1 = min(n, t0 + slice);
+  const int slice = ((n + blocks - 1) / blocks + kEach - 1) / kEach * kEach, t0 = min(n, rank * slice), t1 = min(n, t0 + slice);
   const int shift = c.cache.page_shift, first_page = t0 >> shift;
   if (blocks > 1)
     for (int p = first_page + tid; p <= (min(t1, t0 + kHeld) - 1) >> shift; p += kThreads) pages[p - first_page] = page_of(c.cache, c.table, c.table_stride, b, p << shift);
   __syncthreads();
+  // The page of a token that is a multiple of kEach and inside the slice.
   auto page_at = [&](int t) { return t - t0 < kHeld ? pages[(t >> shift) - first_page] : page_of(c.cache, c.table, c.table_stride, b, t); };
-  auto weight_at = [&](int page, int t) {
-    if (!kPerSequence) return chain_load(c.weights + pool_row(c.cache, page, head, t));
-    double sum = 0.;
-#pragma unroll 4
-    for (int h = 0; h < c.cache.hkv; ++h) sum += (double)chain_load(c.weights + pool_row(c.cache, page, h, t));
-    return (float)sum;
-  };
-  auto key_from = [&](int page, float w, int t) { return t < c.first || t >= n - c.recent ? kStays : page < 0 ? 0u : key_of(w); };
 
-  // ---- keys, all of a thread's loads at once ----
-  unsigned keys[kStripes];
-  {
-    float w[kStripes];
-    int page[kStripes];
+  // ---- keys of the thread's tokens g0 + kEach tid ..; behind the slice's end 0, and not counted anywhere ----
+  auto look_up = [&](int g0, unsigned (&keys)[kEach]) {
+    const int t = g0 + tid * kEach;
+    float w[kEach];
 #pragma unroll
-    for (int i = 0; i < kStripes; ++i) {
-      const int t = t0 + i * kThreads + tid;
-      page[i] = t < t1 ? page_at(t) : -1;
-      if (!kPerSequence) w[i] = page[i] < 0 ? 0.f : weight_at(page[i], t);
+    for (int j = 0; j < kEach; ++j) w[j] = __uint_as_float(0x7FC00000u);
+    if (t < t1) {
+      const int page = page_at(t);
+      if (page >= 0) {
+        const float* const from = c.weights + pool_row(c.cache, page, kPerSequence ? 0 : head, t);
+        if (!kPerSequence) {
+          const float4 lo = chain_load(reinterpret_cast<const float4*>(from)), hi = chain_load(reinterpret_cast<const float4*>(from) + 1);
+          w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+        } else {
+          double sum[kEach] = {};
+          constexpr int kHeads = 8;  // at once
+          for (int h0 = 0; h0 < c.cache.hkv; h0 += kHeads) {
+            float4 lo[kHeads], hi[kHeads];
+#pragma unroll
+            for (int h = 0; h < kHeads; ++h) {
+              const float4* const of_head = reinterpret_cast<const float4*>(from + ((long long)min(h0 + h, c.cache.hkv - 1) << shift));
+              lo[h] = chain_load(of_head);
+              hi[h] = chain_load(of_head + 1);
+            }
+#pragma unroll
+            for (int h = 0; h < kHeads; ++h) {
+              if (h0 + h < c.cache.hkv) {
+                sum[0] += lo[h].x; sum[1] += lo[h].y; sum[2] += lo[h].z; sum[3] += lo[h].w;
+                sum[4] += hi[h].x; sum[5] += hi[h].y; sum[6] += hi[h].z; sum[7] += hi[h].w;
+              }
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kEach; ++j) w[j] = (float)sum[j];
+        }
+      } else if (c.device_status) {
+        atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
+      }
     }
-    if (kPerSequence) {  // all stripes of a head, then the next
-      double sum[kStripes];
 #pragma unroll
-      for (int i = 0; i < kStripes; ++i) sum[i] = 0.;
-#pragma unroll 4
-      for (int h = 0; h < c.cache.hkv; ++h)
-#pragma unroll
-        for (int i = 0; i < kStripes; ++i)
-          if (page[i] >= 0) sum[i] += (double)chain_load(c.weights + pool_row(c.cache, page[i], h, t0 + i * kThreads + tid));
-#pragma unroll
-      for (int i = 0; i < kStripes; ++i) w[i] = (float)sum[i];
-    }
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < kStripes; ++i) {
-      const int t = t0 + i * kThreads + tid;
-      bad |= t < t1 && page[i] < 0;
-      keys[i] = key_from(page[i], w[i], t);
-    }
-    if (bad && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
-  }
-  auto look_up = [&](int t) {
-    const int page = page_at(t);
-    if (page < 0 && c.device_status) atomicOr(c.device_status, FASTAV_DEV_BAD_INDEX);
-    return key_from(page, page < 0 ? 0.f : weight_at(page, t), t);
+    for (int j = 0; j < kEach; ++j) keys[j] = t + j >= t1 ? 0u : t + j < c.first || t + j >= n - c.recent ? kStays : key_of(w[j]);
   };
-
+  unsigned keys[kEach];
+  look_up(t0, keys);
+  // f(key) for every key of the thread
+  auto for_keys = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (t0 + tid * kEach + j < t1) f(keys[j]);
+    for (int g0 = t0 + kHeld; g0 < t1; g0 += kHeld) {
+      unsigned more[kEach];
+      look_up(g0, more);
+#pragma unroll
+      for (int j = 0; j < kEach; ++j)
+        if (g0 + tid * kEach + j < t1) f(more[j]);
+    }
+  };
   if (blocks > 1) cluster_wait();
 
   // ---- the threshold: the k-th largest key, and how many of those equal to it stay (the first ones) ----
@@ -154,13 +166,9 @@ evict_kernel(EvictCall c) {
     unsigned remaining = k, prefix = 0;
     for (int pass = 0; pass < 4; ++pass) {
       const int low = 24 - 8 * pass, buffer = pass & 1;
-      auto count = [&](unsigned key) {
+      for_keys([&](unsigned key) {
         if (pass == 0 || key >> (low + 8) == prefix) atomicAdd(&hist[buffer][key >> low & 255u], 1u);
-      };
-#pragma unroll
-      for (int i = 0; i < kStripes; ++i)
-        if (t0 + i * kThreads + tid < t1) count(keys[i]);
-      for (int t = t0 + kHeld + tid; t < t1; t += kThreads) count(look_up(t));
+      });
       __syncthreads();
       if (tid < 256) {
         const unsigned mine = hist[buffer][tid];
@@ -214,14 +222,10 @@ evict_kernel(EvictCall c) {
   unsigned above_ahead = all ? t0 : 0, equal_ahead = 0;
   if (blocks > 1 && !all && k > 0) {
     unsigned both_above = 0, both_equal = 0;
-#pragma unroll
-    for (int i = 0; i < kStripes; ++i)
-      if (t0 + i * kThreads + tid < t1) both_above += is_above(keys[i]), both_equal += is_equal(keys[i]);
-    for (int t = t0 + kHeld + tid; t < t1; t += kThreads) {
-      const unsigned key = look_up(t);
+    for_keys([&](unsigned key) {
       both_above += is_above(key);
       both_equal += is_equal(key);
-    }
+    });
     both_above = __reduce_add_sync(0xFFFFFFFFu, both_above);
     both_equal = __reduce_add_sync(0xFFFFFFFFu, both_equal);
     if (lane < blocks && lane > rank) {
@@ -233,67 +237,36 @@ evict_kernel(EvictCall c) {
     equal_ahead = totals[1];
   }
 
-  // ---- the survivors' list, kStripes stripes at a time ----
+  // ---- the survivors' list, kHeld tokens at a time ----
   int32_t* const idx = c.keep_idx ? c.keep_idx + (long long)job * (kPerSequence ? c.cache.hkv : 1) * c.max_keep : nullptr;
   for (int g0 = t0; g0 < t1; g0 += kHeld) {
-    if (g0 > t0) {
+    if (g0 > t0) look_up(g0, keys);
+    const int t = g0 + tid * kEach, there = min(kEach, t1 - t);
+    unsigned above = 0, equal = 0;  // a bit per token
 #pragma unroll
-      for (int i = 0; i < kStripes; ++i) {
-        const int t = g0 + i * kThreads + tid;
-        if (t < t1) keys[i] = look_up(t);
+    for (int j = 0; j < kEach; ++j)
+      if (j < there) {
+        above |= (is_above(keys[j]) ? 1u : 0u) << j;
+        equal |= (is_equal(keys[j]) ? 1u : 0u) << j;
       }
-      __syncthreads();
-    }
-    unsigned masks_above[kStripes], masks_equal[kStripes];
-#pragma unroll
-    for (int i = 0; i < kStripes; ++i) {
-      const bool there = g0 + i * kThreads + tid < t1;
-      masks_above[i] = masks_equal[i] = 0;
-      if (g0 + i * kThreads < t1) {
-        masks_above[i] = __ballot_sync(0xFFFFFFFFu, there && is_above(keys[i]));
-        masks_equal[i] = __ballot_sync(0xFFFFFFFFu, there && is_equal(keys[i]));
-      }
-      if (lane == 0) counted[i * kWarps + warp] = __popc(masks_above[i]) | __popc(masks_equal[i]) << 16;
-    }
     __syncthreads();
-    if (warp == 0) {  // prefix sums of 4 counts a lane
-      constexpr int kEach = kStripes * kWarps / 32;
-      unsigned own[kEach], sum = 0;
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        own[j] = counted[lane * kEach + j];
-        sum += own[j];
-      }
-      unsigned before = sum;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const unsigned x = __shfl_up_sync(0xFFFFFFFFu, before, d);
-        if (lane >= d) before += x;
-      }
-      if (lane == 31) found[0][0] = before;  // of all stripes
-      before -= sum;
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        counted[lane * kEach + j] = before;
-        before += own[j];
+    const unsigned own = __popc(above) | __popc(equal) << 16, before = sum_before<kWarps>(own, warp_a, lane, warp);  // (4,096 at most)
+    if (tid == kThreads - 1) found[0][0] = before + own;  // of all threads
+    const unsigned e = equal_ahead + (before >> 16), quota = equal_stay > e ? equal_stay - e : 0u;  // of the equal ones the first stay
+#pragma unroll 1
+    while (__popc(equal) > quota) equal &= ~(0x80000000u >> __clz(equal));
+    unsigned at = above_ahead + (before & 0xFFFFu) + (from_threshold ? 0u : min(e, equal_stay));  // in the list: the thread's survivors lie side by side
+    if (unsigned stay = above | equal) {
+      const int page = page_at(t), row = page < 0 ? -1 : (page * c.cache.hkv << shift) + (t & (1 << shift) - 1);  // (a pool has fewer than 2^31 rows)
+#pragma unroll 1
+      for (; stay && at < (unsigned)k; stay &= stay - 1, ++at) {
+        const int j = __ffs(stay) - 1;
+        list[at] = row < 0 ? -1 : row + j;
+        if (idx)
+          for (int h = 0; h < (kPerSequence ? c.cache.hkv : 1); ++h) idx[(long long)h * c.max_keep + at] = t + j;
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kStripes; ++i) {
-      const int t = g0 + i * kThreads + tid;
-      if (t >= t1) break;
-      const unsigned bit = 1u << lane, before = counted[i * kWarps + warp];
-      const unsigned a = above_ahead + (before & 0xFFFFu) + __popc(masks_above[i] & (bit - 1)), e = equal_ahead + (before >> 16) + __popc(masks_equal[i] & (bit - 1));
-      const bool over = masks_above[i] & bit, same = masks_equal[i] & bit;
-      if (!over && !(same && e < equal_stay)) continue;
-      const unsigned at = a + (from_threshold ? 0u : min(e, equal_stay));
-      if (at >= (unsigned)k) continue;
-      const int page = page_at(t);
-      list[at] = page < 0 ? -1 : (int)pool_row(c.cache, page, 0, t);
-      if (idx)
-        for (int h = 0; h < (kPerSequence ? c.cache.hkv : 1); ++h) idx[(long long)h * c.max_keep + at] = t;
-    }
     above_ahead += found[0][0] & 0xFFFFu;
     equal_ahead += found[0][0] >> 16;
   }
