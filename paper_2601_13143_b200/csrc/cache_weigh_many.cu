@@ -6,16 +6,17 @@
 //
 // A block, one per SM, takes an equal run of units (128 keys of a KV head, against all stacked rows of their sequence, 128 at a time), one or two units together:
 //
-//   warps 0-15  four teams of four, a thread per key: exponentials of 128 columns at a time from tensor memory, twice buffered, summed in a register.  Two
-//               teams share a unit's columns; with one unit the two pairs of teams take turns with the row tiles.
+//   warps 0-15  four teams of four, a thread per key: exponentials of 128 columns from tensor memory, summed in a register.  Each team has an accumulator
+//               of its own: two take turns with the row tiles of a unit, or with one unit all four.
 //   warps 16-23 codes -> bf16 operand tiles in shared memory, scales and weights so far beside them, a group of units ahead
 //   warp 24     query rows by TMA
-//   warp 25     issues the MMAs
-//   warp 26     log-sum-exps and masks of the query rows (27: nothing; registers move by whole teams)
+//   warp 25     log-sum-exps and masks of the query rows
+//   warps 26-27 issue the MMAs, a half of the accumulators each
 //
-// Bound by the exponentials (16 per clock and SM; the special-function unit is busy for some 75 % of the time), while the MMAs of the same elements
-// take half as long.  1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials): 256 us.  With eight summing warps a block instead of
-// sixteen 296 (each waits for its own loads from tensor memory), 336 with 16 columns at a time; a quarter of the exponentials by a polynomial beside the unit: 256, half: 262.
+// 1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials): 256 us, 0.8 PFLOP/s.  A row tile against two units takes 3,160 cycles, of which
+// the exponentials alone 2,048 (16 per clock and SM), the way through MMA and tensor memory without any arithmetic 1,790 (both operands come from shared
+// memory, whose bandwidth 128 columns take up), and neither hides the other fully.  Measured on the way: eight summing warps a block 296 us, 16 columns at a time 336;
+// a quarter of the exponentials by a polynomial 256, half 262; one warp that issues for both units, or two teams that share every accumulator, 256.
 #include <cuda.h>
 #include <limits.h>
 
@@ -26,7 +27,7 @@ namespace fastav {
 namespace {
 
 constexpr int kTile = 128;  // keys of a unit; stacked rows of a row tile, at most
-constexpr int kSumWarps = 16, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kIssueWarp = kLoadWarp + 1, kRowWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
+constexpr int kSumWarps = 16, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kRowWarp = kLoadWarp + 1, kIssueWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
 // Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
 constexpr int kSumRegs = 80, kConvRegs = 64, kLastRegs = 48;
 constexpr int kRegsNeeded = 32 * (kSumWarps * kSumRegs + kConvWarps * kConvRegs + 4 * kLastRegs);
@@ -218,21 +219,21 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.k_full[i]), kConvWarps);
-      ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 2);
       for (int j = 0; j < 2; ++j) {
         ptx::mbar_init(ptx::smem_u32(&ctl.s_full[i][j]), 1);
-        ptx::mbar_init(ptx::smem_u32(&ctl.s_empty[i][j]), kSumWarps / 2);
+        ptx::mbar_init(ptx::smem_u32(&ctl.s_empty[i][j]), kSumWarps / 4);
       }
       ctl.first[i] = w.batch;
       ctl.unit[i] = 0;
     }
     for (int i = 0; i < kStages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.q_full[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&ctl.q_empty[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.q_empty[i]), 2);
     }
     for (int i = 0; i < kRowSlots; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.rows_full[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&ctl.rows_empty[i]), kSumWarps);
+      ptx::mbar_init(ptx::smem_u32(&ctl.rows_empty[i]), kSumWarps / 2);
     }
     for (int i = 0; i < kKeySlots; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.keys_full[i]), kConvWarps);
@@ -261,8 +262,8 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   if (warp < kSumWarps) {
     ptx::more_registers<kSumRegs>();
     const int team = warp >> 2, half = team >> 1, in_tile = threadIdx.x & (kTile - 1);
-    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + half * 2 * kTile;
-    int tiles_seen = 0, mine_seen = 0, group = 0;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + team * kTile;
+    int tiles_seen = 0, of_half = 0, group = 0;
     const int tile_rows = c.rows_per_tile * w.group;
     while (run.next(c)) {
       const bool pair = run.units == 2;
@@ -275,27 +276,31 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       const float2 scale = make_float2(own_scale, own_scale);
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int t = 0; t < row_tiles; ++t, ++tiles_seen) {
+        if (!pair && (t & 1) != half) continue;
+        const int nth = of_half++;  // the half's accumulators in turn: the first team has one buffer, the second the other
+        if ((nth & 1) != (team & 1)) continue;
         const int slot = tiles_seen % kRowSlots;
-        RowSlot& rows = ctl.rows[slot];
+        const RowSlot& rows = ctl.rows[slot];
         ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_full[slot]), tiles_seen / kRowSlots & 1, abort);
-        if (pair || (t & 1) == half) {
-          const int buffer = mine_seen & 1;
-          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[half][buffer]), mine_seen >> 1 & 1, abort);
-          ptx::tc_fence_after_sync();
-          const int columns = min(tile_rows, stacked - t * tile_rows);
-          for (int c0 = kPiece * (team & 1); c0 < columns; c0 += 2 * kPiece) {
-            uint32_t v[kPiece];
-            ptx::tmem_ld32(lanes + buffer * kTile + c0, v);
-            ptx::tmem_ld_wait_for(v);
-            if (rows.least[c0 / kPiece] >= key_end) add_columns<false>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
-            else add_columns<true>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
-            __syncwarp();
-          }
-          ptx::tc_fence_before_sync();
-          ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.s_empty[half][buffer]), lane);
-          ++mine_seen;
+        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[half][team & 1]), nth >> 1 & 1, abort);
+        ptx::tc_fence_after_sync();
+        const int columns = min(tile_rows, stacked - t * tile_rows);
+#pragma unroll 1
+        for (int c0 = 0; c0 < columns; c0 += kPiece) {
+          uint32_t v[kPiece];
+          ptx::tmem_ld32(lanes + c0, v);
+          ptx::tmem_ld_wait_for(v);
+          if (rows.least[c0 / kPiece] >= key_end) add_columns<false>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
+          else add_columns<true>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
+          __syncwarp();
         }
-        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_empty[slot]), lane);
+        ptx::tc_fence_before_sync();
+        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.s_empty[half][team & 1]), lane);
+        if (lane == 0) {
+          ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));
+          if (!pair) ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));  // (for the half that does not read it)
+        }
+        __syncwarp();
       }
       float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       // The teams' sums, in their order.
@@ -459,8 +464,10 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       if (more) ask();
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_full[slot]), lane);
     }
-  } else if (warp == kIssueWarp) {
-    int tiles = 0, issued[2] = {0, 0};
+  } else if (warp >= kIssueWarp) {
+    // A half of the accumulators each, so that neither waits for the other's sums.
+    const int half = warp == kIssueWarp ? 0 : 1;
+    int tiles = 0, issued = 0;
     for (int group = 0; run.next(c);) {
       if (run.row_tiles == 0) continue;
       const int slot = group & 1;
@@ -468,16 +475,15 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
         const int stage = tiles % kStages;
         ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full[stage]), tiles / kStages & 1, abort);
-        const uint32_t idesc = ptx::umma_idesc_bf16(kTile, (run.stacked(c, t) + 15) / 16 * 16);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (run.units == 1 && (t & 1) != half) continue;
-          const int n = issued[half]++, buffer = n & 1;
-          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_empty[half][buffer]), (n >> 1 & 1) ^ 1u, abort);
+        if (run.units == 2 || (t & 1) == half) {
+          const int buffer = issued & 1;
+          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_empty[half][buffer]), (issued >> 1 & 1) ^ 1u, abort);
           ptx::tc_fence_after_sync();
           ptx::umma_bf16_steps<DIM / 16, kHalfBytes, kHalfBytes>(tmem + (2 * half + buffer) * kTile, ptx::umma_desc_sw128(k_tiles + (2 * slot + (run.units == 2 ? half : 0)) * M::kTileBytes, 0),
-                                                                 ptx::umma_desc_sw128(q_tiles + stage * M::kTileBytes, 0), idesc, false);
+                                                                 ptx::umma_desc_sw128(q_tiles + stage * M::kTileBytes, 0),
+                                                                 ptx::umma_idesc_bf16(kTile, (run.stacked(c, t) + 15) / 16 * 16), false);
           ptx::umma_commit(ptx::smem_u32(&ctl.s_full[half][buffer]));
+          ++issued;
         }
         ptx::umma_commit(ptx::smem_u32(&ctl.q_empty[stage]));
       }

@@ -133,8 +133,19 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
     const int pair = !INTERLEAVED ? slot : i < 4 ? 4 * l + i : 4 * (l + turned) + i - 4;
     const int pos = chain_load(c.pos + (first + token) * c.pos_st + c.axis[pair] * c.pos_sa);
     const unsigned long long angle = c.turn[pair] * (unsigned long long)(long long)pos;
+    // The nearest quarter turn off in integers, so that what becomes a float is at most an eighth of a turn (its last bit 2^-25 of that); then turned back by it.
+    const unsigned high = (unsigned)(angle >> 32), quarters = (high + 0x20000000u) >> 30;
     float s, co;
-    sincospif((float)(int)(angle >> 32) * (1.f / 2147483648.f), &s, &co);
+    sincospif((float)(int)(high - (quarters << 30)) * (1.f / 2147483648.f), &s, &co);
+    if (quarters & 1) {
+      const float was = s;
+      s = co;
+      co = -was;
+    }
+    if (quarters & 2) {
+      s = -s;
+      co = -co;
+    }
     if (INTERLEAVED) {
       table[token][i * 8 + l] = make_float4(co, co, -s, s);
     } else {
@@ -179,7 +190,7 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
       float sum = squares.x + squares.y;
 #pragma unroll
       for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
-      float inverse = rsqrtf(fmaf(sum, 1.f / DIM, c.eps));
+      float inverse = __frsqrt_rn(fmaf(sum, 1.f / DIM, c.eps));
       if (!(sum < INFINITY)) {  // squares beyond fp32 (the whole group's): once more, of what is 2^-64 as large (eps is nothing beside them)
         sum = 0.f;
 #pragma unroll
@@ -189,7 +200,7 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
         }
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
-        inverse = rsqrtf(sum * (1.f / DIM)) * 0x1p-64f;
+        inverse = __frsqrt_rn(sum * (1.f / DIM)) * 0x1p-64f;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -263,15 +274,11 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
         const long long at = place[token];
         if (at < 0) return;
         constexpr float kLargest = kFp8 ? 448.f : 127.f;
-        float factor = __fdividef(kLargest, top);
+        float factor = __fdiv_rn(kLargest, top);
         if (top < 0x1p-100f) {  // L / top leaves fp32: everything by 2^100 first (exact)
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = __fmul2_rn(x[i], two(0x1p100f));
-          factor = top > 0.f ? __fdividef(kLargest, top * 0x1p100f) : 0.f;
-        } else if (top > 0x1p100f) {  // (an approximate quotient is 0 for divisors near fp32's end)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = __fmul2_rn(x[i], two(0x1p-60f));
-          factor = __fdividef(kLargest, top * 0x1p-60f);
+          factor = top > 0.f ? __fdiv_rn(kLargest, top * 0x1p100f) : 0.f;
         }
         put_codes(c.cache.k, c.cache.k_scale, at + of_head, codes_of<kFp8>(x, factor), codes_of<kFp8>(x + 4, factor), __fdiv_rn(top, kLargest), top < INFINITY);
       });

@@ -155,6 +155,22 @@ def test_new_tokens_go_into_the_cache(name, fmt):
     assert torch.equal(cache.k_scale, again.k_scale) and torch.equal(cache.v_scale, again.v_scale)
 
 
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("scale", [2.0 ** 120, 2.0 ** -95, 2.0 ** -115, 2.0 ** -125])
+def test_rows_of_extreme_sizes_go_into_the_cache(scale, fmt):
+    """Row maxima near both ends of fp32's range (with values 2^-8 of them that are still normal), and a row of zeros."""
+    gen = torch.Generator().manual_seed(21)
+    k, v = ((torch.randn(20, 2, 64, generator=gen).clamp(-4, 4) * scale).to(torch.bfloat16) for _ in "kv")
+    k[3] = 0
+    v[4, 1] = 0
+    pos, freq = _positions(gen, 1, 20), fastav.rotary_frequencies(64)
+    table, pages = _tables(gen, [20], 16)
+    cache = _cache(pages, 2, 64, 16, fmt)
+    kd, vd = k.cuda(), v.cuda()
+    fastav.fastav_rotate_write(fastav.make_rotate_params(k=kd, v=vd, pos=pos, frequencies=freq), cache, None, kd, vd, pos.cuda(), _cu([20]).cuda(), table.cuda(), None, None)
+    _check_rows(cache, fmt, table, 16, [(0, 0, ref.turned(k, pos, freq), v)])
+
+
 def test_far_and_negative_positions():
     """Out to the ends of 32 bits: angles that fp32 products would miss by whole turns."""
     pos = torch.tensor([0, 1, -1, 999_983, 2 ** 24 + 1, 123_456_789, 2 ** 31 - 1, -2 ** 31, -77_777], dtype=torch.int32)

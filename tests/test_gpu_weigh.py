@@ -157,6 +157,38 @@ def test_peaked_and_tiny_logits(spread):
     w.check()
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("power", [2.0 ** 60, 2.0 ** -60])
+def test_queries_and_keys_whose_sizes_cancel(rows, power):
+    p = Problem(16, 4, 64, "fp8", 32, [300, 45], [rows, 1], spread=1 / power, seed=12)
+    p.q = (p.q.double() * power).to(torch.bfloat16)
+    p.qd = p.q.cuda()
+    w = Weighing(p)
+    w.run()
+    w.check()
+
+
+@pytest.mark.parametrize("rows", [2, 60])
+def test_rows_behind_the_last_sequence_and_between_streams(rows):
+    """q and lse with rows that no sequence has, NaN; two calls at once on streams of their own, on pools of their own."""
+    p = Problem(8, 2, 128, "int8", 64, [500, 130], [rows, rows], seed=15)
+    w = Weighing(p)
+    q = torch.full((2 * rows + 40, 8, 128), math.nan, dtype=torch.bfloat16)
+    lse = torch.full((2 * rows + 40, 8), math.nan)
+    q[:2 * rows], lse[:2 * rows] = p.q, w.lse
+    args = [q.cuda(), lse.cuda(), _cu(p.rows).cuda(), p.tables[0].cuda(), _dev(p.lens)]
+    params = p.params(total_q=len(q))
+    pools = [w.weights.cuda() for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for pool, stream in zip(pools, streams):
+        fastav.fastav_cache_weigh(params, p.cache, pool, *args, device_status=p.status, stream=stream)
+    torch.cuda.synchronize()
+    w.on_gpu = pools[0]
+    w.check()
+    assert torch.equal(pools[0].nan_to_num(-1.0), pools[1].nan_to_num(-1.0))
+
+
 def test_weights_of_the_attention_itself_sum_to_one():
     """Given the log-sum-exp that fastav_attend returns, every row pays 1 per query head: with the prefix's share weighed by a call of its own."""
     lens, rows, plens, groups = [40, 90, 33, 128], [3, 1, 2, 5], [300, 77], [0, 3, 4]
