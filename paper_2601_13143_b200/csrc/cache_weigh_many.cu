@@ -1,6 +1,6 @@
 // fastav_cache_weigh for many query rows: a question's tokens at once, all rows that share a prefix.
 //
-// More than 16 stacked rows (query rows times G).  S^T = K Q^T on the fifth-generation tensor cores (tcgen05.mma, bf16 operands, fp32 sums in tensor memory) with the KEYS as the
+// More stacked rows (query rows times G) than the kernel for few takes.  S^T = K Q^T on the fifth-generation tensor cores (tcgen05.mma, bf16 operands, fp32 sums in tensor memory) with the KEYS as the
 // accumulator's lanes: a token's weight is then a sum over one lane's columns, which one thread adds up by itself, and nothing is joined.  Codes are exact
 // in bf16 (int8 and e4m3 have at most eight significant bits), so queries go to the matrix pipe as they are, by TMA from the caller's tensor.
 //
