@@ -454,7 +454,7 @@ extern "C" int32_t fastav_cache_evict(const fastav_evict_params* p, const fastav
   };
   const bool joint = (p->flags & FASTAV_EVICT_JOINT) != 0, wide = c.cache.dim == 128;
   const int jobs = p->batch * cache->num_kv_heads;
-  const long long chunks = (p->max_keep + kChunk - 1) / kChunk;
+  const long long chunks = ((long long)p->max_keep + kChunk - 1) / kChunk;
   const bool apart = out_table_opt && p->max_keep > 0 && chunks * jobs <= INT_MAX && (joint || p->max_keep > kFewRows * cluster_blocks(jobs, p->max_kv_len, kLeastSlice, kPortableCluster));
   cudaError_t e;
   if (joint) e = go(evict_kernel<64, true, false, true>, p->batch);

@@ -237,7 +237,7 @@ weigh_few_kernel(WeighCall c) {
 
 template <int DIM, bool FP8, int NT>
 cudaError_t launch_few(const WeighCall& c, cudaStream_t stream) {
-  const long long units = (c.max_len + kUnit - 1) / kUnit, blocks = (units * c.cache.hkv * c.batch + kWarps - 1) / kWarps, most = (long long)kNumSMs * kBlocksPerSm<DIM>;
+  const long long units = ((long long)c.max_len + kUnit - 1) / kUnit, blocks = (units * c.cache.hkv * c.batch + kWarps - 1) / kWarps, most = (long long)kNumSMs * kBlocksPerSm<DIM>;
   count_launches(1);
   const dim3 grid((unsigned)(blocks < most ? blocks : most));
   return c.batch <= 32 ? launch_chained(weigh_few_kernel<DIM, FP8, NT, true>, grid, dim3(kThreads), 0, stream, c)

@@ -518,7 +518,7 @@ cudaError_t launch(const ManyCall& c, const CUtensorMap& map, cudaStream_t strea
     return cudaFuncSetAttribute(weigh_many_kernel<DIM, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   });
   if (e != cudaSuccess) return e;
-  const long long units = (long long)c.w.batch * c.w.cache.hkv * ((c.w.max_len + kTile - 1) / kTile);
+  const long long units = (long long)c.w.batch * c.w.cache.hkv * (((long long)c.w.max_len + kTile - 1) / kTile);
   count_launches(1);
   return launch_chained(weigh_many_kernel<DIM, FP8>, dim3((unsigned)(units < kNumSMs ? units : kNumSMs)), dim3(kThreads), kSmem, stream, map, c);
 }

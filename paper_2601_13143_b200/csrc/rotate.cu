@@ -378,12 +378,12 @@ int32_t launch(RotateCall& c, int dim, cudaStream_t stream) {
   const int threads = (c.heads * c.at_once * lanes + 31) / 32 * 32;
   // Few tokens: one per block (or as many as it takes at once), so that more SMs take part.  Many: the block's start is shared by more rows; in
   // whole waves of blocks, four to an SM.
-  const int resident = kNumSMs * 4, waves = (c.total + resident * kMostTokens - 1) / (resident * kMostTokens);
-  c.tokens = (c.total + resident * waves - 1) / (resident * waves);
+  const long long resident = kNumSMs * 4, waves = (c.total + resident * kMostTokens - 1) / (resident * kMostTokens);
+  c.tokens = (int)((c.total + resident * waves - 1) / (resident * waves));
   if (c.tokens < c.at_once) c.tokens = c.at_once;
   // The passes over a token's rows: one behind the other, or side by side where that leaves no SM without room (32 tokens of 36 rows 6.1 -> 4.9 us).
-  const int blocks = (c.total + c.tokens - 1) / c.tokens;
-  const dim3 grid((unsigned)blocks, (long long)blocks * passes <= resident ? passes : 1);
+  const long long blocks = ((long long)c.total + c.tokens - 1) / c.tokens;
+  const dim3 grid((unsigned)blocks, blocks * passes <= resident ? passes : 1);
   count_launches(1);
   auto go = [&](auto kernel) { return launch_chained(kernel, grid, dim3(threads), 0, stream, c); };
   const bool normed = c.q_norm || c.k_norm;
