@@ -4,19 +4,19 @@
 // accumulator's lanes: a token's weight is then a sum over one lane's columns, which one thread adds up by itself, and nothing is joined.  Codes are exact
 // in bf16 (int8 and e4m3 have at most eight significant bits), so queries go to the matrix pipe as they are, by TMA from the caller's tensor.
 //
-// A block, one per SM, takes an equal run of units (128 keys of a KV head, against all stacked rows of their sequence, 128 at a time), one or two units together:
+// A block, one per SM, takes an equal run of units (128 keys of a KV head, against all stacked rows of their sequence, 96 at a time), one or two units together.
+// A PRODUCT is a unit against a row tile; with two units theirs alternate.
 //
-//   warps 0-15  four teams of four, a thread per key: exponentials of 128 columns from tensor memory, summed in a register.  Each team has an accumulator
-//               of its own: two take turns with the row tiles of a unit, or with one unit all four.
+//   warps 0-15  four teams of four, a thread per key: exponentials of a product's columns from tensor memory, summed in a register.  The teams take the products
+//               in turn, from five accumulators in turn: while four are summed up the fifth is made.
 //   warps 16-23 codes -> bf16 operand tiles in shared memory, scales and weights so far beside them, a group of units ahead
 //   warp 24     query rows by TMA
 //   warp 25     log-sum-exps and masks of the query rows
-//   warps 26-27 issue the MMAs, a half of the accumulators each
+//   warps 26-27 issue the MMAs, every other product each
 //
-// 1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials): 256 us, 0.8 PFLOP/s.  A row tile against two units takes 3,160 cycles, of which
-// the exponentials alone 2,048 (16 per clock and SM), the way through MMA and tensor memory without any arithmetic 1,790 (both operands come from shared
-// memory, whose bandwidth 128 columns take up), and neither hides the other fully.  Measured on the way: eight summing warps a block 296 us, 16 columns at a time 336;
-// a quarter of the exponentials by a polynomial 256, half 262; one warp that issues for both units, or two teams that share every accumulator, 256.
+// Bound by the exponentials (16 per clock and SM) and by power: 1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials) take 239 us, 0.86 PFLOP/s,
+// the SMs at some 1.65 GHz.  An eighth of the exponentials is made of multiplications instead (none 250, a sixteenth 246, a quarter 248 us).  Measured on the way:
+// eight summing warps a block 296 us; four accumulators of 128 columns, each summed up and made in turn, 256; eight of 64 columns 267; a third stage of query rows the same.
 #include <cuda.h>
 #include <limits.h>
 
@@ -26,7 +26,9 @@
 namespace fastav {
 namespace {
 
-constexpr int kTile = 128;  // keys of a unit; stacked rows of a row tile, at most
+constexpr int kTile = 128;   // keys of a unit
+constexpr int kTileRows = 96;    // stacked rows of a row tile, at most
+constexpr int kBuffers = 5;  // accumulators of kTileRows columns: one more than there are teams
 constexpr int kSumWarps = 16, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kRowWarp = kLoadWarp + 1, kIssueWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
 // Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
 constexpr int kSumRegs = 80, kConvRegs = 64, kLastRegs = 48;
@@ -34,18 +36,18 @@ constexpr int kRegsNeeded = 32 * (kSumWarps * kSumRegs + kConvWarps * kConvRegs 
 constexpr int kStages = 2, kRowSlots = 4, kKeySlots = 4;
 constexpr int kTmemCols = 512;
 constexpr int kPiece = 32;  // columns of tensor memory in registers at a time
-constexpr int kHalfBytes = 128 * 128;  // 128 rows of 128 bytes: 64 elements
+constexpr int kHalfBytes = kTile * 128, kRowBytes = kTileRows * 128;  // rows of 128 bytes: 64 elements
 
 template <int DIM>
 struct Many {
-  static constexpr int kTileBytes = DIM / 64 * kHalfBytes;
-  static constexpr int kOperands = (4 + kStages) * kTileBytes;  // K: two units, twice; Q
+  static constexpr int kTileBytes = DIM / 64 * kHalfBytes, kStageBytes = DIM / 64 * kRowBytes;
+  static constexpr int kOperands = 4 * kTileBytes + kStages * kStageBytes;  // K: two units, twice; Q
 };
 
 struct RowSlot {
-  alignas(16) float neg_lse[kTile];  // -log2(e) lse
-  alignas(16) int sees[kTile];       // keys that the row sees; 0: it pays nothing
-  int least[kTile / 32];             // the least of 32 of them
+  alignas(16) float neg_lse[kTileRows];  // -log2(e) lse
+  alignas(16) int sees[kTileRows];       // keys that the row sees; 0: it pays nothing
+  int least[kTileRows / 32];             // the least of 32 of them
 };
 struct KeySlot {  // of a group of units
   int row[2 * kTile];  // of the pool; -1: no key, or in no page
@@ -53,7 +55,7 @@ struct KeySlot {  // of a group of units
 };
 struct Control {
   KeySlot keys[kKeySlots];
-  uint64_t keys_full[kKeySlots], keys_empty[kKeySlots], k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[2][2], s_empty[2][2];
+  uint64_t keys_full[kKeySlots], keys_empty[kKeySlots], k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[kBuffers], s_empty[kBuffers];
   RowSlot rows[kRowSlots];
   float join[2][4][kTile];
   long long warp_sum[kWarps];
@@ -111,6 +113,33 @@ __device__ __forceinline__ int unit_cost(const ManyCall& c, const WeighSpan& s) 
 // Finds the block's run: the units whose start, in the call's total cost, lies in the block's share.
 __device__ __forceinline__ void find_run(const ManyCall& c, Control& ctl) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = c.w.batch;
+  if (batch <= 32) {  // one warp, one look
+    if (warp != 0) return;
+    int cost = 0, units = 0;
+    if (lane < batch) {
+      const WeighSpan s = weigh_span(c.w, lane);
+      if (s.bad && blockIdx.x == 0 && c.w.device_status) atomicOr(c.w.device_status, FASTAV_DEV_SHAPE_MISMATCH);
+      units = (s.len + kTile - 1) / kTile * c.w.cache.hkv;
+      cost = unit_cost(c, s);
+    }
+    const long long own = (long long)units * cost;
+    long long upto = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+      if (lane >= d) upto += x;
+    }
+    const long long total = __shfl_sync(0xFFFFFFFFu, upto, 31), start = upto - own, last = start + (long long)(units - 1) * cost;
+    for (int e = 0; e < 2; ++e) {
+      const long long edge = total * (blockIdx.x + e) / gridDim.x;
+      const unsigned behind = __ballot_sync(0xFFFFFFFFu, units > 0 && edge <= last);
+      if (behind && lane == __ffs(behind) - 1) {
+        ctl.first[e] = lane;
+        ctl.unit[e] = edge <= start ? 0 : (int)((edge - start + cost - 1) / cost);
+      }
+    }
+    return;
+  }
   long long total = 0;
   for (int pass = 0; pass < 2; ++pass) {
     long long ahead = 0;
@@ -183,8 +212,25 @@ __device__ __forceinline__ void codes_to_bf16(const uint4& x, uint32_t at) {
   ptx::st_shared4(at ^ 16, h[4], h[5], h[6], h[7]);
 }
 
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
+
+// 2^x of two x by multiplications and additions, beside the special-function unit: x = n + f, n the nearest integer (whose sum with 127 ends up in the low
+// bits of what the first addition gives), 2^f on [-1/2, 1/2] by the polynomial of degree 5 with the least largest relative error (by Remez' exchange; 2.2e-7 with
+// all roundings, as the unit's own).  From 127.5 on infinite, below -126.5 zero; what is not a number stays none.
+__device__ __forceinline__ float2 exp2_by_products(float2 x) {
+  constexpr float kToInteger = 12582912.f + 127.f;  // 1.5 * 2^23, and the exponent's bias
+  x = make_float2(ptx::clamp_nan(x.x, -127.f, 128.f), ptx::clamp_nan(x.y, -127.f, 128.f));
+  const float2 t = __fadd2_rn(x, two(kToInteger)), n = __fadd2_rn(t, two(-kToInteger)), f = __ffma2_rn(n, two(-1.f), x);
+  float2 p = __ffma2_rn(f, two(0.00132764725f), two(0.00967554096f));
+  p = __ffma2_rn(p, f, two(0.0555071309f));
+  p = __ffma2_rn(p, f, two(0.240221202f));
+  p = __ffma2_rn(p, f, two(0.693146944f));
+  p = __ffma2_rn(p, f, two(1.00000012f));
+  return __fmul2_rn(p, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
+}
+
 // What kPiece columns of rows add to the weight of the thread's key.  MASKED: a mask's edge, rows that pay nothing or do not exist (what stands in their
-// columns may be anything).
+// columns may be anything).  An eighth of the exponentials goes without the special-function unit (of four columns in sixteen the second two).
 template <bool MASKED>
 __device__ __forceinline__ void add_columns(const uint32_t (&v)[kPiece], const float* neg_lse, const int* sees, int key, const float2& scale, float2 (&sum)[2]) {
   const float4* const nl = reinterpret_cast<const float4*>(neg_lse);
@@ -194,7 +240,7 @@ __device__ __forceinline__ void add_columns(const uint32_t (&v)[kPiece], const f
     const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), scale, make_float2(l.x, l.y));
     const float2 b = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), scale, make_float2(l.z, l.w));
     float2 p = make_float2(ptx::ex2_approx(a.x), ptx::ex2_approx(a.y));
-    float2 q = make_float2(ptx::ex2_approx(b.x), ptx::ex2_approx(b.y));
+    float2 q = !MASKED && j % 4 == 1 ? exp2_by_products(b) : make_float2(ptx::ex2_approx(b.x), ptx::ex2_approx(b.y));
     if (MASKED) {
       const int4 n = reinterpret_cast<const int4*>(sees)[j];
       p = make_float2(key < n.x ? p.x : 0.f, key < n.y ? p.y : 0.f);
@@ -220,12 +266,12 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.k_full[i]), kConvWarps);
       ptx::mbar_init(ptx::smem_u32(&ctl.k_empty[i]), 2);
-      for (int j = 0; j < 2; ++j) {
-        ptx::mbar_init(ptx::smem_u32(&ctl.s_full[i][j]), 1);
-        ptx::mbar_init(ptx::smem_u32(&ctl.s_empty[i][j]), kSumWarps / 4);
-      }
       ctl.first[i] = w.batch;
       ctl.unit[i] = 0;
+    }
+    for (int i = 0; i < kBuffers; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.s_full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.s_empty[i]), kSumWarps / 4);
     }
     for (int i = 0; i < kStages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.q_full[i]), 1);
@@ -246,12 +292,12 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   if (w.head_wait) pdl_wait();
   pdl_trigger();
   pdl_wait();
-  __syncthreads();
-  find_run(c, ctl);
   if (warp == kIssueWarp) {
     ptx::tmem_alloc(ptx::smem_u32(&ctl.tmem_base), kTmemCols);
     ptx::tmem_relinquish();
   }
+  __syncthreads();
+  find_run(c, ctl);
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
@@ -261,54 +307,60 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   // (A wait that gives up changes nothing in the way a warp goes: it only marks the results as invalid.)
   if (warp < kSumWarps) {
     ptx::more_registers<kSumRegs>();
-    const int team = warp >> 2, half = team >> 1, in_tile = threadIdx.x & (kTile - 1);
-    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + team * kTile;
-    int tiles_seen = 0, of_half = 0, group = 0;
+    const int team = warp >> 2, in_tile = threadIdx.x & (kTile - 1);
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    int tiles_before = 0, products = 0, group = 0;  // row tiles, and products, of the groups before
     const int tile_rows = c.rows_per_tile * w.group;
     while (run.next(c)) {
       const bool pair = run.units == 2;
-      const int key0 = (run.tile + (pair ? half : 0)) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
-      const int stacked = run.s.rows * w.group, of_group = (pair ? half * kTile : 0) + in_tile, keys = group % kKeySlots;
+      const int nth = (team - products) & 3, half = pair ? nth & 1 : 0;  // of the group's products the team takes nth, nth + 4, ..: all of one unit
+      const int key0 = (run.tile + half) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
+      const int stacked = run.s.rows * w.group, of_group = half * kTile + in_tile, keys = group % kKeySlots;
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.keys_full[keys]), group / kKeySlots & 1, abort);
       const int mine = ctl.keys[keys].row[of_group];
       const float own_scale = ctl.keys[keys].scale[of_group], before = ctl.keys[keys].before[of_group];
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.keys_empty[keys]), lane);
       const float2 scale = make_float2(own_scale, own_scale);
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-      for (int t = 0; t < row_tiles; ++t, ++tiles_seen) {
-        if (!pair && (t & 1) != half) continue;
-        const int nth = of_half++;  // the half's accumulators in turn: the first team has one buffer, the second the other
-        if ((nth & 1) != (team & 1)) continue;
-        const int slot = tiles_seen % kRowSlots;
+      const int of_run = row_tiles << (pair ? 1 : 0);
+      for (int i = nth; i < of_run; i += 4) {
+        const int t = pair ? i >> 1 : i, slot = (tiles_before + t) % kRowSlots, product = products + i, buffer = product % kBuffers;
         const RowSlot& rows = ctl.rows[slot];
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_full[slot]), tiles_seen / kRowSlots & 1, abort);
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_full[half][team & 1]), nth >> 1 & 1, abort);
+        const uint32_t rows_bar = ptx::smem_u32(&ctl.rows_full[slot]), s_bar = ptx::smem_u32(&ctl.s_full[buffer]);
+        const uint32_t rows_parity = (tiles_before + t) / kRowSlots & 1, s_parity = product / kBuffers & 1;
+        const bool there = ptx::mbar_try_wait(rows_bar, rows_parity) & ptx::mbar_try_wait(s_bar, s_parity);
+        if (!__all_sync(0xFFFFFFFFu, there)) {
+          ptx::mbar_wait_warp(rows_bar, rows_parity, abort);
+          ptx::mbar_wait_warp(s_bar, s_parity, abort);
+        }
         ptx::tc_fence_after_sync();
         const int columns = min(tile_rows, stacked - t * tile_rows);
 #pragma unroll 1
         for (int c0 = 0; c0 < columns; c0 += kPiece) {
           uint32_t v[kPiece];
-          ptx::tmem_ld32(lanes + c0, v);
+          ptx::tmem_ld32(lanes + buffer * kTileRows + c0, v);
           ptx::tmem_ld_wait_for(v);
           if (rows.least[c0 / kPiece] >= key_end) add_columns<false>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
           else add_columns<true>(v, rows.neg_lse + c0, rows.sees + c0, key, scale, sum);
           __syncwarp();
         }
         ptx::tc_fence_before_sync();
-        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.s_empty[half][team & 1]), lane);
+        ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.s_empty[buffer]), lane);
         if (lane == 0) {
           ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));
-          if (!pair) ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));  // (for the half that does not read it)
+          if (!pair) ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));  // (for the team of another unit)
         }
         __syncwarp();
       }
+      tiles_before += row_tiles;
+      products += of_run;
       float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       // The teams' sums, in their order.
-      const bool joins = team == 0 || (pair && team == 2);
-      if (!joins) ctl.join[group & 1][team][in_tile] = total;
+      const bool joins = nth == 0 || (pair && nth == 1);
+      if (!joins) ctl.join[group & 1][nth][in_tile] = total;
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
       if (joins) {
-        total += ctl.join[group & 1][team + 1][in_tile];
+        total += ctl.join[group & 1][pair ? nth + 2 : 1][in_tile];
         if (!pair) total += ctl.join[group & 1][2][in_tile] + ctl.join[group & 1][3][in_tile];
         if (mine >= 0) w.weights[mine] = fmaf(w.decay, before, total);
       }
@@ -317,7 +369,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   } else if (warp < kLoadWarp) {
     ptx::fewer_registers<kConvRegs>();
     // Loads of 4 keys of 8 pieces (head_dim 64: 8 of 4); the eight lanes of a phase store to eight different quarters of the banks.
-    constexpr int kLoads = DIM / 32, kRows = 16 / kLoads;
+    constexpr int kLoads = DIM / 32, kKeysAtOnce = 16 / kLoads;
     const int cw = warp - kSumWarps;
     const int piece = DIM == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = DIM == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
     // A warp has two sixteens of a group's keys, each in one page.  A group is asked for as soon as the one before is in the tiles, its pages a group earlier.
@@ -358,7 +410,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         if (i >= g.units || g.key0 + i * 16 >= g.len) continue;
         const uint8_t* const from = codes + (long long)max(first[i], 0) * DIM;  // (the weights of a page that is none are left out)
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kRows * DIM));
+        for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kKeysAtOnce * DIM));
       }
     };
     Group now, next;
@@ -394,7 +446,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           const uint32_t tile = k_tiles + (2 * slot + in_group / kTile) * M::kTileBytes + (piece >> 2) * kHalfBytes;
 #pragma unroll
           for (int j = 0; j < kLoads; ++j) {
-            const int r = in_group % kTile + j * kRows + row;
+            const int r = in_group % kTile + j * kKeysAtOnce + row;
             codes_to_bf16<FP8>(x[i][j], tile + r * 128 + (((2 * (piece & 3)) ^ (r & 7)) << 4));
           }
         }
@@ -419,7 +471,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ptx::mbar_expect_tx_warp(bar, box_bytes * (DIM / 64));
 #pragma unroll
         for (int sub = 0; sub < DIM / 64; ++sub)
-          ptx::tma_load_3d_warp(q_tiles + stage * M::kTileBytes + sub * kHalfBytes, &q_map, sub * 64, run.head * w.group, run.s.row0 + t * c.rows_per_tile, bar);
+          ptx::tma_load_3d_warp(q_tiles + stage * M::kStageBytes + sub * kRowBytes, &q_map, sub * 64, run.head * w.group, run.s.row0 + t * c.rows_per_tile, bar);
       }
     // The copies write into this block's shared memory: they have to be waited for before it may exit.
     int never = 0;
@@ -427,7 +479,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     __syncwarp();
   } else if (warp == kRowWarp) {
     int tiles = 0, t = 0;
-    constexpr int kEach = kTile / 32;
+    constexpr int kEach = kTileRows / 32;
     float lse[kEach];  // of the next row tile, asked for ahead of the wait for its place
     int sees[kEach];
     auto ask = [&] {
@@ -467,7 +519,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   } else if (warp >= kIssueWarp) {
     // A half of the accumulators each, so that neither waits for the other's sums.
     const int half = warp == kIssueWarp ? 0 : 1;
-    int tiles = 0, issued = 0;
+    int tiles = 0, products = 0;
     for (int group = 0; run.next(c);) {
       if (run.row_tiles == 0) continue;
       const int slot = group & 1;
@@ -475,16 +527,17 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
         const int stage = tiles % kStages;
         ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full[stage]), tiles / kStages & 1, abort);
-        if (run.units == 2 || (t & 1) == half) {
-          const int buffer = issued & 1;
-          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_empty[half][buffer]), (issued >> 1 & 1) ^ 1u, abort);
+        const bool pair = run.units == 2;
+        if (pair || (t & 1) == half) {
+          const int product = products + (pair ? half : 0), buffer = product % kBuffers;
+          ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_empty[buffer]), (product / kBuffers & 1) ^ 1u, abort);
           ptx::tc_fence_after_sync();
-          ptx::umma_bf16_steps<DIM / 16, kHalfBytes, kHalfBytes>(tmem + (2 * half + buffer) * kTile, ptx::umma_desc_sw128(k_tiles + (2 * slot + (run.units == 2 ? half : 0)) * M::kTileBytes, 0),
-                                                                 ptx::umma_desc_sw128(q_tiles + stage * M::kTileBytes, 0),
-                                                                 ptx::umma_idesc_bf16(kTile, (run.stacked(c, t) + 15) / 16 * 16), false);
-          ptx::umma_commit(ptx::smem_u32(&ctl.s_full[half][buffer]));
-          ++issued;
+          ptx::umma_bf16_steps<DIM / 16, kHalfBytes, kRowBytes>(tmem + buffer * kTileRows, ptx::umma_desc_sw128(k_tiles + (2 * slot + (pair ? half : 0)) * M::kTileBytes, 0),
+                                                                ptx::umma_desc_sw128(q_tiles + stage * M::kStageBytes, 0),
+                                                                ptx::umma_idesc_bf16(kTile, (run.stacked(c, t) + 15) / 16 * 16), false);
+          ptx::umma_commit(ptx::smem_u32(&ctl.s_full[buffer]));
         }
+        products += run.units;
         ptx::umma_commit(ptx::smem_u32(&ctl.q_empty[stage]));
       }
       ptx::umma_commit(ptx::smem_u32(&ctl.k_empty[slot]));
@@ -525,10 +578,10 @@ cudaError_t launch(const ManyCall& c, const CUtensorMap& map, cudaStream_t strea
 
 }  // namespace
 
-bool weigh_many_applies(const WeighCall& c) { return c.group <= kTile; }
+bool weigh_many_applies(const WeighCall& c) { return c.group <= kTileRows; }
 
 cudaError_t launch_weigh_many(const WeighCall& w, cudaStream_t stream, bool* used) {
-  ManyCall c{w, kTile / w.group};
+  ManyCall c{w, kTileRows / w.group};
   if (c.rows_per_tile > w.max_qlen) c.rows_per_tile = w.max_qlen;
   CUtensorMap map;
   *used = encode_rows_map(w.q, w.cache.dim, w.hq, w.total_q, w.q_st, w.q_sh, w.group, c.rows_per_tile, &map);

@@ -366,6 +366,11 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
+// Between two bounds; what is not a number stays none.
+__device__ __forceinline__ float clamp_nan(float x, float least, float most) {
+  asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %0, %1;\n\tmin.NaN.f32 %0, t, %2;\n\t}" : "+f"(x) : "f"(least), "f"(most));
+  return x;
+}
 // The largest; of what is a number.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
