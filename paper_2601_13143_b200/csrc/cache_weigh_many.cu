@@ -29,11 +29,11 @@ namespace {
 constexpr int kTile = 128;   // keys of a unit
 constexpr int kTileRows = 96;    // stacked rows of a row tile, at most
 constexpr int kBuffers = 5;  // accumulators of kTileRows columns: one more than there are teams
-constexpr int kSumWarps = 16, kConvWarps = 8, kLoadWarp = kSumWarps + kConvWarps, kRowWarp = kLoadWarp + 1, kIssueWarp = kLoadWarp + 2, kWarps = kLoadWarp + 4, kThreads = 32 * kWarps;
+constexpr int kSumWarps = 16, kConvWarps = 8, kPlanWarp = kSumWarps + kConvWarps, kRowWarp = kPlanWarp + 1, kIssueWarp = kPlanWarp + 2, kWarps = kPlanWarp + 4, kThreads = 32 * kWarps;
 // Registers a thread has per role.  What the three take together has to fit into what the block is launched with (checked before the launch).
 constexpr int kSumRegs = 80, kConvRegs = 64, kLastRegs = 48;
 constexpr int kRegsNeeded = 32 * (kSumWarps * kSumRegs + kConvWarps * kConvRegs + 4 * kLastRegs);
-constexpr int kStages = 2, kRowSlots = 4, kKeySlots = 4;
+constexpr int kStages = 2, kRowSlots = 8, kKeySlots = 4, kPlans = 8;
 constexpr int kTmemCols = 512;
 constexpr int kPiece = 32;  // columns of tensor memory in registers at a time
 constexpr int kHalfBytes = kTile * 128, kRowBytes = kTileRows * 128;  // rows of 128 bytes: 64 elements
@@ -53,9 +53,15 @@ struct KeySlot {  // of a group of units
   int row[2 * kTile];  // of the pool; -1: no key, or in no page
   float scale[2 * kTile], before[2 * kTile];  // (of such, too: 0)
 };
+struct Plan {  // what the converting warps have to know of a group
+  int row[2 * kTile / 16];  // of the pool, of each sixteen keys; -1: in no page
+  int units, keys, fresh;   // units 0: there is no further group; keys that exist, and that have a weight so far
+  int convert;              // there are query rows
+};
 struct Control {
   KeySlot keys[kKeySlots];
-  uint64_t keys_full[kKeySlots], keys_empty[kKeySlots], k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[kBuffers], s_empty[kBuffers];
+  Plan plans[kPlans];
+  uint64_t plan_full[kPlans], plan_empty[kPlans], keys_full[kKeySlots], keys_empty[kKeySlots], k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], rows_full[kRowSlots], rows_empty[kRowSlots], s_full[kBuffers], s_empty[kBuffers];
   RowSlot rows[kRowSlots];
   float join[2][4][kTile];
   long long warp_sum[kWarps];
@@ -281,6 +287,10 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       ptx::mbar_init(ptx::smem_u32(&ctl.rows_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.rows_empty[i]), kSumWarps / 2);
     }
+    for (int i = 0; i < kPlans; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.plan_full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.plan_empty[i]), kConvWarps);
+    }
     for (int i = 0; i < kKeySlots; ++i) {
       ptx::mbar_init(ptx::smem_u32(&ctl.keys_full[i]), kConvWarps);
       ptx::mbar_init(ptx::smem_u32(&ctl.keys_empty[i]), kSumWarps);
@@ -366,83 +376,54 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       }
       ++group;
     }
-  } else if (warp < kLoadWarp) {
+  } else if (warp < kPlanWarp) {
     ptx::fewer_registers<kConvRegs>();
     // Loads of 4 keys of 8 pieces (head_dim 64: 8 of 4); the eight lanes of a phase store to eight different quarters of the banks.
     constexpr int kLoads = DIM / 32, kKeysAtOnce = 16 / kLoads;
     const int cw = warp - kSumWarps;
     const int piece = DIM == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3, row = DIM == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
-    // A warp has two sixteens of a group's keys, each in one page.  A group is asked for as soon as the one before is in the tiles, its pages a group earlier.
-    struct Group { int head, len, key0, units, row_tiles, fresh; const int32_t* pages; };  // key0: the warp's first
-    int fresh = 0, fresh_of = -1;  // tokens of a sequence from there on have no weight yet
-    auto next_group = [&](Group& g) {
-      if (!run.next(c)) return false;
-      if (run.b != fresh_of) {
-        fresh_of = run.b;
-        fresh = w.decay == 0.f ? 0 : w.weighed ? chain_load_cached(w.weighed + run.b) : INT_MAX;
-      }
-      g = Group{run.head, run.s.len, run.tile * kTile + cw * run.units * 16, run.units, run.row_tiles, fresh, w.table + (long long)run.b * w.table_stride};
-      return true;
-    };
-    auto page_entry = [&](const Group& g, int i) {
-      const int key0 = g.key0 + i * 16;
-      return i < g.units && key0 < g.len ? chain_load_cached(g.pages + (key0 >> w.cache.page_shift)) : 0;
-    };
+    // A warp has two sixteens of a group's keys (one of a single unit's), each in one page; a group is asked for as soon as the one before is in the tiles.
     uint4 x[2][kLoads];
     int at = -1;  // of key `lane` of the 32 (16)
     float scale = 0.f, before = 0.f;
     const uint8_t* const codes = w.cache.k + row * DIM + piece * 16;
-    auto ask = [&](const Group& g, const int (&pages)[2]) {
-      const int key = g.key0 + lane, in_page = (1 << w.cache.page_shift) - 1;
-      int first[2];  // the sixteens' rows of the pool (which has fewer than 2^31); -1: the page is none
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        first[i] = (unsigned)pages[i] < (unsigned)w.cache.num_pages ? (pages[i] * w.cache.hkv + g.head << w.cache.page_shift) + (g.key0 + i * 16 & in_page) : -1;
-      const bool there = lane < 16 * g.units && key < g.len;
+    auto ask = [&](const Plan& g) {
+      const int units = g.units, own = cw * units, key = own * 16 + lane;
+      const int first[2] = {g.row[own], g.row[own + units - 1]};
       const int mine = lane < 16 ? first[0] : first[1];
-      if (there && mine < 0 && w.device_status) atomicOr(w.device_status, FASTAV_DEV_BAD_INDEX);
-      at = there && mine >= 0 ? mine + (lane & 15) : -1;
+      at = lane < 16 * units && key < g.keys && mine >= 0 ? mine + (lane & 15) : -1;
       scale = at >= 0 ? chain_load(w.cache.k_scale + at) : 0.f;
       before = at >= 0 && key < g.fresh ? chain_load(w.weights + at) : 0.f;
-      if (g.row_tiles == 0) return;
+      if (!g.convert) return;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        if (i >= g.units || g.key0 + i * 16 >= g.len) continue;
+        if (i >= units || (own + i) * 16 >= g.keys) continue;
         const uint8_t* const from = codes + (long long)max(first[i], 0) * DIM;  // (the weights of a page that is none are left out)
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) x[i][j] = chain_load(reinterpret_cast<const uint4*>(from + j * kKeysAtOnce * DIM));
       }
     };
-    Group now, next;
-    bool more = next_group(now);
-    int pages[2] = {0, 0};
-    if (more) {
-      pages[0] = page_entry(now, 0);
-      pages[1] = page_entry(now, 1);
-      ask(now, pages);
-    }
+    // (Where a plan's wait gives up there is no plan to go by.)
+    bool more = ptx::mbar_wait_warp(ptx::smem_u32(&ctl.plan_full[0]), 0, abort) && ctl.plans[0].units > 0;
+    if (more) ask(ctl.plans[0]);
     for (int group = 0, converted = 0; more; ++group) {
-      more = next_group(next);
-      if (more) {
-        pages[0] = page_entry(next, 0);
-        pages[1] = page_entry(next, 1);
-      }
-      const int keys = group % kKeySlots;
+      const Plan& now = ctl.plans[group % kPlans];
+      const int keys = group % kKeySlots, units = now.units;
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.keys_empty[keys]), (group / kKeySlots & 1) ^ 1u, abort);
-      if (lane < 16 * now.units) {
-        const int of_group = cw * now.units * 16 + lane;
+      if (lane < 16 * units) {
+        const int of_group = cw * units * 16 + lane;
         ctl.keys[keys].row[of_group] = at;
         ctl.keys[keys].scale[of_group] = scale * w.scale_log2;
         ctl.keys[keys].before[of_group] = before;
       }
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.keys_full[keys]), lane);
-      if (now.row_tiles > 0) {
+      if (now.convert) {
         const int slot = converted & 1;
         ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_empty[slot]), (converted >> 1 & 1) ^ 1u, abort);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int in_group = (cw * now.units + i) * 16;
-          if (i >= now.units || now.key0 + i * 16 >= now.len) continue;
+          const int in_group = (cw * units + i) * 16;
+          if (i >= units || in_group >= now.keys) continue;
           const uint32_t tile = k_tiles + (2 * slot + in_group / kTile) * M::kTileBytes + (piece >> 2) * kHalfBytes;
 #pragma unroll
           for (int j = 0; j < kLoads; ++j) {
@@ -454,31 +435,69 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.k_full[slot]), lane);
         ++converted;
       }
-      now = next;
-      if (more) ask(now, pages);
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.plan_empty[group % kPlans]), lane);
+      const Plan& next = ctl.plans[(group + 1) % kPlans];
+      more = ptx::mbar_wait_warp(ptx::smem_u32(&ctl.plan_full[(group + 1) % kPlans]), (group + 1) / kPlans & 1, abort) && next.units > 0;
+      if (more) ask(next);
     }
   } else {
     ptx::fewer_registers<kLastRegs>();
   }
-  if (warp == kLoadWarp) {
-    int tiles = 0;
-    const uint32_t box_bytes = (uint32_t)(c.rows_per_tile * w.group) * 128u;
-    while (run.next(c))
-      for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
-        const int stage = tiles % kStages;
-        const uint32_t bar = ptx::smem_u32(&ctl.q_full[stage]);
-        ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_empty[stage]), (tiles / kStages & 1) ^ 1u, abort);
-        ptx::mbar_expect_tx_warp(bar, box_bytes * (DIM / 64));
-#pragma unroll
-        for (int sub = 0; sub < DIM / 64; ++sub)
-          ptx::tma_load_3d_warp(q_tiles + stage * M::kStageBytes + sub * kRowBytes, &q_map, sub * 64, run.head * w.group, run.s.row0 + t * c.rows_per_tile, bar);
+  if (warp == kPlanWarp) {
+    // Plans of the groups, some groups ahead: a lane per sixteen keys, the pages of a group asked for a group earlier still.  Codes, scales and weights are called
+    // into L2 by the way.
+    int fresh = 0, fresh_of = -1;  // tokens of a sequence from there on have no weight yet
+    int page = 0, keys = 0, planned = 0;
+    bool last = !run.next(c), done = false;
+    auto look_up = [&] {
+      if (run.b != fresh_of) {
+        fresh_of = run.b;
+        fresh = w.decay == 0.f ? 0 : w.weighed ? chain_load_cached(w.weighed + run.b) : INT_MAX;
       }
-    // The copies write into this block's shared memory: they have to be waited for before it may exit.
-    int never = 0;
-    for (int i = max(0, tiles - kStages); i < tiles; ++i) ptx::mbar_wait_bounded(ptx::smem_u32(&ctl.q_full[i % kStages]), i / kStages & 1, &never);
-    __syncwarp();
+      keys = min(run.units * kTile, run.s.len - run.tile * kTile);
+      if (16 * lane < keys) page = chain_load_cached(w.table + (long long)run.b * w.table_stride + (run.tile * kTile + 16 * lane >> w.cache.page_shift));
+    };
+    if (!last) look_up();
+    auto plan_next = [&] {
+      const int slot = planned % kPlans;
+      if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl.plan_empty[slot]), (planned / kPlans & 1) ^ 1u, abort)) {
+        done = true;
+        return;
+      }
+      Plan& g = ctl.plans[slot];
+      if (last) {
+        if (lane == 0) g.units = 0;
+      } else {
+        const int key0 = run.tile * kTile, weighed = min(max(fresh, key0) - key0, keys);
+        int row = -1;
+        if (16 * lane < keys) {
+          if ((unsigned)page < (unsigned)w.cache.num_pages) {
+            row = (int)pool_row(w.cache, page, run.head, key0 + 16 * lane);
+            if (run.row_tiles > 0) ptx::prefetch_l2_bulk(w.cache.k + (long long)row * DIM, 16 * DIM);
+            ptx::prefetch_l2(w.cache.k_scale + row);
+            if (16 * lane < weighed) ptx::prefetch_l2(w.weights + row);
+          } else if (w.device_status) {
+            atomicOr(w.device_status, FASTAV_DEV_BAD_INDEX);
+          }
+        }
+        if (lane < 2 * kTile / 16) g.row[lane] = row;
+        if (lane == 0) {
+          g.units = run.units;
+          g.keys = keys;
+          g.fresh = weighed;
+          g.convert = run.row_tiles > 0;
+        }
+      }
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.plan_full[slot]), lane);
+      ++planned;
+      done = last;
+      last = last || !run.next(c);
+      if (!last) look_up();
+    };
+    while (!done) plan_next();
   } else if (warp == kRowWarp) {
     int tiles = 0, t = 0;
+    const uint32_t box_bytes = (uint32_t)(c.rows_per_tile * w.group) * 128u;
     constexpr int kEach = kTileRows / 32;
     float lse[kEach];  // of the next row tile, asked for ahead of the wait for its place
     int sees[kEach];
@@ -503,7 +522,13 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     bool more = advance();
     if (more) ask();
     for (; more; ++tiles) {
-      const int slot = tiles % kRowSlots;
+      const int slot = tiles % kRowSlots, stage = tiles % kStages;
+      const uint32_t bar = ptx::smem_u32(&ctl.q_full[stage]);
+      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_empty[stage]), (tiles / kStages & 1) ^ 1u, abort);
+      ptx::mbar_expect_tx_warp(bar, box_bytes * (DIM / 64));
+#pragma unroll
+      for (int sub = 0; sub < DIM / 64; ++sub)
+        ptx::tma_load_3d_warp(q_tiles + stage * M::kStageBytes + sub * kRowBytes, &q_map, sub * 64, run.head * w.group, run.s.row0 + t * c.rows_per_tile, bar);
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.rows_empty[slot]), (tiles / kRowSlots & 1) ^ 1u, abort);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
@@ -512,32 +537,37 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ctl.rows[slot].sees[32 * i + lane] = n;
         if (lane == 0) ctl.rows[slot].least[i] = least;
       }
+      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_full[slot]), lane);
       more = advance();
       if (more) ask();
-      ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.rows_full[slot]), lane);
     }
+    // The copies write into this block's shared memory: they have to be waited for before it may exit.
+    int never = 0;
+    for (int i = max(0, tiles - kStages); i < tiles; ++i) ptx::mbar_wait_bounded(ptx::smem_u32(&ctl.q_full[i % kStages]), i / kStages & 1, &never);
+    __syncwarp();
   } else if (warp >= kIssueWarp) {
-    // A half of the accumulators each, so that neither waits for the other's sums.
-    const int half = warp == kIssueWarp ? 0 : 1;
+    // Every other product each, so that neither waits for the other's sums.
+    const int parity = warp - kIssueWarp;
     int tiles = 0, products = 0;
     for (int group = 0; run.next(c);) {
       if (run.row_tiles == 0) continue;
       const int slot = group & 1;
+      const bool pair = run.units == 2;
       ptx::mbar_wait_warp(ptx::smem_u32(&ctl.k_full[slot]), group >> 1 & 1, abort);
       for (int t = 0; t < run.row_tiles; ++t, ++tiles) {
         const int stage = tiles % kStages;
         ptx::mbar_wait_warp(ptx::smem_u32(&ctl.q_full[stage]), tiles / kStages & 1, abort);
-        const bool pair = run.units == 2;
-        if (pair || (t & 1) == half) {
-          const int product = products + (pair ? half : 0), buffer = product % kBuffers;
+        const int unit = (parity - products) & 1, product = products + unit;
+        products += run.units;
+        if (pair || unit == 0) {
+          const int buffer = product % kBuffers;
           ptx::mbar_wait_warp(ptx::smem_u32(&ctl.s_empty[buffer]), (product / kBuffers & 1) ^ 1u, abort);
           ptx::tc_fence_after_sync();
-          ptx::umma_bf16_steps<DIM / 16, kHalfBytes, kRowBytes>(tmem + buffer * kTileRows, ptx::umma_desc_sw128(k_tiles + (2 * slot + (pair ? half : 0)) * M::kTileBytes, 0),
+          ptx::umma_bf16_steps<DIM / 16, kHalfBytes, kRowBytes>(tmem + buffer * kTileRows, ptx::umma_desc_sw128(k_tiles + (2 * slot + unit) * M::kTileBytes, 0),
                                                                 ptx::umma_desc_sw128(q_tiles + stage * M::kStageBytes, 0),
                                                                 ptx::umma_idesc_bf16(kTile, (run.stacked(c, t) + 15) / 16 * 16), false);
           ptx::umma_commit(ptx::smem_u32(&ctl.s_full[buffer]));
         }
-        products += run.units;
         ptx::umma_commit(ptx::smem_u32(&ctl.q_empty[stage]));
       }
       ptx::umma_commit(ptx::smem_u32(&ctl.k_empty[slot]));
