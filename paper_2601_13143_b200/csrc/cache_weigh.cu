@@ -14,9 +14,9 @@
 namespace fastav {
 namespace {
 
-// Stacked rows that the kernel for few takes, 16 at a time (the keys again for every 16); beyond, the kernel for many.  us, few / many: 20 rows on 4 x 16,384 tokens of 8
-// heads 44 / 57, 64 rows 73 / 57; one sequence of 1,000, 20 rows 14.4 / 14.4, 64 rows 20.5 / 14.4; 35 rows on 16 x 3,000 of 4 heads 29.6 (48 at a time) / 32.7.
-constexpr int kMostFew = 32;
+// Stacked rows that the kernel for few takes; beyond, the kernel for many (which then is as quick or quicker: us, this one with up to 32 rows / that one: 20 rows on
+// 4 x 16,384 tokens of 8 heads 44 / 41, on one sequence of 1,000 14.4 / 12.4; 21 rows on 16 x 3,000 of 4 heads 22.6 / 24.6; 12 rows on 4 x 16,384 29 / 41).
+constexpr int kMostFew = 16;
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = 32;  // keys of a unit
 
 // 16 stacked rows (query rows times G) at once, more by turns.  mma.sync with the keys as rows, S^T = K Q^T, the codes from global memory straight to

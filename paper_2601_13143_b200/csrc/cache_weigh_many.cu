@@ -10,13 +10,15 @@
 //   warps 0-15  four teams of four, a thread per key: exponentials of a product's columns from tensor memory, summed in a register.  The teams take the products
 //               in turn, from five accumulators in turn: while four are summed up the fifth is made.
 //   warps 16-23 codes -> bf16 operand tiles in shared memory, scales and weights so far beside them, a group of units ahead
-//   warp 24     query rows by TMA
-//   warp 25     log-sum-exps and masks of the query rows
+//   warp 24     plans of the groups for those, as far ahead as there is room: rows of the pool, which it calls into L2
+//   warp 25     query rows by TMA, their log-sum-exps and masks
 //   warps 26-27 issue the MMAs, every other product each
 //
 // Bound by the exponentials (16 per clock and SM) and by power: 1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials) take 239 us, 0.86 PFLOP/s,
 // the SMs at some 1.65 GHz.  An eighth of the exponentials is made of multiplications instead (none 250, a sixteenth 246, a quarter 248 us).  Measured on the way:
 // eight summing warps a block 296 us; four accumulators of 128 columns, each summed up and made in turn, 256; eight of 64 columns 267; a third stage of query rows the same.
+// With few row tiles bound by the chain from a group's codes to its sums: 64 rows on 4 x 16,384 tokens 43 us (55 where the converting warps look up pages and walk the
+// list by themselves, and have no registers left for it; 45 without the call into L2), 96 rows on 8 x 3,000 27 us (31).
 #include <cuda.h>
 #include <limits.h>
 
