@@ -94,6 +94,10 @@ CASES = {
     "questions": (28, 4, 128, 32, [700, 300, 64], [130, 37, 64]),
     "a_long_question": (4, 2, 64, 16, [400], [399]),
     "ragged": (28, 4, 128, 64, [2500, 31, 1200, 3, 777], [1, 1, 1, 1, 1]),
+    "one_kv_head_of_96": (96, 1, 64, 64, [300, 130], [3, 1]),      # as many heads as the kernel for many rows takes at once
+    "one_kv_head_of_130": (130, 1, 128, 64, [200, 77], [2, 1]),    # more
+    "more_sequences_than_a_warp": (16, 4, 128, 16, [5 + 29 * i % 190 for i in range(45)], [5 + i % 9 for i in range(45)]),
+    "many_groups_a_block": (8, 2, 64, 16, [1 + 83 * i % 300 for i in range(1100)], [7 * (i % 5 > 0) for i in range(1100)]),
     "no_groups": (16, 16, 64, 32, [333, 64, 1000], [1, 2, 1]),
 }
 
