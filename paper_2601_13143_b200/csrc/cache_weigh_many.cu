@@ -329,8 +329,8 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       const int nth = (team - products) & 3, half = pair ? nth & 1 : 0;  // of the group's products the team takes nth, nth + 4, ..: all of one unit
       const int key0 = (run.tile + half) * kTile, key = key0 + in_tile, key_end = min(run.s.len, key0 + kTile), row_tiles = run.row_tiles;
       const int stacked = run.s.rows * w.group, of_group = half * kTile + in_tile, keys = group % kKeySlots;
-      ptx::mbar_wait_warp(ptx::smem_u32(&ctl.keys_full[keys]), group / kKeySlots & 1, abort);
-      const int mine = ctl.keys[keys].row[of_group];
+      const bool known = ptx::mbar_wait_warp(ptx::smem_u32(&ctl.keys_full[keys]), group / kKeySlots & 1, abort);
+      const int mine = known ? ctl.keys[keys].row[of_group] : -1;
       const float own_scale = ctl.keys[keys].scale[of_group], before = ctl.keys[keys].before[of_group];
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.keys_empty[keys]), lane);
       const float2 scale = make_float2(own_scale, own_scale);
