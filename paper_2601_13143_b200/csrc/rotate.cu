@@ -192,16 +192,20 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
 #pragma unroll
       for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
       float inverse = __frsqrt_rn(fmaf(sum, 1.f / DIM, c.eps));
-      if (!(sum < INFINITY)) {  // squares beyond fp32 (the whole group's): once more, of what is 2^-64 as large (eps is nothing beside them)
+      if (!(sum < INFINITY)) {  // squares beyond fp32 (the whole group's): once more, of what is 2^-80 as large, 2^103 in all at most (eps is nothing beside them)
         sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float2 small = __fmul2_rn(x[i], two(0x1p-64f));
+          const float2 small = __fmul2_rn(x[i], two(0x1p-80f));
           sum = fmaf(small.x, small.x, fmaf(small.y, small.y, sum));
         }
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
-        inverse = __frsqrt_rn(sum * (1.f / DIM)) * 0x1p-64f;
+        // The small row's root, 2^-20 to 2^48, goes to the row itself: its own root's reciprocal may be subnormal, and small rows' elements too.
+        inverse = __frsqrt_rn(sum * (1.f / DIM));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __fmul2_rn(x[i], two(inverse));
+        inverse = 0x1p-80f;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
