@@ -191,8 +191,9 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
       float sum = squares.x + squares.y;
 #pragma unroll
       for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
-      float inverse = __frsqrt_rn(fmaf(sum, 1.f / DIM, c.eps));
-      if (!(sum < INFINITY)) {  // squares beyond fp32 (the whole group's): once more, of what is 2^-80 as large, 2^103 in all at most (eps is nothing beside them)
+      const float mean = fmaf(sum, 1.f / DIM, c.eps);
+      float inverse = __frsqrt_rn(mean);
+      if (!(mean < INFINITY)) {  // beyond fp32 (the whole group's): once more, of what is 2^-80 as large, 2^103 in all at most
         sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -202,7 +203,7 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(mates, sum, d);
         // The small row's root, 2^-20 to 2^48, goes to the row itself: its own root's reciprocal may be subnormal, and small rows' elements too.
-        inverse = __frsqrt_rn(sum * (1.f / DIM));
+        inverse = __frsqrt_rn(fmaf(sum, 1.f / DIM, c.eps * 0x1p-80f * 0x1p-80f));
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = __fmul2_rn(x[i], two(inverse));
         inverse = 0x1p-80f;

@@ -8,6 +8,7 @@ from test_gpu_cache import _cache, _cu, _tables
 from test_gpu_rotate import _check_rows, _near, _positions
 
 pytestmark = pytest.mark.gpu
+LARGEST = torch.finfo(torch.float32).max
 
 
 def _rows(n, heads, dim, scale, seed=8):
@@ -26,6 +27,15 @@ def test_rows_whose_norm_leaves_fp32(scale, dim):
     y = torch.empty_like(x).cuda()
     fastav.fastav_rotate(fastav.make_rotate_params(q=x, q_out=y, norm_eps=1e-6), x.cuda(), None, None, y, None, w.cuda())
     want, size = ref.turned(x, torch.zeros(1, 5, dtype=torch.int32), [], norm=w, eps=1e-6)
+    _near(y, want, size)
+
+
+@pytest.mark.parametrize("scale,eps", [(2.0 ** 63, 2.0 ** 126), (2.0 ** 62, 2.0 ** 127), (2.0 ** 70, 2.0 ** 127), (2.0 ** 40, 2.0 ** 100), (2.0 ** 60, LARGEST)])
+def test_eps_counts_beside_squares_of_its_size(scale, eps):
+    x, w = _rows(5, 3, 128, scale), torch.ones(128, dtype=torch.bfloat16)
+    y = torch.empty_like(x).cuda()
+    fastav.fastav_rotate(fastav.make_rotate_params(q=x, q_out=y, norm_eps=eps), x.cuda(), None, None, y, None, w.cuda())
+    want, size = ref.turned(x, torch.zeros(1, 5, dtype=torch.int32), [], norm=w, eps=eps)
     _near(y, want, size)
 
 
