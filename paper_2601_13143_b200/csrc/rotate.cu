@@ -211,8 +211,8 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 w = weights[NORMED ? side : 0][NORMED ? i * kLanes + lane : 0];
-        x[2 * i] = __fmul2_rn(x[2 * i], __fmul2_rn(make_float2(w.x, w.y), two(inverse)));
-        x[2 * i + 1] = __fmul2_rn(x[2 * i + 1], __fmul2_rn(make_float2(w.z, w.w), two(inverse)));
+        x[2 * i] = __fmul2_rn(__fmul2_rn(x[2 * i], two(inverse)), make_float2(w.x, w.y));  // (w / rms alone may leave fp32; x / rms is 11.4 at most)
+        x[2 * i + 1] = __fmul2_rn(__fmul2_rn(x[2 * i + 1], two(inverse)), make_float2(w.z, w.w));
       }
     }
     if (lane >= turned) return;

@@ -50,3 +50,13 @@ def test_large_rows_normed_into_the_cache(fmt):
     params = fastav.make_rotate_params(k=kd, v=vd, pos=pos, frequencies=freq, norm_eps=1e-6)
     fastav.fastav_rotate_write(params, cache, None, kd, vd, pos.cuda(), _cu([20]).cuda(), table.cuda(), None, None, None, w.cuda())
     _check_rows(cache, fmt, table, 16, [(0, 0, ref.turned(k, pos, freq, norm=w, eps=1e-6), v)])
+
+
+@pytest.mark.parametrize("scale,weight,eps", [(2.0 ** 60, 2.0 ** -100, 1e-6), (2.0 ** 100, 2.0 ** -120, 1e-6), (2.0 ** -40, 2.0 ** 120, 1e-20), (2.0 ** -30, 2.0 ** 100, 1e-20)])
+def test_norm_weights_far_from_one(scale, weight, eps):
+    """x w / rms is an ordinary number where w / rms is none of fp32's."""
+    x, w = _rows(5, 3, 128, scale), ((1 + torch.arange(128) / 128).double() * weight).to(torch.bfloat16)
+    y = torch.empty_like(x).cuda()
+    fastav.fastav_rotate(fastav.make_rotate_params(q=x, q_out=y, norm_eps=eps), x.cuda(), None, None, y, None, w.cuda())
+    want, size = ref.turned(x, torch.zeros(1, 5, dtype=torch.int32), [], norm=w, eps=eps)
+    _near(y, want, size)
