@@ -498,7 +498,7 @@ int32_t fastav_attend(const fastav_attend_params* params, const fastav_cache* ca
 typedef struct fastav_rotate_params { /* host memory; read at call time */
   int32_t batch;                      /* fastav_rotate_write: B >= 1.  fastav_rotate does not read it */
   int32_t total_tokens;               /* N (fastav_rotate_write: cu_seqlens[B], an upper bound is fine) */
-  int32_t num_q_heads, num_kv_heads, head_dim; /* any counts >= 1; head_dim 64 or 128 */
+  int32_t num_q_heads, num_kv_heads, head_dim; /* 1 to 2^26 heads; head_dim 64 or 128 */
   int32_t rotary_dim;                 /* a multiple of 16 up to head_dim; 0: no rotation (pos may be NULL) */
   int32_t num_axes;                   /* 1 to 4 */
   float norm_eps;                     /* 1e-20 or more where norm weights are given (squares below 2^-126 are lost beside it) */

@@ -25,6 +25,7 @@ namespace {
 constexpr int kMostThreads = 256;
 constexpr int kMostTokens = 4;  // of a block: what all blocks have in flight should lie close together (65,536 tokens of 40 rows: 4 or 8 tokens 223 and 229 us, 16 249, 32 272)
 constexpr int kPairs = FASTAV_ROTATE_MAX_PAIRS;
+constexpr int kMostHeads = 1 << 26;  // of a side: the lanes of a token's rows are counted in 32 bits
 
 struct RotateCall {
   CacheView cache;
@@ -330,6 +331,7 @@ int32_t check_side(const void* in, const void* out, int64_t in_st, int64_t in_sh
   if (!in) return FASTAV_OK;
   int32_t rc;
   if (heads < 1) return FASTAV_ERR_INVALID_ARG;
+  if (heads > kMostHeads) return FASTAV_ERR_UNSUPPORTED;
   if ((rc = check_strides(in_st, in_sh, heads, dim)) != FASTAV_OK || (rc = check_strides(out_st, out_sh, heads, dim)) != FASTAV_OK) return rc;
   if (in == out && (in_st != out_st || (heads > 1 && in_sh != out_sh))) return FASTAV_ERR_INVALID_ARG;
   return aligned(in, 16) && aligned(out, 16) ? FASTAV_OK : FASTAV_ERR_UNSUPPORTED;
