@@ -558,7 +558,9 @@ int32_t fastav_rotate_write(const fastav_rotate_params* params, const fastav_cac
  *
  * q and lse hold total_q rows (those behind cu_qlens[B] may be anything).  Sums are fp32, in a fixed order; parts below 2^-126 count as 0; query elements of
  * 2^110 and more may overflow.  No two sequences may have a token in the same place.  A sequence without query rows gets decay * weights.  An entry
- * of the table that names no page sets FASTAV_DEV_BAD_INDEX, and its tokens are left out.  decay: finite, >= 0.
+ * of the table that names no page sets FASTAV_DEV_BAD_INDEX, and its tokens are left out.  decay: finite, >= 0.  Weights are added up in place: with
+ * FASTAV_DEV_WAIT_EXPIRED some tokens have theirs of after the call and the others theirs of before, so the pool has to be made anew (no weight is
+ * then a wrong sum).
  */
 int32_t fastav_cache_weigh(const fastav_attend_params* params, const fastav_cache* cache, float* weights, float decay, const void* q,
                            const float* lse, const int32_t* cu_qlens, const int32_t* page_table, const int32_t* kv_lens,

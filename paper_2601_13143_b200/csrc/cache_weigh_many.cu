@@ -317,7 +317,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   const uint32_t tmem = ctl.tmem_base;
   Run run(ctl);
 
-  // (A wait that gives up changes nothing in the way a warp goes: it only marks the results as invalid.)
+  // (A wait that gives up changes nothing in the way a warp goes: it only marks the results as invalid, and sums behind the mark are not stored.)
   if (warp < kSumWarps) {
     ptx::more_registers<kSumRegs>();
     const int team = warp >> 2, in_tile = threadIdx.x & (kTile - 1);
@@ -375,7 +375,8 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       if (joins) {
         total += ctl.join[group & 1][pair ? nth + 2 : 1][in_tile];
         if (!pair) total += ctl.join[group & 1][2][in_tile] + ctl.join[group & 1][3][in_tile];
-        if (mine >= 0) w.weights[mine] = fmaf(w.decay, before, total);
+        const bool valid = *abort == 0;  // whoever gave up left the flag before what came of it: no wrong sum is added to the weights
+        if (mine >= 0 && valid) w.weights[mine] = fmaf(w.decay, before, total);
       }
       ++group;
     }
