@@ -556,8 +556,9 @@ int32_t fastav_rotate_write(const fastav_rotate_params* params, const fastav_cac
  * tokens are weighed by a call of their own, with the prefixes as sequences, the rows that share one as its rows (cu_qlens at its sequences' edges) and without
  * FASTAV_CAUSAL.
  *
- * q and lse hold total_q rows (those behind cu_qlens[B] may be anything).  Sums are fp32, in a fixed order; parts below 2^-126 count as 0; query elements of
- * 2^110 and more may overflow.  No two sequences may have a token in the same place.  A sequence without query rows gets decay * weights.  An entry
+ * q and lse hold total_q rows (those behind cu_qlens[B] may be anything).  Sums are fp32; equal calls give equal bits, and a sequence's do not depend on
+ * what else the batch holds (but two kernels sum in different orders: one up to max_qlen * num_q_heads / num_kv_heads = 16, one beyond).  Parts below 2^-126
+ * count as 0; query elements of 2^110 and more may overflow.  No two sequences may have a token in the same place.  A sequence without query rows gets decay * weights.  An entry
  * of the table that names no page sets FASTAV_DEV_BAD_INDEX, and its tokens are left out.  decay: finite, >= 0.  Weights are added up in place: with
  * FASTAV_DEV_WAIT_EXPIRED some tokens have theirs of after the call and the others theirs of before, so the pool has to be made anew (no weight is
  * then a wrong sum).

@@ -1,8 +1,8 @@
 // fastav_cache_weigh for many query rows: a question's tokens at once, all rows that share a prefix.
 //
 // More stacked rows (query rows times G) than the kernel for few takes.  S^T = K Q^T on the fifth-generation tensor cores (tcgen05.mma, bf16 operands, fp32 sums in tensor memory) with the KEYS as the
-// accumulator's lanes: a token's weight is then a sum over one lane's columns, which one thread adds up by itself, and nothing is joined.  Codes are exact
-// in bf16 (int8 and e4m3 have at most eight significant bits), so queries go to the matrix pipe as they are, by TMA from the caller's tensor.
+// accumulator's lanes: a token's weight is then a sum over one lane's columns, which one thread adds up by itself; only what the teams (below) have of a token's row tiles is
+// joined.  Codes are exact in bf16 (int8 and e4m3 have at most eight significant bits), so queries go to the matrix pipe as they are, by TMA from the caller's tensor.
 //
 // A block, one per SM, takes an equal run of units (128 keys of a KV head, against all stacked rows of their sequence, 96 at a time), one or two units together.
 // A PRODUCT is a unit against a row tile; with two units theirs alternate.
@@ -334,7 +334,7 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       const float own_scale = ctl.keys[keys].scale[of_group], before = ctl.keys[keys].before[of_group];
       ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.keys_empty[keys]), lane);
       const float2 scale = make_float2(own_scale, own_scale);
-      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, other[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};  // other: see the swap
       const int of_run = row_tiles << (pair ? 1 : 0);
       for (int i = nth; i < of_run; i += 4) {
         const int t = pair ? i >> 1 : i, slot = (tiles_before + t) % kRowSlots, product = products + i, buffer = product % kBuffers;
@@ -359,6 +359,11 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         }
         ptx::tc_fence_before_sync();
         ptx::mbar_arrive_warp(ptx::smem_u32(&ctl.s_empty[buffer]), lane);
+        if (pair) {  // of a pair's units a team has every other row tile: in turns to either sum, each four tiles apart as a single unit's
+          const float2 s0 = sum[0], s1 = sum[1];
+          sum[0] = other[0]; sum[1] = other[1];
+          other[0] = s0; other[1] = s1;
+        }
         if (lane == 0) {
           ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));
           if (!pair) ptx::mbar_arrive(ptx::smem_u32(&ctl.rows_empty[slot]));  // (for the team of another unit)
@@ -367,14 +372,16 @@ weigh_many_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
       }
       tiles_before += row_tiles;
       products += of_run;
-      float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-      // The teams' sums, in their order.
+      float total = ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y)) + ((other[0].x + other[0].y) + (other[1].x + other[1].y));
+      // The teams' sums.  With s_i what the row tiles i, i + 4, .. come to, a token is paid (s_0 + s_2) + (s_1 + s_3), whether its unit is one of a pair or
+      // not: that depends on where a block's run begins, hence on the rest of the batch.  (One sum for a pair's tiles, in another order: 250.3 instead of 252.4 us for
+      // 1,536 rows on 16,384 tokens call upon call, but with the registers that this leaves 43.0 instead of 41.1 for 64 rows on 4 x 16,384.)
       const bool joins = nth == 0 || (pair && nth == 1);
       if (!joins) ctl.join[group & 1][nth][in_tile] = total;
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
       if (joins) {
-        total += ctl.join[group & 1][pair ? nth + 2 : 1][in_tile];
-        if (!pair) total += ctl.join[group & 1][2][in_tile] + ctl.join[group & 1][3][in_tile];
+        if (pair) total += ctl.join[group & 1][nth + 2][in_tile];
+        else total = (total + ctl.join[group & 1][2][in_tile]) + (ctl.join[group & 1][1][in_tile] + ctl.join[group & 1][3][in_tile]);
         const bool valid = *abort == 0;  // whoever gave up left the flag before what came of it: no wrong sum is added to the weights
         if (mine >= 0 && valid) w.weights[mine] = fmaf(w.decay, before, total);
       }
