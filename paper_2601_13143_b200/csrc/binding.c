@@ -11,8 +11,8 @@
 
 #include "fastav.h"
 
-static PyObject* s_data_ptr;
-static PyObject* s_nbytes;
+static PyObject *s_data_ptr, *s_nbytes, *s_dtype, *s_is_contiguous;
+static PyObject* bf16;  /* torch.bfloat16 */
 
 /* An address given as an int (0 on error, with the exception set). */
 static void* address(PyObject* o) { return PyLong_AsVoidPtr(o); }
@@ -44,6 +44,25 @@ static int size_of(PyObject* o, size_t* out) {
   *out = PyLong_AsSize_t(r);
   Py_DECREF(r);
   return *out == (size_t)-1 && PyErr_Occurred() ? -1 : 0;
+}
+
+/* Device pointer of a tensor that has to lie in one piece of `bytes` bytes of this type; None is NULL. */
+static int typed(PyObject* o, PyObject* dtype, size_t bytes, const char* wanted, void** out) {
+  size_t have;
+  *out = NULL;
+  if (o == Py_None) return 0;
+  PyObject* t = PyObject_GetAttr(o, s_dtype);
+  if (!t) return -1;
+  Py_DECREF(t); /* (its module keeps it; compared by identity only) */
+  if (size_of(o, &have)) return -1;
+  PyObject* c = PyObject_VectorcallMethod(s_is_contiguous, &o, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, NULL);
+  if (!c) return -1;
+  Py_DECREF(c);
+  if (t != dtype || have != bytes || c != Py_True) {
+    PyErr_Format(PyExc_ValueError, "expected %s", wanted);
+    return -1;
+  }
+  return pointer(o, out);
 }
 
 static int expect(const char* name, Py_ssize_t got, Py_ssize_t want) {
@@ -157,10 +176,19 @@ static int weights_of(PyObject* o, PyObject* scales, void** out) {
   return pointer(o, out);
 }
 
+/* A norm's weights, of a side that is there: they are read as head_dim bf16 in a row. */
+static int norm_of(PyObject* o, const void* params, const void* side, void** out) {
+  *out = NULL;
+  if (!side) return 0;
+  return typed(o, bf16, (size_t)((const fastav_rotate_params*)params)->head_dim * 2, "norm weights [head_dim], bf16, in one piece", out);
+}
+
 /* (function, params, q, k, pos, q_norm, k_norm, q_out, k_out, stream) */
 static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void *f, *p, *t[7], *stream;
-  if (expect("rotate", n, 10) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || pointers(a + 2, 7, t)) return NULL;
+  if (expect("rotate", n, 10) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || pointers(a + 2, 3, t) || norm_of(a[5], p, t[0], &t[3]) ||
+      norm_of(a[6], p, t[1], &t[4]) || pointers(a + 7, 2, t + 5))
+    return NULL;
   stream = address(a[9]);
   if (PyErr_Occurred()) return NULL;
   int32_t rc;
@@ -174,7 +202,7 @@ static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 static PyObject* rotate_write(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void *f, *p, *c, *t[8], *u[3], *stream;
   if (expect("rotate_write", n, 16) || ((f = address(a[0])) == NULL) || ((p = address(a[1])) == NULL) || ((c = address(a[2])) == NULL) ||
-      pointers(a + 3, 8, t) || pointers(a + 12, 3, u))
+      pointers(a + 3, 4, t) || norm_of(a[7], p, t[0], &t[4]) || norm_of(a[8], p, t[1], &t[5]) || pointers(a + 9, 2, t + 6) || pointers(a + 12, 3, u))
     return NULL;
   const long stride = PyLong_AsLong(a[11]);
   stream = address(a[15]);
@@ -238,5 +266,11 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument
 PyMODINIT_FUNC PyInit__binding(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_nbytes = PyUnicode_InternFromString("nbytes");
-  return s_data_ptr && s_nbytes ? PyModule_Create(&module) : NULL;
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  PyObject* torch = PyImport_ImportModule("torch");
+  if (!torch) return NULL;
+  bf16 = PyObject_GetAttrString(torch, "bfloat16");
+  Py_DECREF(torch);
+  return s_data_ptr && s_nbytes && s_dtype && s_is_contiguous && bf16 ? PyModule_Create(&module) : NULL;
 }

@@ -231,11 +231,14 @@ def _p(t: torch.Tensor | None) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+_cuda_ready, _raw_stream, _current_device = torch.cuda.is_initialized, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _stream(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
-    if torch.cuda.is_initialized():  # the current stream's handle without a Stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if _cuda_ready():  # the current stream's handle without a Stream object around it
+        return _raw_stream(_current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -539,8 +542,9 @@ def make_rotate_params(*, q=None, k=None, v=None, q_out=None, k_out=None, pos=No
 
 def fastav_rotate(params, q, k, pos, q_out, k_out, q_norm_opt=None, k_norm_opt=None, stream=None) -> None:
     """Norm per head (optional) and rotation by position of a prompt's queries and keys; either side may be None."""
-    _check(_native().rotate(_address("fastav_rotate"), _struct(params, fastav_rotate_params), q, k, pos, q_norm_opt, k_norm_opt, q_out, k_out, _stream(stream)),
-           "fastav_rotate")
+    status = _native().rotate(_address("fastav_rotate"), _struct(params, fastav_rotate_params), q, k, pos, q_norm_opt, k_norm_opt, q_out, k_out, _stream(stream))
+    if status:
+        _check(status, "fastav_rotate")
 
 
 def fastav_rotate_write(params, cache: KvCache, q, k, v, pos, cu_seqlens, page_table, start_opt, q_out, q_norm_opt=None, k_norm_opt=None, device_status=None,

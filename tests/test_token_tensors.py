@@ -1,0 +1,54 @@
+"""What the binding refuses of the rotation's, the weighing's and the eviction's tensors, without a GPU: their addresses alone do not say how they are read."""
+import pytest
+import torch
+
+from paper_2601_13143_b200 import build as fbuild
+from paper_2601_13143_b200 import fastav
+
+
+class _Stream:
+    cuda_stream = 0
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    fbuild.build()
+    fbuild.build_binding()
+
+
+DIM = 64
+BAD_NORMS = {
+    "fp32": torch.ones(DIM),
+    "fp32, as many bytes": torch.ones(DIM // 2),
+    "fp16": torch.ones(DIM, dtype=torch.float16),
+    "too short": torch.ones(DIM - 8, dtype=torch.bfloat16),
+    "too long": torch.ones(2 * DIM, dtype=torch.bfloat16),
+    "every other element": torch.ones(2 * DIM, dtype=torch.bfloat16)[::2],
+}
+
+
+@pytest.mark.parametrize("name", BAD_NORMS)
+@pytest.mark.parametrize("side", ["q", "k"])
+def test_norm_weights_that_are_no_row_of_bf16(name, side):
+    x = torch.zeros(5, 2, DIM, dtype=torch.bfloat16)
+    norms = [None, None]
+    norms["qk".index(side)] = BAD_NORMS[name]
+    params = fastav.make_rotate_params(q=x, k=x, v=x, q_out=x, k_out=x)
+    cache, table = fastav.make_cache(3, 2, DIM, 32, device="cpu"), torch.zeros(1, 8, dtype=torch.int32)
+    cu = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="norm weights"):
+        fastav.fastav_rotate(params, x, x, None, x, x, *norms, stream=_Stream)
+    with pytest.raises(ValueError, match="norm weights"):
+        fastav.fastav_rotate_write(params, cache, x, x, x, None, cu, table, None, x, *norms, stream=_Stream)
+
+
+def test_norm_weights_that_are_right_get_to_the_library():
+    """... which refuses the call for another reason (rotary_dim), ahead of the GPU; weights of a side that is not there are not looked at."""
+    x, w = torch.zeros(5, 2, DIM, dtype=torch.bfloat16), torch.ones(DIM, dtype=torch.bfloat16)
+    params = fastav.make_rotate_params(q=x, k=x, q_out=x, k_out=x)
+    params.rotary_dim = 24
+    for q, norm in ((x, w), (None, torch.ones(3))):
+        with pytest.raises(fastav.FastavError):
+            fastav.fastav_rotate(params, q, x, None, q, x, norm, w, stream=_Stream)
+    with pytest.raises(fastav.FastavError):
+        fastav.fastav_rotate(params, x, x, None, x, x, None, None, stream=_Stream)
