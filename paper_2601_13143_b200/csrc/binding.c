@@ -12,7 +12,7 @@
 #include "fastav.h"
 
 static PyObject *s_data_ptr, *s_nbytes, *s_dtype, *s_is_contiguous;
-static PyObject* bf16;  /* torch.bfloat16 */
+static PyObject *bf16, *fp32; /* torch.bfloat16, torch.float32 */
 
 /* An address given as an int (0 on error, with the exception set). */
 static void* address(PyObject* o) { return PyLong_AsVoidPtr(o); }
@@ -167,13 +167,13 @@ static PyObject* attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 
 /* A pool of weights beside a cache's scales: as many bytes as those. */
 static int weights_of(PyObject* o, PyObject* scales, void** out) {
-  size_t bytes, want;
-  if (size_of(o, &bytes) || size_of(scales, &want)) return -1;
-  if (bytes != want) {
-    PyErr_SetString(PyExc_ValueError, "expected fp32 weights [pages, KV heads, page tokens], as the cache's scales");
+  size_t bytes;
+  if (size_of(scales, &bytes)) return -1;
+  if (o == Py_None) {
+    PyErr_SetString(PyExc_ValueError, "expected fp32 weights, not None");
     return -1;
   }
-  return pointer(o, out);
+  return typed(o, fp32, bytes, "fp32 weights [pages, KV heads, page tokens] in one piece, as the cache's scales", out);
 }
 
 /* A norm's weights, of a side that is there: they are read as head_dim bf16 in a row. */
@@ -271,6 +271,7 @@ PyMODINIT_FUNC PyInit__binding(void) {
   PyObject* torch = PyImport_ImportModule("torch");
   if (!torch) return NULL;
   bf16 = PyObject_GetAttrString(torch, "bfloat16");
+  fp32 = PyObject_GetAttrString(torch, "float32");
   Py_DECREF(torch);
-  return s_data_ptr && s_nbytes && s_dtype && s_is_contiguous && bf16 ? PyModule_Create(&module) : NULL;
+  return s_data_ptr && s_nbytes && s_dtype && s_is_contiguous && bf16 && fp32 ? PyModule_Create(&module) : NULL;
 }

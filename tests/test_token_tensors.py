@@ -52,3 +52,34 @@ def test_norm_weights_that_are_right_get_to_the_library():
             fastav.fastav_rotate(params, q, x, None, q, x, norm, w, stream=_Stream)
     with pytest.raises(fastav.FastavError):
         fastav.fastav_rotate(params, x, x, None, x, x, None, None, stream=_Stream)
+
+
+POOL = (3, 2, 32)  # pages, KV heads, page tokens
+BAD_WEIGHTS = {
+    "int32": torch.zeros(POOL, dtype=torch.int32),
+    "fp64, as many bytes": torch.zeros(3, 2, 16, dtype=torch.float64),
+    "bf16": torch.zeros(POOL, dtype=torch.bfloat16),
+    "a page too few": torch.zeros(2, 2, 32),
+    "heads and tokens exchanged": torch.zeros(3, 32, 2).transpose(1, 2),
+    "none": None,
+}
+
+
+@pytest.mark.parametrize("name", BAD_WEIGHTS)
+def test_weights_that_are_no_pool_of_fp32(name):
+    cache, table = fastav.make_cache(3, 2, DIM, 32, device="cpu"), torch.zeros(1, 3, dtype=torch.int32)
+    assert tuple(cache.k_scale.shape) == POOL
+    x, one = torch.zeros(5, 2, DIM, dtype=torch.bfloat16), torch.ones(1, dtype=torch.int32)
+    attend = fastav.make_attend_params(batch=1, total_q=5, max_qlen=5, num_q_heads=2, max_kv_len=96, q=x, out=x, page_table=table)
+    evict = fastav.make_evict_params(batch=1, max_kv_len=96, max_keep=10, page_table=table)
+    with pytest.raises(ValueError, match="fp32 weights"):
+        fastav.fastav_cache_weigh(attend, cache, BAD_WEIGHTS[name], x, torch.zeros(5, 2), torch.zeros(2, dtype=torch.int32), table, one, stream=_Stream)
+    with pytest.raises(ValueError, match="fp32 weights"):
+        fastav.fastav_cache_evict(evict, cache, BAD_WEIGHTS[name], table, one, one, one, torch.zeros(4096, dtype=torch.uint8), stream=_Stream)
+
+
+def test_weights_that_are_right_get_to_the_library():
+    cache, table, one = fastav.make_cache(3, 2, DIM, 32, device="cpu"), torch.zeros(1, 3, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    evict = fastav.make_evict_params(batch=1, max_kv_len=97, max_keep=10, page_table=table)      # more tokens than the table has places
+    with pytest.raises(fastav.FastavError):
+        fastav.fastav_cache_evict(evict, cache, torch.zeros_like(cache.k_scale), table, one, one, one, torch.zeros(4096, dtype=torch.uint8), stream=_Stream)
