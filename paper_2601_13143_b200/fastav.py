@@ -51,6 +51,7 @@ EXPORTS = ("fastav_version", "fastav_status_string", "fastav_last_cuda_error", "
            "fastav_attend", "fastav_rotate", "fastav_rotate_write", "fastav_cache_weigh", "fastav_evict_workspace_bytes", "fastav_cache_evict")
 
 ROTATE_MAX_PAIRS = 64
+ROTATE_MAX_AXES = 4
 
 
 class fastav_params(ctypes.Structure):
@@ -535,7 +536,9 @@ def make_rotate_params(*, q=None, k=None, v=None, q_out=None, k_out=None, pos=No
         p.pos_stride_tok, p.pos_stride_axis = pos.stride(-1), pos.stride(0) if pos.dim() == 2 else 0
     for i, f in enumerate(frequencies):
         p.frequency[i] = f
-        p.axis[i] = 0 if axis is None else axis[i]
+        p.axis[i] = at = 0 if axis is None else axis[i]
+        if p.axis[i] != at or at >= ROTATE_MAX_AXES:
+            raise ValueError(f"expected an axis below {ROTATE_MAX_AXES} for each pair, got {at}")
     p.norm_eps, p.flags = float(norm_eps), int(flags) | (FASTAV_ROTATE_INTERLEAVED if interleaved else 0)
     return p
 

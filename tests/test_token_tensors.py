@@ -83,3 +83,13 @@ def test_weights_that_are_right_get_to_the_library():
     evict = fastav.make_evict_params(batch=1, max_kv_len=97, max_keep=10, page_table=table)      # more tokens than the table has places
     with pytest.raises(fastav.FastavError):
         fastav.fastav_cache_evict(evict, cache, torch.zeros_like(cache.k_scale), table, one, one, one, torch.zeros(4096, dtype=torch.uint8), stream=_Stream)
+
+
+@pytest.mark.parametrize("bad", [256, 257, -256, -1, 4])
+def test_an_axis_is_one_of_the_positions_rows(bad):
+    """(Held as a byte, where 256 is 0.)"""
+    x, pos = torch.zeros(5, 2, DIM, dtype=torch.bfloat16), torch.zeros(3, 5, dtype=torch.int32)
+    with pytest.raises(ValueError, match="axis"):
+        fastav.make_rotate_params(q=x, q_out=x, pos=pos, frequencies=[1.0] * 8, axis=[0, 1, 2, 0, 1, bad, 0, 0])
+    p = fastav.make_rotate_params(q=x, q_out=x, pos=pos, frequencies=[1.0] * 8, axis=[0, 1, 2, 0, 1, 2, 0, 0, 7])   # (entries of pairs that are not turned do not count)
+    assert list(p.axis[:9]) == [0, 1, 2, 0, 1, 2, 0, 0, 0]
