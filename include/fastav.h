@@ -523,7 +523,8 @@ int32_t fastav_rotate(const fastav_rotate_params* params, const void* q, const v
 /*
  * Sequence b's new tokens are cu_seqlens[b] ... of q, k, v and pos, and become tokens start_opt[b], start_opt[b] + 1, ... of the cached
  * sequence (NULL: 0, 1, ...), laid down as fastav_cache_write lays rows down (its rules for rows without a place hold).  q and q_out may be
- * NULL.  Rows of q_out behind cu_seqlens[B] are left as they are.  ko_ strides are not read.
+ * NULL.  Rows of q_out behind cu_seqlens[B] are left as they are.  ko_ strides are not read.  A row of K whose elements leave fp32 when they are rotated (a pair
+ * near bf16's largest numbers) or normed is one that is not finite, as if it had held an infinite element: codes 0 and a scale that is NaN.
  */
 int32_t fastav_rotate_write(const fastav_rotate_params* params, const fastav_cache* cache, const void* q, const void* k, const void* v,
                             const int32_t* pos, const void* q_norm_opt, const void* k_norm_opt, const int32_t* cu_seqlens,

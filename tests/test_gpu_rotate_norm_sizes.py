@@ -1,4 +1,6 @@
 """The norm per head near the ends of fp32's range, against the definition in 64 bits (tolerances: those of the rotation's other tests)."""
+import math
+
 import pytest
 import torch
 
@@ -60,3 +62,20 @@ def test_norm_weights_far_from_one(scale, weight, eps):
     fastav.fastav_rotate(fastav.make_rotate_params(q=x, q_out=y, norm_eps=eps), x.cuda(), None, None, y, None, w.cuda())
     want, size = ref.turned(x, torch.zeros(1, 5, dtype=torch.int32), [], norm=w, eps=eps)
     _near(y, want, size)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_a_key_that_leaves_fp32_when_it_is_rotated_is_a_row_that_is_not_finite(fmt):
+    """A pair (a, -a) by an eighth of a turn: a sqrt(2) beyond fp32's largest number.  The rows beside it are not touched by it."""
+    k, v = _rows(3, 2, 64, 1.0), _rows(3, 2, 64, 1.0, 9)
+    k[1, 0, 3], k[1, 0, 35] = 3e38, -3e38
+    pos, freq = torch.ones(1, 3, dtype=torch.int32), [math.pi / 4] * 32
+    table, pages = _tables(torch.Generator().manual_seed(1), [3], 16)
+    cache = _cache(pages, 2, 64, 16, fmt)
+    kd, vd = k.cuda(), v.cuda()
+    fastav.fastav_rotate_write(fastav.make_rotate_params(k=kd, v=vd, pos=pos, frequencies=freq), cache, None, kd, vd, pos.cuda(), _cu([3]).cuda(), table.cuda(), None, None)
+    page = int(table[0, 0])
+    assert bool(torch.isnan(cache.k_scale[page, 0, 1])) and not bool(cache.k[page, 0, 1].view(torch.int8).any())
+    cache.k_scale[page, 0, 1] = 0
+    k[1, 0] = 0
+    _check_rows(cache, fmt, table, 16, [(0, 0, ref.turned(k, pos, freq), v)])
