@@ -9,7 +9,8 @@
 // Moving: the same clusters go on with it in place and where there is little to move (one launch), in rounds of kMoved rows a block in the survivors' order; else a
 // kernel with a block per kChunk rows, that many in flight.  Bound by the rows that move (codes and scales of K and V, weights: 2 (d + 4) + 4 bytes each
 // way), for one sequence by the selection's chain.  32 sequences of 512 to 4,096 tokens, half of them kept, to other pages: 21.4 us a call, 7 of them selection (69 MB: 10.8 us
-// at a copy's rate); 32 x 4,096 tokens of 4 heads to 2,048: 40 us alone, in place or not; 819 of 1,024 tokens 8.9 us.
+// at a copy's rate); 32 x 4,096 tokens of 4 heads to 2,048: 33 us a call to other pages, 39 alone in place; 819 of 1,024 tokens 8.7 us (8.5 when a thread's tokens lay kThreads
+// apart, and the 32 sequences 22.0: eight in a row keep fewer threads of a short slice busy).
 //
 // In place.  Survivor i comes from a place >= i, and sources ascend.  So a round's rows may be written as soon as all of that round have been read: what later
 // rounds read lies behind their own targets.  (The rows of the round after are asked for ahead of that.)  One set for all heads is selected by a launch of its own, since rows
@@ -25,11 +26,13 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kChunk = 128, kChunkThreads = 256;  // rows of a block that only moves
 constexpr int kEach = 8, kHeld = kEach * kThreads;  // keys that a thread, a block holds; those of a longer slice are looked up again
-// Tokens of a block's slice, at least: a cluster of blocks is 0.5 us a digit slower than one block, which takes 1,024 tokens in hardly more time than 256 (1 x 300 tokens
-// 16 -> 12 us alone, in clusters from 256 and from 1,024 on).
+// Tokens of a block's slice, at least.  More blocks move rows sooner where the selecting clusters go on with it, and cost a cluster barrier a digit.  us with 512 / 1,024 /
+// 2,048 / 4,096.  In place (and a copy of the weights): one sequence of 4,096 tokens to 2,048 15.5 / 17.4 / 22.6 / 22.6, eight of 4,000 less one 22.5 / 22.5 / 30.9 / 34.9, one of 16,384
+// to 16,000 34.4 / 34.4 / 34.4 / 53.5.  To other pages: 1,500 to 1,200 11.9 / 11.5 / 9.5 / 9.1, eight of 4,000 to 2,000 15.5 / 15.5 / 15.0 / 12.6, 16,384 to 6,553 16.6 / 16.6 / 16.6 / 15.6;
+// four of 16,384 jointly 30.9 / 31.0 / 30.9 / 31.4.
 constexpr int kLeastSlice = 1024;
-// A block's survivors up to which the selecting clusters move them, one round of theirs; beyond, another launch with more blocks is quicker (819 of 1,024 tokens,
-// 4 heads: 8.1 us instead of 12.2).
+// A block's survivors up to which the selecting clusters move them, one or two rounds of theirs; beyond, another launch with more blocks is quicker (4 heads, by the selecting
+// clusters / by another launch: 240 of 300 tokens 7.2 / 7.8 us, 819 of 1,024 11.2 / 8.7, 1,638 of 2,048 17.8 / 11.0; but 750 of 32 x 1,500 12.5 / 13.6).
 constexpr int kFewRows = 256;
 
 struct EvictCall {

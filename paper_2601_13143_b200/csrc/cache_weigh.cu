@@ -2,7 +2,8 @@
 //
 // A token's weight is a sum over query rows of exp(scale q.k - lse): with the rows' log-sum-exp given, tokens are independent of one another, so K's codes
 // are read once, and tokens of different blocks have nothing to join.  Bound by reading the codes where rows are few: 8 heads of 4 x 16,384 tokens, one query row of 32
-// heads, 73 MB: 18.9 us a call (3.9 TB/s), of which some 15 the kernel; 32 sequences of 512 to 4,096 tokens 12.3 us.
+// heads, 73 MB: 19.0 us a call (3.9 TB/s), of which some 15 the kernel; 32 sequences of 512 to 4,096 tokens 12.3 us.  Three blocks of 168 registers an SM; with
+// more than 8 stacked rows of 128 elements the compiler spills 8 to 44 bytes a thread.
 #include <limits.h>
 
 #include <algorithm>

@@ -14,12 +14,12 @@
 //   warp 25     query rows by TMA, their log-sum-exps and masks
 //   warps 26-27 issue the MMAs, every other product each
 //
-// Bound by the exponentials (16 per clock and SM) and by power: 1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials) take 239 us, 0.86 PFLOP/s;
-// call upon call, at the power limit and some 1.65 GHz, 252.  An eighth of the exponentials is made of multiplications instead (none 250, a sixteenth 246, a quarter 248 us;
-// at the power limit none, a sixteenth and an eighth are alike, three sixteenths 258).  Measured on the way:
+// Bound by the exponentials (16 per clock and SM) and by power: 1,536 rows on 16,384 keys of 8 heads (206 GFLOP, 805 million exponentials) take 242 us, 0.85 PFLOP/s;
+// call upon call, at the power limit and some 1.65 GHz, 252.  An eighth of the exponentials is made of multiplications instead: none 250 us, a sixteenth 246 (call upon call
+// 4 and 2 % more than an eighth).  The compiler spills some 200 bytes a thread without them and nothing with them, which shows where row tiles are few (below).  Measured on the way:
 // eight summing warps a block 296 us; four accumulators of 128 columns, each summed up and made in turn, 256; eight of 64 columns 267; a third stage of query rows the same.
-// With few row tiles bound by the chain from a group's codes to its sums: 64 rows on 4 x 16,384 tokens 43 us (55 where the converting warps look up pages and walk the
-// list by themselves, and have no registers left for it; 45 without the call into L2), 96 rows on 8 x 3,000 27 us (31).
+// With few row tiles bound by the chain from a group's codes to its sums: 64 rows on 4 x 16,384 tokens 41 us (47 with spills, 55 where the converting warps look up pages and
+// walk the list by themselves), 192 rows 57 (64), 96 rows on 8 x 3,000 27 (29).
 #include <cuda.h>
 #include <limits.h>
 

@@ -5,8 +5,9 @@
 // so they are made once into shared memory, in the order in which lanes read them.  d / 16 lanes take a row, a lane two pieces of 8
 // elements: pieces that hold the two halves of the same pairs, so that a rotation needs no other lane.  A group of lanes keeps to one head and walks over
 // the block's tokens, so that addresses, the norm's weights and what becomes of the row are known beforehand, and a block has as many threads as that
-// takes.  65,536 tokens of 40 rows: 224 us, 6.0 TB/s, 93 % of a copy.  16 x 900 tokens of 48 rows into the cache: 73 us, 3.9 TB/s, 241 instructions of a warp
-// for four rows, 0.55 of them a cycle and scheduler.  (Groups that walk over the heads of a token instead: 324 instructions, 102 us.)
+// takes.  65,536 tokens of 40 rows: 220 us, 6.1 TB/s, 95 % of a copy.  16 x 900 tokens of 48 rows into the cache: 72 us, 3.9 TB/s, 177 instructions of a warp
+// for four rows; with norms 80 us and 260, 0.57 of them a cycle and scheduler.  (Groups that walk over the heads of a token instead: 324 instructions, 102 us.)  With pairs
+// of neighbours (INTERLEAVED) four blocks an SM leave the compiler 64 registers, and it spills 4 to 20 bytes a thread.
 //
 // Angles.  frequency / (2 pi) as a 64-bit binary fraction of a turn times the position, modulo 2^64, IS the angle modulo a turn: integers wrap where floats
 // lose bits (fp32 is 0.06 rad off at position 10^6).
@@ -47,7 +48,7 @@ inline void mark_head(RotateCall& c, bool head) { c.head_wait = head ? 1 : 0; }
 
 enum { kToRows, kToInt8, kToFp8 };
 
-// Sixteen values of a row as pairs, and the row's place.
+// Sixteen values of a row, as they lie in memory: a lane's two pieces.
 struct Row {
   uint4 lo, hi;
 };
@@ -79,7 +80,7 @@ rotate_kernel(const __grid_constant__ RotateCall c) {
   __shared__ __align__(16) float4 weights[NORMED ? 2 : 1][NORMED ? DIM / 4 : 1];  // the norm's, of lane l's four j at [j * kLanes + l]
   __shared__ long long place[kMostTokens];  // row of the pool, head 0; -1: left out
   const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
-  const unsigned mates = (kLanes == 32 ? 0xFFFFFFFFu : (1u << kLanes) - 1u) << (threadIdx.x & 31 & ~(kLanes - 1));  // the group's lanes of the warp
+  const unsigned mates = ((1u << kLanes) - 1u) << (threadIdx.x & 31 & ~(kLanes - 1));  // the group's lanes of the warp
   const int turned = c.rotary / 16;  // lanes whose pieces are turned
   const int piece0 = lane < turned ? lane : 2 * lane, piece1 = lane < turned ? lane + turned : piece0 + 1;
 
