@@ -232,7 +232,8 @@ def _p(t: torch.Tensor | None) -> int | None:
     return None if t is None else t.data_ptr()
 
 
-_cuda_ready, _raw_stream, _current_device = torch.cuda.is_initialized, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_cuda_ready = torch.cuda.is_initialized
+_raw_stream, _current_device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))  # (a torch without CUDA has neither)
 
 
 def _stream(stream) -> int:
